@@ -1,0 +1,165 @@
+// Rows of a table pooled per (record, slot): the first step of a model that is fed with signs.
+#include "train_common.h"
+
+#include <stdio.h>
+
+namespace fbx {
+namespace train {
+
+namespace {
+thread_local char g_error[256];
+}
+
+fbx_status refuse(fbx_status s, const char* why) {
+  snprintf(g_error, sizeof g_error, "%s", why);
+  return s;
+}
+
+fbx_status launched() {
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? FBX_OK : refuse(FBX_E_HIP, hipGetErrorString(e));
+}
+
+fbx_status check_slots(const fbx_slot_view* slots, uint32_t n_slots, uint64_t n_records, uint32_t tile, uint64_t* total) {
+  if (!slots && n_slots) return refuse(FBX_E_ARG, "slots is NULL");
+  if (n_records >> 32) return refuse(FBX_E_ARG, "n_records must be below 2^32");
+  uint64_t sum = 0;
+  for (uint32_t i = 0; i < n_slots; ++i) {
+    const fbx_slot_view& s = slots[i];
+    if (s.n_values && !s.values) return refuse(FBX_E_ARG, "a slot has n_values but no values");
+    if (s.n_values >> 40) return refuse(FBX_E_ARG, "a slot has 2^40 values or more");
+    if (s.fixed_arity ? s.n_values != n_records * s.fixed_arity : !s.offsets)
+      return refuse(FBX_E_ARG, s.fixed_arity ? "a slot of fixed arity must have fixed_arity * n_records values" : "a slot without fixed arity needs offsets");
+    if (!s.fixed_arity && s.tile_ends && !tile) return refuse(FBX_E_ARG, "a slot has tile_ends: arrival_tile_records is needed");
+    if (!s.fixed_arity && !s.tile_ends && tile) return refuse(FBX_E_ARG, "arrival_tile_records is given: every list slot needs tile_ends");
+    sum += s.n_values;
+  }
+  if (total) *total = sum;
+  return FBX_OK;
+}
+
+SlotRef slot_ref(const fbx_slot_view& v, uint32_t base) {
+  return SlotRef{v.values, v.fixed_arity ? nullptr : v.offsets, v.fixed_arity ? nullptr : v.tile_ends, v.n_values, v.fixed_arity, base};
+}
+
+namespace {
+
+constexpr uint32_t kTileRecords = 32;
+
+struct EmbedArgs {
+  SlotRef slots[kSlotsPerLaunch];
+  const void* table;
+  void* out;                 // of the launch's first slot
+  uint64_t n_records, table_stride, record_stride;
+  uint32_t n_slots, rows, dim, tile, lanes_log2, mean;
+};
+
+// A workgroup takes 32 records of up to 64 slots.  Its lanes first find, records side by side (slot-major signs
+// are read whole lines at a time), where each (record, slot)'s signs lie and the first one's row; then 2^lanes_log2
+// lanes a (record, slot), slots side by side (a record's pooled rows are written whole lines at a time), each
+// lane N adjacent columns, add the rows up in the order of the signs.
+template <class T, int N>
+__global__ __launch_bounds__(256) void k_embed(EmbedArgs) {
+  const EmbedArgs& a = launch_args<EmbedArgs>();
+  __shared__ uint64_t begin[kSlotsPerLaunch * (kTileRecords + 1)];
+  __shared__ uint32_t count[kSlotsPerLaunch * (kTileRecords + 1)], first[kSlotsPerLaunch * (kTileRecords + 1)];
+  const uint64_t r0 = (uint64_t)blockIdx.x * kTileRecords;
+  const uint32_t n = (uint32_t)(a.n_records - r0 < kTileRecords ? a.n_records - r0 : kTileRecords);
+  for (uint32_t i = threadIdx.x; i < a.n_slots * kTileRecords; i += 256u) {
+    const uint32_t s = i / kTileRecords, r = i % kTileRecords;
+    if (r >= n) continue;
+    uint64_t b;
+    uint32_t c;
+    signs_of(a.slots[s], r0 + r, a.n_records, a.tile, b, c);
+    const uint32_t at = s * (kTileRecords + 1) + r;
+    begin[at] = b;
+    count[at] = c;
+    first[at] = c ? row_of(a.slots[s].values[b], a.rows) : 0u;
+  }
+  __syncthreads();
+  const uint32_t lanes = 1u << a.lanes_log2, mine = threadIdx.x & (lanes - 1u), groups = 256u >> a.lanes_log2;
+  const T* table = (const T*)a.table;
+  T* out = (T*)a.out + r0 * a.record_stride;
+  for (uint32_t i = threadIdx.x >> a.lanes_log2; i < n * a.n_slots; i += groups) {
+    const uint32_t r = i / a.n_slots, s = i - r * a.n_slots, at = s * (kTileRecords + 1) + r, c = count[at];
+    const uint64_t* signs = a.slots[s].values + begin[at];
+    for (uint32_t col = mine * N; col < a.dim; col += lanes * N) {
+      float sum[N] = {};
+      for (uint32_t k = 0; k < c; ++k) {
+        const uint32_t row = k ? row_of(signs[k], a.rows) : first[at];
+        const Pack<T, N> p = *(const Pack<T, N>*)(table + row * a.table_stride + col);
+#pragma unroll
+        for (int j = 0; j < N; ++j) sum[j] += (float)p.v[j];
+      }
+      Pack<T, N> p;
+#pragma unroll
+      for (int j = 0; j < N; ++j) p.v[j] = (T)(a.mean && c > 1u ? sum[j] / (float)c : sum[j]);
+      *(Pack<T, N>*)(out + r * a.record_stride + (uint64_t)s * a.dim + col) = p;
+    }
+  }
+}
+
+template <class T, int N>
+void launch(const EmbedArgs& a, hipStream_t stream) {
+  hipLaunchKernelGGL((k_embed<T, N>), dim3((uint32_t)ceil_div(a.n_records, kTileRecords)), dim3(256), 0, stream, a);
+}
+
+template <class T>
+void launch_by_width(const EmbedArgs& a, uint32_t n, hipStream_t stream) {
+  if (n == 8) {
+    if constexpr (sizeof(T) == 2) launch<T, 8>(a, stream);
+  } else if (n == 4) {
+    launch<T, 4>(a, stream);
+  } else if (n == 2) {
+    launch<T, 2>(a, stream);
+  } else {
+    launch<T, 1>(a, stream);
+  }
+}
+
+}  // namespace
+}  // namespace train
+}  // namespace fbx
+
+using namespace fbx::train;
+
+extern "C" const char* fbx_train_last_error(void) { return g_error; }
+
+extern "C" fbx_status fbx_embed_forward(const fbx_slot_view* slots, uint32_t n_slots, uint64_t n_records, uint32_t arrival_tile_records,
+                                        const void* d_table, uint64_t rows, uint32_t dim, uint64_t table_stride, fbx_dtype dtype, int mean,
+                                        void* d_out, uint64_t record_stride, void* hip_stream) {
+  if (!known(dtype)) return refuse(FBX_E_ARG, "unknown dtype");
+  if (!rows || rows >> 31) return refuse(FBX_E_ARG, "rows must be 1 .. 2^31 - 1");
+  if (!dim || dim > 65536u || table_stride < dim || table_stride >> 32) return refuse(FBX_E_ARG, "dim must be 1 .. 65536 and table_stride at least dim");
+  if (record_stride < (uint64_t)n_slots * dim || record_stride >> 40) return refuse(FBX_E_ARG, "record_stride must be at least n_slots * dim");
+  const fbx_status st = check_slots(slots, n_slots, n_records, arrival_tile_records, nullptr);
+  if (st != FBX_OK) return st;
+  if (!n_slots || !n_records) return FBX_OK;
+  if (!d_table || !d_out) return refuse(FBX_E_ARG, "d_table or d_out is NULL");
+  const uint32_t e = size_of(dtype);
+  if (((uintptr_t)d_table | (uintptr_t)d_out) % e) return refuse(FBX_E_ARG, "d_table and d_out must be aligned to their elements");
+  // the widest pack, up to 16 bytes, that every row on either side is a multiple of
+  const uint64_t all = (uintptr_t)d_table | (uintptr_t)d_out | dim * e | table_stride * e | record_stride * e;
+  uint32_t n = 16u / e;
+  while (n > 1u && all % (n * e)) n /= 2u;
+  EmbedArgs a{};
+  a.table = d_table;
+  a.n_records = n_records;
+  a.table_stride = table_stride;
+  a.record_stride = record_stride;
+  a.rows = (uint32_t)rows;
+  a.dim = dim;
+  a.tile = arrival_tile_records;
+  a.mean = mean != 0;
+  while ((1u << a.lanes_log2) * n < dim && a.lanes_log2 < 6u) ++a.lanes_log2;
+  for (uint32_t s0 = 0; s0 < n_slots; s0 += kSlotsPerLaunch) {
+    a.n_slots = n_slots - s0 < kSlotsPerLaunch ? n_slots - s0 : kSlotsPerLaunch;
+    for (uint32_t i = 0; i < a.n_slots; ++i) a.slots[i] = slot_ref(slots[s0 + i], 0u);
+    a.out = (char*)d_out + (uint64_t)s0 * dim * e;
+    const hipStream_t stream = (hipStream_t)hip_stream;
+    if (dtype == FBX_F32) launch_by_width<float>(a, n, stream);
+    else if (dtype == FBX_F16) launch_by_width<_Float16>(a, n, stream);
+    else launch_by_width<__bf16>(a, n, stream);
+  }
+  return launched();
+}

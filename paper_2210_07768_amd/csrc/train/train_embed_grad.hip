@@ -1,0 +1,406 @@
+// The gradient of pooled rows with respect to their table, without atomics on it: (row, where it came from) pairs
+// are sorted by row, stably, and a row's terms are then neighbours.
+#include "train_common.h"
+
+namespace fbx {
+namespace train {
+namespace {
+
+constexpr uint32_t kSortItems = 16, kSortTile = 256 * kSortItems;  // pairs of a lane, of a workgroup
+constexpr uint32_t kRun = 32;                                      // sorted terms a group of lanes adds up
+constexpr uint32_t kNone = 0xffffffffu;
+
+struct PairArgs {
+  SlotRef slots[kSlotsPerLaunch];
+  uint32_t* keys;
+  uint32_t* from;   // record * all slots + slot
+  float* share;     // 1 / signs of (record, slot), by the same number; null for sums
+  uint64_t n_records;
+  uint32_t n_slots, first_slot, all_slots, rows, tile;
+};
+
+// A lane a (record, slot): its signs' rows, and where each came from, at the signs' own positions.
+__global__ __launch_bounds__(256) void k_pairs(PairArgs) {
+  const PairArgs& a = launch_args<PairArgs>();
+  const uint64_t r = (uint64_t)blockIdx.x * 256u + threadIdx.x;
+  if (r >= a.n_records) return;
+  const SlotRef& s = a.slots[blockIdx.y];
+  uint64_t b;
+  uint32_t c;
+  signs_of(s, r, a.n_records, a.tile, b, c);
+  const uint32_t from = (uint32_t)r * a.all_slots + a.first_slot + blockIdx.y;
+  for (uint32_t i = 0; i < c; ++i) {
+    a.keys[s.base + b + i] = row_of(s.values[b + i], a.rows);
+    a.from[s.base + b + i] = from;
+  }
+  if (a.share) a.share[from] = c > 1u ? 1.f / (float)c : 1.f;
+}
+
+// Per tile of pairs, how many have each value of the digit; counts lie digit by digit.
+__global__ __launch_bounds__(256) void k_digit_counts(const uint32_t* keys, uint32_t n, uint32_t shift, uint32_t n_tiles, uint32_t* counts) {
+  __shared__ uint32_t h[256];
+  h[threadIdx.x] = 0u;
+  __syncthreads();
+  const uint64_t at = (uint64_t)blockIdx.x * kSortTile;
+  for (uint32_t i = threadIdx.x; i < kSortTile; i += 256u)
+    if (at + i < n) atomicAdd(&h[(keys[at + i] >> shift) & 255u], 1u);
+  __syncthreads();
+  counts[threadIdx.x * (uint64_t)n_tiles + blockIdx.x] = h[threadIdx.x];
+}
+
+// Inclusive sums over the workgroup's 256 lanes.
+__device__ __forceinline__ uint32_t sums_256(uint32_t v, uint32_t* four) {
+  for (uint32_t d = 1; d < 64u; d <<= 1) {
+    const uint32_t t = __shfl_up(v, d, 64);
+    if (threadIdx.x % 64u >= d) v += t;
+  }
+  __syncthreads();
+  if (threadIdx.x % 64u == 63u) four[threadIdx.x / 64u] = v;
+  __syncthreads();
+  for (uint32_t w = 0; w < threadIdx.x / 64u; ++w) v += four[w];
+  return v;
+}
+
+// A workgroup a digit: counts of its tiles become how many pairs of earlier tiles have the digit.
+__global__ __launch_bounds__(256) void k_digit_sums(uint32_t* counts, uint32_t n_tiles, uint32_t* totals) {
+  __shared__ uint32_t four[4];
+  __shared__ uint32_t all;
+  uint32_t* c = counts + blockIdx.x * (uint64_t)n_tiles;
+  uint32_t before = 0u;
+  for (uint32_t i0 = 0; i0 < n_tiles; i0 += 256u) {
+    const uint32_t i = i0 + threadIdx.x, v = i < n_tiles ? c[i] : 0u, sum = sums_256(v, four);
+    if (i < n_tiles) c[i] = before + sum - v;
+    if (threadIdx.x == 255u) all = sum;
+    __syncthreads();
+    before += all;
+  }
+  if (threadIdx.x == 0u) totals[blockIdx.x] = before;
+}
+
+// Moves a tile's pairs to where their digit's pairs go, in order: ranks inside a wavefront by comparing digits over
+// its lanes, then over wavefronts and digits by sums; the tile is put in order in LDS, so that pairs of one digit are
+// written next to each other.
+__global__ __launch_bounds__(256) void k_move_pairs(const uint32_t* keys, const uint32_t* from, uint32_t n, uint32_t shift, uint32_t n_tiles,
+                                                    const uint32_t* counts, const uint32_t* totals, uint32_t* keys_out, uint32_t* from_out) {
+  __shared__ uint32_t seen[4][256], to[256], begin[256], four[4];
+  __shared__ uint32_t k_lds[kSortTile], f_lds[kSortTile];
+  const uint32_t lane = threadIdx.x % 64u, wave = threadIdx.x / 64u;
+  for (uint32_t w = 0; w < 4u; ++w) seen[w][threadIdx.x] = 0u;
+  __syncthreads();
+  const uint64_t at = (uint64_t)blockIdx.x * kSortTile + wave * (kSortItems * 64u) + lane;
+  uint32_t k[kSortItems], f[kSortItems], rank[kSortItems];
+#pragma unroll
+  for (uint32_t i = 0; i < kSortItems; ++i) {
+    const bool in = at + i * 64u < n;
+    k[i] = in ? keys[at + i * 64u] : 0u;
+    f[i] = in ? from[at + i * 64u] : 0u;
+  }
+  const uint64_t below = (1ull << lane) - 1ull;
+#pragma unroll
+  for (uint32_t i = 0; i < kSortItems; ++i) {
+    const bool in = at + i * 64u < n;
+    const uint32_t d = (k[i] >> shift) & 255u;
+    uint64_t same = __ballot(in);
+#pragma unroll
+    for (uint32_t b = 0; b < 8u; ++b) {
+      const uint64_t set = __ballot((d >> b) & 1u);
+      same &= (d >> b) & 1u ? set : ~set;
+    }
+    const uint32_t before = in ? seen[wave][d] : 0u;
+    rank[i] = before + __popcll(same & below);
+    if (in && (same & below) == 0ull) seen[wave][d] = before + __popcll(same);
+    __builtin_amdgcn_wave_barrier();
+  }
+  __syncthreads();
+  uint32_t mine = 0u;
+  for (uint32_t w = 0; w < 4u; ++w) {
+    const uint32_t c = seen[w][threadIdx.x];
+    seen[w][threadIdx.x] = mine;
+    mine += c;
+  }
+  begin[threadIdx.x] = sums_256(mine, four) - mine;
+  const uint32_t total = totals[threadIdx.x];
+  to[threadIdx.x] = sums_256(total, four) - total + counts[threadIdx.x * (uint64_t)n_tiles + blockIdx.x];
+  __syncthreads();
+#pragma unroll
+  for (uint32_t i = 0; i < kSortItems; ++i)
+    if (at + i * 64u < n) {
+      const uint32_t d = (k[i] >> shift) & 255u, p = begin[d] + seen[wave][d] + rank[i];
+      k_lds[p] = k[i];
+      f_lds[p] = f[i];
+    }
+  __syncthreads();
+  const uint64_t first = (uint64_t)blockIdx.x * kSortTile;
+  const uint32_t here = n - first < kSortTile ? (uint32_t)(n - first) : kSortTile;
+  for (uint32_t i = threadIdx.x; i < here; i += 256u) {
+    const uint32_t d = (k_lds[i] >> shift) & 255u, p = to[d] + i - begin[d];
+    keys_out[p] = k_lds[i];
+    from_out[p] = f_lds[i];
+  }
+}
+
+struct SumArgs {
+  const uint32_t* keys;       // ascending; kNone: no term
+  const uint32_t* from;       // terms are rows of dout ...
+  const float* share;
+  const float* terms;         // ... or, later, sums of stretches
+  const void* dout;
+  void* dtable;
+  uint32_t* part_keys;        // two a group: a run that began before it, a run that goes on after it
+  float* parts;
+  uint64_t record_stride, table_stride;
+  uint32_t n, n_records, all_slots, rows, dim, lanes_log2;
+};
+
+// 2^lanes_log2 lanes, each N adjacent columns, add up 32 neighbouring terms; a row's sum that lies inside them is
+// written to the table, one that begins before them or ends after them is left to the next launch, which adds such sums
+// up the same way.  kFirst: terms are rows of dout.
+template <class T, int N, bool kFirst>
+__global__ __launch_bounds__(256) void k_sum_rows(SumArgs a) {
+  const uint32_t lanes = 1u << a.lanes_log2, mine = threadIdx.x & (lanes - 1u);
+  const uint64_t group = ((uint64_t)blockIdx.x * 256u + threadIdx.x) >> a.lanes_log2;
+  const uint64_t e0 = group * kRun;
+  if (e0 >= a.n) return;
+  const uint32_t n = a.n - e0 < kRun ? (uint32_t)(a.n - e0) : kRun;
+  const uint32_t before = e0 ? a.keys[e0 - 1] : kNone, after = e0 + n < a.n ? a.keys[e0 + n] : kNone;
+  for (uint32_t col = mine * N; col < a.dim; col += lanes * N) {
+    float sum[N] = {};
+    uint32_t key = a.keys[e0];
+    bool open = key == before && key != kNone;  // the run at hand began before this group
+    uint32_t head = kNone;
+    auto close = [&](bool goes_on) {
+      if (key == kNone) return;
+      if (!open && !goes_on) {
+        if (key >= a.rows) return;
+        Pack<T, N> p;
+#pragma unroll
+        for (int j = 0; j < N; ++j) p.v[j] = (T)sum[j];
+        *(Pack<T, N>*)((T*)a.dtable + key * a.table_stride + col) = p;
+      } else {
+        float* to = a.parts + (2 * group + (open ? 0 : 1)) * a.dim + col;
+#pragma unroll
+        for (int j = 0; j < N; ++j) to[j] = sum[j];
+      }
+    };
+    uint32_t tail = kNone;
+    for (uint32_t i = 0; i < n; ++i) {
+      const uint32_t k = a.keys[e0 + i];
+      if (k != key) {
+        close(false);
+        if (open) head = key;
+        open = false;
+        key = k;
+#pragma unroll
+        for (int j = 0; j < N; ++j) sum[j] = 0.f;
+      }
+      if (k == kNone) continue;
+      if (kFirst) {
+        const uint32_t from = a.from[e0 + i];
+        const uint32_t r = from / a.all_slots, s = from - r * a.all_slots;
+        if (r >= a.n_records) continue;
+        const Pack<T, N> p = *(const Pack<T, N>*)((const T*)a.dout + r * a.record_stride + (uint64_t)s * a.dim + col);
+        if (a.share) {
+          const float w = a.share[from];
+#pragma unroll
+          for (int j = 0; j < N; ++j) sum[j] += (float)p.v[j] * w;
+        } else {
+#pragma unroll
+          for (int j = 0; j < N; ++j) sum[j] += (float)p.v[j];
+        }
+      } else {
+        const float* p = a.terms + (e0 + i) * a.dim + col;
+#pragma unroll
+        for (int j = 0; j < N; ++j) sum[j] += p[j];
+      }
+    }
+    const bool goes_on = key == after && key != kNone;
+    close(goes_on);
+    if (open) {
+      head = key;
+      if (goes_on) {  // all of the group is one run's: a second part, of nothing, keeps the run's parts neighbours
+        tail = key;
+        for (int j = 0; j < N; ++j) a.parts[(2 * group + 1) * a.dim + col + j] = 0.f;
+      }
+    } else if (goes_on) {
+      tail = key;
+    }
+    if (col == 0u && a.part_keys) {
+      a.part_keys[2 * group] = head;
+      a.part_keys[2 * group + 1] = tail;
+    }
+  }
+}
+
+template <class T, int N>
+__global__ __launch_bounds__(256) void k_clear_rows(void* to, uint64_t rows, uint32_t dim, uint64_t stride) {
+  const uint32_t packs = dim / N;
+  const uint64_t all = rows * packs;
+  const Pack<T, N> zero{};
+  for (uint64_t i = (uint64_t)blockIdx.x * 256u + threadIdx.x; i < all; i += (uint64_t)gridDim.x * 256u)
+    *(Pack<T, N>*)((T*)to + i / packs * stride + i % packs * N) = zero;
+}
+
+// Where things lie in the scratch.
+struct Layout {
+  uint64_t keys[2], from[2], counts, totals, share, part_keys[2], parts[2], bytes;
+  uint32_t n, n_tiles, passes;
+};
+
+bool lay_out(Layout& l, uint64_t total, uint64_t n_records, uint32_t n_slots, uint64_t rows, uint32_t dim, bool mean) {
+  if (total >> 32 || n_records * n_slots >> 32) return false;
+  l.n = (uint32_t)total;
+  l.n_tiles = (uint32_t)ceil_div(total, kSortTile);
+  uint32_t bits = 1;
+  while ((rows - 1) >> bits) ++bits;
+  l.passes = (bits + 7u) / 8u;
+  uint64_t at = 0;
+  auto take = [&](uint64_t bytes) {
+    const uint64_t was = at;
+    at = round_up(at + bytes, 256);
+    return was;
+  };
+  for (int i = 0; i < 2; ++i) l.keys[i] = take(4 * total);
+  for (int i = 0; i < 2; ++i) l.from[i] = take(4 * total);
+  l.counts = take(4ull * 256 * l.n_tiles);
+  l.totals = take(4 * 256);
+  l.share = take(mean ? 4 * n_records * n_slots : 0);
+  uint64_t groups = ceil_div(total, kRun);
+  for (int i = 0; i < 2; ++i) {
+    l.part_keys[i] = take(4 * 2 * groups);
+    l.parts[i] = take(4ull * 2 * groups * dim);
+    groups = ceil_div(2 * groups, kRun);
+  }
+  l.bytes = at;
+  return true;
+}
+
+template <class T, int N>
+void sum_rows(SumArgs a, const Layout& l, char* scratch, uint64_t rows, hipStream_t stream) {
+  const uint64_t packs = rows * (a.dim / N);
+  const uint32_t clear = (uint32_t)(ceil_div(packs, 256) < 16384 ? ceil_div(packs, 256) : 16384);
+  hipLaunchKernelGGL((k_clear_rows<T, N>), dim3(clear), dim3(256), 0, stream, a.dtable, rows, a.dim, a.table_stride);
+  int side = 0;
+  for (bool first = true; a.n; first = false) {
+    const uint64_t groups = ceil_div(a.n, kRun);
+    const bool last = groups == 1;
+    a.part_keys = last ? nullptr : (uint32_t*)(scratch + l.part_keys[side]);
+    a.parts = last ? nullptr : (float*)(scratch + l.parts[side]);
+    const dim3 grid((uint32_t)ceil_div(groups << a.lanes_log2, 256));
+    if (first) hipLaunchKernelGGL((k_sum_rows<T, N, true>), grid, dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((k_sum_rows<T, N, false>), grid, dim3(256), 0, stream, a);
+    if (last) break;
+    a.keys = a.part_keys;
+    a.terms = a.parts;
+    a.n = (uint32_t)(2 * groups);
+    side ^= 1;
+  }
+}
+
+template <class T>
+void sum_rows_by_width(const SumArgs& a, uint32_t n, const Layout& l, char* scratch, uint64_t rows, hipStream_t stream) {
+  if (n == 8) {
+    if constexpr (sizeof(T) == 2) sum_rows<T, 8>(a, l, scratch, rows, stream);
+  } else if (n == 4) {
+    sum_rows<T, 4>(a, l, scratch, rows, stream);
+  } else if (n == 2) {
+    sum_rows<T, 2>(a, l, scratch, rows, stream);
+  } else {
+    sum_rows<T, 1>(a, l, scratch, rows, stream);
+  }
+}
+
+}  // namespace
+}  // namespace train
+}  // namespace fbx
+
+using namespace fbx::train;
+
+extern "C" fbx_status fbx_embed_backward_scratch(const fbx_slot_view* slots, uint32_t n_slots, uint64_t n_records, uint64_t rows, uint32_t dim,
+                                                 int mean, uint64_t* bytes) {
+  if (!bytes) return refuse(FBX_E_ARG, "bytes is NULL");
+  if (!rows || rows >> 31 || !dim || dim > 65536u) return refuse(FBX_E_ARG, "rows must be 1 .. 2^31 - 1, dim 1 .. 65536");
+  if ((!slots && n_slots) || n_records >> 32) return refuse(FBX_E_ARG, "slots is NULL, or n_records is 2^32 or more");
+  uint64_t total = 0;
+  for (uint32_t i = 0; i < n_slots; ++i) {
+    if (slots[i].n_values >> 32) return refuse(FBX_E_ARG, "2^32 signs or more");
+    total += slots[i].n_values;
+  }
+  Layout l;
+  if (!lay_out(l, total, n_records, n_slots, rows, dim, mean != 0)) return refuse(FBX_E_ARG, "2^32 signs, or records * slots, or more");
+  *bytes = l.bytes;
+  return FBX_OK;
+}
+
+extern "C" fbx_status fbx_embed_backward(const fbx_slot_view* slots, uint32_t n_slots, uint64_t n_records, uint32_t arrival_tile_records,
+                                         const void* d_dout, uint64_t record_stride, uint64_t rows, uint32_t dim, uint64_t table_stride,
+                                         fbx_dtype dtype, int mean, void* d_dtable, void* d_scratch, uint64_t scratch_bytes, void* hip_stream) {
+  if (!known(dtype)) return refuse(FBX_E_ARG, "unknown dtype");
+  if (!rows || rows >> 31) return refuse(FBX_E_ARG, "rows must be 1 .. 2^31 - 1");
+  if (!dim || dim > 65536u || table_stride < dim || table_stride >> 32) return refuse(FBX_E_ARG, "dim must be 1 .. 65536 and table_stride at least dim");
+  if (record_stride < (uint64_t)n_slots * dim || record_stride >> 40) return refuse(FBX_E_ARG, "record_stride must be at least n_slots * dim");
+  uint64_t total = 0;
+  const fbx_status st = check_slots(slots, n_slots, n_records, arrival_tile_records, &total);
+  if (st != FBX_OK) return st;
+  Layout l;
+  if (!lay_out(l, total, n_records, n_slots, rows, dim, mean != 0)) return refuse(FBX_E_ARG, "2^32 signs, or records * slots, or more");
+  if (!d_dtable || (!d_dout && total)) return refuse(FBX_E_ARG, "d_dtable or d_dout is NULL");
+  const uint32_t e = size_of(dtype);
+  if (((uintptr_t)d_dtable | (uintptr_t)d_dout) % e) return refuse(FBX_E_ARG, "d_dtable and d_dout must be aligned to their elements");
+  if (l.bytes && (!d_scratch || (uintptr_t)d_scratch % 256u)) return refuse(FBX_E_ARG, "d_scratch is NULL or not 256-byte aligned");
+  if (scratch_bytes < l.bytes) return refuse(FBX_E_NOMEM, "scratch too small: fbx_embed_backward_scratch gives its size");
+  const hipStream_t stream = (hipStream_t)hip_stream;
+  char* scratch = (char*)d_scratch;
+  uint32_t* keys[2] = {(uint32_t*)(scratch + l.keys[0]), (uint32_t*)(scratch + l.keys[1])};
+  uint32_t* from[2] = {(uint32_t*)(scratch + l.from[0]), (uint32_t*)(scratch + l.from[1])};
+  uint32_t* counts = (uint32_t*)(scratch + l.counts);
+  uint32_t* totals = (uint32_t*)(scratch + l.totals);
+  float* share = mean ? (float*)(scratch + l.share) : nullptr;
+  int side = 0;
+  if (l.n) {
+    PairArgs p{};
+    p.keys = keys[0];
+    p.from = from[0];
+    p.share = share;
+    p.n_records = n_records;
+    p.all_slots = n_slots;
+    p.rows = (uint32_t)rows;
+    p.tile = arrival_tile_records;
+    uint32_t base = 0;
+    for (uint32_t s0 = 0; s0 < n_slots; s0 += kSlotsPerLaunch) {
+      p.first_slot = s0;
+      p.n_slots = n_slots - s0 < kSlotsPerLaunch ? n_slots - s0 : kSlotsPerLaunch;
+      for (uint32_t i = 0; i < p.n_slots; ++i) {
+        p.slots[i] = slot_ref(slots[s0 + i], base);
+        base += (uint32_t)slots[s0 + i].n_values;
+      }
+      hipLaunchKernelGGL(k_pairs, dim3((uint32_t)ceil_div(n_records, 256), p.n_slots), dim3(256), 0, stream, p);
+    }
+    for (uint32_t pass = 0; pass < l.passes; ++pass, side ^= 1) {
+      hipLaunchKernelGGL(k_digit_counts, dim3(l.n_tiles), dim3(256), 0, stream, keys[side], l.n, 8 * pass, l.n_tiles, counts);
+      hipLaunchKernelGGL(k_digit_sums, dim3(256), dim3(256), 0, stream, counts, l.n_tiles, totals);
+      hipLaunchKernelGGL(k_move_pairs, dim3(l.n_tiles), dim3(256), 0, stream, keys[side], from[side], l.n, 8 * pass, l.n_tiles, counts, totals,
+                         keys[side ^ 1], from[side ^ 1]);
+    }
+  }
+  const uint64_t all = (uintptr_t)d_dout | (uintptr_t)d_dtable | dim * e | table_stride * e | record_stride * e;
+  uint32_t n = 16u / e;
+  while (n > 1u && all % (n * e)) n /= 2u;
+  SumArgs a{};
+  a.keys = keys[side];
+  a.from = from[side];
+  a.share = share;
+  a.dout = d_dout;
+  a.dtable = d_dtable;
+  a.record_stride = record_stride;
+  a.table_stride = table_stride;
+  a.n = l.n;
+  a.n_records = (uint32_t)n_records;
+  a.all_slots = n_slots;
+  a.rows = (uint32_t)rows;
+  a.dim = dim;
+  while ((1u << a.lanes_log2) * n < dim && a.lanes_log2 < 6u) ++a.lanes_log2;
+  if (dtype == FBX_F32) sum_rows_by_width<float>(a, n, l, scratch, rows, stream);
+  else if (dtype == FBX_F16) sum_rows_by_width<_Float16>(a, n, l, scratch, rows, stream);
+  else sum_rows_by_width<__bf16>(a, n, l, scratch, rows, stream);
+  return launched();
+}
