@@ -1,6 +1,8 @@
 // The gated feed-forward block h = act(x Wg^T) * (x Wu^T) and its gradient.
 #include "train_common.h"
 
+#include <math.h>
+
 namespace fbx {
 namespace train {
 namespace {
@@ -27,93 +29,380 @@ __device__ __forceinline__ float slope(float a) {
   return s * (1.f - s);
 }
 
-enum Form { kForward, kSlopes, kPlain };
+// One launch's product: C (rows x columns) = A B^T over depth, A and B in one of two orders.
+//   kForward  A = x, B = the two weights side by side;  c: h
+//   kSlopes   the same product;  c: a row of da, then of du, each `half` elements wide (zeros beyond columns)
+//   kInputs   A = the rows kSlopes wrote, B = the weights, read along their rows;  c: dx
+//   kWeights  A = those rows and B = x, both read along their rows (depth: the records);  c, c2: dWg, dWu
+enum Form { kForward, kSlopes, kInputs, kWeights };
 
-// A rows x depth times the transpose of B columns x depth, element (i, k) of A at a[i * a_row + k * a_step].
 struct MmArgs {
-  const void *a, *b, *b2;    // kForward, kSlopes: b, b2 the two weights; kPlain: b2 the matrix that depth goes on with
-  uint64_t a_row, a_step, b_row, b_step, b2_row, b2_step;
-  const void* dh;            // kSlopes
-  void *c, *c2;              // kForward: h; kSlopes: da, du; kPlain: rows below split, and from it on
-  uint64_t ld_dh, ld_c, ld_c2;
-  uint64_t rows, columns, depth, depth2;  // (depth2: of b2)
-  uint64_t split;
+  const void *a, *b, *b2;
+  uint64_t ld_a, ld_b, ld_b2;  // in bytes
+  const void* dh;
+  void *c, *c2;
+  uint64_t ld_dh, ld_c, ld_c2;  // in elements
+  uint32_t rows, columns;      // of c (kForward, kSlopes: columns of each half; kWeights: rows of both weights, `half` apart)
+  uint32_t depth, half;        // half: width of a half of what kSlopes writes, whole steps of depth
+  uint32_t b_columns;          // kInputs, kWeights: elements in a row of B (a multiple of a load's)
+  uint32_t row_tiles, column_tiles, steps_each;  // steps_each: steps of depth that a share of it takes
+  uint32_t act, wide;          // wide: c (and dh) can be moved four elements at a time
+  float* parts;                // shares of depth: their sums, one array of rows x columns after the other; null: one share
 };
 
-constexpr int kTile = 64, kDeep = 16;
+constexpr uint32_t kOutside = 0xfffffff0u;  // an offset beyond every buffer
+constexpr int kStepBytes = 128;  // of depth that are staged at a time: 64 elements of 16 bits, 32 of 32
 
-template <class T, Form kForm, int kAct>
-__global__ __launch_bounds__(256) void k_mm(MmArgs p) {
-  constexpr int kCols = kForm == kPlain ? kTile : kTile / 2;
-  __shared__ float a_lds[kDeep][kTile + 4], b_lds[kDeep][kTile + 4];
-  const uint64_t i0 = (uint64_t)blockIdx.x * kTile, j0 = (uint64_t)blockIdx.y * kCols;
-  const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-  float sum[4][4] = {};
-  const uint64_t depth = p.depth + p.depth2;
-  for (uint64_t k0 = 0; k0 < depth; k0 += kDeep) {
-    for (int e = threadIdx.x; e < kTile * kDeep; e += 256) {
-      const int i = e / kDeep, k = e % kDeep;
-      const uint64_t kk = k0 + k;
-      float v = 0.f;
-      if (i0 + i < p.rows && kk < depth) v = (float)((const T*)p.a)[(i0 + i) * p.a_row + kk * p.a_step];
-      a_lds[k][i] = v;
-      v = 0.f;
-      if (kForm == kPlain) {
-        if (j0 + i < p.columns && kk < depth)
-          v = kk < p.depth ? (float)((const T*)p.b)[(j0 + i) * p.b_row + kk * p.b_step] : (float)((const T*)p.b2)[(j0 + i) * p.b2_row + (kk - p.depth) * p.b2_step];
-      } else if (kk < depth && j0 + i % kCols < p.columns) {
-        v = i < kCols ? (float)((const T*)p.b)[(j0 + i) * p.b_row + kk] : (float)((const T*)p.b2)[(j0 + i - kCols) * p.b2_row + kk];
-      }
-      b_lds[k][i] = v;
-    }
-    __syncthreads();
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+template <class T>
+struct Frag {
+  typedef T type __attribute__((ext_vector_type(16 / sizeof(T))));
+};
+typedef __attribute__((address_space(3))) void lds_void;
+typedef __attribute__((address_space(3))) char lds_char;
+
+// 16 x 16 of C += 16 of one side's rows x 16 of the other's over a load's depth (16 bytes a lane): lane l holds row l % 16
+// of either side and the depth's (l / 16)-th part; of C, column l % 16 and rows 4 (l / 16) .. + 3.
+__device__ __forceinline__ f32x4 mma(Frag<__bf16>::type a, Frag<__bf16>::type b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 mma(Frag<_Float16>::type a, Frag<_Float16>::type b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 mma(Frag<float>::type a, Frag<float>::type b, f32x4 c) {
 #pragma unroll
-    for (int k = 0; k < kDeep; ++k)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j)  // (columns tx, tx + 16 of each half)
-          sum[i][j] += a_lds[k][ty * 4 + i] * b_lds[k][tx + 16 * j];
-    __syncthreads();
+  for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], c, 0, 0, 0);
+  return c;
+}
+
+// A tile of one operand in LDS: kStepBytes of depth for R rows, R * 128 bytes, filled by loads that go past the
+// registers: lane l's 16 bytes land at 16 l behind the wavefront's place, so the layout is made by which 16 bytes a lane asks for.
+//   along depth (kAcross = false): a row's 128 bytes are eight chunks, chunk c of row r at place c ^ (r % 8), so that the 16
+//     rows a read takes the same chunk of lie in different banks;
+//   across (kAcross = true): for every element of depth a line of R elements, sixteen to a unit, unit u of line k at
+//     place u ^ turn(k), so that the lines a transposing read takes the same unit of lie in different banks.
+// What lies outside the operand is asked for beyond the buffer's end, which gives zeros.
+template <class T, int R, int kWaves, bool kAcross>
+struct Tile {
+  static constexpr int kSize = sizeof(T), kDepth = kStepBytes / kSize, kLoads = R * kStepBytes / 1024 / kWaves, kUnits = R / 16;
+  static_assert(kLoads >= 1, "");
+
+  __device__ static uint32_t turn(uint32_t k) {
+    if (kSize == 4) return (k >> 2) & 3u;
+    if (R == 64) return ((k >> 1) & 1u) | ((k >> 3) & 1u) << 1;
+    return (k & 3u) | ((k >> 3) & 1u) << 2;
   }
-  for (int i = 0; i < 4; ++i) {
-    const uint64_t r = i0 + ty * 4 + i;
-    if (r >= p.rows) break;
-    if (kForm == kPlain) {
-      T* c = r < p.split ? (T*)p.c + r * p.ld_c : (T*)p.c2 + (r - p.split) * p.ld_c2;
-      for (int j = 0; j < 4; ++j)
-        if (j0 + tx + 16 * j < p.columns) c[j0 + tx + 16 * j] = (T)sum[i][j];
+
+  uint32_t offset[kLoads];  // bytes from the tile's first element
+  uint32_t deep;            // along depth: the first element of depth that this lane's loads take
+
+  // wave: of kWaves; columns_left (across): elements from the tile's first to the operand's last
+  __device__ void begin(uint32_t wave, uint32_t lane, uint64_t ld, uint32_t columns_left) {
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      const uint32_t piece = wave * kLoads + j;  // 1024 bytes of the tile
+      if (!kAcross) {
+        const uint32_t chunk = (lane % 8u) ^ (lane / 8u);
+        deep = chunk * (16 / kSize);
+        offset[j] = (piece * 8u + lane / 8u) * (uint32_t)ld + chunk * 16u;
+      } else {
+        constexpr uint32_t chunks = R * kSize / 16;  // of a line
+        const uint32_t at = piece * 64u + lane, k = at / chunks, c = at % chunks;
+        const uint32_t column = (((c / kSize) ^ turn(k)) * kSize + c % kSize) * (16 / kSize);
+        offset[j] = column < columns_left ? k * (uint32_t)ld + column * kSize : kOutside;
+      }
+    }
+  }
+  // from: the tile's first element at this step; lines: rows (along) or elements of depth (across) there are from it on;
+  // depth_left (along): elements of depth from this step on
+  __device__ void load(lds_char* to, const char* from, uint64_t ld, uint32_t lines, uint32_t depth_left, uint32_t line_bytes, uint32_t wave) const {
+    const uint32_t most = kAcross ? (uint32_t)kDepth : (uint32_t)R, n = lines < most ? lines : most;
+    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)from, 0, n ? (n - 1u) * (uint32_t)ld + line_bytes : 0u, 0x00020000);
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(to + (wave * kLoads + j) * 1024), 16, kAcross || deep < depth_left ? offset[j] : kOutside, 0, 0, 0);
+  }
+
+  // Rows first .. first + 15 of the operand, part `part` (0, 1) of the step's depth.
+  __device__ static typename Frag<T>::type read(const lds_char* tile, uint32_t first, int part, uint32_t lane) {
+    typedef typename Frag<T>::type F;
+    const uint32_t i = lane % 16u, g = lane / 16u;
+    if constexpr (!kAcross) {
+      return *(const __attribute__((address_space(3))) F*)(tile + (first + i) * kStepBytes + (((4u * part + g) ^ (i & 7u)) * 16u));
+    } else if constexpr (kSize == 4) {
+      F f;
+#pragma unroll
+      for (uint32_t j = 0; j < 4u; ++j)
+        f[j] = *(const __attribute__((address_space(3))) float*)(tile + (part * 16u + 4u * g + j) * (R * 4u) + ((first / 16u) ^ g) * 64u + i * 4u);
+      return f;
     } else {
-      for (int j = 0; j < 2; ++j) {
-        const uint64_t at = j0 + tx + 16 * j;
-        if (at >= p.columns) continue;
-        const float g = sum[i][j], u = sum[i][j + 2];
+      typedef short s16x4 __attribute__((ext_vector_type(4)));
+      typedef short s16x8 __attribute__((ext_vector_type(8)));
+      s16x4 h[2];
+#pragma unroll
+      for (uint32_t q = 0; q < 2u; ++q) {
+        const uint32_t k = part * 32u + 8u * g + 4u * q + i / 4u;
+        h[q] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(tile + k * (R * 2u) + ((first / 16u) ^ turn(k)) * 32u + (i % 4u) * 8u));
+      }
+      return __builtin_bit_cast(F, (s16x8)__builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+  }
+};
+
+__device__ __forceinline__ float act(uint32_t kind, float a) {
+  return kind == FBX_ACT_SILU ? act<FBX_ACT_SILU>(a) : kind == FBX_ACT_GELU ? act<FBX_ACT_GELU>(a) : kind == FBX_ACT_RELU ? act<FBX_ACT_RELU>(a) : act<FBX_ACT_SIGMOID>(a);
+}
+__device__ __forceinline__ float slope(uint32_t kind, float a) {
+  return kind == FBX_ACT_SILU ? slope<FBX_ACT_SILU>(a) : kind == FBX_ACT_GELU ? slope<FBX_ACT_GELU>(a) : kind == FBX_ACT_RELU ? slope<FBX_ACT_RELU>(a) : slope<FBX_ACT_SIGMOID>(a);
+}
+
+// Four adjacent elements, of which the first n exist.
+template <class T>
+__device__ __forceinline__ void put(T* to, f32x4 v, uint32_t n, bool wide) {
+  if (wide && n >= 4u) {
+    *(Pack<T, 4>*)to = Pack<T, 4>{{(T)v[0], (T)v[1], (T)v[2], (T)v[3]}};
+  } else {
+#pragma unroll
+    for (uint32_t j = 0; j < 4u; ++j)
+      if (j < n) to[j] = (T)v[j];
+  }
+}
+
+// BM x BN of C a workgroup, its WM x WN wavefronts side by side.  C's rows come from A; its columns from B, which is the
+// first side of the matrix instructions, so that a lane holds four adjacent columns of a row.
+template <class T, Form kForm, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(WM * WN * 64) void k_mm(MmArgs p) {
+#ifdef __HIP_DEVICE_COMPILE__  // (the host's pass, which makes the launch stub of it, does not know the buffer's type)
+  constexpr bool kTwo = kForm == kForward || kForm == kSlopes;
+  constexpr int kWaves = WM * WN, kRows = BM / WM, kCols = BN / WN, kMF = kRows / 16, kNF = kCols / 16;
+  constexpr int kDepth = kStepBytes / sizeof(T);
+  typedef Tile<T, BM, kWaves, kForm == kWeights> TileA;
+  typedef Tile<T, BN, kWaves, !kTwo> TileB;
+  __shared__ alignas(1024) char a0[BM * kStepBytes], b0[BN * kStepBytes], a1[BM * kStepBytes], b1[BN * kStepBytes];
+  const uint32_t lane = threadIdx.x % 64u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64u), wm = wave % WM, wn = wave / WM;
+
+  // Workgroups are handed to the eight dies in turn: each die takes a stretch of the tiles, eight row tiles wide, so that
+  // those at work on it at one time share rows of both sides in its cache.
+  const uint32_t tiles = p.row_tiles * p.column_tiles;
+  uint32_t t = blockIdx.x;
+  {
+    const uint32_t each = tiles / 8u, more = tiles % 8u, die = t % 8u, k = t / 8u;
+    t = die * each + (die < more ? die : more) + k;
+  }
+  const uint32_t band = t / (8u * p.column_tiles), in_band = t - band * 8u * p.column_tiles;
+  const uint32_t high = p.row_tiles - band * 8u < 8u ? p.row_tiles - band * 8u : 8u;
+  const uint32_t row0 = (band * 8u + in_band % high) * BM, col0 = in_band / high * (kTwo ? BN / 2 : BN);
+
+  TileA ta;
+  TileB tb;
+  const bool up = kTwo && wave >= kWaves / 2;  // this wavefront loads of Wu
+  const char *a = (const char*)p.a, *b = (const char*)(up ? p.b2 : p.b);
+  const uint64_t ld_b = up ? p.ld_b2 : p.ld_b;
+  uint32_t b_lines = 0;
+  if (kForm == kWeights) {
+    a += (uint64_t)row0 * sizeof(T);
+    ta.begin(wave, lane, p.ld_a, 2 * p.half - row0);
+  } else {
+    a += (uint64_t)row0 * p.ld_a;
+    ta.begin(wave, lane, p.ld_a, 0);
+  }
+  if (kTwo) {
+    b += (uint64_t)col0 * ld_b;
+    b_lines = col0 < p.columns ? p.columns - col0 : 0u;
+    tb.begin(up ? wave - kWaves / 2 : wave, lane, ld_b, 0);
+  } else {
+    b += (uint64_t)col0 * sizeof(T);
+    tb.begin(wave, lane, ld_b, p.b_columns - col0);
+  }
+  const uint32_t turn = kForm == kInputs ? p.half / kDepth : 0u;  // kInputs: the first step whose lines are Wu's
+  const uint32_t all_steps = kForm == kInputs ? 2 * turn : (p.depth + kDepth - 1) / kDepth;
+  const uint32_t first = blockIdx.y * p.steps_each, end = all_steps - first < p.steps_each ? all_steps : first + p.steps_each;
+
+  auto load = [&](char* to_a, char* to_b, uint32_t step) {
+    if (kTwo) {
+      const uint32_t left = p.depth - step * kDepth;
+      ta.load((lds_char*)to_a, a + step * kStepBytes, p.ld_a, p.rows - row0, left, left * sizeof(T), wave);
+      tb.load((lds_char*)to_b, b + step * kStepBytes, ld_b, b_lines, left, left * sizeof(T), wave);
+    } else if (kForm == kInputs) {
+      const uint32_t left = 2 * p.half - step * kDepth, k = step * kDepth;
+      ta.load((lds_char*)to_a, a + step * kStepBytes, p.ld_a, p.rows - row0, left, left * sizeof(T), wave);
+      // (the weights one below the other, each made up to `half` lines: a step's lines are of one of them)
+      const bool second = step >= turn;
+      const uint32_t line = second ? k - p.half : k;
+      if (second && (step == turn || step == first)) tb.begin(wave, lane, p.ld_b2, p.b_columns - col0);
+      tb.load((lds_char*)to_b, (const char*)(second ? p.b2 : p.b) + (uint64_t)col0 * sizeof(T) + (uint64_t)line * (second ? p.ld_b2 : p.ld_b), second ? p.ld_b2 : p.ld_b,
+              p.depth - line, 0, (p.b_columns - col0) * sizeof(T), wave);
+    } else {
+      const uint32_t left = p.depth - step * kDepth;
+      ta.load((lds_char*)to_a, a + (uint64_t)step * kDepth * p.ld_a, p.ld_a, left, 0, (2 * p.half - row0) * sizeof(T), wave);
+      tb.load((lds_char*)to_b, b + (uint64_t)step * kDepth * p.ld_b, p.ld_b, left, 0, (p.b_columns - col0) * sizeof(T), wave);
+    }
+  };
+
+  f32x4 sum[kNF][kMF] = {};
+  auto multiply = [&](const char* in_a, const char* in_b) {
+#pragma unroll
+    for (int part = 0; part < 2; ++part) {
+      typename Frag<T>::type fa[kMF], fb[kNF];
+#pragma unroll
+      for (int i = 0; i < kMF; ++i) fa[i] = TileA::read((const lds_char*)in_a, wm * kRows + i * 16, part, lane);
+#pragma unroll
+      for (int j = 0; j < kNF; ++j) {
+        const uint32_t at = !kTwo ? wn * kCols + j * 16 : wn * (kCols / 2) + j % (kNF / 2) * 16 + j / (kNF / 2) * (BN / 2);
+        fb[j] = TileB::read((const lds_char*)in_b, at, part, lane);
+      }
+#pragma unroll
+      for (int j = 0; j < kNF; ++j)
+#pragma unroll
+        for (int i = 0; i < kMF; ++i) sum[j][i] = mma(fb[j], fa[i], sum[j][i]);
+    }
+  };
+  auto arrived = [] {  // (loads that go past the registers are not among what a barrier waits for)
+    __builtin_amdgcn_s_waitcnt(0x0f70);
+    __syncthreads();
+  };
+  if (first < end) load(a0, b0, first);
+  arrived();
+  for (uint32_t s = first; s < end; s += 2) {
+    if (s + 1 < end) load(a1, b1, s + 1);
+    multiply(a0, b0);
+    arrived();
+    if (s + 1 < end) {
+      if (s + 2 < end) load(a0, b0, s + 2);
+      multiply(a1, b1);
+      arrived();
+    }
+  }
+
+#pragma unroll
+  for (int i = 0; i < kMF; ++i) {
+    const uint32_t r = row0 + wm * kRows + i * 16 + lane % 16u;
+    if (kTwo) {
+      if (r >= p.rows) continue;
+#pragma unroll
+      for (int j = 0; j < kNF / 2; ++j) {
+        const uint32_t c = col0 + wn * (kCols / 2) + j * 16 + lane / 16u * 4u;
+        const uint32_t n = c < p.columns ? p.columns - c : 0u;
+        const f32x4 g = sum[j][i], u = sum[j + kNF / 2][i];
         if (kForm == kForward) {
-          ((T*)p.c)[r * p.ld_c + at] = (T)(act<kAct>(g) * u);
+          f32x4 h;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) h[e] = act(p.act, g[e]) * u[e];
+          put((T*)p.c + (uint64_t)r * p.ld_c + c, h, n, p.wide);
+        } else if (c < p.half) {
+          const T* from = (const T*)p.dh + (uint64_t)r * p.ld_dh + c;
+          Pack<T, 4> dh{};
+          if (p.wide && n >= 4u) {
+            dh = *(const Pack<T, 4>*)from;
+          } else {
+#pragma unroll
+            for (uint32_t e = 0; e < 4u; ++e)
+              if (e < n) dh.v[e] = from[e];
+          }
+          f32x4 da, du;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            da[e] = (float)dh.v[e] * u[e] * slope(p.act, g[e]);
+            du[e] = (float)dh.v[e] * act(p.act, g[e]);
+          }
+          put((T*)p.c + (uint64_t)r * p.ld_c + c, da, 4u, true);
+          put((T*)p.c + (uint64_t)r * p.ld_c + p.half + c, du, 4u, true);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < kNF; ++j) {
+        const uint32_t c = col0 + wn * kCols + j * 16 + lane / 16u * 4u;
+        if (c >= p.columns) continue;
+        if (kForm == kInputs) {
+          if (r >= p.rows) continue;
+          if (p.parts) put(p.parts + ((uint64_t)blockIdx.y * p.rows + r) * p.columns + c, sum[j][i], p.columns - c, p.columns % 4u == 0u);
+          else put((T*)p.c + (uint64_t)r * p.ld_c + c, sum[j][i], p.columns - c, p.wide);
         } else {
-          const float dh = (float)((const T*)p.dh)[r * p.ld_dh + at];
-          ((T*)p.c)[r * p.ld_c + at] = (T)(dh * u * slope<kAct>(g));
-          ((T*)p.c2)[r * p.ld_c2 + at] = (T)(dh * act<kAct>(g));
+          const uint32_t weight = r >= p.half ? 1u : 0u, row = r - weight * p.half;
+          if (row >= p.rows) continue;
+          if (p.parts) put(p.parts + ((uint64_t)(blockIdx.y * 2u + weight) * p.rows + row) * p.columns + c, sum[j][i], p.columns - c, p.columns % 4u == 0u);
+          else if (weight) put((T*)p.c2 + (uint64_t)row * p.ld_c2 + c, sum[j][i], p.columns - c, p.wide);
+          else put((T*)p.c + (uint64_t)row * p.ld_c + c, sum[j][i], p.columns - c, p.wide);
         }
       }
     }
   }
+#else
+  (void)p;
+#endif
+}
+
+// Adds the sums of shares up, in their order.
+template <class T>
+__global__ __launch_bounds__(256) void k_add_parts(const float* parts, uint32_t shares, uint64_t each, uint32_t rows, uint32_t columns, void* c, uint64_t ld_c, void* c2,
+                                                   uint64_t ld_c2) {
+  const uint64_t i = (uint64_t)blockIdx.x * 256u + threadIdx.x;
+  if (i >= each) return;
+  float sum = 0.f;
+  for (uint32_t s = 0; s < shares; ++s) sum += parts[s * each + i];
+  uint64_t r = i / columns;
+  const uint64_t at = i - r * columns;
+  if (r < rows) ((T*)c)[r * ld_c + at] = (T)sum;
+  else ((T*)c2)[(r - rows) * ld_c2 + at] = (T)sum;
+}
+
+// Rows of n elements, each made `to` bytes long with zeros behind.
+template <class T>
+__global__ __launch_bounds__(256) void k_pad_rows(const T* from, uint64_t ld, uint32_t n, T* to, uint32_t wide, uint64_t all) {
+  const uint64_t i = (uint64_t)blockIdx.x * 256u + threadIdx.x;
+  if (i >= all) return;
+  const uint64_t r = i / wide;
+  const uint32_t c = (uint32_t)(i - r * wide);
+  to[i] = c < n ? from[r * ld + c] : (T)0.f;
+}
+
+// How a product is cut: tiles of C, and shares of depth where there are too few of those to fill the card.
+struct Cut {
+  uint32_t size;    // 0: 256 x 256, 1: 128 x 128, 2: 64 x 64
+  uint32_t row_tiles, column_tiles, shares, steps_each;
+};
+constexpr uint32_t kSide[3] = {256, 128, 64};
+
+Cut cut(uint64_t rows, uint64_t columns, uint64_t steps, bool shares) {
+  Cut c{};
+  for (c.size = 0; c.size < 2; ++c.size)
+    if (ceil_div(rows, kSide[c.size]) * ceil_div(columns, kSide[c.size]) >= 256) break;
+  c.row_tiles = (uint32_t)ceil_div(rows, kSide[c.size]);
+  c.column_tiles = (uint32_t)ceil_div(columns, kSide[c.size]);
+  uint64_t n = 1;
+  if (shares) {
+    const uint64_t tiles = (uint64_t)c.row_tiles * c.column_tiles;
+    while (tiles * n < 256 && steps / (2 * n) >= 8) n *= 2;
+  }
+  c.steps_each = (uint32_t)(steps ? ceil_div(steps, n) : 1);
+  c.shares = (uint32_t)(steps ? ceil_div(steps, c.steps_each) : 1);
+  return c;
 }
 
 template <class T, Form kForm>
-void launch(const MmArgs& p, fbx_act act, hipStream_t stream) {
-  const dim3 grid((uint32_t)ceil_div(p.rows, kTile), (uint32_t)ceil_div(p.columns, kForm == kPlain ? kTile : kTile / 2));
-  if (kForm == kPlain || act == FBX_ACT_SILU) hipLaunchKernelGGL((k_mm<T, kForm, FBX_ACT_SILU>), grid, dim3(256), 0, stream, p);
-  else if (act == FBX_ACT_GELU) hipLaunchKernelGGL((k_mm<T, kForm, FBX_ACT_GELU>), grid, dim3(256), 0, stream, p);
-  else if (act == FBX_ACT_RELU) hipLaunchKernelGGL((k_mm<T, kForm, FBX_ACT_RELU>), grid, dim3(256), 0, stream, p);
-  else hipLaunchKernelGGL((k_mm<T, kForm, FBX_ACT_SIGMOID>), grid, dim3(256), 0, stream, p);
+void launch(MmArgs& p, const Cut& c, hipStream_t stream) {
+  p.row_tiles = c.row_tiles;
+  p.column_tiles = c.column_tiles;
+  p.steps_each = c.steps_each;
+  const dim3 grid(c.row_tiles * c.column_tiles, c.shares);
+  if (c.size == 0) hipLaunchKernelGGL((k_mm<T, kForm, 256, 256, 2, 4>), grid, dim3(512), 0, stream, p);
+  else if (c.size == 1) hipLaunchKernelGGL((k_mm<T, kForm, 128, 128, 2, 2>), grid, dim3(256), 0, stream, p);
+  else hipLaunchKernelGGL((k_mm<T, kForm, 64, 64, 2, 2>), grid, dim3(256), 0, stream, p);
 }
 
 template <Form kForm>
-void launch_by_type(const MmArgs& p, fbx_dtype t, fbx_act act, hipStream_t stream) {
-  if (t == FBX_F32) launch<float, kForm>(p, act, stream);
-  else if (t == FBX_F16) launch<_Float16, kForm>(p, act, stream);
-  else launch<__bf16, kForm>(p, act, stream);
+void launch_by_type(MmArgs& p, const Cut& c, fbx_dtype t, hipStream_t stream) {
+  if (t == FBX_F32) launch<float, kForm>(p, c, stream);
+  else if (t == FBX_F16) launch<_Float16, kForm>(p, c, stream);
+  else launch<__bf16, kForm>(p, c, stream);
+}
+
+template <class T>
+void add_parts(const MmArgs& p, const Cut& c, uint64_t rows_of_both, hipStream_t stream) {
+  const uint64_t each = rows_of_both * p.columns;
+  hipLaunchKernelGGL((k_add_parts<T>), dim3((uint32_t)ceil_div(each, 256)), dim3(256), 0, stream, p.parts, c.shares, each, p.rows, p.columns, p.c, p.ld_c, p.c2, p.ld_c2);
+}
+void add_parts_by_type(const MmArgs& p, const Cut& c, fbx_dtype t, uint64_t rows_of_both, hipStream_t stream) {
+  if (t == FBX_F32) add_parts<float>(p, c, rows_of_both, stream);
+  else if (t == FBX_F16) add_parts<_Float16>(p, c, rows_of_both, stream);
+  else add_parts<__bf16>(p, c, rows_of_both, stream);
 }
 
 fbx_status check(const fbx_gated* g) {
@@ -131,6 +420,80 @@ fbx_status check_pointers(const fbx_gated* g, uintptr_t others) {
   if (((uintptr_t)g->d_x | (uintptr_t)g->d_w_gate | (uintptr_t)g->d_w_up | others) % size_of(g->dtype)) return refuse(FBX_E_ARG, "a matrix is not aligned to its elements");
   return FBX_OK;
 }
+// What a call keeps in its scratch, and what the kernels read: a matrix whose rows are not whole 16-byte loads (its
+// address, its stride or its width) is first copied to one whose are.
+struct Shape {
+  uint32_t size, lanes;        // bytes of an element; elements of a load
+  uint32_t wide;               // inputs, rounded up to whole loads
+  uint32_t half;               // hidden, rounded up to a step of depth
+  bool pad[3];                 // x, w_gate, w_up
+  uint64_t at[3], slopes, parts, bytes;
+  Cut forward, inputs, weights;
+  bool fits() const {  // a grid's limit
+    const Cut all[3] = {forward, inputs, weights};
+    for (const Cut& c : all)
+      if ((uint64_t)c.row_tiles * c.column_tiles >> 31) return false;
+    return true;
+  }
+};
+
+Shape shape_of(const fbx_gated* g, bool backward) {
+  Shape s{};
+  s.size = size_of(g->dtype);
+  s.lanes = 16u / s.size;
+  s.wide = (uint32_t)round_up(g->inputs, s.lanes);
+  s.half = (uint32_t)round_up(g->hidden, kStepBytes / s.size);
+  const void* from[3] = {g->d_x, g->d_w_gate, g->d_w_up};
+  const uint64_t ld[3] = {g->ld_x, g->ld_w_gate, g->ld_w_up};
+  auto take = [&](uint64_t bytes) {
+    const uint64_t was = s.bytes;
+    s.bytes = round_up(s.bytes + bytes, 256);
+    return was;
+  };
+  for (int i = 0; i < 3; ++i) {
+    s.pad[i] = g->inputs % s.lanes || ld[i] % s.lanes || (uintptr_t)from[i] % 16u;
+    s.at[i] = take(s.pad[i] ? (i ? g->hidden : g->records) * (uint64_t)s.wide * s.size : 0);
+  }
+  const uint64_t depth = kStepBytes / s.size;
+  s.forward = cut(g->records, 2ull * (backward ? s.half : g->hidden), ceil_div(s.wide, depth), false);
+  if (backward) {
+    s.slopes = take(g->records * 2ull * s.half * s.size);
+    s.inputs = cut(g->records, g->inputs, 2ull * s.half / depth, true);
+    s.weights = cut(2ull * s.half, g->inputs, ceil_div(g->records, depth), true);
+    const uint64_t a = s.inputs.shares > 1 ? s.inputs.shares * g->records * g->inputs : 0, b = s.weights.shares > 1 ? s.weights.shares * 2ull * g->hidden * g->inputs : 0;
+    s.parts = take(4 * (a > b ? a : b));
+  }
+  return s;
+}
+
+template <class T>
+void pad_rows(const void* from, uint64_t ld, uint32_t n, void* to, uint32_t wide, uint64_t rows, hipStream_t stream) {
+  const uint64_t all = rows * wide;
+  if (all) hipLaunchKernelGGL((k_pad_rows<T>), dim3((uint32_t)ceil_div(all, 256)), dim3(256), 0, stream, (const T*)from, ld, n, (T*)to, wide, all);
+}
+
+// Fills in where the kernels read x and the weights, copying those that need it.
+void operands(const fbx_gated* g, const Shape& s, char* scratch, const void* (&from)[3], uint64_t (&ld)[3], hipStream_t stream) {
+  from[0] = g->d_x;
+  from[1] = g->d_w_gate;
+  from[2] = g->d_w_up;
+  ld[0] = g->ld_x;
+  ld[1] = g->ld_w_gate;
+  ld[2] = g->ld_w_up;
+  for (int i = 0; i < 3; ++i) {
+    if (s.pad[i]) {
+      char* to = scratch + s.at[i];
+      if (s.size == 4u) pad_rows<float>(from[i], ld[i], g->inputs, to, s.wide, i ? g->hidden : g->records, stream);
+      else pad_rows<_Float16>(from[i], ld[i], g->inputs, to, s.wide, i ? g->hidden : g->records, stream);
+      from[i] = to;
+      ld[i] = s.wide;
+    }
+    ld[i] *= s.size;
+  }
+}
+
+bool four_at_a_time(const void* p, uint64_t ld, uint32_t size) { return (uintptr_t)p % (4 * size) == 0 && ld % 4 == 0; }
+
 fbx_status check_scratch(const fbx_gated* g, int backward, const void* d_scratch, uint64_t scratch_bytes) {
   uint64_t need = 0;
   fbx_gated_scratch(g, backward, &need);
@@ -148,7 +511,7 @@ extern "C" fbx_status fbx_gated_scratch(const fbx_gated* g, int backward, uint64
   const fbx_status st = check(g);
   if (st != FBX_OK) return st;
   if (!bytes) return refuse(FBX_E_ARG, "bytes is NULL");
-  *bytes = backward ? round_up(2ull * g->records * g->hidden * size_of(g->dtype), 256) : 0;
+  *bytes = shape_of(g, backward != 0).bytes;
   return FBX_OK;
 }
 
@@ -160,20 +523,27 @@ extern "C" fbx_status fbx_gated_forward(const fbx_gated* g, void* d_h, uint64_t 
   if (ld_h < g->hidden || ld_h >> 22) return refuse(FBX_E_ARG, "ld_h is smaller than hidden, or 2^22 or more");
   if (!g->records) return FBX_OK;
   if (!d_h) return refuse(FBX_E_ARG, "d_h is NULL");
+  const hipStream_t stream = (hipStream_t)hip_stream;
+  const Shape s = shape_of(g, false);
+  if (!s.fits()) return refuse(FBX_E_ARG, "records x hidden is too large for one call");
+  const void* from[3];
+  uint64_t ld[3];
+  operands(g, s, (char*)d_scratch, from, ld, stream);
   MmArgs p{};
-  p.a = g->d_x;
-  p.a_row = g->ld_x;
-  p.a_step = 1;
-  p.b = g->d_w_gate;
-  p.b_row = g->ld_w_gate;
-  p.b2 = g->d_w_up;
-  p.b2_row = g->ld_w_up;
+  p.a = from[0];
+  p.b = from[1];
+  p.b2 = from[2];
+  p.ld_a = ld[0];
+  p.ld_b = ld[1];
+  p.ld_b2 = ld[2];
   p.c = d_h;
   p.ld_c = ld_h;
-  p.rows = g->records;
+  p.rows = (uint32_t)g->records;
   p.columns = g->hidden;
-  p.depth = g->inputs;
-  launch_by_type<kForward>(p, g->dtype, g->act, (hipStream_t)hip_stream);
+  p.depth = s.wide;
+  p.act = g->act;
+  p.wide = four_at_a_time(d_h, ld_h, s.size);
+  launch_by_type<kForward>(p, s.forward, g->dtype, stream);
   return launched();
 }
 
@@ -190,61 +560,74 @@ extern "C" fbx_status fbx_gated_backward(const fbx_gated* g, const void* d_dh, u
   if (g->records && !d_dh) return refuse(FBX_E_ARG, "d_dh is NULL");
   st = check_scratch(g, 1, d_scratch, scratch_bytes);
   if (st != FBX_OK) return st;
+  if (!d_dx && !d_dw_gate) return FBX_OK;
   const hipStream_t stream = (hipStream_t)hip_stream;
-  const uint64_t n = g->hidden, wide = 2 * n;
-  char* slopes = (char*)d_scratch;  // a row: da, then du
-  MmArgs p{};
-  p.a = g->d_x;
-  p.a_row = g->ld_x;
-  p.a_step = 1;
-  p.b = g->d_w_gate;
-  p.b_row = g->ld_w_gate;
-  p.b2 = g->d_w_up;
-  p.b2_row = g->ld_w_up;
-  p.dh = d_dh;
-  p.ld_dh = ld_dh;
-  p.c = slopes;
-  p.c2 = slopes + n * size_of(g->dtype);
-  p.ld_c = p.ld_c2 = wide;
-  p.rows = g->records;
-  p.columns = n;
-  p.depth = g->inputs;
-  if (g->records && (d_dx || d_dw_gate)) launch_by_type<kSlopes>(p, g->dtype, g->act, stream);
+  const Shape s = shape_of(g, true);
+  if (!s.fits()) return refuse(FBX_E_ARG, "records x hidden is too large for one call");
+  char* scratch = (char*)d_scratch;
+  const void* from[3];
+  uint64_t ld[3];
+  operands(g, s, scratch, from, ld, stream);
+  float* parts = (float*)(scratch + s.parts);
+  if (g->records) {
+    MmArgs p{};
+    p.a = from[0];
+    p.b = from[1];
+    p.b2 = from[2];
+    p.ld_a = ld[0];
+    p.ld_b = ld[1];
+    p.ld_b2 = ld[2];
+    p.dh = d_dh;
+    p.ld_dh = ld_dh;
+    p.c = scratch + s.slopes;
+    p.ld_c = 2ull * s.half;
+    p.rows = (uint32_t)g->records;
+    p.columns = g->hidden;
+    p.half = s.half;
+    p.depth = s.wide;
+    p.act = g->act;
+    p.wide = four_at_a_time(d_dh, ld_dh, s.size);
+    launch_by_type<kSlopes>(p, s.forward, g->dtype, stream);
+  }
   if (g->records && d_dx) {
-    MmArgs q{};
-    q.a = slopes;
-    q.a_row = wide;
-    q.a_step = 1;
-    q.b = g->d_w_gate;
-    q.b_row = 1;
-    q.b_step = g->ld_w_gate;
-    q.b2 = g->d_w_up;
-    q.b2_row = 1;
-    q.b2_step = g->ld_w_up;
-    q.c = d_dx;
-    q.ld_c = ld_dx;
-    q.rows = q.split = g->records;
-    q.columns = g->inputs;
-    q.depth = q.depth2 = n;
-    launch_by_type<kPlain>(q, g->dtype, g->act, stream);
+    MmArgs p{};
+    p.a = scratch + s.slopes;
+    p.ld_a = 2ull * s.half * s.size;
+    p.b = from[1];
+    p.b2 = from[2];
+    p.ld_b = ld[1];
+    p.ld_b2 = ld[2];
+    p.c = d_dx;
+    p.ld_c = ld_dx;
+    p.rows = (uint32_t)g->records;
+    p.columns = g->inputs;
+    p.depth = g->hidden;
+    p.half = s.half;
+    p.b_columns = s.wide;
+    p.wide = four_at_a_time(d_dx, ld_dx, s.size);
+    p.parts = s.inputs.shares > 1 ? parts : nullptr;
+    launch_by_type<kInputs>(p, s.inputs, g->dtype, stream);
+    if (p.parts) add_parts_by_type(p, s.inputs, g->dtype, p.rows, stream);
   }
   if (d_dw_gate) {
-    MmArgs q{};
-    q.a = slopes;
-    q.a_row = 1;
-    q.a_step = wide;
-    q.b = g->d_x;
-    q.b_row = 1;
-    q.b_step = g->ld_x;
-    q.c = d_dw_gate;
-    q.ld_c = ld_dw_gate;
-    q.c2 = d_dw_up;
-    q.ld_c2 = ld_dw_up;
-    q.rows = wide;
-    q.split = n;
-    q.columns = g->inputs;
-    q.depth = g->records;
-    launch_by_type<kPlain>(q, g->dtype, g->act, stream);
+    MmArgs p{};
+    p.a = scratch + s.slopes;
+    p.ld_a = 2ull * s.half * s.size;
+    p.b = from[0];
+    p.ld_b = ld[0];
+    p.c = d_dw_gate;
+    p.ld_c = ld_dw_gate;
+    p.c2 = d_dw_up;
+    p.ld_c2 = ld_dw_up;
+    p.rows = g->hidden;
+    p.columns = g->inputs;
+    p.depth = (uint32_t)g->records;
+    p.half = s.half;
+    p.b_columns = s.wide;
+    p.wide = four_at_a_time(d_dw_gate, ld_dw_gate, s.size) && four_at_a_time(d_dw_up, ld_dw_up, s.size);
+    p.parts = s.weights.shares > 1 ? parts : nullptr;
+    launch_by_type<kWeights>(p, s.weights, g->dtype, stream);
+    if (p.parts) add_parts_by_type(p, s.weights, g->dtype, 2ull * p.rows, stream);
   }
   return launched();
 }

@@ -307,6 +307,16 @@ def test_gated_backward(shape, dtype):
         assert torch.equal(a, b), "the same inputs give the same bits"
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("shape", [(1030, 40, 2100), (2100, 72, 4100), (70, 2056, 1030), (4200, 4100, 40), (33, 4104, 2050), (20_000, 24, 40), (40, 24, 9000), (513, 1100, 1027)], ids=str)
+def test_gated_large(shape, dtype):
+    """Sizes at which tiles are larger, and at which the depth of a product is shared out."""
+    m, k, n = shape
+    x, wg, wu, dh = _inputs(m, k, n, dtype, m + 3 * n)
+    _check_forward(T.gated(x.cuda(), wg.cuda(), wu.cuda()), x, wg, wu, "silu")
+    _check_backward(T.gated_backward(dh.cuda(), x.cuda(), wg.cuda(), wu.cuda()), dh, x, wg, wu, "silu")
+
+
 @pytest.mark.parametrize("act", sorted(T.ACTS))
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
 def test_gated_activations(act, dtype):
