@@ -145,12 +145,10 @@ struct Tile {
   }
 };
 
-__device__ __forceinline__ float act(uint32_t kind, float a) {
-  return kind == FBX_ACT_SILU ? act<FBX_ACT_SILU>(a) : kind == FBX_ACT_GELU ? act<FBX_ACT_GELU>(a) : kind == FBX_ACT_RELU ? act<FBX_ACT_RELU>(a) : act<FBX_ACT_SIGMOID>(a);
-}
-__device__ __forceinline__ float slope(uint32_t kind, float a) {
-  return kind == FBX_ACT_SILU ? slope<FBX_ACT_SILU>(a) : kind == FBX_ACT_GELU ? slope<FBX_ACT_GELU>(a) : kind == FBX_ACT_RELU ? slope<FBX_ACT_RELU>(a) : slope<FBX_ACT_SIGMOID>(a);
-}
+template <int kAct>
+struct Kind {
+  static constexpr int value = kAct;
+};
 
 // Four adjacent elements, of which the first n exist.
 template <class T>
@@ -214,98 +212,135 @@ __global__ __launch_bounds__(WM * WN * 64) void k_mm(MmArgs p) {
   const uint32_t all_steps = kForm == kInputs ? 2 * turn : (p.depth + kDepth - 1) / kDepth;
   const uint32_t first = blockIdx.y * p.steps_each, end = all_steps - first < p.steps_each ? all_steps : first + p.steps_each;
 
-  auto load = [&](char* to_a, char* to_b, uint32_t step) {
+  auto load = [&](char* to_a, char* to_b, uint32_t s) {
     if (kTwo) {
-      const uint32_t left = p.depth - step * kDepth;
-      ta.load((lds_char*)to_a, a + step * kStepBytes, p.ld_a, p.rows - row0, left, left * sizeof(T), wave);
-      tb.load((lds_char*)to_b, b + step * kStepBytes, ld_b, b_lines, left, left * sizeof(T), wave);
+      const uint32_t left = p.depth - s * kDepth;
+      ta.load((lds_char*)to_a, a + s * kStepBytes, p.ld_a, p.rows - row0, left, left * sizeof(T), wave);
+      tb.load((lds_char*)to_b, b + s * kStepBytes, ld_b, b_lines, left, left * sizeof(T), wave);
     } else if (kForm == kInputs) {
-      const uint32_t left = 2 * p.half - step * kDepth, k = step * kDepth;
-      ta.load((lds_char*)to_a, a + step * kStepBytes, p.ld_a, p.rows - row0, left, left * sizeof(T), wave);
+      const uint32_t left = 2 * p.half - s * kDepth, k = s * kDepth;
+      ta.load((lds_char*)to_a, a + s * kStepBytes, p.ld_a, p.rows - row0, left, left * sizeof(T), wave);
       // (the weights one below the other, each made up to `half` lines: a step's lines are of one of them)
-      const bool second = step >= turn;
+      const bool second = s >= turn;
       const uint32_t line = second ? k - p.half : k;
-      if (second && (step == turn || step == first)) tb.begin(wave, lane, p.ld_b2, p.b_columns - col0);
+      if (second && (s == turn || s == first)) tb.begin(wave, lane, p.ld_b2, p.b_columns - col0);
       tb.load((lds_char*)to_b, (const char*)(second ? p.b2 : p.b) + (uint64_t)col0 * sizeof(T) + (uint64_t)line * (second ? p.ld_b2 : p.ld_b), second ? p.ld_b2 : p.ld_b,
               p.depth - line, 0, (p.b_columns - col0) * sizeof(T), wave);
     } else {
-      const uint32_t left = p.depth - step * kDepth;
-      ta.load((lds_char*)to_a, a + (uint64_t)step * kDepth * p.ld_a, p.ld_a, left, 0, (2 * p.half - row0) * sizeof(T), wave);
-      tb.load((lds_char*)to_b, b + (uint64_t)step * kDepth * p.ld_b, p.ld_b, left, 0, (p.b_columns - col0) * sizeof(T), wave);
+      const uint32_t left = p.depth - s * kDepth;
+      ta.load((lds_char*)to_a, a + (uint64_t)s * kDepth * p.ld_a, p.ld_a, left, 0, (2 * p.half - row0) * sizeof(T), wave);
+      tb.load((lds_char*)to_b, b + (uint64_t)s * kDepth * p.ld_b, p.ld_b, left, 0, (p.b_columns - col0) * sizeof(T), wave);
     }
   };
 
+  // Two halves of a step's depth in turn: while one is multiplied out of registers the other's rows are read from LDS.
+  // A step's barrier lies between the halves: behind it the next step's tile is there (its loads had a whole step) and
+  // nobody reads this step's any more, so the loads of the step after the next go there.
   f32x4 sum[kNF][kMF] = {};
-  auto multiply = [&](const char* in_a, const char* in_b) {
+  typename Frag<T>::type fa[2][kMF], fb[2][kNF];
+  auto read = [&](int part, const char* in_a, const char* in_b) {
 #pragma unroll
-    for (int part = 0; part < 2; ++part) {
-      typename Frag<T>::type fa[kMF], fb[kNF];
+    for (int i = 0; i < kMF; ++i) fa[part][i] = TileA::read((const lds_char*)in_a, wm * kRows + i * 16, part, lane);
 #pragma unroll
-      for (int i = 0; i < kMF; ++i) fa[i] = TileA::read((const lds_char*)in_a, wm * kRows + i * 16, part, lane);
+    for (int j = 0; j < kNF; ++j) {
+      const uint32_t at = !kTwo ? wn * kCols + j * 16 : wn * (kCols / 2) + j % (kNF / 2) * 16 + j / (kNF / 2) * (BN / 2);
+      fb[part][j] = TileB::read((const lds_char*)in_b, at, part, lane);
+    }
+  };
+  auto multiply = [&](int part) {
 #pragma unroll
-      for (int j = 0; j < kNF; ++j) {
-        const uint32_t at = !kTwo ? wn * kCols + j * 16 : wn * (kCols / 2) + j % (kNF / 2) * 16 + j / (kNF / 2) * (BN / 2);
-        fb[j] = TileB::read((const lds_char*)in_b, at, part, lane);
-      }
+    for (int j = 0; j < kNF; ++j)
 #pragma unroll
-      for (int j = 0; j < kNF; ++j)
+      for (int i = 0; i < kMF; ++i) sum[j][i] = mma(fb[part][j], fa[part][i], sum[j][i]);
+  };
+  auto mixed = [] {  // a read, then its share of the products
 #pragma unroll
-        for (int i = 0; i < kMF; ++i) sum[j][i] = mma(fb[j], fa[i], sum[j][i]);
+    for (int i = 0; i < kMF + kNF; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, kMF * kNF / (kMF + kNF), 0);
     }
   };
   auto arrived = [] {  // (loads that go past the registers are not among what a barrier waits for)
     __builtin_amdgcn_s_waitcnt(0x0f70);
     __syncthreads();
   };
-  if (first < end) load(a0, b0, first);
-  arrived();
-  for (uint32_t s = first; s < end; s += 2) {
-    if (s + 1 < end) load(a1, b1, s + 1);
-    multiply(a0, b0);
+  auto step = [&](char* at_a, char* at_b, const char* next_a, const char* next_b, uint32_t s) {
+    read(1, at_a, at_b);
+    multiply(0);
+    mixed();
+    __builtin_amdgcn_sched_barrier(0);
     arrived();
-    if (s + 1 < end) {
-      if (s + 2 < end) load(a0, b0, s + 2);
-      multiply(a1, b1);
-      arrived();
+    if (s + 2 < end) load(at_a, at_b, s + 2);
+    __builtin_amdgcn_sched_barrier(0);
+    read(0, next_a, next_b);  // (behind the last step: what is there, unused)
+    multiply(1);
+    mixed();
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  if (first < end) {
+    load(a0, b0, first);
+    if (first + 1 < end) load(a1, b1, first + 1);
+    arrived();
+    read(0, a0, b0);
+    for (uint32_t s = first; s < end; s += 2) {
+      step(a0, b0, a1, b1, s);
+      if (s + 1 < end) step(a1, b1, a0, b0, s + 1);
     }
   }
 
+  if constexpr (kTwo) {
+    auto finish = [&](auto kind) {
+      constexpr int kAct = decltype(kind)::value;
 #pragma unroll
-  for (int i = 0; i < kMF; ++i) {
-    const uint32_t r = row0 + wm * kRows + i * 16 + lane % 16u;
-    if (kTwo) {
-      if (r >= p.rows) continue;
+      for (int i = 0; i < kMF; ++i) {
+        const uint32_t r = row0 + wm * kRows + i * 16 + lane % 16u;
+        if (r >= p.rows) continue;
+        const uint32_t c0 = col0 + wn * (kCols / 2) + lane / 16u * 4u;
+        Pack<T, 4> dh[kNF / 2] = {};
+        if (kForm == kSlopes) {
 #pragma unroll
-      for (int j = 0; j < kNF / 2; ++j) {
-        const uint32_t c = col0 + wn * (kCols / 2) + j * 16 + lane / 16u * 4u;
-        const uint32_t n = c < p.columns ? p.columns - c : 0u;
-        const f32x4 g = sum[j][i], u = sum[j + kNF / 2][i];
-        if (kForm == kForward) {
-          f32x4 h;
+          for (int j = 0; j < kNF / 2; ++j) {
+            const uint32_t c = c0 + j * 16;
+            const T* from = (const T*)p.dh + (uint64_t)r * p.ld_dh + c;
+            if (p.wide && c + 4u <= p.columns) {
+              dh[j] = *(const Pack<T, 4>*)from;
+            } else {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) h[e] = act(p.act, g[e]) * u[e];
-          put((T*)p.c + (uint64_t)r * p.ld_c + c, h, n, p.wide);
-        } else if (c < p.half) {
-          const T* from = (const T*)p.dh + (uint64_t)r * p.ld_dh + c;
-          Pack<T, 4> dh{};
-          if (p.wide && n >= 4u) {
-            dh = *(const Pack<T, 4>*)from;
-          } else {
-#pragma unroll
-            for (uint32_t e = 0; e < 4u; ++e)
-              if (e < n) dh.v[e] = from[e];
+              for (uint32_t e = 0; e < 4u; ++e)
+                if (c + e < p.columns) dh[j].v[e] = from[e];
+            }
           }
-          f32x4 da, du;
+        }
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            da[e] = (float)dh.v[e] * u[e] * slope(p.act, g[e]);
-            du[e] = (float)dh.v[e] * act(p.act, g[e]);
+        for (int j = 0; j < kNF / 2; ++j) {
+          const uint32_t c = c0 + j * 16;
+          const f32x4 g = sum[j][i], u = sum[j + kNF / 2][i];
+          if (kForm == kForward) {
+            f32x4 h;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) h[e] = act<kAct>(g[e]) * u[e];
+            put((T*)p.c + (uint64_t)r * p.ld_c + c, h, c < p.columns ? p.columns - c : 0u, p.wide);
+          } else if (c < p.half) {
+            f32x4 da, du;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              da[e] = (float)dh[j].v[e] * u[e] * slope<kAct>(g[e]);
+              du[e] = (float)dh[j].v[e] * act<kAct>(g[e]);
+            }
+            put((T*)p.c + (uint64_t)r * p.ld_c + c, da, 4u, true);
+            put((T*)p.c + (uint64_t)r * p.ld_c + p.half + c, du, 4u, true);
           }
-          put((T*)p.c + (uint64_t)r * p.ld_c + c, da, 4u, true);
-          put((T*)p.c + (uint64_t)r * p.ld_c + p.half + c, du, 4u, true);
         }
       }
-    } else {
+    };
+    if (p.act == FBX_ACT_SILU) finish(Kind<FBX_ACT_SILU>());
+    else if (p.act == FBX_ACT_GELU) finish(Kind<FBX_ACT_GELU>());
+    else if (p.act == FBX_ACT_RELU) finish(Kind<FBX_ACT_RELU>());
+    else finish(Kind<FBX_ACT_SIGMOID>());
+  } else {
+#pragma unroll
+    for (int i = 0; i < kMF; ++i) {
+      const uint32_t r = row0 + wm * kRows + i * 16 + lane % 16u;
 #pragma unroll
       for (int j = 0; j < kNF; ++j) {
         const uint32_t c = col0 + wn * kCols + j * 16 + lane / 16u * 4u;
