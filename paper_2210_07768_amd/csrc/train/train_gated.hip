@@ -253,13 +253,6 @@ __global__ __launch_bounds__(WM * WN * 64) void k_mm(MmArgs p) {
 #pragma unroll
       for (int i = 0; i < kMF; ++i) sum[j][i] = mma(fb[part][j], fa[part][i], sum[j][i]);
   };
-  auto mixed = [] {  // a read, then its share of the products
-#pragma unroll
-    for (int i = 0; i < kMF + kNF; ++i) {
-      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x008, kMF * kNF / (kMF + kNF), 0);
-    }
-  };
   auto arrived = [] {  // (loads that go past the registers are not among what a barrier waits for)
     __builtin_amdgcn_s_waitcnt(0x0f70);
     __syncthreads();
@@ -267,14 +260,12 @@ __global__ __launch_bounds__(WM * WN * 64) void k_mm(MmArgs p) {
   auto step = [&](char* at_a, char* at_b, const char* next_a, const char* next_b, uint32_t s) {
     read(1, at_a, at_b);
     multiply(0);
-    mixed();
     __builtin_amdgcn_sched_barrier(0);
     arrived();
     if (s + 2 < end) load(at_a, at_b, s + 2);
     __builtin_amdgcn_sched_barrier(0);
     read(0, next_a, next_b);  // (behind the last step: what is there, unused)
     multiply(1);
-    mixed();
     __builtin_amdgcn_sched_barrier(0);
   };
   if (first < end) {
