@@ -29,6 +29,8 @@ __device__ __forceinline__ float slope(float a) {
   return s * (1.f - s);
 }
 
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
 // One launch's product: C (rows x columns) = A B^T over depth, A and B in one of two orders.
 //   kForward  A = x, B = the two weights side by side;  c: h
 //   kSlopes   the same product;  c: a row of da, then of du, each `half` elements wide (zeros beyond columns)
@@ -45,15 +47,15 @@ struct MmArgs {
   uint32_t rows, columns;      // of c (kForward, kSlopes: columns of each half; kWeights: rows of both weights, `half` apart)
   uint32_t depth, half;        // half: width of a half of what kSlopes writes, whole steps of depth
   uint32_t b_columns;          // kInputs, kWeights: elements in a row of B (a multiple of a load's)
-  uint32_t row_tiles, column_tiles, steps_each;  // steps_each: steps of depth that a share of it takes
   uint32_t act, wide;          // wide: c (and dh) can be moved four elements at a time
-  float* parts;                // shares of depth: their sums, one array of rows x columns after the other; null: one share
+  uint32_t row_tiles, column_tiles, steps;  // steps: of depth, of a tile
+  uint32_t whole, shares;      // tiles that are one workgroup's; workgroups that share the steps of each further tile
+  f32x4* parts;                // of those: a share's sums, a tile's registers
 };
 
 constexpr uint32_t kOutside = 0xfffffff0u;  // an offset beyond every buffer
 constexpr int kStepBytes = 128;  // of depth that are staged at a time: 64 elements of 16 bits, 32 of 32
 
-typedef float f32x4 __attribute__((ext_vector_type(4)));
 template <class T>
 struct Frag {
   typedef T type __attribute__((ext_vector_type(16 / sizeof(T))));
@@ -113,7 +115,10 @@ struct Tile {
   // depth_left (along): elements of depth from this step on
   __device__ void load(lds_char* to, const char* from, uint64_t ld, uint32_t lines, uint32_t depth_left, uint32_t line_bytes, uint32_t wave) const {
     const uint32_t most = kAcross ? (uint32_t)kDepth : (uint32_t)R, n = lines < most ? lines : most;
-    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)from, 0, n ? (n - 1u) * (uint32_t)ld + line_bytes : 0u, 0x00020000);
+    // (one for the wavefront: said so, lest the compiler loop over its lanes)
+    const uint32_t bytes = __builtin_amdgcn_readfirstlane(n ? (n - 1u) * (uint32_t)ld + line_bytes : 0u);
+    const uint32_t low = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)from), high = __builtin_amdgcn_readfirstlane((uint32_t)((uintptr_t)from >> 32));
+    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)((uint64_t)high << 32 | low), 0, bytes, 0x00020000);
 #pragma unroll
     for (int j = 0; j < kLoads; ++j)
       __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(to + (wave * kLoads + j) * 1024), 16, kAcross || deep < depth_left ? offset[j] : kOutside, 0, 0, 0);
@@ -162,37 +167,133 @@ __device__ __forceinline__ void put(T* to, f32x4 v, uint32_t n, bool wide) {
   }
 }
 
-// BM x BN of C a workgroup, its WM x WN wavefronts side by side.  C's rows come from A; its columns from B, which is the
-// first side of the matrix instructions, so that a lane holds four adjacent columns of a row.
+// Eight row tiles wide, down the columns: tiles that are worked on at one time share rows of both sides in a die's cache.
+template <int BM, int BN>
+__device__ __forceinline__ void place(const MmArgs& p, uint32_t t, uint32_t& row0, uint32_t& col0) {
+  const uint32_t band = t / (8u * p.column_tiles), in_band = t - band * 8u * p.column_tiles;
+  const uint32_t high = p.row_tiles - band * 8u < 8u ? p.row_tiles - band * 8u : 8u;
+  row0 = (band * 8u + in_band % high) * BM;
+  col0 = in_band / high * BN;
+}
+
+// What becomes of 16 rows of a wavefront's sums (r: this lane's row; c0: its first column): they are rounded and stored.
+template <class T, Form kForm, int kNF, int kAct>
+__device__ __forceinline__ void finish_rows(const MmArgs& p, uint32_t r, uint32_t c0, const f32x4 (&sum)[kNF]) {
+  if constexpr (kForm == kForward || kForm == kSlopes) {
+    if (r >= p.rows) return;
+    Pack<T, 4> dh[kNF / 2] = {};
+    if (kForm == kSlopes) {
+#pragma unroll
+      for (int j = 0; j < kNF / 2; ++j) {
+        const uint32_t c = c0 + j * 16;
+        const T* from = (const T*)p.dh + (uint64_t)r * p.ld_dh + c;
+        if (p.wide && c + 4u <= p.columns) {
+          dh[j] = *(const Pack<T, 4>*)from;
+        } else {
+#pragma unroll
+          for (uint32_t e = 0; e < 4u; ++e)
+            if (c + e < p.columns) dh[j].v[e] = from[e];
+        }
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kNF / 2; ++j) {
+      const uint32_t c = c0 + j * 16;
+      const f32x4 g = sum[j], u = sum[j + kNF / 2];
+      if (kForm == kForward) {
+        f32x4 h;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) h[e] = act<kAct>(g[e]) * u[e];
+        put((T*)p.c + (uint64_t)r * p.ld_c + c, h, c < p.columns ? p.columns - c : 0u, p.wide);
+      } else if (c < p.half) {
+        f32x4 da, du;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          da[e] = (float)dh[j].v[e] * u[e] * slope<kAct>(g[e]);
+          du[e] = (float)dh[j].v[e] * act<kAct>(g[e]);
+        }
+        put((T*)p.c + (uint64_t)r * p.ld_c + c, da, 4u, true);
+        put((T*)p.c + (uint64_t)r * p.ld_c + p.half + c, du, 4u, true);
+      }
+    }
+  } else {
+    const uint32_t second = kForm == kWeights && r >= p.half ? 1u : 0u, row = r - second * p.half;
+    if (row >= p.rows) return;
+    T* to = second ? (T*)p.c2 + (uint64_t)row * p.ld_c2 : (T*)p.c + (uint64_t)row * p.ld_c;
+#pragma unroll
+    for (int j = 0; j < kNF; ++j) {
+      const uint32_t c = c0 + j * 16;
+      put(to + c, sum[j], c < p.columns ? p.columns - c : 0u, p.wide);
+    }
+  }
+}
+
+template <class T, Form kForm, int BM, int BN, int WM, int WN>
+struct Split {
+  static constexpr bool kTwo = kForm == kForward || kForm == kSlopes;
+  static constexpr int kRows = BM / WM, kCols = BN / WN, kMF = kRows / 16, kNF = kCols / 16, kLanes = WM * WN * 64;
+  // first row and column of C that a lane of wavefront (wm, wn) holds in its i-th 16 rows
+  __device__ static uint32_t row(uint32_t row0, uint32_t wm, uint32_t lane, int i) { return row0 + wm * kRows + i * 16 + lane % 16u; }
+  __device__ static uint32_t column(uint32_t col0, uint32_t wn, uint32_t lane) { return (kTwo ? col0 / 2u + wn * (kCols / 2) : col0 + wn * kCols) + lane / 16u * 4u; }
+
+  template <int kN>
+  __device__ __forceinline__ static void finish(const MmArgs& p, uint32_t row0, uint32_t col0, uint32_t wm, uint32_t wn, uint32_t lane, int i0, const f32x4 (&sum)[kN][kNF]) {
+    const uint32_t c = column(col0, wn, lane);
+    auto all = [&](auto kind) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < kN; ++i) {
+        finish_rows<T, kForm, kNF, decltype(kind)::value>(p, row(row0, wm, lane, i0 + i), c, sum[i]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    if (!kTwo || p.act == FBX_ACT_SILU) all(Kind<FBX_ACT_SILU>());
+    else if (p.act == FBX_ACT_GELU) all(Kind<FBX_ACT_GELU>());
+    else if (p.act == FBX_ACT_RELU) all(Kind<FBX_ACT_RELU>());
+    else all(Kind<FBX_ACT_SIGMOID>());
+  }
+};
+
+// BM x BN of C a workgroup at a time, its WM x WN wavefronts side by side (kForward, kSlopes: BN / 2 columns of either
+// product).  C's rows come from A; its columns from B, which is the first side of the matrix instructions, so that a lane holds
+// four adjacent columns of a row.
 template <class T, Form kForm, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(WM * WN * 64) void k_mm(MmArgs p) {
 #ifdef __HIP_DEVICE_COMPILE__  // (the host's pass, which makes the launch stub of it, does not know the buffer's type)
-  constexpr bool kTwo = kForm == kForward || kForm == kSlopes;
-  constexpr int kWaves = WM * WN, kRows = BM / WM, kCols = BN / WN, kMF = kRows / 16, kNF = kCols / 16;
-  constexpr int kDepth = kStepBytes / sizeof(T);
+  typedef Split<T, kForm, BM, BN, WM, WN> S;
+  constexpr bool kTwo = S::kTwo;
+  constexpr int kWaves = WM * WN, kMF = S::kMF, kNF = S::kNF, kDepth = kStepBytes / sizeof(T);
   typedef Tile<T, BM, kWaves, kForm == kWeights> TileA;
   typedef Tile<T, BN, kWaves, !kTwo> TileB;
   __shared__ alignas(1024) char a0[BM * kStepBytes], b0[BN * kStepBytes], a1[BM * kStepBytes], b1[BN * kStepBytes];
   const uint32_t lane = threadIdx.x % 64u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64u), wm = wave % WM, wn = wave / WM;
-
-  // Workgroups are handed to the eight dies in turn: each die takes a stretch of the tiles, eight row tiles wide, so that
-  // those at work on it at one time share rows of both sides in its cache.
-  const uint32_t tiles = p.row_tiles * p.column_tiles;
-  uint32_t t = blockIdx.x;
+  // Workgroups go to the eight dies in turn: each die takes a stretch of the whole tiles, then one of the shares.
+  uint32_t t, first = 0, end = p.steps, part = 0;
   {
-    const uint32_t each = tiles / 8u, more = tiles % 8u, die = t % 8u, k = t / 8u;
-    t = die * each + (die < more ? die : more) + k;
+    const bool whole = blockIdx.x < p.whole;
+    const uint32_t n = whole ? p.whole : gridDim.x - p.whole, i = whole ? blockIdx.x : blockIdx.x - p.whole, each = n / 8u, more = n % 8u, die = i % 8u;
+    t = die * each + (die < more ? die : more) + i / 8u;
+    if (!whole) {
+      part = t;
+      const uint32_t share = t % p.shares, steps = p.steps / p.shares, longer = p.steps % p.shares;
+      first = share * steps + (share < longer ? share : longer);
+      end = first + steps + (share < longer ? 1u : 0u);
+      t = p.whole + t / p.shares;
+    }
   }
-  const uint32_t band = t / (8u * p.column_tiles), in_band = t - band * 8u * p.column_tiles;
-  const uint32_t high = p.row_tiles - band * 8u < 8u ? p.row_tiles - band * 8u : 8u;
-  const uint32_t row0 = (band * 8u + in_band % high) * BM, col0 = in_band / high * (kTwo ? BN / 2 : BN);
+  uint32_t row0, col0;
+  place<BM, BN>(p, t, row0, col0);
+  row0 = __builtin_amdgcn_readfirstlane(row0);  // (quotients are worked out in vector registers)
+  col0 = __builtin_amdgcn_readfirstlane(col0);
+  first = __builtin_amdgcn_readfirstlane(first);
+  end = __builtin_amdgcn_readfirstlane(end);
 
   TileA ta;
   TileB tb;
   const bool up = kTwo && wave >= kWaves / 2;  // this wavefront loads of Wu
-  const char *a = (const char*)p.a, *b = (const char*)(up ? p.b2 : p.b);
-  const uint64_t ld_b = up ? p.ld_b2 : p.ld_b;
-  uint32_t b_lines = 0;
+  const uint32_t turn = kForm == kInputs ? p.half / kDepth : 0u;  // kInputs: the first step whose lines are Wu's
+  const char *a = (const char*)p.a, *b = (const char*)(up || (kForm == kInputs && first >= turn) ? p.b2 : p.b);
+  const uint64_t ld_b = up || (kForm == kInputs && first >= turn) ? p.ld_b2 : p.ld_b;
+  const uint32_t b_lines = kTwo && col0 / 2u < p.columns ? __builtin_amdgcn_readfirstlane(p.columns - col0 / 2u) : 0u;
   if (kForm == kWeights) {
     a += (uint64_t)row0 * sizeof(T);
     ta.begin(wave, lane, p.ld_a, 2 * p.half - row0);
@@ -201,57 +302,53 @@ __global__ __launch_bounds__(WM * WN * 64) void k_mm(MmArgs p) {
     ta.begin(wave, lane, p.ld_a, 0);
   }
   if (kTwo) {
-    b += (uint64_t)col0 * ld_b;
-    b_lines = col0 < p.columns ? p.columns - col0 : 0u;
+    b += (uint64_t)(col0 / 2u) * ld_b;
     tb.begin(up ? wave - kWaves / 2 : wave, lane, ld_b, 0);
   } else {
     b += (uint64_t)col0 * sizeof(T);
     tb.begin(wave, lane, ld_b, p.b_columns - col0);
   }
-  const uint32_t turn = kForm == kInputs ? p.half / kDepth : 0u;  // kInputs: the first step whose lines are Wu's
-  const uint32_t all_steps = kForm == kInputs ? 2 * turn : (p.depth + kDepth - 1) / kDepth;
-  const uint32_t first = blockIdx.y * p.steps_each, end = all_steps - first < p.steps_each ? all_steps : first + p.steps_each;
-
   auto load = [&](char* to_a, char* to_b, uint32_t s) {
-    if (kTwo) {
-      const uint32_t left = p.depth - s * kDepth;
-      ta.load((lds_char*)to_a, a + s * kStepBytes, p.ld_a, p.rows - row0, left, left * sizeof(T), wave);
-      tb.load((lds_char*)to_b, b + s * kStepBytes, ld_b, b_lines, left, left * sizeof(T), wave);
-    } else if (kForm == kInputs) {
-      const uint32_t left = 2 * p.half - s * kDepth, k = s * kDepth;
-      ta.load((lds_char*)to_a, a + s * kStepBytes, p.ld_a, p.rows - row0, left, left * sizeof(T), wave);
-      // (the weights one below the other, each made up to `half` lines: a step's lines are of one of them)
-      const bool second = s >= turn;
-      const uint32_t line = second ? k - p.half : k;
-      if (second && (s == turn || s == first)) tb.begin(wave, lane, p.ld_b2, p.b_columns - col0);
-      tb.load((lds_char*)to_b, (const char*)(second ? p.b2 : p.b) + (uint64_t)col0 * sizeof(T) + (uint64_t)line * (second ? p.ld_b2 : p.ld_b), second ? p.ld_b2 : p.ld_b,
-              p.depth - line, 0, (p.b_columns - col0) * sizeof(T), wave);
-    } else {
+    if (kForm == kWeights) {
       const uint32_t left = p.depth - s * kDepth;
       ta.load((lds_char*)to_a, a + (uint64_t)s * kDepth * p.ld_a, p.ld_a, left, 0, (2 * p.half - row0) * sizeof(T), wave);
       tb.load((lds_char*)to_b, b + (uint64_t)s * kDepth * p.ld_b, p.ld_b, left, 0, (p.b_columns - col0) * sizeof(T), wave);
+    } else {
+      const uint32_t left = (kTwo ? p.depth : 2 * p.half) - s * kDepth;
+      ta.load((lds_char*)to_a, a + s * kStepBytes, p.ld_a, p.rows - row0, left, left * sizeof(T), wave);
+      if (kTwo) {
+        tb.load((lds_char*)to_b, b + s * kStepBytes, ld_b, b_lines, left, left * sizeof(T), wave);
+      } else {  // (the weights one below the other, each made up to `half` lines: a step's lines are of one of them)
+        if (s == turn) {
+          b = (const char*)p.b2 + (uint64_t)col0 * sizeof(T);
+          tb.begin(wave, lane, p.ld_b2, p.b_columns - col0);
+        }
+        const uint32_t line = (s >= turn ? s - turn : s) * kDepth;
+        const uint64_t ld = s >= turn ? p.ld_b2 : p.ld_b;
+        tb.load((lds_char*)to_b, b + line * ld, ld, p.depth - line, 0, (p.b_columns - col0) * sizeof(T), wave);
+      }
     }
   };
 
   // Two halves of a step's depth in turn: while one is multiplied out of registers the other's rows are read from LDS.
   // A step's barrier lies between the halves: behind it the next step's tile is there (its loads had a whole step) and
   // nobody reads this step's any more, so the loads of the step after the next go there.
-  f32x4 sum[kNF][kMF] = {};
+  f32x4 sum[kMF][kNF] = {};
   typename Frag<T>::type fa[2][kMF], fb[2][kNF];
   auto read = [&](int part, const char* in_a, const char* in_b) {
 #pragma unroll
-    for (int i = 0; i < kMF; ++i) fa[part][i] = TileA::read((const lds_char*)in_a, wm * kRows + i * 16, part, lane);
+    for (int i = 0; i < kMF; ++i) fa[part][i] = TileA::read((const lds_char*)in_a, wm * S::kRows + i * 16, part, lane);
 #pragma unroll
     for (int j = 0; j < kNF; ++j) {
-      const uint32_t at = !kTwo ? wn * kCols + j * 16 : wn * (kCols / 2) + j % (kNF / 2) * 16 + j / (kNF / 2) * (BN / 2);
-      fb[part][j] = TileB::read((const lds_char*)in_b, at, part, lane);
+      const uint32_t first = !kTwo ? wn * S::kCols + j * 16 : wn * (S::kCols / 2) + j % (kNF / 2) * 16 + j / (kNF / 2) * (BN / 2);
+      fb[part][j] = TileB::read((const lds_char*)in_b, first, part, lane);
     }
   };
   auto multiply = [&](int part) {
 #pragma unroll
     for (int j = 0; j < kNF; ++j)
 #pragma unroll
-      for (int i = 0; i < kMF; ++i) sum[j][i] = mma(fb[part][j], fa[part][i], sum[j][i]);
+      for (int i = 0; i < kMF; ++i) sum[i][j] = mma(fb[part][j], fa[part][i], sum[i][j]);
   };
   auto arrived = [] {  // (loads that go past the registers are not among what a barrier waits for)
     __builtin_amdgcn_s_waitcnt(0x0f70);
@@ -268,105 +365,43 @@ __global__ __launch_bounds__(WM * WN * 64) void k_mm(MmArgs p) {
     multiply(1);
     __builtin_amdgcn_sched_barrier(0);
   };
-  if (first < end) {
-    load(a0, b0, first);
-    if (first + 1 < end) load(a1, b1, first + 1);
-    arrived();
-    read(0, a0, b0);
-    for (uint32_t s = first; s < end; s += 2) {
-      step(a0, b0, a1, b1, s);
-      if (s + 1 < end) step(a1, b1, a0, b0, s + 1);
-    }
+  load(a0, b0, first);
+  if (first + 1 < end) load(a1, b1, first + 1);
+  arrived();
+  read(0, a0, b0);
+  for (uint32_t s = first; s < end; s += 2) {
+    step(a0, b0, a1, b1, s);
+    if (s + 1 < end) step(a1, b1, a0, b0, s + 1);
   }
 
-  if constexpr (kTwo) {
-    auto finish = [&](auto kind) {
-      constexpr int kAct = decltype(kind)::value;
-#pragma unroll
-      for (int i = 0; i < kMF; ++i) {
-        const uint32_t r = row0 + wm * kRows + i * 16 + lane % 16u;
-        if (r >= p.rows) continue;
-        const uint32_t c0 = col0 + wn * (kCols / 2) + lane / 16u * 4u;
-        Pack<T, 4> dh[kNF / 2] = {};
-        if (kForm == kSlopes) {
-#pragma unroll
-          for (int j = 0; j < kNF / 2; ++j) {
-            const uint32_t c = c0 + j * 16;
-            const T* from = (const T*)p.dh + (uint64_t)r * p.ld_dh + c;
-            if (p.wide && c + 4u <= p.columns) {
-              dh[j] = *(const Pack<T, 4>*)from;
-            } else {
-#pragma unroll
-              for (uint32_t e = 0; e < 4u; ++e)
-                if (c + e < p.columns) dh[j].v[e] = from[e];
-            }
-          }
-        }
-#pragma unroll
-        for (int j = 0; j < kNF / 2; ++j) {
-          const uint32_t c = c0 + j * 16;
-          const f32x4 g = sum[j][i], u = sum[j + kNF / 2][i];
-          if (kForm == kForward) {
-            f32x4 h;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) h[e] = act<kAct>(g[e]) * u[e];
-            put((T*)p.c + (uint64_t)r * p.ld_c + c, h, c < p.columns ? p.columns - c : 0u, p.wide);
-          } else if (c < p.half) {
-            f32x4 da, du;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              da[e] = (float)dh[j].v[e] * u[e] * slope<kAct>(g[e]);
-              du[e] = (float)dh[j].v[e] * act<kAct>(g[e]);
-            }
-            put((T*)p.c + (uint64_t)r * p.ld_c + c, da, 4u, true);
-            put((T*)p.c + (uint64_t)r * p.ld_c + p.half + c, du, 4u, true);
-          }
-        }
-      }
-    };
-    if (p.act == FBX_ACT_SILU) finish(Kind<FBX_ACT_SILU>());
-    else if (p.act == FBX_ACT_GELU) finish(Kind<FBX_ACT_GELU>());
-    else if (p.act == FBX_ACT_RELU) finish(Kind<FBX_ACT_RELU>());
-    else finish(Kind<FBX_ACT_SIGMOID>());
+  if (blockIdx.x < p.whole) {
+    S::template finish<kMF>(p, row0, col0, wm, wn, lane, 0, sum);
   } else {
+    f32x4* to = p.parts + (uint64_t)part * (BM * BN / 4) + threadIdx.x;
 #pragma unroll
-    for (int i = 0; i < kMF; ++i) {
-      const uint32_t r = row0 + wm * kRows + i * 16 + lane % 16u;
+    for (int i = 0; i < kMF; ++i)
 #pragma unroll
-      for (int j = 0; j < kNF; ++j) {
-        const uint32_t c = col0 + wn * kCols + j * 16 + lane / 16u * 4u;
-        if (c >= p.columns) continue;
-        if (kForm == kInputs) {
-          if (r >= p.rows) continue;
-          if (p.parts) put(p.parts + ((uint64_t)blockIdx.y * p.rows + r) * p.columns + c, sum[j][i], p.columns - c, p.columns % 4u == 0u);
-          else put((T*)p.c + (uint64_t)r * p.ld_c + c, sum[j][i], p.columns - c, p.wide);
-        } else {
-          const uint32_t weight = r >= p.half ? 1u : 0u, row = r - weight * p.half;
-          if (row >= p.rows) continue;
-          if (p.parts) put(p.parts + ((uint64_t)(blockIdx.y * 2u + weight) * p.rows + row) * p.columns + c, sum[j][i], p.columns - c, p.columns % 4u == 0u);
-          else if (weight) put((T*)p.c2 + (uint64_t)row * p.ld_c2 + c, sum[j][i], p.columns - c, p.wide);
-          else put((T*)p.c + (uint64_t)row * p.ld_c + c, sum[j][i], p.columns - c, p.wide);
-        }
-      }
-    }
+      for (int j = 0; j < kNF; ++j) to[(i * kNF + j) * S::kLanes] = sum[i][j];
   }
 #else
   (void)p;
 #endif
 }
 
-// Adds the sums of shares up, in their order.
-template <class T>
-__global__ __launch_bounds__(256) void k_add_parts(const float* parts, uint32_t shares, uint64_t each, uint32_t rows, uint32_t columns, void* c, uint64_t ld_c, void* c2,
-                                                   uint64_t ld_c2) {
-  const uint64_t i = (uint64_t)blockIdx.x * 256u + threadIdx.x;
-  if (i >= each) return;
-  float sum = 0.f;
-  for (uint32_t s = 0; s < shares; ++s) sum += parts[s * each + i];
-  uint64_t r = i / columns;
-  const uint64_t at = i - r * columns;
-  if (r < rows) ((T*)c)[r * ld_c + at] = (T)sum;
-  else ((T*)c2)[(r - rows) * ld_c2 + at] = (T)sum;
+// Adds up the shares of a tile, in the order of their steps, and finishes it.  A workgroup takes 16 rows of each
+// wavefront's part of it.
+template <class T, Form kForm, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(WM * WN * 64) void k_join(MmArgs p) {
+  typedef Split<T, kForm, BM, BN, WM, WN> S;
+  f32x4 sum[1][S::kNF] = {};
+  const f32x4* in = p.parts + (uint64_t)blockIdx.x * p.shares * (BM * BN / 4) + (blockIdx.y * S::kNF) * S::kLanes + threadIdx.x;
+  for (uint32_t n = 0; n < p.shares; ++n, in += BM * BN / 4)
+#pragma unroll
+    for (int j = 0; j < S::kNF; ++j) sum[0][j] += in[j * S::kLanes];
+  uint32_t row0, col0;
+  place<BM, BN>(p, p.whole + blockIdx.x, row0, col0);
+  const uint32_t wave = threadIdx.x / 64u;
+  S::template finish<1>(p, row0, col0, wave % WM, wave / WM, threadIdx.x % 64u, (int)blockIdx.y, sum);
 }
 
 // Rows of n elements, each made `to` bytes long with zeros behind.
@@ -379,56 +414,61 @@ __global__ __launch_bounds__(256) void k_pad_rows(const T* from, uint64_t ld, ui
   to[i] = c < n ? from[r * ld + c] : (T)0.f;
 }
 
-// How a product is cut: tiles of C, and shares of depth where there are too few of those to fill the card.
+// How a product is cut: tiles of C, of which the last `shared` are shared out by steps of depth.
 struct Cut {
-  uint32_t size;    // 0: 256 x 256, 1: 128 x 128, 2: 64 x 64
-  uint32_t row_tiles, column_tiles, shares, steps_each;
+  uint32_t size;  // 0: tiles of 256 x 256, 1: 128 x 128, 2: 64 x 64
+  uint32_t row_tiles, column_tiles, steps, shared, shares;
+  uint64_t parts_bytes() const { return (uint64_t)shared * shares * kSide[size] * kSide[size] * 4; }
+  static constexpr uint32_t kSide[3] = {256, 128, 64};
 };
-constexpr uint32_t kSide[3] = {256, 128, 64};
+constexpr uint32_t Cut::kSide[3];
 
-Cut cut(uint64_t rows, uint64_t columns, uint64_t steps, bool shares) {
+// Tiles that do not fill the card another time are shared out, into as many shares as let them end soonest: `at once`
+// workgroups run at a time, a share costs steps / shares and what it takes to begin, write its sums and have them read.
+Cut cut(uint64_t rows, uint64_t columns, uint64_t steps) {
+  constexpr uint32_t kAtOnce[3] = {256, 512, 1024};
   Cut c{};
   for (c.size = 0; c.size < 2; ++c.size)
-    if (ceil_div(rows, kSide[c.size]) * ceil_div(columns, kSide[c.size]) >= 256) break;
-  c.row_tiles = (uint32_t)ceil_div(rows, kSide[c.size]);
-  c.column_tiles = (uint32_t)ceil_div(columns, kSide[c.size]);
-  uint64_t n = 1;
-  if (shares) {
-    const uint64_t tiles = (uint64_t)c.row_tiles * c.column_tiles;
-    while (tiles * n < 256 && steps / (2 * n) >= 8) n *= 2;
+    if (ceil_div(rows, Cut::kSide[c.size]) * ceil_div(columns, Cut::kSide[c.size]) >= 128) break;
+  c.row_tiles = (uint32_t)ceil_div(rows, Cut::kSide[c.size]);
+  c.column_tiles = (uint32_t)ceil_div(columns, Cut::kSide[c.size]);
+  c.steps = (uint32_t)(steps ? steps : 1);
+  const uint32_t rest = (uint32_t)((uint64_t)c.row_tiles * c.column_tiles % kAtOnce[c.size]);
+  constexpr double kBegin = 4.0, kSums = 6.0;  // in steps
+  double best = c.steps + kBegin;
+  for (uint32_t n = 2; rest && n <= 32 && n * 4 <= c.steps; ++n) {
+    const double takes = (double)ceil_div((uint64_t)rest * n, kAtOnce[c.size]) * (ceil_div(c.steps, n) + kBegin + kSums) + kSums;
+    if (takes < best) {
+      best = takes;
+      c.shared = rest;
+      c.shares = n;
+    }
   }
-  c.steps_each = (uint32_t)(steps ? ceil_div(steps, n) : 1);
-  c.shares = (uint32_t)(steps ? ceil_div(steps, c.steps_each) : 1);
   return c;
 }
 
+template <class T, Form kForm, int BM, int BN, int WM, int WN>
+void launch(const MmArgs& p, uint32_t shared, hipStream_t stream) {
+  hipLaunchKernelGGL((k_mm<T, kForm, BM, BN, WM, WN>), dim3(p.whole + shared * p.shares), dim3(WM * WN * 64), 0, stream, p);
+  if (shared) hipLaunchKernelGGL((k_join<T, kForm, BM, BN, WM, WN>), dim3(shared, BM / WM / 16), dim3(WM * WN * 64), 0, stream, p);
+}
 template <class T, Form kForm>
-void launch(MmArgs& p, const Cut& c, hipStream_t stream) {
+void launch_by_size(const MmArgs& p, const Cut& c, hipStream_t stream) {
+  if (c.size == 0) launch<T, kForm, 256, 256, 2, 4>(p, c.shared, stream);
+  else if (c.size == 1) launch<T, kForm, 128, 128, 2, 2>(p, c.shared, stream);
+  else launch<T, kForm, 64, 64, 2, 2>(p, c.shared, stream);
+}
+template <Form kForm>
+void launch_by_type(MmArgs& p, const Cut& c, fbx_dtype t, char* parts, hipStream_t stream) {
   p.row_tiles = c.row_tiles;
   p.column_tiles = c.column_tiles;
-  p.steps_each = c.steps_each;
-  const dim3 grid(c.row_tiles * c.column_tiles, c.shares);
-  if (c.size == 0) hipLaunchKernelGGL((k_mm<T, kForm, 256, 256, 2, 4>), grid, dim3(512), 0, stream, p);
-  else if (c.size == 1) hipLaunchKernelGGL((k_mm<T, kForm, 128, 128, 2, 2>), grid, dim3(256), 0, stream, p);
-  else hipLaunchKernelGGL((k_mm<T, kForm, 64, 64, 2, 2>), grid, dim3(256), 0, stream, p);
-}
-
-template <Form kForm>
-void launch_by_type(MmArgs& p, const Cut& c, fbx_dtype t, hipStream_t stream) {
-  if (t == FBX_F32) launch<float, kForm>(p, c, stream);
-  else if (t == FBX_F16) launch<_Float16, kForm>(p, c, stream);
-  else launch<__bf16, kForm>(p, c, stream);
-}
-
-template <class T>
-void add_parts(const MmArgs& p, const Cut& c, uint64_t rows_of_both, hipStream_t stream) {
-  const uint64_t each = rows_of_both * p.columns;
-  hipLaunchKernelGGL((k_add_parts<T>), dim3((uint32_t)ceil_div(each, 256)), dim3(256), 0, stream, p.parts, c.shares, each, p.rows, p.columns, p.c, p.ld_c, p.c2, p.ld_c2);
-}
-void add_parts_by_type(const MmArgs& p, const Cut& c, fbx_dtype t, uint64_t rows_of_both, hipStream_t stream) {
-  if (t == FBX_F32) add_parts<float>(p, c, rows_of_both, stream);
-  else if (t == FBX_F16) add_parts<_Float16>(p, c, rows_of_both, stream);
-  else add_parts<__bf16>(p, c, rows_of_both, stream);
+  p.steps = c.steps;
+  p.whole = c.row_tiles * c.column_tiles - c.shared;
+  p.shares = c.shares;
+  p.parts = (f32x4*)parts;
+  if (t == FBX_F32) launch_by_size<float, kForm>(p, c, stream);
+  else if (t == FBX_F16) launch_by_size<_Float16, kForm>(p, c, stream);
+  else launch_by_size<__bf16, kForm>(p, c, stream);
 }
 
 fbx_status check(const fbx_gated* g) {
@@ -481,14 +521,15 @@ Shape shape_of(const fbx_gated* g, bool backward) {
     s.at[i] = take(s.pad[i] ? (i ? g->hidden : g->records) * (uint64_t)s.wide * s.size : 0);
   }
   const uint64_t depth = kStepBytes / s.size;
-  s.forward = cut(g->records, 2ull * (backward ? s.half : g->hidden), ceil_div(s.wide, depth), false);
+  s.forward = cut(g->records, 2ull * (backward ? s.half : g->hidden), ceil_div(s.wide, depth));
+  uint64_t parts = s.forward.parts_bytes();
   if (backward) {
     s.slopes = take(g->records * 2ull * s.half * s.size);
-    s.inputs = cut(g->records, g->inputs, 2ull * s.half / depth, true);
-    s.weights = cut(2ull * s.half, g->inputs, ceil_div(g->records, depth), true);
-    const uint64_t a = s.inputs.shares > 1 ? s.inputs.shares * g->records * g->inputs : 0, b = s.weights.shares > 1 ? s.weights.shares * 2ull * g->hidden * g->inputs : 0;
-    s.parts = take(4 * (a > b ? a : b));
+    s.inputs = cut(g->records, g->inputs, 2ull * s.half / depth);
+    s.weights = cut(2ull * s.half, g->inputs, ceil_div(g->records, depth));
+    for (uint64_t b : {s.inputs.parts_bytes(), s.weights.parts_bytes()}) parts = b > parts ? b : parts;
   }
+  s.parts = take(parts);
   return s;
 }
 
@@ -569,7 +610,7 @@ extern "C" fbx_status fbx_gated_forward(const fbx_gated* g, void* d_h, uint64_t 
   p.depth = s.wide;
   p.act = g->act;
   p.wide = four_at_a_time(d_h, ld_h, s.size);
-  launch_by_type<kForward>(p, s.forward, g->dtype, stream);
+  launch_by_type<kForward>(p, s.forward, g->dtype, (char*)d_scratch + s.parts, stream);
   return launched();
 }
 
@@ -594,7 +635,7 @@ extern "C" fbx_status fbx_gated_backward(const fbx_gated* g, const void* d_dh, u
   const void* from[3];
   uint64_t ld[3];
   operands(g, s, scratch, from, ld, stream);
-  float* parts = (float*)(scratch + s.parts);
+  char* parts = scratch + s.parts;
   if (g->records) {
     MmArgs p{};
     p.a = from[0];
@@ -613,7 +654,7 @@ extern "C" fbx_status fbx_gated_backward(const fbx_gated* g, const void* d_dh, u
     p.depth = s.wide;
     p.act = g->act;
     p.wide = four_at_a_time(d_dh, ld_dh, s.size);
-    launch_by_type<kSlopes>(p, s.forward, g->dtype, stream);
+    launch_by_type<kSlopes>(p, s.forward, g->dtype, parts, stream);
   }
   if (g->records && d_dx) {
     MmArgs p{};
@@ -631,9 +672,7 @@ extern "C" fbx_status fbx_gated_backward(const fbx_gated* g, const void* d_dh, u
     p.half = s.half;
     p.b_columns = s.wide;
     p.wide = four_at_a_time(d_dx, ld_dx, s.size);
-    p.parts = s.inputs.shares > 1 ? parts : nullptr;
-    launch_by_type<kInputs>(p, s.inputs, g->dtype, stream);
-    if (p.parts) add_parts_by_type(p, s.inputs, g->dtype, p.rows, stream);
+    launch_by_type<kInputs>(p, s.inputs, g->dtype, parts, stream);
   }
   if (d_dw_gate) {
     MmArgs p{};
@@ -651,9 +690,7 @@ extern "C" fbx_status fbx_gated_backward(const fbx_gated* g, const void* d_dh, u
     p.half = s.half;
     p.b_columns = s.wide;
     p.wide = four_at_a_time(d_dw_gate, ld_dw_gate, s.size) && four_at_a_time(d_dw_up, ld_dw_up, s.size);
-    p.parts = s.weights.shares > 1 ? parts : nullptr;
-    launch_by_type<kWeights>(p, s.weights, g->dtype, stream);
-    if (p.parts) add_parts_by_type(p, s.weights, g->dtype, 2ull * p.rows, stream);
+    launch_by_type<kWeights>(p, s.weights, g->dtype, parts, stream);
   }
   return launched();
 }
