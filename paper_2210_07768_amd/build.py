@@ -11,6 +11,8 @@ CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libfbx.so")
 NATIVE = os.path.join(_HERE, "_native.so")          # the part of the Python binding that runs once per call
 NATIVE_SOURCE = os.path.join(CSRC, "fbx_native.cpp")
+TRAIN_NATIVE = os.path.join(_HERE, "_train.so")     # the same for the trainer's operators
+TRAIN_NATIVE_SOURCE = os.path.join(CSRC, "train", "train_native.cpp")
 SOURCES = ["fbx_plan.cpp", "fbx_api.cpp", "fbx_jit.cpp", "fbx_support.hip", "fbx_walk.hip", "fbx_tile.hip", "fbx_clean.hip",
            "train/train_embed.hip", "train/train_embed_grad.hip", "train/train_gated.hip", "train/train_adamw.hip"]
 HEADERS = ["fbx_internal.h", "fbx_device.h", "fbx_arena.h", "fbx_lists.h", "fbx_split.h", "train/train_common.h",
@@ -39,7 +41,7 @@ def command() -> list:
     ] + [os.path.join(CSRC, s) for s in SOURCES] + ["-ldl"]
 
 
-def native_command() -> list:
+def native_command(out: str = NATIVE, source: str = NATIVE_SOURCE) -> list:
     import sysconfig
 
     import torch
@@ -50,15 +52,16 @@ def native_command() -> list:
         f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
         "-I", os.path.join(_ROOT, "include"), "-I", os.path.join(root, "include"),
         "-I", os.path.join(root, "include", "torch", "csrc", "api", "include"), "-I", sysconfig.get_paths()["include"],
-        "-o", NATIVE, NATIVE_SOURCE,
+        "-o", out, source,
         "-L", os.path.join(root, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10",
     ]
 
 
 def stale() -> bool:
-    if not os.path.exists(LIB) or not os.path.exists(NATIVE):
+    if not all(os.path.exists(x) for x in (LIB, NATIVE, TRAIN_NATIVE)):
         return True
-    if os.path.getmtime(NATIVE) < max(os.path.getmtime(NATIVE_SOURCE), os.path.getmtime(HEADERS[-1])):
+    headers = max(os.path.getmtime(h) for h in HEADERS[-2:])
+    if any(os.path.getmtime(x) < max(os.path.getmtime(source), headers) for x, source in ((NATIVE, NATIVE_SOURCE), (TRAIN_NATIVE, TRAIN_NATIVE_SOURCE))):
         return True
     t = os.path.getmtime(LIB)
     deps = [os.path.join(CSRC, s) for s in SOURCES] + [h if os.path.isabs(h) else os.path.join(CSRC, h) for h in HEADERS]
@@ -70,10 +73,11 @@ def build(force: bool = True, verbose: bool = False) -> str:
         cmd = command()
         if verbose:
             print(" ".join(cmd), flush=True)
-        native = subprocess.Popen(native_command())   # (beside the device code, which takes longer)
+        natives = [subprocess.Popen(c) for c in (native_command(), native_command(TRAIN_NATIVE, TRAIN_NATIVE_SOURCE))]   # (beside the device code, which takes longer)
         subprocess.check_call(cmd)
-        if native.wait():
-            raise subprocess.CalledProcessError(native.returncode, native.args)
+        for native in natives:
+            if native.wait():
+                raise subprocess.CalledProcessError(native.returncode, native.args)
     return LIB
 
 

@@ -404,6 +404,67 @@ __global__ __launch_bounds__(WM * WN * 64) void k_join(MmArgs p) {
   S::template finish<1>(p, row0, col0, wave % WM, wave / WM, threadIdx.x % 64u, (int)blockIdx.y, sum);
 }
 
+// Up to 16 records: the weights are read once, straight into the matrix units' registers, and bound it.  A workgroup takes
+// 16 columns of either product, its wavefronts a share of the depth each; their sums meet in LDS and are added in order.
+// kWhole: rows begin at, and are, whole 16-byte loads; else they are read element by element, which for so few records
+// costs less than a copy of the weights.
+constexpr int kFewWaves = 8;
+template <class T, bool kWhole>
+__global__ __launch_bounds__(kFewWaves * 64) void k_few(MmArgs p) {
+#ifdef __HIP_DEVICE_COMPILE__
+  typedef typename Frag<T>::type F;
+  constexpr uint32_t kLanes = 16 / sizeof(T), kStep = 4 * kLanes, kAhead = 4;
+  __shared__ f32x4 sums[kFewWaves][2][64];
+  const uint32_t lane = threadIdx.x % 64u, wave = threadIdx.x / 64u, i = lane % 16u, g = lane / 16u;
+  const uint32_t n = blockIdx.x * 16u + i;
+  const T* rows[3] = {(const T*)((const char*)p.b + n * p.ld_b), (const T*)((const char*)p.b2 + n * p.ld_b2), (const T*)((const char*)p.a + i * p.ld_a)};
+  const bool in[3] = {n < p.columns, n < p.columns, i < p.rows};
+  auto load = [&](int which, uint32_t k) {
+    F f = {};
+    if (in[which]) {
+      if (kWhole) {
+        if (k < p.depth) f = *(const F*)(rows[which] + k);
+      } else {
+#pragma unroll
+        for (uint32_t e = 0; e < kLanes; ++e)
+          if (k + e < p.depth) f[e] = rows[which][k + e];
+      }
+    }
+    return f;
+  };
+  f32x4 sum[2] = {};
+  for (uint32_t k0 = wave * kStep + g * kLanes; k0 - g * kLanes < p.depth; k0 += kFewWaves * kStep * kAhead) {
+    F f[kAhead][3];
+#pragma unroll
+    for (uint32_t u = 0; u < kAhead; ++u)
+#pragma unroll
+      for (int which = 0; which < 3; ++which) f[u][which] = load(which, k0 + u * kFewWaves * kStep);
+#pragma unroll
+    for (uint32_t u = 0; u < kAhead; ++u) {
+      sum[0] = mma(f[u][0], f[u][2], sum[0]);
+      sum[1] = mma(f[u][1], f[u][2], sum[1]);
+    }
+  }
+  sums[wave][0][lane] = sum[0];
+  sums[wave][1][lane] = sum[1];
+  __syncthreads();
+  if (wave) return;
+  f32x4 both[2] = {};
+#pragma unroll
+  for (int w = 0; w < kFewWaves; ++w) {
+    both[0] += sums[w][0][lane];
+    both[1] += sums[w][1][lane];
+  }
+  const uint32_t c = blockIdx.x * 16u + g * 4u;
+  if (p.act == FBX_ACT_SILU) finish_rows<T, kForward, 2, FBX_ACT_SILU>(p, i, c, both);
+  else if (p.act == FBX_ACT_GELU) finish_rows<T, kForward, 2, FBX_ACT_GELU>(p, i, c, both);
+  else if (p.act == FBX_ACT_RELU) finish_rows<T, kForward, 2, FBX_ACT_RELU>(p, i, c, both);
+  else finish_rows<T, kForward, 2, FBX_ACT_SIGMOID>(p, i, c, both);
+#else
+  (void)p;
+#endif
+}
+
 // Rows of n elements, each made `to` bytes long with zeros behind.
 template <class T>
 __global__ __launch_bounds__(256) void k_pad_rows(const T* from, uint64_t ld, uint32_t n, T* to, uint32_t wide, uint64_t all) {
@@ -479,6 +540,18 @@ void launch_by_type(MmArgs& p, const Cut& c, fbx_dtype t, char* parts, hipStream
   else launch_by_size<__bf16, kForm>(p, c, stream);
 }
 
+template <class T>
+void launch_few(const MmArgs& p, bool whole, hipStream_t stream) {
+  const dim3 grid((uint32_t)ceil_div(p.columns, 16));
+  if (whole) hipLaunchKernelGGL((k_few<T, true>), grid, dim3(kFewWaves * 64), 0, stream, p);
+  else hipLaunchKernelGGL((k_few<T, false>), grid, dim3(kFewWaves * 64), 0, stream, p);
+}
+void launch_few_by_type(const MmArgs& p, fbx_dtype t, bool whole, hipStream_t stream) {
+  if (t == FBX_F32) launch_few<float>(p, whole, stream);
+  else if (t == FBX_F16) launch_few<_Float16>(p, whole, stream);
+  else launch_few<__bf16>(p, whole, stream);
+}
+
 fbx_status check(const fbx_gated* g) {
   if (!g) return refuse(FBX_E_ARG, "g is NULL");
   if (!known(g->dtype)) return refuse(FBX_E_ARG, "unknown dtype");
@@ -496,10 +569,12 @@ fbx_status check_pointers(const fbx_gated* g, uintptr_t others) {
 }
 // What a call keeps in its scratch, and what the kernels read: a matrix whose rows are not whole 16-byte loads (its
 // address, its stride or its width) is first copied to one whose are.
+constexpr uint32_t kFewRecords = 16;
 struct Shape {
   uint32_t size, lanes;        // bytes of an element; elements of a load
   uint32_t wide;               // inputs, rounded up to whole loads
   uint32_t half;               // hidden, rounded up to a step of depth
+  bool few;                    // so few records that the weights are read as they are
   bool pad[3];                 // x, w_gate, w_up
   uint64_t at[3], slopes, parts, bytes;
   Cut forward, inputs, weights;
@@ -517,6 +592,7 @@ Shape shape_of(const fbx_gated* g, bool backward) {
   s.lanes = 16u / s.size;
   s.wide = (uint32_t)round_up(g->inputs, s.lanes);
   s.half = (uint32_t)round_up(g->hidden, kStepBytes / s.size);
+  s.few = !backward && g->records <= kFewRecords;
   const void* from[3] = {g->d_x, g->d_w_gate, g->d_w_up};
   const uint64_t ld[3] = {g->ld_x, g->ld_w_gate, g->ld_w_up};
   auto take = [&](uint64_t bytes) {
@@ -526,11 +602,11 @@ Shape shape_of(const fbx_gated* g, bool backward) {
   };
   for (int i = 0; i < 3; ++i) {
     s.pad[i] = g->inputs % s.lanes || ld[i] % s.lanes || (uintptr_t)from[i] % 16u;
-    s.at[i] = take(s.pad[i] ? (i ? g->hidden : g->records) * (uint64_t)s.wide * s.size : 0);
+    s.at[i] = take(s.pad[i] && !s.few ? (i ? g->hidden : g->records) * (uint64_t)s.wide * s.size : 0);
   }
   const uint64_t depth = kStepBytes / s.size;
   s.forward = cut(g->records, 2ull * (backward ? s.half : g->hidden), ceil_div(s.wide, depth), s.size == 4);
-  uint64_t parts = s.forward.parts_bytes();
+  uint64_t parts = s.few ? 0 : s.forward.parts_bytes();
   if (backward) {
     s.slopes = take(g->records * 2ull * s.half * s.size);
     s.inputs = cut(g->records, g->inputs, 2ull * s.half / depth, s.size == 4);
@@ -556,7 +632,7 @@ void operands(const fbx_gated* g, const Shape& s, char* scratch, const void* (&f
   ld[1] = g->ld_w_gate;
   ld[2] = g->ld_w_up;
   for (int i = 0; i < 3; ++i) {
-    if (s.pad[i]) {
+    if (s.pad[i] && !s.few) {
       char* to = scratch + s.at[i];
       if (s.size == 4u) pad_rows<float>(from[i], ld[i], g->inputs, to, s.wide, i ? g->hidden : g->records, stream);
       else pad_rows<_Float16>(from[i], ld[i], g->inputs, to, s.wide, i ? g->hidden : g->records, stream);
@@ -615,9 +691,13 @@ extern "C" fbx_status fbx_gated_forward(const fbx_gated* g, void* d_h, uint64_t 
   p.ld_c = ld_h;
   p.rows = (uint32_t)g->records;
   p.columns = g->hidden;
-  p.depth = s.wide;
+  p.depth = s.few ? g->inputs : s.wide;
   p.act = g->act;
   p.wide = four_at_a_time(d_h, ld_h, s.size);
+  if (s.few) {
+    launch_few_by_type(p, g->dtype, !(s.pad[0] || s.pad[1] || s.pad[2]), stream);
+    return launched();
+  }
   launch_by_type<kForward>(p, s.forward, g->dtype, (char*)d_scratch + s.parts, stream);
   return launched();
 }
