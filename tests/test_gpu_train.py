@@ -175,8 +175,8 @@ def test_embed_table_beyond_32_bits():
         assert torch.equal(table[r0:r0 + (1 << 21)].sum(1, dtype=torch.float32), count[r0:r0 + (1 << 21)] * dim)
 
 
-@pytest.mark.parametrize("placement", [0, 1])
-def test_embed_takes_extraction_results(placement):
+@pytest.mark.parametrize("placement, tile_log2", [(0, -1), (1, -1), (1, 2), (1, 0)])
+def test_embed_takes_extraction_results(placement, tile_log2):
     """What extraction returns, in record order and in arrival order: every list pools to the same."""
     from paper_2210_07768_amd import workloads as W
 
@@ -192,6 +192,7 @@ def test_embed_takes_extraction_results(placement):
     want_grad = T.embed_backward(want, res, 5003)
     if placement:
         plan.set_option("placement", 1)
+        plan.set_option("tile_log2", tile_log2)
         for _ in range(2):
             res = plan.extract(d_raw, d_off)
         assert res.arrival_tile_records
