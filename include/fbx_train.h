@@ -48,7 +48,8 @@ const char* fbx_train_last_error(void);
  *   arrival_tile_records : fbx_result.arrival_tile_records, 0 for slots in record order
  *   d_table    : DEVICE, rows x dim, table_stride elements from row to row
  *   d_out      : DEVICE, n_records x (n_slots * dim), record_stride elements from record to record
- * Signs of a record are added in their order.  Limits: rows < 2^31, 1 <= dim <= 65536, n_records < 2^32.
+ * Signs of a record are added in their order.  Limits: rows < 2^31, 1 <= dim <= 65536, n_records < 2^32, fewer than 2^32
+ * signs a slot.
  * Errors: FBX_E_ARG, FBX_E_HIP.
  */
 fbx_status fbx_embed_forward(const fbx_slot_view* slots, uint32_t n_slots, uint64_t n_records,
@@ -60,8 +61,8 @@ fbx_status fbx_embed_forward(const fbx_slot_view* slots, uint32_t n_slots, uint6
  * fbx_embed_backward — the gradient of fbx_embed_forward with respect to the table:
  *   dtable[v][:] = sum over all signs with row(sign) = v of w * dout[record][slot][:]
  * w = 1, or 1 / (signs of that record in that slot) where mean is set.  All of dtable is written,
- * zeros where no sign leads.  A row's terms are added in an order fixed by slot, record and position
- * alone (ascending inside stretches of signs, the stretches' sums pairwise in a fixed order).
+ * zeros where no sign leads.  A row's terms are ordered by slot, record and position; stretches of them are
+ * added up in that order, and then the stretches' sums in theirs.
  * Arguments as above.  Limits also: fewer than 2^32 signs in all, n_records * n_slots < 2^32.
  * Errors: FBX_E_ARG, FBX_E_NOMEM (scratch too small), FBX_E_HIP.
  */

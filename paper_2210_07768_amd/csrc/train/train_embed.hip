@@ -27,7 +27,7 @@ fbx_status check_slots(const fbx_slot_view* slots, uint32_t n_slots, uint64_t n_
   for (uint32_t i = 0; i < n_slots; ++i) {
     const fbx_slot_view& s = slots[i];
     if (s.n_values && !s.values) return refuse(FBX_E_ARG, "a slot has n_values but no values");
-    if (s.n_values >> 40) return refuse(FBX_E_ARG, "a slot has 2^40 values or more");
+    if (s.n_values >> 32) return refuse(FBX_E_ARG, "a slot has 2^32 values or more");
     if (s.fixed_arity ? s.n_values != n_records * s.fixed_arity : !s.offsets)
       return refuse(FBX_E_ARG, s.fixed_arity ? "a slot of fixed arity must have fixed_arity * n_records values" : "a slot without fixed arity needs offsets");
     if (!s.fixed_arity && s.tile_ends && !tile) return refuse(FBX_E_ARG, "a slot has tile_ends: arrival_tile_records is needed");

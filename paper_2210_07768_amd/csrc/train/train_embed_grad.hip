@@ -7,7 +7,7 @@ namespace train {
 namespace {
 
 constexpr uint32_t kSortItems = 16, kSortTile = 256 * kSortItems;  // pairs of a lane, of a workgroup
-constexpr uint32_t kRun = 32;                                      // sorted terms a group of lanes adds up
+constexpr uint32_t kRun = 16, kAhead = 8;                          // sorted terms a group of lanes adds up, and has on their way
 constexpr uint32_t kNone = 0xffffffffu;
 
 struct PairArgs {
@@ -146,88 +146,146 @@ struct SumArgs {
   const float* terms;         // ... or, later, sums of stretches
   const void* dout;
   void* dtable;
-  uint32_t* part_keys;        // two a group: a run that began before it, a run that goes on after it
+  uint32_t* part_keys;        // two a workgroup: a row that began before it, a row that goes on after it
   float* parts;
   uint64_t record_stride, table_stride;
-  uint32_t n, n_records, all_slots, rows, dim, lanes_log2;
+  uint32_t n, n_from, all_slots, rows, dim, lanes_log2, dense;  // dense: a record's rows of dout directly follow the last one's
 };
 
-// 2^lanes_log2 lanes, each N adjacent columns, add up 32 neighbouring terms; a row's sum that lies inside them is
-// written to the table, one that begins before them or ends after them is left to the next launch, which adds such sums
-// up the same way.  kFirst: terms are rows of dout.
+// The sorted terms of a workgroup: 16 for every group of 2^lanes_log2 lanes, each lane N adjacent columns (blockIdx.y: which
+// stretch of them).  A group adds its terms up one after the other.  A row that begins and ends in a group is written to the
+// table; one that goes on is taken up by the group it begins in, which adds the next groups' shares of it; what
+// began before the workgroup or goes on after it is left to the next launch, which adds such sums up the same way (at most two a
+// workgroup, so three launches do for 10^8 terms).  kFirst: terms are rows of dout.
+// Bound by the rows of dout, which are fetched in lines of 128 bytes in the order of the keys.
 template <class T, int N, bool kFirst>
 __global__ __launch_bounds__(256) void k_sum_rows(SumArgs a) {
-  const uint32_t lanes = 1u << a.lanes_log2, mine = threadIdx.x & (lanes - 1u);
-  const uint64_t group = ((uint64_t)blockIdx.x * 256u + threadIdx.x) >> a.lanes_log2;
-  const uint64_t e0 = group * kRun;
-  if (e0 >= a.n) return;
-  const uint32_t n = a.n - e0 < kRun ? (uint32_t)(a.n - e0) : kRun;
-  const uint32_t before = e0 ? a.keys[e0 - 1] : kNone, after = e0 + n < a.n ? a.keys[e0 + n] : kNone;
-  for (uint32_t col = mine * N; col < a.dim; col += lanes * N) {
-    float sum[N] = {};
-    uint32_t key = a.keys[e0];
-    bool open = key == before && key != kNone;  // the run at hand began before this group
-    uint32_t head = kNone;
-    auto close = [&](bool goes_on) {
-      if (key == kNone) return;
-      if (!open && !goes_on) {
-        if (key >= a.rows) return;
-        Pack<T, N> p;
+  constexpr uint32_t kPad = kRun + 1;  // (a group's terms begin in another bank than the next one's)
+  extern __shared__ uint32_t lds[];
+  const uint32_t lanes = 1u << a.lanes_log2, groups = 256u >> a.lanes_log2, mine = threadIdx.x & (lanes - 1u), group = threadIdx.x >> a.lanes_log2;
+  const uint32_t columns = lanes * N;
+  uint32_t* key_of = lds;                                        // groups * kPad, then the one before and the one after
+  uint32_t* from_of = lds + groups * kPad + 2u;                  // groups * kPad
+  uint32_t* open = from_of + (kFirst ? groups * kPad : 0u);      // a group's flags: 1 began before it, 2 goes on after it, 4 all of it is one row's
+  float* shares = (float*)(open + groups);                       // groups x {head, tail} x columns
+  const uint64_t b0 = (uint64_t)blockIdx.x * groups * kRun;
+  const uint32_t here = a.n - b0 < groups * kRun ? (uint32_t)(a.n - b0) : groups * kRun;
+  for (uint32_t i = threadIdx.x; i < groups * kRun; i += 256u) {
+    const uint32_t at = i / kRun * kPad + i % kRun;
+    key_of[at] = i < here ? a.keys[b0 + i] : kNone;
+    if (kFirst) from_of[at] = i < here ? a.from[b0 + i] : 0u;
+  }
+  uint32_t* ends = key_of + groups * kPad;
+  if (threadIdx.x == 0u) {
+    ends[0] = b0 ? a.keys[b0 - 1u] : kNone;
+    ends[1] = b0 + here < a.n ? a.keys[b0 + here] : kNone;
+  }
+  __syncthreads();
+  const uint32_t* keys = key_of + group * kPad;
+  const uint32_t before = group ? key_of[(group - 1u) * kPad + kRun - 1u] : ends[0], last = keys[kRun - 1u];
+  const uint32_t after = group + 1u < groups ? key_of[(group + 1u) * kPad] : ends[1];
+  const uint32_t col = blockIdx.y * columns + mine * N;
+  const bool in = col < a.dim;
+  float* head = shares + group * 2u * columns + mine * N;
+  float* tail = head + columns;
+  auto write = [&](uint32_t row, const float (&sum)[N]) {
+    if (row >= a.rows || !in) return;
+    Pack<T, N> p;
 #pragma unroll
-        for (int j = 0; j < N; ++j) p.v[j] = (T)sum[j];
-        *(Pack<T, N>*)((T*)a.dtable + key * a.table_stride + col) = p;
+    for (int j = 0; j < N; ++j) p.v[j] = (T)sum[j];
+    *(Pack<T, N>*)((T*)a.dtable + row * a.table_stride + col) = p;
+  };
+
+  float sum[N] = {};
+  uint32_t key = keys[0];
+  bool began = key == before && key != kNone, first = true;  // the row at hand began before this group; it is the group's first
+  const bool goes_on = last == after && last != kNone;
+#pragma unroll
+  for (uint32_t i0 = 0; i0 < kRun; i0 += kAhead) {
+    Pack<T, N> p[kAhead] = {};
+    Pack<float, N> q[kAhead] = {};
+    float w[kAhead] = {};
+#pragma unroll
+    for (uint32_t e = 0; e < kAhead; ++e) {
+      if (!in || keys[i0 + e] == kNone) continue;
+      if (kFirst) {
+        const uint32_t from = from_of[group * kPad + i0 + e];
+        if (from >= a.n_from) continue;
+        uint64_t at = (uint64_t)from * a.dim;
+        if (!a.dense) {
+          const uint32_t r = from / a.all_slots;
+          at = r * a.record_stride + (uint64_t)(from - r * a.all_slots) * a.dim;
+        }
+        p[e] = *(const Pack<T, N>*)((const T*)a.dout + at + col);
+        w[e] = a.share ? a.share[from] : 1.f;
       } else {
-        float* to = a.parts + (2 * group + (open ? 0 : 1)) * a.dim + col;
-#pragma unroll
-        for (int j = 0; j < N; ++j) to[j] = sum[j];
+        q[e] = *(const Pack<float, N>*)(a.terms + (b0 + group * kRun + i0 + e) * a.dim + col);
       }
-    };
-    uint32_t tail = kNone;
-    for (uint32_t i = 0; i < n; ++i) {
-      const uint32_t k = a.keys[e0 + i];
+    }
+#pragma unroll
+    for (uint32_t e = 0; e < kAhead; ++e) {
+      const uint32_t k = keys[i0 + e];
       if (k != key) {
-        close(false);
-        if (open) head = key;
-        open = false;
+        if (began) {
+#pragma unroll
+          for (int j = 0; j < N; ++j) head[j] = sum[j];
+        } else {
+          write(key, sum);  // (kNone is no row)
+        }
+        began = first = false;
         key = k;
 #pragma unroll
         for (int j = 0; j < N; ++j) sum[j] = 0.f;
       }
-      if (k == kNone) continue;
-      if (kFirst) {
-        const uint32_t from = a.from[e0 + i];
-        const uint32_t r = from / a.all_slots, s = from - r * a.all_slots;
-        if (r >= a.n_records) continue;
-        const Pack<T, N> p = *(const Pack<T, N>*)((const T*)a.dout + r * a.record_stride + (uint64_t)s * a.dim + col);
-        if (a.share) {
-          const float w = a.share[from];
 #pragma unroll
-          for (int j = 0; j < N; ++j) sum[j] += (float)p.v[j] * w;
-        } else {
+      for (int j = 0; j < N; ++j) sum[j] += kFirst ? (a.share ? (float)p[e].v[j] * w[e] : (float)p[e].v[j]) : q[e].v[j];
+    }
+  }
+  const bool whole = began && goes_on;
+  if (began || goes_on) {
+    float* to = began ? head : tail;
 #pragma unroll
-          for (int j = 0; j < N; ++j) sum[j] += (float)p.v[j];
-        }
-      } else {
-        const float* p = a.terms + (e0 + i) * a.dim + col;
+    for (int j = 0; j < N; ++j) to[j] = sum[j];
+  } else {
+    write(key, sum);
+  }
+  if (mine == 0u) open[group] = (keys[0] == before && keys[0] != kNone ? 1u : 0u) | (goes_on ? 2u : 0u) | (whole ? 4u : 0u);
+  __syncthreads();
+
+  // Adds the heads from group g on to sum, up to the row's end; true: the row goes on after the workgroup.
+  auto follow = [&](uint32_t g, float (&total)[N]) {
+    for (; g < groups; ++g) {
+      const float* more = shares + g * 2u * columns + mine * N;
 #pragma unroll
-        for (int j = 0; j < N; ++j) sum[j] += p[j];
-      }
+      for (int j = 0; j < N; ++j) total[j] += more[j];
+      if (!(open[g] & 4u)) return false;
     }
-    const bool goes_on = key == after && key != kNone;
-    close(goes_on);
-    if (open) {
-      head = key;
-      if (goes_on) {  // all of the group is one run's: a second part, of nothing, keeps the run's parts neighbours
-        tail = key;
-        for (int j = 0; j < N; ++j) a.parts[(2 * group + 1) * a.dim + col + j] = 0.f;
-      }
-    } else if (goes_on) {
-      tail = key;
+    return true;
+  };
+  auto leave = [&](uint32_t which, uint32_t row, const float (&total)[N]) {
+    if (mine == 0u && blockIdx.y == 0u) a.part_keys[2u * blockIdx.x + which] = row;
+    if (in)
+#pragma unroll
+      for (int j = 0; j < N; ++j) a.parts[(2ull * blockIdx.x + which) * a.dim + col + j] = total[j];
+  };
+  const float none[N] = {};
+  if (group == 0u && a.part_keys) {
+    if (open[0] & 1u) {  // (all of the workgroup one row's: a second sum, of nothing, keeps the row's sums neighbours)
+      float total[N] = {};
+      const uint32_t row = key_of[0];
+      if (follow(0u, total)) leave(1u, row, none);
+      leave(0u, row, total);
+    } else if (mine == 0u && blockIdx.y == 0u) {
+      a.part_keys[2u * blockIdx.x] = kNone;
     }
-    if (col == 0u && a.part_keys) {
-      a.part_keys[2 * group] = head;
-      a.part_keys[2 * group + 1] = tail;
-    }
+    if (!(open[groups - 1u] & 2u) && mine == 0u && blockIdx.y == 0u) a.part_keys[2u * blockIdx.x + 1u] = kNone;
+  }
+  if (goes_on && !whole) {
+    float total[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) total[j] = tail[j];
+    if (follow(group + 1u, total)) leave(1u, last, total);
+    else write(last, total);
   }
 }
 
@@ -264,11 +322,12 @@ bool lay_out(Layout& l, uint64_t total, uint64_t n_records, uint32_t n_slots, ui
   l.counts = take(4ull * 256 * l.n_tiles);
   l.totals = take(4 * 256);
   l.share = take(mean ? 4 * n_records * n_slots : 0);
-  uint64_t groups = ceil_div(total, kRun);
+  // (as many workgroups as there are where each has the fewest terms: a wavefront for each group)
+  uint64_t blocks = ceil_div(total, 4 * kRun);
   for (int i = 0; i < 2; ++i) {
-    l.part_keys[i] = take(4 * 2 * groups);
-    l.parts[i] = take(4ull * 2 * groups * dim);
-    groups = ceil_div(2 * groups, kRun);
+    l.part_keys[i] = take(4 * 2 * blocks);
+    l.parts[i] = take(4ull * 2 * blocks * dim);
+    blocks = ceil_div(2 * blocks, 4 * kRun);
   }
   l.bytes = at;
   return true;
@@ -279,19 +338,21 @@ void sum_rows(SumArgs a, const Layout& l, char* scratch, uint64_t rows, hipStrea
   const uint64_t packs = rows * (a.dim / N);
   const uint32_t clear = (uint32_t)(ceil_div(packs, 256) < 16384 ? ceil_div(packs, 256) : 16384);
   hipLaunchKernelGGL((k_clear_rows<T, N>), dim3(clear), dim3(256), 0, stream, a.dtable, rows, a.dim, a.table_stride);
+  const uint32_t groups = 256u >> a.lanes_log2, columns = N << a.lanes_log2;
   int side = 0;
   for (bool first = true; a.n; first = false) {
-    const uint64_t groups = ceil_div(a.n, kRun);
-    const bool last = groups == 1;
+    const uint64_t blocks = ceil_div(a.n, groups * kRun);
+    const bool last = blocks == 1;
     a.part_keys = last ? nullptr : (uint32_t*)(scratch + l.part_keys[side]);
     a.parts = last ? nullptr : (float*)(scratch + l.parts[side]);
-    const dim3 grid((uint32_t)ceil_div(groups << a.lanes_log2, 256));
-    if (first) hipLaunchKernelGGL((k_sum_rows<T, N, true>), grid, dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL((k_sum_rows<T, N, false>), grid, dim3(256), 0, stream, a);
+    const dim3 grid((uint32_t)blocks, (uint32_t)ceil_div(a.dim, columns));
+    const uint32_t lds = 4u * ((first ? 2u : 1u) * groups * (kRun + 1u) + 2u + groups + groups * 2u * columns);
+    if (first) hipLaunchKernelGGL((k_sum_rows<T, N, true>), grid, dim3(256), lds, stream, a);
+    else hipLaunchKernelGGL((k_sum_rows<T, N, false>), grid, dim3(256), lds, stream, a);
     if (last) break;
     a.keys = a.part_keys;
     a.terms = a.parts;
-    a.n = (uint32_t)(2 * groups);
+    a.n = (uint32_t)(2 * blocks);
     side ^= 1;
   }
 }
@@ -394,11 +455,14 @@ extern "C" fbx_status fbx_embed_backward(const fbx_slot_view* slots, uint32_t n_
   a.record_stride = record_stride;
   a.table_stride = table_stride;
   a.n = l.n;
-  a.n_records = (uint32_t)n_records;
+  a.n_from = (uint32_t)(n_records * n_slots);
+  a.dense = record_stride == (uint64_t)n_slots * dim;
   a.all_slots = n_slots;
   a.rows = (uint32_t)rows;
   a.dim = dim;
-  while ((1u << a.lanes_log2) * n < dim && a.lanes_log2 < 6u) ++a.lanes_log2;
+  // (as many lanes as rows of whole 16 bytes take, whatever they are: in what order sums are formed is not to follow from
+  // where a tensor lies)
+  while ((1u << a.lanes_log2) * (16u / e) < dim && a.lanes_log2 < 6u) ++a.lanes_log2;
   if (dtype == FBX_F32) sum_rows_by_width<float>(a, n, l, scratch, rows, stream);
   else if (dtype == FBX_F16) sum_rows_by_width<_Float16>(a, n, l, scratch, rows, stream);
   else sum_rows_by_width<__bf16>(a, n, l, scratch, rows, stream);
