@@ -19,33 +19,64 @@ struct PairArgs {
   uint32_t n_slots, first_slot, all_slots, rows, tile;
 };
 
-// A lane a (record, slot): its signs' rows, and where each came from, at the signs' own positions.
+// A workgroup 256 records of a slot: their signs' rows, and where each came from, at the signs' own positions.  A lane takes
+// a record's signs where there is one a record, or where records need not follow each other (arrival order); else lanes
+// take neighbouring signs and look up whose they are.
 __global__ __launch_bounds__(256) void k_pairs(PairArgs) {
   const PairArgs& a = launch_args<PairArgs>();
-  const uint64_t r = (uint64_t)blockIdx.x * 256u + threadIdx.x;
-  if (r >= a.n_records) return;
+  __shared__ uint32_t ends[256];  // of the records' signs, from the first record's first on
   const SlotRef& s = a.slots[blockIdx.y];
-  uint64_t b;
-  uint32_t c;
-  signs_of(s, r, a.n_records, a.tile, b, c);
-  const uint32_t from = (uint32_t)r * a.all_slots + a.first_slot + blockIdx.y;
-  for (uint32_t i = 0; i < c; ++i) {
-    a.keys[s.base + b + i] = row_of(s.values[b + i], a.rows);
-    a.from[s.base + b + i] = from;
+  const uint64_t r0 = (uint64_t)blockIdx.x * 256u, r = r0 + threadIdx.x;
+  const uint32_t n = (uint32_t)(a.n_records - r0 < 256u ? a.n_records - r0 : 256u);
+  const uint32_t first = (uint32_t)r0 * a.all_slots + a.first_slot + blockIdx.y;  // of the first record
+  uint64_t b = 0;
+  uint32_t c = 0;
+  if (threadIdx.x < n) {
+    signs_of(s, r, a.n_records, a.tile, b, c);
+    if (a.share) a.share[first + threadIdx.x * a.all_slots] = c > 1u ? 1.f / (float)c : 1.f;
   }
-  if (a.share) a.share[from] = c > 1u ? 1.f / (float)c : 1.f;
+  if (!s.offsets || s.tile_ends) {
+    const uint32_t from = first + threadIdx.x * a.all_slots;
+    for (uint32_t i = 0; i < c; ++i) {
+      a.keys[s.base + b + i] = row_of(s.values[b + i], a.rows);
+      a.from[s.base + b + i] = from;
+    }
+    return;
+  }
+  const uint64_t begin = s.offsets[r0];
+  if (threadIdx.x < n) ends[threadIdx.x] = (uint32_t)(b + c - begin);
+  __syncthreads();
+  const uint32_t all = begin < s.n_values ? ends[n - 1u] : 0u;
+  const uint64_t room = begin < s.n_values ? s.n_values - begin : 0u;
+  for (uint32_t i = threadIdx.x; i < all && i < room; i += 256u) {
+    uint32_t lo = 0, hi = n;  // the first record that ends behind sign i
+    while (lo < hi) {
+      const uint32_t mid = (lo + hi) / 2u;
+      if (ends[mid] > i) hi = mid;
+      else lo = mid + 1u;
+    }
+    a.keys[s.base + begin + i] = row_of(s.values[begin + i], a.rows);
+    a.from[s.base + begin + i] = first + lo * a.all_slots;
+  }
 }
 
-// Per tile of pairs, how many have each value of the digit; counts lie digit by digit.
+// Per tile of pairs, how many have each value of the digit; counts lie digit by digit.  (A wavefront has counters of its
+// own: the most frequent rows' digits are most of a tile's.)
+template <uint32_t kBits>
 __global__ __launch_bounds__(256) void k_digit_counts(const uint32_t* keys, uint32_t n, uint32_t shift, uint32_t n_tiles, uint32_t* counts) {
-  __shared__ uint32_t h[256];
-  h[threadIdx.x] = 0u;
+  constexpr uint32_t kBins = 1u << kBits;
+  __shared__ uint32_t h[4][kBins];
+  for (uint32_t i = threadIdx.x; i < 4u * kBins; i += 256u) h[i / kBins][i % kBins] = 0u;
   __syncthreads();
   const uint64_t at = (uint64_t)blockIdx.x * kSortTile;
-  for (uint32_t i = threadIdx.x; i < kSortTile; i += 256u)
-    if (at + i < n) atomicAdd(&h[(keys[at + i] >> shift) & 255u], 1u);
+  uint32_t k[kSortItems];
+#pragma unroll
+  for (uint32_t i = 0; i < kSortItems; ++i) k[i] = at + i * 256u + threadIdx.x < n ? keys[at + i * 256u + threadIdx.x] : 0u;
+#pragma unroll
+  for (uint32_t i = 0; i < kSortItems; ++i)
+    if (at + i * 256u + threadIdx.x < n) atomicAdd(&h[threadIdx.x / 64u][(k[i] >> shift) % kBins], 1u);
   __syncthreads();
-  counts[threadIdx.x * (uint64_t)n_tiles + blockIdx.x] = h[threadIdx.x];
+  for (uint32_t d = threadIdx.x; d < kBins; d += 256u) counts[d * (uint64_t)n_tiles + blockIdx.x] = h[0][d] + h[1][d] + h[2][d] + h[3][d];
 }
 
 // Inclusive sums over the workgroup's 256 lanes.
@@ -63,13 +94,25 @@ __device__ __forceinline__ uint32_t sums_256(uint32_t v, uint32_t* four) {
 
 // A workgroup a digit: counts of its tiles become how many pairs of earlier tiles have the digit.
 __global__ __launch_bounds__(256) void k_digit_sums(uint32_t* counts, uint32_t n_tiles, uint32_t* totals) {
+  constexpr uint32_t kEach = 8;
   __shared__ uint32_t four[4];
   __shared__ uint32_t all;
   uint32_t* c = counts + blockIdx.x * (uint64_t)n_tiles;
   uint32_t before = 0u;
-  for (uint32_t i0 = 0; i0 < n_tiles; i0 += 256u) {
-    const uint32_t i = i0 + threadIdx.x, v = i < n_tiles ? c[i] : 0u, sum = sums_256(v, four);
-    if (i < n_tiles) c[i] = before + sum - v;
+  for (uint32_t i0 = 0; i0 < n_tiles; i0 += 256u * kEach) {
+    const uint32_t i = i0 + threadIdx.x * kEach;
+    uint32_t v[kEach], mine = 0u;
+#pragma unroll
+    for (uint32_t e = 0; e < kEach; ++e) v[e] = i + e < n_tiles ? c[i + e] : 0u;
+#pragma unroll
+    for (uint32_t e = 0; e < kEach; ++e) mine += v[e];
+    const uint32_t sum = sums_256(mine, four);
+    uint32_t at = before + sum - mine;
+#pragma unroll
+    for (uint32_t e = 0; e < kEach; ++e) {
+      if (i + e < n_tiles) c[i + e] = at;
+      at += v[e];
+    }
     if (threadIdx.x == 255u) all = sum;
     __syncthreads();
     before += all;
@@ -80,12 +123,14 @@ __global__ __launch_bounds__(256) void k_digit_sums(uint32_t* counts, uint32_t n
 // Moves a tile's pairs to where their digit's pairs go, in order: ranks inside a wavefront by comparing digits over
 // its lanes, then over wavefronts and digits by sums; the tile is put in order in LDS, so that pairs of one digit are
 // written next to each other.
+template <uint32_t kBits>
 __global__ __launch_bounds__(256) void k_move_pairs(const uint32_t* keys, const uint32_t* from, uint32_t n, uint32_t shift, uint32_t n_tiles,
                                                     const uint32_t* counts, const uint32_t* totals, uint32_t* keys_out, uint32_t* from_out) {
-  __shared__ uint32_t seen[4][256], to[256], begin[256], four[4];
+  constexpr uint32_t kBins = 1u << kBits, kMine = kBins / 256u;  // a lane's digits: kMine neighbours
+  __shared__ uint32_t seen[4][kBins], to[kBins], begin[kBins], four[4];
   __shared__ uint32_t k_lds[kSortTile], f_lds[kSortTile];
   const uint32_t lane = threadIdx.x % 64u, wave = threadIdx.x / 64u;
-  for (uint32_t w = 0; w < 4u; ++w) seen[w][threadIdx.x] = 0u;
+  for (uint32_t i = threadIdx.x; i < 4u * kBins; i += 256u) seen[i / kBins][i % kBins] = 0u;
   __syncthreads();
   const uint64_t at = (uint64_t)blockIdx.x * kSortTile + wave * (kSortItems * 64u) + lane;
   uint32_t k[kSortItems], f[kSortItems], rank[kSortItems];
@@ -99,10 +144,10 @@ __global__ __launch_bounds__(256) void k_move_pairs(const uint32_t* keys, const 
 #pragma unroll
   for (uint32_t i = 0; i < kSortItems; ++i) {
     const bool in = at + i * 64u < n;
-    const uint32_t d = (k[i] >> shift) & 255u;
+    const uint32_t d = (k[i] >> shift) % kBins;
     uint64_t same = __ballot(in);
 #pragma unroll
-    for (uint32_t b = 0; b < 8u; ++b) {
+    for (uint32_t b = 0; b < kBits; ++b) {
       const uint64_t set = __ballot((d >> b) & 1u);
       same &= (d >> b) & 1u ? set : ~set;
     }
@@ -112,31 +157,53 @@ __global__ __launch_bounds__(256) void k_move_pairs(const uint32_t* keys, const 
     __builtin_amdgcn_wave_barrier();
   }
   __syncthreads();
-  uint32_t mine = 0u;
-  for (uint32_t w = 0; w < 4u; ++w) {
-    const uint32_t c = seen[w][threadIdx.x];
-    seen[w][threadIdx.x] = mine;
-    mine += c;
+  uint32_t mine[kMine], total[kMine], sum = 0u, sum_all = 0u;
+#pragma unroll
+  for (uint32_t e = 0; e < kMine; ++e) {
+    const uint32_t d = threadIdx.x * kMine + e;
+    mine[e] = 0u;
+    for (uint32_t w = 0; w < 4u; ++w) {
+      const uint32_t c = seen[w][d];
+      seen[w][d] = mine[e];
+      mine[e] += c;
+    }
+    total[e] = totals[d];
+    sum += mine[e];
+    sum_all += total[e];
   }
-  begin[threadIdx.x] = sums_256(mine, four) - mine;
-  const uint32_t total = totals[threadIdx.x];
-  to[threadIdx.x] = sums_256(total, four) - total + counts[threadIdx.x * (uint64_t)n_tiles + blockIdx.x];
+  uint32_t first = sums_256(sum, four) - sum, first_all = sums_256(sum_all, four) - sum_all;
+#pragma unroll
+  for (uint32_t e = 0; e < kMine; ++e) {
+    const uint32_t d = threadIdx.x * kMine + e;
+    begin[d] = first;
+    to[d] = first_all + counts[d * (uint64_t)n_tiles + blockIdx.x];
+    first += mine[e];
+    first_all += total[e];
+  }
   __syncthreads();
 #pragma unroll
   for (uint32_t i = 0; i < kSortItems; ++i)
     if (at + i * 64u < n) {
-      const uint32_t d = (k[i] >> shift) & 255u, p = begin[d] + seen[wave][d] + rank[i];
+      const uint32_t d = (k[i] >> shift) % kBins, p = begin[d] + seen[wave][d] + rank[i];
       k_lds[p] = k[i];
       f_lds[p] = f[i];
     }
   __syncthreads();
-  const uint64_t first = (uint64_t)blockIdx.x * kSortTile;
-  const uint32_t here = n - first < kSortTile ? (uint32_t)(n - first) : kSortTile;
+  const uint64_t first_pair = (uint64_t)blockIdx.x * kSortTile;
+  const uint32_t here = n - first_pair < kSortTile ? (uint32_t)(n - first_pair) : kSortTile;
   for (uint32_t i = threadIdx.x; i < here; i += 256u) {
-    const uint32_t d = (k_lds[i] >> shift) & 255u, p = to[d] + i - begin[d];
+    const uint32_t d = (k_lds[i] >> shift) % kBins, p = to[d] + i - begin[d];
     keys_out[p] = k_lds[i];
     from_out[p] = f_lds[i];
   }
+}
+
+template <uint32_t kBits>
+void sort_pass(uint32_t* const (&keys)[2], uint32_t* const (&from)[2], int side, uint32_t n, uint32_t shift, uint32_t n_tiles, uint32_t* counts, uint32_t* totals,
+               hipStream_t stream) {
+  hipLaunchKernelGGL(k_digit_counts<kBits>, dim3(n_tiles), dim3(256), 0, stream, keys[side], n, shift, n_tiles, counts);
+  hipLaunchKernelGGL(k_digit_sums, dim3(1u << kBits), dim3(256), 0, stream, counts, n_tiles, totals);
+  hipLaunchKernelGGL(k_move_pairs<kBits>, dim3(n_tiles), dim3(256), 0, stream, keys[side], from[side], n, shift, n_tiles, counts, totals, keys[side ^ 1], from[side ^ 1]);
 }
 
 struct SumArgs {
@@ -301,7 +368,7 @@ __global__ __launch_bounds__(256) void k_clear_rows(void* to, uint64_t rows, uin
 // Where things lie in the scratch.
 struct Layout {
   uint64_t keys[2], from[2], counts, totals, share, part_keys[2], parts[2], bytes;
-  uint32_t n, n_tiles, passes;
+  uint32_t n, n_tiles, passes, bits;  // bits: of a pass's digit
 };
 
 bool lay_out(Layout& l, uint64_t total, uint64_t n_records, uint32_t n_slots, uint64_t rows, uint32_t dim, bool mean) {
@@ -310,7 +377,8 @@ bool lay_out(Layout& l, uint64_t total, uint64_t n_records, uint32_t n_slots, ui
   l.n_tiles = (uint32_t)ceil_div(total, kSortTile);
   uint32_t bits = 1;
   while ((rows - 1) >> bits) ++bits;
-  l.passes = (bits + 7u) / 8u;
+  l.passes = (bits + 8u) / 9u;  // (digits of nine bits where they save a pass)
+  l.bits = (bits + l.passes - 1u) / l.passes > 8u ? 9u : 8u;
   uint64_t at = 0;
   auto take = [&](uint64_t bytes) {
     const uint64_t was = at;
@@ -319,8 +387,8 @@ bool lay_out(Layout& l, uint64_t total, uint64_t n_records, uint32_t n_slots, ui
   };
   for (int i = 0; i < 2; ++i) l.keys[i] = take(4 * total);
   for (int i = 0; i < 2; ++i) l.from[i] = take(4 * total);
-  l.counts = take(4ull * 256 * l.n_tiles);
-  l.totals = take(4 * 256);
+  l.counts = take(4ull * l.n_tiles << l.bits);
+  l.totals = take(4ull << l.bits);
   l.share = take(mean ? 4 * n_records * n_slots : 0);
   // (as many workgroups as there are where each has the fewest terms: a wavefront for each group)
   uint64_t blocks = ceil_div(total, 4 * kRun);
@@ -437,10 +505,8 @@ extern "C" fbx_status fbx_embed_backward(const fbx_slot_view* slots, uint32_t n_
       hipLaunchKernelGGL(k_pairs, dim3((uint32_t)ceil_div(n_records, 256), p.n_slots), dim3(256), 0, stream, p);
     }
     for (uint32_t pass = 0; pass < l.passes; ++pass, side ^= 1) {
-      hipLaunchKernelGGL(k_digit_counts, dim3(l.n_tiles), dim3(256), 0, stream, keys[side], l.n, 8 * pass, l.n_tiles, counts);
-      hipLaunchKernelGGL(k_digit_sums, dim3(256), dim3(256), 0, stream, counts, l.n_tiles, totals);
-      hipLaunchKernelGGL(k_move_pairs, dim3(l.n_tiles), dim3(256), 0, stream, keys[side], from[side], l.n, 8 * pass, l.n_tiles, counts, totals,
-                         keys[side ^ 1], from[side ^ 1]);
+      if (l.bits == 9u) sort_pass<9>(keys, from, side, l.n, 9 * pass, l.n_tiles, counts, totals, stream);
+      else sort_pass<8>(keys, from, side, l.n, 8 * pass, l.n_tiles, counts, totals, stream);
     }
   }
   const uint64_t all = (uintptr_t)d_dout | (uintptr_t)d_dtable | dim * e | table_stride * e | record_stride * e;
