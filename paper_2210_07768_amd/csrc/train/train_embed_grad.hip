@@ -6,7 +6,9 @@ namespace fbx {
 namespace train {
 namespace {
 
-constexpr uint32_t kSortItems = 16, kSortTile = 256 * kSortItems;  // pairs of a lane, of a workgroup
+// Pairs of a lane when sorting; a workgroup has 256 lanes.  Sixteen put more pairs of one digit next to each other; four
+// make a pass shorter where there are too few pairs to fill the card (98,000 pairs: 10.8 us a pass and 6.4).
+constexpr uint32_t kManyItems = 16, kFewItems = 4, kFewPairs = 1u << 18;
 constexpr uint32_t kRun = 16, kAhead = 8;                          // sorted terms a group of lanes adds up, and has on their way
 constexpr uint32_t kNone = 0xffffffffu;
 
@@ -62,18 +64,18 @@ __global__ __launch_bounds__(256) void k_pairs(PairArgs) {
 
 // Per tile of pairs, how many have each value of the digit; counts lie digit by digit.  (A wavefront has counters of its
 // own: the most frequent rows' digits are most of a tile's.)
-template <uint32_t kBits>
+template <uint32_t kBits, uint32_t kItems>
 __global__ __launch_bounds__(256) void k_digit_counts(const uint32_t* keys, uint32_t n, uint32_t shift, uint32_t n_tiles, uint32_t* counts) {
   constexpr uint32_t kBins = 1u << kBits;
   __shared__ uint32_t h[4][kBins];
   for (uint32_t i = threadIdx.x; i < 4u * kBins; i += 256u) h[i / kBins][i % kBins] = 0u;
   __syncthreads();
-  const uint64_t at = (uint64_t)blockIdx.x * kSortTile;
-  uint32_t k[kSortItems];
+  const uint64_t at = (uint64_t)blockIdx.x * (256u * kItems);
+  uint32_t k[kItems];
 #pragma unroll
-  for (uint32_t i = 0; i < kSortItems; ++i) k[i] = at + i * 256u + threadIdx.x < n ? keys[at + i * 256u + threadIdx.x] : 0u;
+  for (uint32_t i = 0; i < kItems; ++i) k[i] = at + i * 256u + threadIdx.x < n ? keys[at + i * 256u + threadIdx.x] : 0u;
 #pragma unroll
-  for (uint32_t i = 0; i < kSortItems; ++i)
+  for (uint32_t i = 0; i < kItems; ++i)
     if (at + i * 256u + threadIdx.x < n) atomicAdd(&h[threadIdx.x / 64u][(k[i] >> shift) % kBins], 1u);
   __syncthreads();
   for (uint32_t d = threadIdx.x; d < kBins; d += 256u) counts[d * (uint64_t)n_tiles + blockIdx.x] = h[0][d] + h[1][d] + h[2][d] + h[3][d];
@@ -123,26 +125,26 @@ __global__ __launch_bounds__(256) void k_digit_sums(uint32_t* counts, uint32_t n
 // Moves a tile's pairs to where their digit's pairs go, in order: ranks inside a wavefront by comparing digits over
 // its lanes, then over wavefronts and digits by sums; the tile is put in order in LDS, so that pairs of one digit are
 // written next to each other.
-template <uint32_t kBits>
+template <uint32_t kBits, uint32_t kItems>
 __global__ __launch_bounds__(256) void k_move_pairs(const uint32_t* keys, const uint32_t* from, uint32_t n, uint32_t shift, uint32_t n_tiles,
                                                     const uint32_t* counts, const uint32_t* totals, uint32_t* keys_out, uint32_t* from_out) {
   constexpr uint32_t kBins = 1u << kBits, kMine = kBins / 256u;  // a lane's digits: kMine neighbours
   __shared__ uint32_t seen[4][kBins], to[kBins], begin[kBins], four[4];
-  __shared__ uint32_t k_lds[kSortTile], f_lds[kSortTile];
+  __shared__ uint32_t k_lds[(256u * kItems)], f_lds[(256u * kItems)];
   const uint32_t lane = threadIdx.x % 64u, wave = threadIdx.x / 64u;
   for (uint32_t i = threadIdx.x; i < 4u * kBins; i += 256u) seen[i / kBins][i % kBins] = 0u;
   __syncthreads();
-  const uint64_t at = (uint64_t)blockIdx.x * kSortTile + wave * (kSortItems * 64u) + lane;
-  uint32_t k[kSortItems], f[kSortItems], rank[kSortItems];
+  const uint64_t at = (uint64_t)blockIdx.x * (256u * kItems) + wave * (kItems * 64u) + lane;
+  uint32_t k[kItems], f[kItems], rank[kItems];
 #pragma unroll
-  for (uint32_t i = 0; i < kSortItems; ++i) {
+  for (uint32_t i = 0; i < kItems; ++i) {
     const bool in = at + i * 64u < n;
     k[i] = in ? keys[at + i * 64u] : 0u;
     f[i] = in ? from[at + i * 64u] : 0u;
   }
   const uint64_t below = (1ull << lane) - 1ull;
 #pragma unroll
-  for (uint32_t i = 0; i < kSortItems; ++i) {
+  for (uint32_t i = 0; i < kItems; ++i) {
     const bool in = at + i * 64u < n;
     const uint32_t d = (k[i] >> shift) % kBins;
     uint64_t same = __ballot(in);
@@ -182,15 +184,15 @@ __global__ __launch_bounds__(256) void k_move_pairs(const uint32_t* keys, const 
   }
   __syncthreads();
 #pragma unroll
-  for (uint32_t i = 0; i < kSortItems; ++i)
+  for (uint32_t i = 0; i < kItems; ++i)
     if (at + i * 64u < n) {
       const uint32_t d = (k[i] >> shift) % kBins, p = begin[d] + seen[wave][d] + rank[i];
       k_lds[p] = k[i];
       f_lds[p] = f[i];
     }
   __syncthreads();
-  const uint64_t first_pair = (uint64_t)blockIdx.x * kSortTile;
-  const uint32_t here = n - first_pair < kSortTile ? (uint32_t)(n - first_pair) : kSortTile;
+  const uint64_t first_pair = (uint64_t)blockIdx.x * (256u * kItems);
+  const uint32_t here = n - first_pair < (256u * kItems) ? (uint32_t)(n - first_pair) : (256u * kItems);
   for (uint32_t i = threadIdx.x; i < here; i += 256u) {
     const uint32_t d = (k_lds[i] >> shift) % kBins, p = to[d] + i - begin[d];
     keys_out[p] = k_lds[i];
@@ -198,12 +200,12 @@ __global__ __launch_bounds__(256) void k_move_pairs(const uint32_t* keys, const 
   }
 }
 
-template <uint32_t kBits>
+template <uint32_t kBits, uint32_t kItems>
 void sort_pass(uint32_t* const (&keys)[2], uint32_t* const (&from)[2], int side, uint32_t n, uint32_t shift, uint32_t n_tiles, uint32_t* counts, uint32_t* totals,
                hipStream_t stream) {
-  hipLaunchKernelGGL(k_digit_counts<kBits>, dim3(n_tiles), dim3(256), 0, stream, keys[side], n, shift, n_tiles, counts);
+  hipLaunchKernelGGL((k_digit_counts<kBits, kItems>), dim3(n_tiles), dim3(256), 0, stream, keys[side], n, shift, n_tiles, counts);
   hipLaunchKernelGGL(k_digit_sums, dim3(1u << kBits), dim3(256), 0, stream, counts, n_tiles, totals);
-  hipLaunchKernelGGL(k_move_pairs<kBits>, dim3(n_tiles), dim3(256), 0, stream, keys[side], from[side], n, shift, n_tiles, counts, totals, keys[side ^ 1], from[side ^ 1]);
+  hipLaunchKernelGGL((k_move_pairs<kBits, kItems>), dim3(n_tiles), dim3(256), 0, stream, keys[side], from[side], n, shift, n_tiles, counts, totals, keys[side ^ 1], from[side ^ 1]);
 }
 
 struct SumArgs {
@@ -368,13 +370,14 @@ __global__ __launch_bounds__(256) void k_clear_rows(void* to, uint64_t rows, uin
 // Where things lie in the scratch.
 struct Layout {
   uint64_t keys[2], from[2], counts, totals, share, part_keys[2], parts[2], bytes;
-  uint32_t n, n_tiles, passes, bits;  // bits: of a pass's digit
+  uint32_t n, n_tiles, passes, bits, items;  // bits: of a pass's digit; items: pairs of a lane
 };
 
 bool lay_out(Layout& l, uint64_t total, uint64_t n_records, uint32_t n_slots, uint64_t rows, uint32_t dim, bool mean) {
   if (total >> 32 || n_records * n_slots >> 32) return false;
   l.n = (uint32_t)total;
-  l.n_tiles = (uint32_t)ceil_div(total, kSortTile);
+  l.items = total <= kFewPairs ? kFewItems : kManyItems;
+  l.n_tiles = (uint32_t)ceil_div(total, 256u * l.items);
   uint32_t bits = 1;
   while ((rows - 1) >> bits) ++bits;
   l.passes = (bits + 8u) / 9u;  // (digits of nine bits where they save a pass)
@@ -505,8 +508,9 @@ extern "C" fbx_status fbx_embed_backward(const fbx_slot_view* slots, uint32_t n_
       hipLaunchKernelGGL(k_pairs, dim3((uint32_t)ceil_div(n_records, 256), p.n_slots), dim3(256), 0, stream, p);
     }
     for (uint32_t pass = 0; pass < l.passes; ++pass, side ^= 1) {
-      if (l.bits == 9u) sort_pass<9>(keys, from, side, l.n, 9 * pass, l.n_tiles, counts, totals, stream);
-      else sort_pass<8>(keys, from, side, l.n, 8 * pass, l.n_tiles, counts, totals, stream);
+      const auto sort = l.bits == 9u ? (l.items == kFewItems ? sort_pass<9, kFewItems> : sort_pass<9, kManyItems>)
+                                     : (l.items == kFewItems ? sort_pass<8, kFewItems> : sort_pass<8, kManyItems>);
+      sort(keys, from, side, l.n, l.bits * pass, l.n_tiles, counts, totals, stream);
     }
   }
   const uint64_t all = (uintptr_t)d_dout | (uintptr_t)d_dtable | dim * e | table_stride * e | record_stride * e;
