@@ -7,7 +7,10 @@ namespace fbx {
 namespace train {
 namespace {
 
-__device__ __forceinline__ float logistic(float a) { return 1.f / (1.f + expf(-a)); }
+// e^a and 1 / a by the hardware's approximations (one unit in the last place each, and |a| units for what a log2 e is rounded
+// by): the exact division and exponential of 64 elements a lane were an eighth of a large product's time.
+__device__ __forceinline__ float exponential(float a) { return __builtin_amdgcn_exp2f(a * 1.4426950408889634f); }
+__device__ __forceinline__ float logistic(float a) { return __builtin_amdgcn_rcpf(1.f + exponential(-a)); }
 __device__ __forceinline__ float bell_below(float a) { return 0.5f * (1.f + erff(a * 0.70710678118654752f)); }
 
 template <int kAct>
@@ -23,7 +26,7 @@ __device__ __forceinline__ float slope(float a) {
     const float s = logistic(a);
     return s * (1.f + a * (1.f - s));
   }
-  if (kAct == FBX_ACT_GELU) return bell_below(a) + a * expf(-0.5f * a * a) * 0.39894228040143268f;
+  if (kAct == FBX_ACT_GELU) return bell_below(a) + a * exponential(-0.5f * a * a) * 0.39894228040143268f;
   if (kAct == FBX_ACT_RELU) return a > 0.f ? 1.f : 0.f;
   const float s = logistic(a);
   return s * (1.f - s);
@@ -73,6 +76,8 @@ __device__ __forceinline__ f32x4 mma(Frag<float>::type a, Frag<float>::type b, f
   return c;
 }
 
+__device__ __forceinline__ uint32_t same(uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); }  // (in all lanes)
+
 // A tile of one operand in LDS: kStepBytes of depth for R rows, R * 128 bytes, filled by loads that go past the
 // registers: lane l's 16 bytes land at 16 l behind the wavefront's place, so the layout is made by which 16 bytes a lane asks for.
 //   along depth (kAcross = false): a row's 128 bytes are eight chunks, chunk c of row r at place c ^ (r % 8), so that the 16
@@ -115,13 +120,19 @@ struct Tile {
   // depth_left (along): elements of depth from this step on
   __device__ void load(lds_char* to, const char* from, uint64_t ld, uint32_t lines, uint32_t depth_left, uint32_t line_bytes, uint32_t wave) const {
     const uint32_t most = kAcross ? (uint32_t)kDepth : (uint32_t)R, n = lines < most ? lines : most;
-    // (one for the wavefront: said so, lest the compiler loop over its lanes)
-    const uint32_t bytes = __builtin_amdgcn_readfirstlane(n ? (n - 1u) * (uint32_t)ld + line_bytes : 0u);
-    const uint32_t low = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)from), high = __builtin_amdgcn_readfirstlane((uint32_t)((uintptr_t)from >> 32));
-    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)((uint64_t)high << 32 | low), 0, bytes, 0x00020000);
+    // The buffer's descriptor (address, bytes, raw data): one for the wavefront, and said so, lest the compiler loop over
+    // its lanes.  The load is written out because the compiler, where it knows of loads into LDS, waits for all of them
+    // before a transposing read, whichever array that reads.  It has no result register; `arrived` waits for it.
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    const u32x4 r = {same((uint32_t)(uintptr_t)from), same((uint32_t)((uintptr_t)from >> 32) & 0xffffu), same(n ? (n - 1u) * (uint32_t)ld + line_bytes : 0u), 0x00020000u};
 #pragma unroll
-    for (int j = 0; j < kLoads; ++j)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(to + (wave * kLoads + j) * 1024), 16, kAcross || deep < depth_left ? offset[j] : kOutside, 0, 0, 0);
+    for (int j = 0; j < kLoads; ++j) {
+      const uint32_t at = same((uint32_t)(uintptr_t)to + (wave * kLoads + j) * 1024u);
+      const uint32_t o = kAcross || deep < depth_left ? offset[j] : kOutside;
+      // (five wait states between a vector instruction's write of a scalar register, the descriptor's, and its use here)
+      if (j == 0) asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(o), "s"(r) : "memory", "m0");
+      else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(o), "s"(r) : "memory", "m0");
+    }
   }
 
   // Rows first .. first + 15 of the operand, part `part` (0, 1) of the step's depth.
@@ -150,9 +161,9 @@ struct Tile {
   }
 };
 
-template <int kAct>
+template <int kValue>
 struct Kind {
-  static constexpr int value = kAct;
+  static constexpr int value = kValue;
 };
 
 // Four adjacent elements, of which the first n exist.
@@ -176,26 +187,31 @@ __device__ __forceinline__ void place(const MmArgs& p, uint32_t t, uint32_t& row
   col0 = in_band / high * BN;
 }
 
+// kSlopes: dh at four columns from c on, and from every 16th further on, of row r; zeros beyond it.
+template <class T, int kN>
+__device__ __forceinline__ void fetch_dh(const MmArgs& p, uint32_t r, uint32_t c0, Pack<T, 4> (&dh)[kN]) {
+#pragma unroll
+  for (int j = 0; j < kN; ++j) {
+    const uint32_t c = c0 + j * 16;
+    const T* from = (const T*)p.dh + (uint64_t)r * p.ld_dh + c;
+    dh[j] = Pack<T, 4>{};
+    if (r >= p.rows) continue;
+    if (p.wide && c + 4u <= p.columns) {
+      dh[j] = *(const Pack<T, 4>*)from;
+    } else {
+#pragma unroll
+      for (uint32_t e = 0; e < 4u; ++e)
+        if (c + e < p.columns) dh[j].v[e] = from[e];
+    }
+  }
+}
+
 // What becomes of 16 rows of a wavefront's sums (r: this lane's row; c0: its first column): they are rounded and stored.
+// dh: kSlopes, of the same places.
 template <class T, Form kForm, int kNF, int kAct>
-__device__ __forceinline__ void finish_rows(const MmArgs& p, uint32_t r, uint32_t c0, const f32x4 (&sum)[kNF]) {
+__device__ __forceinline__ void finish_rows(const MmArgs& p, uint32_t r, uint32_t c0, const f32x4 (&sum)[kNF], const Pack<T, 4> (&dh)[kNF / 2]) {
   if constexpr (kForm == kForward || kForm == kSlopes) {
     if (r >= p.rows) return;
-    Pack<T, 4> dh[kNF / 2] = {};
-    if (kForm == kSlopes) {
-#pragma unroll
-      for (int j = 0; j < kNF / 2; ++j) {
-        const uint32_t c = c0 + j * 16;
-        const T* from = (const T*)p.dh + (uint64_t)r * p.ld_dh + c;
-        if (p.wide && c + 4u <= p.columns) {
-          dh[j] = *(const Pack<T, 4>*)from;
-        } else {
-#pragma unroll
-          for (uint32_t e = 0; e < 4u; ++e)
-            if (c + e < p.columns) dh[j].v[e] = from[e];
-        }
-      }
-    }
 #pragma unroll
     for (int j = 0; j < kNF / 2; ++j) {
       const uint32_t c = c0 + j * 16;
@@ -236,13 +252,18 @@ struct Split {
   __device__ static uint32_t row(uint32_t row0, uint32_t wm, uint32_t lane, int i) { return row0 + wm * kRows + i * 16 + lane % 16u; }
   __device__ static uint32_t column(uint32_t col0, uint32_t wn, uint32_t lane) { return (kTwo ? col0 / 2u + wn * (kCols / 2) : col0 + wn * kCols) + lane / 16u * 4u; }
 
+  // (all of dh is asked for before any is needed: asked for while the products are formed it does not fit the registers)
   template <int kN>
   __device__ __forceinline__ static void finish(const MmArgs& p, uint32_t row0, uint32_t col0, uint32_t wm, uint32_t wn, uint32_t lane, int i0, const f32x4 (&sum)[kN][kNF]) {
     const uint32_t c = column(col0, wn, lane);
+    Pack<T, 4> dh[kN][kNF / 2];
+#pragma unroll
+    for (int i = 0; i < kN; ++i)
+      if (kForm == kSlopes) fetch_dh(p, row(row0, wm, lane, i0 + i), c, dh[i]);
     auto all = [&](auto kind) __attribute__((always_inline)) {
 #pragma unroll
       for (int i = 0; i < kN; ++i) {
-        finish_rows<T, kForm, kNF, decltype(kind)::value>(p, row(row0, wm, lane, i0 + i), c, sum[i]);
+        finish_rows<T, kForm, kNF, decltype(kind)::value>(p, row(row0, wm, lane, i0 + i), c, sum[i], dh[i]);
         __builtin_amdgcn_sched_barrier(0);
       }
     };
@@ -256,7 +277,8 @@ struct Split {
 // BM x BN of C a workgroup at a time, its WM x WN wavefronts side by side (kForward, kSlopes: BN / 2 columns of either
 // product).  C's rows come from A; its columns from B, which is the first side of the matrix instructions, so that a lane holds
 // four adjacent columns of a row.
-template <class T, Form kForm, int BM, int BN, int WM, int WN>
+// kStages: steps whose tiles are in LDS or on their way there.
+template <class T, Form kForm, int BM, int BN, int WM, int WN, int kStages>
 __global__ __launch_bounds__(WM * WN * 64) void k_mm(MmArgs p) {
 #ifdef __HIP_DEVICE_COMPILE__  // (the host's pass, which makes the launch stub of it, does not know the buffer's type)
   typedef Split<T, kForm, BM, BN, WM, WN> S;
@@ -264,8 +286,11 @@ __global__ __launch_bounds__(WM * WN * 64) void k_mm(MmArgs p) {
   constexpr int kWaves = WM * WN, kMF = S::kMF, kNF = S::kNF, kDepth = kStepBytes / sizeof(T);
   typedef Tile<T, BM, kWaves, kForm == kWeights> TileA;
   typedef Tile<T, BN, kWaves, !kTwo> TileB;
+  // (arrays of their own, so that the compiler knows which of them a load goes to)
   __shared__ alignas(1024) char a0[BM * kStepBytes], b0[BN * kStepBytes], a1[BM * kStepBytes], b1[BN * kStepBytes];
-  const uint32_t lane = threadIdx.x % 64u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64u), wm = wave % WM, wn = wave / WM;
+  __shared__ alignas(1024) char a2[kStages > 2 ? BM * kStepBytes : 16], b2[kStages > 2 ? BN * kStepBytes : 16];
+  __shared__ alignas(1024) char a3[kStages > 2 ? BM * kStepBytes : 16], b3[kStages > 2 ? BN * kStepBytes : 16];
+  const uint32_t lane = threadIdx.x % 64u, wave = same(threadIdx.x / 64u), wm = wave % WM, wn = wave / WM;
   // Workgroups go to the eight dies in turn: each die takes a stretch of the whole tiles, then one of the shares.
   uint32_t t, first = 0, end = p.steps, part = 0;
   {
@@ -282,10 +307,10 @@ __global__ __launch_bounds__(WM * WN * 64) void k_mm(MmArgs p) {
   }
   uint32_t row0, col0;
   place<BM, BN>(p, t, row0, col0);
-  row0 = __builtin_amdgcn_readfirstlane(row0);  // (quotients are worked out in vector registers)
-  col0 = __builtin_amdgcn_readfirstlane(col0);
-  first = __builtin_amdgcn_readfirstlane(first);
-  end = __builtin_amdgcn_readfirstlane(end);
+  row0 = same(row0);  // (quotients are worked out in vector registers)
+  col0 = same(col0);
+  first = same(first);
+  end = same(end);
 
   TileA ta;
   TileB tb;
@@ -293,7 +318,7 @@ __global__ __launch_bounds__(WM * WN * 64) void k_mm(MmArgs p) {
   const uint32_t turn = kForm == kInputs ? p.half / kDepth : 0u;  // kInputs: the first step whose lines are Wu's
   const char *a = (const char*)p.a, *b = (const char*)(up || (kForm == kInputs && first >= turn) ? p.b2 : p.b);
   const uint64_t ld_b = up || (kForm == kInputs && first >= turn) ? p.ld_b2 : p.ld_b;
-  const uint32_t b_lines = kTwo && col0 / 2u < p.columns ? __builtin_amdgcn_readfirstlane(p.columns - col0 / 2u) : 0u;
+  const uint32_t b_lines = kTwo && col0 / 2u < p.columns ? same(p.columns - col0 / 2u) : 0u;
   if (kForm == kWeights) {
     a += (uint64_t)row0 * sizeof(T);
     ta.begin(wave, lane, p.ld_a, 2 * p.half - row0);
@@ -308,16 +333,18 @@ __global__ __launch_bounds__(WM * WN * 64) void k_mm(MmArgs p) {
     b += (uint64_t)col0 * sizeof(T);
     tb.begin(wave, lane, ld_b, p.b_columns - col0);
   }
+  // (behind the last step: of nothing, so that every step's loads are as many)
   auto load = [&](char* to_a, char* to_b, uint32_t s) {
+    const bool none = s >= end;
     if (kForm == kWeights) {
-      const uint32_t left = p.depth - s * kDepth;
+      const uint32_t left = none ? 0u : p.depth - s * kDepth;
       ta.load((lds_char*)to_a, a + (uint64_t)s * kDepth * p.ld_a, p.ld_a, left, 0, (2 * p.half - row0) * sizeof(T), wave);
       tb.load((lds_char*)to_b, b + (uint64_t)s * kDepth * p.ld_b, p.ld_b, left, 0, (p.b_columns - col0) * sizeof(T), wave);
     } else {
       const uint32_t left = (kTwo ? p.depth : 2 * p.half) - s * kDepth;
-      ta.load((lds_char*)to_a, a + s * kStepBytes, p.ld_a, p.rows - row0, left, left * sizeof(T), wave);
+      ta.load((lds_char*)to_a, a + s * kStepBytes, p.ld_a, none ? 0u : p.rows - row0, left, left * sizeof(T), wave);
       if (kTwo) {
-        tb.load((lds_char*)to_b, b + s * kStepBytes, ld_b, b_lines, left, left * sizeof(T), wave);
+        tb.load((lds_char*)to_b, b + s * kStepBytes, ld_b, none ? 0u : b_lines, left, left * sizeof(T), wave);
       } else {  // (the weights one below the other, each made up to `half` lines: a step's lines are of one of them)
         if (s == turn) {
           b = (const char*)p.b2 + (uint64_t)col0 * sizeof(T);
@@ -325,14 +352,14 @@ __global__ __launch_bounds__(WM * WN * 64) void k_mm(MmArgs p) {
         }
         const uint32_t line = (s >= turn ? s - turn : s) * kDepth;
         const uint64_t ld = s >= turn ? p.ld_b2 : p.ld_b;
-        tb.load((lds_char*)to_b, b + line * ld, ld, p.depth - line, 0, (p.b_columns - col0) * sizeof(T), wave);
+        tb.load((lds_char*)to_b, b + line * ld, ld, none ? 0u : p.depth - line, 0, (p.b_columns - col0) * sizeof(T), wave);
       }
     }
   };
 
   // Two halves of a step's depth in turn: while one is multiplied out of registers the other's rows are read from LDS.
-  // A step's barrier lies between the halves: behind it the next step's tile is there (its loads had a whole step) and
-  // nobody reads this step's any more, so the loads of the step after the next go there.
+  // A step's barrier lies between the halves: behind it the next step's tile is there (its loads had kStages - 1 steps) and
+  // nobody reads this step's any more, so the loads of the step kStages later go there.
   f32x4 sum[kMF][kNF] = {};
   typename Frag<T>::type fa[2][kMF], fb[2][kNF];
   auto read = [&](int part, const char* in_a, const char* in_b) {
@@ -350,29 +377,52 @@ __global__ __launch_bounds__(WM * WN * 64) void k_mm(MmArgs p) {
 #pragma unroll
       for (int i = 0; i < kMF; ++i) sum[i][j] = mma(fb[part][j], fa[part][i], sum[i][j]);
   };
-  auto arrived = [] {  // (loads that go past the registers are not among what a barrier waits for)
-    __builtin_amdgcn_s_waitcnt(0x0f70);
-    __syncthreads();
+  // All but the last `steps` steps' loads are done, in every wavefront, and so are its reads.  (Loads that go past the
+  // registers are not among what a barrier waits for, and it is not to wait for more of them than this.)
+  auto arrived = [](auto steps) {
+    constexpr int n = decltype(steps)::value * (TileA::kLoads + TileB::kLoads);
+    static_assert(n < 64, "");
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt((n & 15) | (n >> 4) << 14 | 0x0070);  // (vmcnt n, lgkmcnt 0)
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
   };
   auto step = [&](char* at_a, char* at_b, const char* next_a, const char* next_b, uint32_t s) {
     read(1, at_a, at_b);
     multiply(0);
-    __builtin_amdgcn_sched_barrier(0);
-    arrived();
-    if (s + 2 < end) load(at_a, at_b, s + 2);
+    arrived(Kind<kStages - 2>());
+    load(at_a, at_b, s + kStages);
     __builtin_amdgcn_sched_barrier(0);
     read(0, next_a, next_b);  // (behind the last step: what is there, unused)
     multiply(1);
     __builtin_amdgcn_sched_barrier(0);
   };
   load(a0, b0, first);
-  if (first + 1 < end) load(a1, b1, first + 1);
-  arrived();
-  read(0, a0, b0);
-  for (uint32_t s = first; s < end; s += 2) {
-    step(a0, b0, a1, b1, s);
-    if (s + 1 < end) step(a1, b1, a0, b0, s + 1);
+  load(a1, b1, first + 1);
+  if constexpr (kStages == 4) {
+    load(a2, b2, first + 2);
+    load(a3, b3, first + 3);
   }
+  arrived(Kind<kStages - 1>());
+  read(0, a0, b0);
+  if constexpr (kStages == 4) {  // (left from within: on a way round that skips steps the compiler would wait for their loads)
+    for (uint32_t s = first;; s += 4) {
+      step(a0, b0, a1, b1, s);
+      if (s + 1 >= end) break;
+      step(a1, b1, a2, b2, s + 1);
+      if (s + 2 >= end) break;
+      step(a2, b2, a3, b3, s + 2);
+      if (s + 3 >= end) break;
+      step(a3, b3, a0, b0, s + 3);
+      if (s + 4 >= end) break;
+    }
+  } else {  // (not left from within: that costs a copy of the sums, which large tiles have no registers for)
+    for (uint32_t s = first; s < end; s += 2) {
+      step(a0, b0, a1, b1, s);
+      if (s + 1 < end) step(a1, b1, a0, b0, s + 1);
+    }
+  }
+  arrived(Kind<0>());  // (nothing is to land in LDS that may be another workgroup's by then)
 
   if (blockIdx.x < p.whole) {
     S::template finish<kMF>(p, row0, col0, wm, wn, lane, 0, sum);
@@ -456,23 +506,33 @@ __global__ __launch_bounds__(kFewWaves * 64) void k_few(MmArgs p) {
     both[1] += sums[w][1][lane];
   }
   const uint32_t c = blockIdx.x * 16u + g * 4u;
-  if (p.act == FBX_ACT_SILU) finish_rows<T, kForward, 2, FBX_ACT_SILU>(p, i, c, both);
-  else if (p.act == FBX_ACT_GELU) finish_rows<T, kForward, 2, FBX_ACT_GELU>(p, i, c, both);
-  else if (p.act == FBX_ACT_RELU) finish_rows<T, kForward, 2, FBX_ACT_RELU>(p, i, c, both);
-  else finish_rows<T, kForward, 2, FBX_ACT_SIGMOID>(p, i, c, both);
+  const Pack<T, 4> none[1] = {};
+  if (p.act == FBX_ACT_SILU) finish_rows<T, kForward, 2, FBX_ACT_SILU>(p, i, c, both, none);
+  else if (p.act == FBX_ACT_GELU) finish_rows<T, kForward, 2, FBX_ACT_GELU>(p, i, c, both, none);
+  else if (p.act == FBX_ACT_RELU) finish_rows<T, kForward, 2, FBX_ACT_RELU>(p, i, c, both, none);
+  else finish_rows<T, kForward, 2, FBX_ACT_SIGMOID>(p, i, c, both, none);
 #else
   (void)p;
 #endif
 }
 
-// Rows of n elements, each made `to` bytes long with zeros behind.
+// Copies of up to three matrices (blockIdx.y) whose rows of n elements are made `wide` long with zeros behind.
+struct PadArgs {
+  const void* from[3];
+  void* to[3];
+  uint64_t ld[3], rows[3];
+  uint32_t n, wide;
+};
 template <class T>
-__global__ __launch_bounds__(256) void k_pad_rows(const T* from, uint64_t ld, uint32_t n, T* to, uint32_t wide, uint64_t all) {
-  const uint64_t i = (uint64_t)blockIdx.x * 256u + threadIdx.x;
-  if (i >= all) return;
-  const uint64_t r = i / wide;
-  const uint32_t c = (uint32_t)(i - r * wide);
-  to[i] = c < n ? from[r * ld + c] : (T)0.f;
+__global__ __launch_bounds__(256) void k_pad_rows(PadArgs a) {
+  const T* from = (const T*)a.from[blockIdx.y];
+  T* to = (T*)a.to[blockIdx.y];
+  const uint64_t ld = a.ld[blockIdx.y], all = a.rows[blockIdx.y] * a.wide;
+  for (uint64_t i = (uint64_t)blockIdx.x * 256u + threadIdx.x; i < all; i += (uint64_t)gridDim.x * 256u) {
+    const uint64_t r = i / a.wide;
+    const uint32_t c = (uint32_t)(i - r * a.wide);
+    to[i] = c < a.n ? from[r * ld + c] : (T)0.f;
+  }
 }
 
 // How a product is cut: tiles of C, of which the last `shared` are shared out by steps of depth.
@@ -486,13 +546,13 @@ constexpr uint32_t Cut::kSide[3];
 
 // The cut that takes the least time, by what was measured (forward product, microseconds).  A workgroup takes `begin` and
 // its steps; `lone`: a step of one that has a compute unit to itself, `full`: of one among the `at_once` that fit one.
-// Large tiles read less from LDS for a product of 16-bit numbers (1.6 us a step of four 128 x 128 tiles' size against 1.9 and
-// 2.6), small ones begin sooner and leave fewer compute units idle; products of 32-bit numbers are bound by the matrix
+// Large tiles read less from LDS for a product of 16-bit numbers (1.6 us for 256 x 256 a step and compute unit, against 1.9
+// in tiles of 128 and 2.4 in tiles of 64), small ones begin sooner and leave fewer compute units idle; products of 32-bit numbers are bound by the matrix
 // units at every size.  Tiles that do not fill the card another time can be shared out by steps, which
 // costs a launch and their sums' way through memory: a write and a read at 5 TB/s.
 Cut cut(uint64_t rows, uint64_t columns, uint64_t steps, bool single) {
   struct Cost { uint32_t at_once; double begin, lone, full; };
-  constexpr Cost kCost[2][3] = {{{1, 8, 1.4, 1.6}, {2, 5.5, 0.5, 0.95}, {4, 3.5, 0.2, 0.65}}, {{1, 10, 7.0, 7.0}, {2, 6, 1.95, 3.9}, {4, 3, 0.55, 2.15}}};
+  constexpr Cost kCost[2][3] = {{{1, 8, 1.4, 1.6}, {2, 5.5, 0.5, 0.95}, {2, 3.5, 0.22, 0.3}}, {{1, 10, 7.0, 7.0}, {2, 6, 1.95, 3.9}, {4, 3, 0.55, 2.15}}};
   constexpr uint32_t kUnits = 256;  // compute units
   constexpr double kJoin = 3.5, kBytes = 2 / 5e6;
   Cut best{};
@@ -516,16 +576,16 @@ Cut cut(uint64_t rows, uint64_t columns, uint64_t steps, bool single) {
   return best;
 }
 
-template <class T, Form kForm, int BM, int BN, int WM, int WN>
+template <class T, Form kForm, int BM, int BN, int WM, int WN, int kStages>
 void launch(const MmArgs& p, uint32_t shared, hipStream_t stream) {
-  hipLaunchKernelGGL((k_mm<T, kForm, BM, BN, WM, WN>), dim3(p.whole + shared * p.shares), dim3(WM * WN * 64), 0, stream, p);
+  hipLaunchKernelGGL((k_mm<T, kForm, BM, BN, WM, WN, kStages>), dim3(p.whole + shared * p.shares), dim3(WM * WN * 64), 0, stream, p);
   if (shared) hipLaunchKernelGGL((k_join<T, kForm, BM, BN, WM, WN>), dim3(shared, BM / WM / 16), dim3(WM * WN * 64), 0, stream, p);
 }
 template <class T, Form kForm>
 void launch_by_size(const MmArgs& p, const Cut& c, hipStream_t stream) {
-  if (c.size == 0) launch<T, kForm, 256, 256, 2, 4>(p, c.shared, stream);
-  else if (c.size == 1) launch<T, kForm, 128, 128, 2, 2>(p, c.shared, stream);
-  else launch<T, kForm, 64, 64, 2, 2>(p, c.shared, stream);
+  if (c.size == 0) launch<T, kForm, 256, 256, 2, 4, 2>(p, c.shared, stream);
+  else if (c.size == 1) launch<T, kForm, 128, 128, 2, 2, 2>(p, c.shared, stream);
+  else launch<T, kForm, 64, 64, 2, 2, sizeof(T) == 2 ? 4 : 2>(p, c.shared, stream);
 }
 template <Form kForm>
 void launch_by_type(MmArgs& p, const Cut& c, fbx_dtype t, char* parts, hipStream_t stream) {
@@ -617,12 +677,6 @@ Shape shape_of(const fbx_gated* g, bool backward) {
   return s;
 }
 
-template <class T>
-void pad_rows(const void* from, uint64_t ld, uint32_t n, void* to, uint32_t wide, uint64_t rows, hipStream_t stream) {
-  const uint64_t all = rows * wide;
-  if (all) hipLaunchKernelGGL((k_pad_rows<T>), dim3((uint32_t)ceil_div(all, 256)), dim3(256), 0, stream, (const T*)from, ld, n, (T*)to, wide, all);
-}
-
 // Fills in where the kernels read x and the weights, copying those that need it.
 void operands(const fbx_gated* g, const Shape& s, char* scratch, const void* (&from)[3], uint64_t (&ld)[3], hipStream_t stream) {
   from[0] = g->d_x;
@@ -631,16 +685,31 @@ void operands(const fbx_gated* g, const Shape& s, char* scratch, const void* (&f
   ld[0] = g->ld_x;
   ld[1] = g->ld_w_gate;
   ld[2] = g->ld_w_up;
+  PadArgs a{};
+  a.n = g->inputs;
+  a.wide = s.wide;
+  uint32_t n = 0;
+  uint64_t most = 0;
   for (int i = 0; i < 3; ++i) {
+    const uint64_t rows = i ? g->hidden : g->records;
+    if (s.pad[i] && !s.few && rows) {
+      a.from[n] = from[i];
+      a.ld[n] = ld[i];
+      a.to[n] = scratch + s.at[i];
+      a.rows[n++] = rows;
+      most = rows > most ? rows : most;
+    }
     if (s.pad[i] && !s.few) {
-      char* to = scratch + s.at[i];
-      if (s.size == 4u) pad_rows<float>(from[i], ld[i], g->inputs, to, s.wide, i ? g->hidden : g->records, stream);
-      else pad_rows<_Float16>(from[i], ld[i], g->inputs, to, s.wide, i ? g->hidden : g->records, stream);
-      from[i] = to;
+      from[i] = scratch + s.at[i];
       ld[i] = s.wide;
     }
     ld[i] *= s.size;
   }
+  if (!n) return;
+  const uint64_t blocks = ceil_div(most * s.wide, 256);
+  const dim3 grid((uint32_t)(blocks < 65536 ? blocks : 65536), n);
+  if (s.size == 4u) hipLaunchKernelGGL(k_pad_rows<float>, grid, dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL(k_pad_rows<_Float16>, grid, dim3(256), 0, stream, a);
 }
 
 bool four_at_a_time(const void* p, uint64_t ld, uint32_t size) { return (uintptr_t)p % (4 * size) == 0 && ld % 4 == 0; }
