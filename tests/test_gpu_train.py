@@ -23,7 +23,7 @@ TYPES = [torch.float32, torch.float16, torch.bfloat16]
 def _close(got, want, bound, what):
     """|got - want| <= bound, plus rounding to got's type."""
     dtype = got.dtype
-    got, want, bound = got.double().cpu(), want.double().cpu(), bound.double().cpu()
+    got, want, bound = got.double().to(want.device), want.double(), bound.double().to(want.device)
     limit = bound + HALF_UNIT[dtype] * (want.abs() + bound) + TINY[dtype]
     off = (got - want).abs()
     assert torch.isfinite(got).all(), f"{what}: not finite"
@@ -251,17 +251,17 @@ def _inputs(m, k, n, dtype, seed, scale=1.0):
     return (r(m, k) * scale).to(dtype), (r(n, k) / math.sqrt(k)).to(dtype), (r(n, k) / math.sqrt(k)).to(dtype), r(m, n).to(dtype)
 
 
-def _check_forward(got, x, wg, wu, act):
-    x, wg, wu = x.double().cpu(), wg.double().cpu(), wu.double().cpu()
+def _check_forward(got, x, wg, wu, act, where="cpu"):
+    x, wg, wu = (t.double().to(where) for t in (x, wg, wu))
     a, u, ea, eu = _projections(x, wg, wu)
     f, _ = _act64(a, act)
     ef = SLOPE[act] * ea + OWN * a.abs().clamp(min=1)
     _close(got, f * u, ef * u.abs() + f.abs() * eu + ef * eu, "gated")
 
 
-def _check_backward(got, dh, x, wg, wu, act):
+def _check_backward(got, dh, x, wg, wu, act, where="cpu"):
     dtype, half = x.dtype, HALF_UNIT[x.dtype]
-    x, wg, wu, dh = x.double().cpu(), wg.double().cpu(), wu.double().cpu(), dh.double().cpu()
+    x, wg, wu, dh = (t.double().to(where) for t in (x, wg, wu, dh))
     a, u, ea, eu = _projections(x, wg, wu)
     f, s = _act64(a, act)
     ef, es = SLOPE[act] * ea + OWN * a.abs().clamp(min=1), BEND[act] * ea + OWN * a.abs().clamp(min=1)
@@ -316,6 +316,27 @@ def test_gated_large(shape, dtype):
     x, wg, wu, dh = _inputs(m, k, n, dtype, m + 3 * n)
     _check_forward(T.gated(x.cuda(), wg.cuda(), wu.cuda()), x, wg, wu, "silu")
     _check_backward(T.gated_backward(dh.cuda(), x.cuda(), wg.cuda(), wu.cuda()), dh, x, wg, wu, "silu")
+
+
+# Together these take each of the four products (h, the slopes, dx, the weights' gradients) through tiles of each size, whole
+# and with their depth shared out, in 16 and in 32 bits.
+TILINGS = {torch.bfloat16: [(24, 1450, 2732), (19, 3156, 331), (889, 1102, 3585), (3450, 35, 21), (4660, 1665, 23), (4308, 463, 20), (193, 2901, 3786), (48, 38, 1327),
+                            (3457, 21, 1294), (3870, 20, 262), (947, 901, 4142), (139, 1490, 27), (772, 21, 1225), (30, 26, 394)],
+           torch.float16: [(10_936, 997, 730), (1166, 3232, 2505), (16_396, 958, 500)],
+           torch.float32: [(18, 1678, 3734), (2139, 694, 1500), (21, 1507, 2504), (1375, 590, 877), (1254, 88, 21), (4684, 2684, 21), (1227, 1717, 983), (3619, 2118, 23),
+                           (196, 4176, 735), (85, 323, 21), (30, 26, 394), (1835, 22, 3601), (4152, 1960, 236), (912, 27, 3812), (616, 1539, 814), (52, 744, 57)]}
+
+
+@pytest.mark.parametrize("dtype, shape", [(d, s) for d in TILINGS for s in TILINGS[d]], ids=str)
+def test_gated_tilings(dtype, shape):
+    m, k, n = shape
+    x, wg, wu, dh = (t.cuda() for t in _inputs(m, k, n, dtype, m + 3 * n))
+    act = sorted(T.ACTS)[m % 4]
+    _check_forward(T.gated(x, wg, wu, act=act), x, wg, wu, act, where="cuda")
+    got = T.gated_backward(dh, x, wg, wu, act=act)
+    _check_backward(got, dh, x, wg, wu, act, where="cuda")
+    for a, b in zip(got, T.gated_backward(dh, x, wg, wu, act=act)):
+        assert torch.equal(a, b), "the same inputs give the same bits"
 
 
 @pytest.mark.parametrize("act", sorted(T.ACTS))
