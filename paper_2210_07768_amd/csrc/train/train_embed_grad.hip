@@ -200,6 +200,45 @@ __global__ __launch_bounds__(256) void k_move_pairs(const uint32_t* keys, const 
   }
 }
 
+// A few pairs in one launch: a wavefront, which holds all keys in its registers, counts for each of four pairs the keys below
+// its own, and equal ones before it, and writes it to that place.  (4,096 pairs of 17 bits: 11 us against 21 us for two
+// passes.)
+constexpr uint32_t kRankPairs = 4096, kRankEach = 4;
+__global__ __launch_bounds__(256) void k_rank_pairs(const uint32_t* keys, const uint32_t* from, uint32_t n, uint32_t* keys_out, uint32_t* from_out) {
+  constexpr uint32_t kPacks = kRankPairs / 256u;  // of four keys, of a lane
+  const uint32_t lane = threadIdx.x % 64u, i0 = (blockIdx.x * 4u + threadIdx.x / 64u) * kRankEach;
+  uint32_t all[kPacks][4];
+#pragma unroll
+  for (uint32_t j = 0; j < kPacks; ++j) {
+    const uint32_t at = (j * 64u + lane) * 4u;
+    if (at + 4u <= n) {
+      const Pack<uint32_t, 4> q = *(const Pack<uint32_t, 4>*)(keys + at);
+#pragma unroll
+      for (uint32_t e = 0; e < 4u; ++e) all[j][e] = q.v[e];
+    } else {
+#pragma unroll
+      for (uint32_t e = 0; e < 4u; ++e) all[j][e] = at + e < n ? keys[at + e] : kNone;  // (no key is as large)
+    }
+  }
+#pragma unroll
+  for (uint32_t h = 0; h < kRankEach; ++h) {
+    const uint32_t i = i0 + h;
+    if (i >= n) return;
+    const uint32_t k = keys[i];
+    uint32_t rank = 0u;
+#pragma unroll
+    for (uint32_t j = 0; j < kPacks; ++j)
+#pragma unroll
+      for (uint32_t e = 0; e < 4u; ++e) rank += all[j][e] < k || (all[j][e] == k && (j * 64u + lane) * 4u + e < i) ? 1u : 0u;
+#pragma unroll
+    for (uint32_t d = 1; d < 64u; d <<= 1) rank += __shfl_xor(rank, d, 64);
+    if (lane == 0u) {
+      keys_out[rank] = k;
+      from_out[rank] = from[i];
+    }
+  }
+}
+
 template <uint32_t kBits, uint32_t kItems>
 void sort_pass(uint32_t* const (&keys)[2], uint32_t* const (&from)[2], int side, uint32_t n, uint32_t shift, uint32_t n_tiles, uint32_t* counts, uint32_t* totals,
                hipStream_t stream) {
@@ -507,7 +546,11 @@ extern "C" fbx_status fbx_embed_backward(const fbx_slot_view* slots, uint32_t n_
       }
       hipLaunchKernelGGL(k_pairs, dim3((uint32_t)ceil_div(n_records, 256), p.n_slots), dim3(256), 0, stream, p);
     }
-    for (uint32_t pass = 0; pass < l.passes; ++pass, side ^= 1) {
+    if (l.n <= kRankPairs) {
+      hipLaunchKernelGGL(k_rank_pairs, dim3((uint32_t)ceil_div(l.n, 4 * kRankEach)), dim3(256), 0, stream, keys[0], from[0], l.n, keys[1], from[1]);
+      side = 1;
+    }
+    for (uint32_t pass = 0; l.n > kRankPairs && pass < l.passes; ++pass, side ^= 1) {
       const auto sort = l.bits == 9u ? (l.items == kFewItems ? sort_pass<9, kFewItems> : sort_pass<9, kManyItems>)
                                      : (l.items == kFewItems ? sort_pass<8, kFewItems> : sort_pass<8, kManyItems>);
       sort(keys, from, side, l.n, l.bits * pass, l.n_tiles, counts, totals, stream);
