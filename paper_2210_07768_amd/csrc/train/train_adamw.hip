@@ -7,7 +7,7 @@ namespace fbx {
 namespace train {
 namespace {
 
-constexpr uint32_t kTensorsPerLaunch = 40;
+constexpr uint32_t kTensorsPerLaunch = 128;  // (10 KB of arguments)
 constexpr uint32_t kEach = 8;                 // elements of a lane
 constexpr uint32_t kBlock = 256 * kEach;      // elements of a workgroup
 

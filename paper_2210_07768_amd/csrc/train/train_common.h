@@ -54,7 +54,7 @@ struct SlotRef {
   uint32_t arity;
   uint32_t base;              // gradient: signs of the slots before
 };
-constexpr uint32_t kSlotsPerLaunch = 64;
+constexpr uint32_t kSlotsPerLaunch = 192;  // (9 KB of arguments; a launch fewer saves more than their way costs)
 
 // Where record r's signs lie: [begin, begin + count), never outside the slot's values.
 __device__ __forceinline__ void signs_of(const SlotRef& s, uint64_t r, uint64_t n_records, uint32_t tile, uint64_t& begin, uint32_t& count) {

@@ -44,7 +44,7 @@ SlotRef slot_ref(const fbx_slot_view& v, uint32_t base) {
 
 namespace {
 
-constexpr uint32_t kTileRecords = 16;
+constexpr uint32_t kTileRecords = 16, kTileSlots = 64;  // of a workgroup
 
 struct EmbedArgs {
   SlotRef slots[kSlotsPerLaunch];
@@ -67,8 +67,8 @@ constexpr uint32_t kSigns = 4;
 template <class T, int N>
 __global__ __launch_bounds__(256) void k_embed(EmbedArgs) {
   const EmbedArgs& a = launch_args<EmbedArgs>();
-  __shared__ uint64_t begin[kSlotsPerLaunch * (kTileRecords + 1)];
-  __shared__ uint32_t count[kSlotsPerLaunch * (kTileRecords + 1)], first[kSlotsPerLaunch * (kTileRecords + 1)];
+  __shared__ uint64_t begin[kTileSlots * (kTileRecords + 1)];
+  __shared__ uint32_t count[kTileSlots * (kTileRecords + 1)], first[kTileSlots * (kTileRecords + 1)];
   const uint64_t r0 = (uint64_t)blockIdx.x * kTileRecords;
   const uint32_t s0 = blockIdx.y * a.each, n_slots = a.n_slots - s0 < a.each ? a.n_slots - s0 : a.each;
   const SlotRef* slots = a.slots + s0;
@@ -182,7 +182,7 @@ extern "C" fbx_status fbx_embed_forward(const fbx_slot_view* slots, uint32_t n_s
   for (uint32_t s0 = 0; s0 < n_slots; s0 += kSlotsPerLaunch) {
     a.n_slots = n_slots - s0 < kSlotsPerLaunch ? n_slots - s0 : kSlotsPerLaunch;
     // (two workgroups a compute unit, as long as each has four slots: 5 records of 137 slots 46 us with 64 slots each, 12 with four)
-    a.each = kSlotsPerLaunch;
+    a.each = kTileSlots;
     while (a.each > 4u && ceil_div(n_records, kTileRecords) * ceil_div(a.n_slots, a.each) < 512u) a.each /= 2u;
     for (uint32_t i = 0; i < a.n_slots; ++i) a.slots[i] = slot_ref(slots[s0 + i], 0u);
     a.out = (char*)d_out + (uint64_t)s0 * dim * e;

@@ -83,6 +83,7 @@ CASES = [  # records, slots, dim, rows, distinct signs
     (1, [1], 1, 1, 3), (1, [1, 1, 1], 16, 1000, 50), (5, ["empty", 1, "empty"], 8, 10, 4), (33, [1, "list", 3, "list"], 16, 300, 1000),
     (64, ["list"] * 65, 4, 77, 500), (129, [1] * 130, 2, 1001, 3000), (257, ["long", 2], 33, 100, 90), (100, [1, "list"], 300, 64, 1000),
     (1000, [1, "list", 1], 24, 5, 40), (3000, ["list", "long", 1, 1], 12, 4099, 100_000), (31, [2, "list"], 1030, 50, 60),
+    (40, [1, "list"] * 100 + [2], 8, 1009, 3000),
 ]
 
 
@@ -526,7 +527,7 @@ SIZES = [1, 2, 7, 8, 9, 31, 32, 33, 63, 65, 2047, 2048, 2049, 0, 10_000, 4096 + 
 def test_adamw_32_bit_states(param, grad):
     """Three steps over tensors of many sizes (more than one launch takes), against the formulas in 64 bits, and copies."""
     g = torch.Generator().manual_seed(4)
-    sizes = SIZES * 3
+    sizes = SIZES * 9
     p = [torch.randn(n, generator=g).to(param) for n in sizes]
     gpu = [t.clone().cuda() for t in p]
     m, v = [torch.zeros(n, device="cuda") for n in sizes], [torch.zeros(n, device="cuda") for n in sizes]
