@@ -213,6 +213,7 @@ extern "C" fbx_status fbx_adamw_step(const fbx_adamw* h, const fbx_adamw_tensor*
     any = true;
   }
   if (!any) return FBX_OK;
+  launching();
   for (uint32_t i = 0; copy && i < n_tensors; ++i)
     if (tensors[i].n && !tensors[i].d_copy) return refuse(FBX_E_ARG, "either all tensors have a copy or none");
   AdamwArgs a{};

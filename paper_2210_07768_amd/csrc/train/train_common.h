@@ -12,7 +12,9 @@ namespace train {
 
 // Notes why a call fails and returns `s`.
 fbx_status refuse(fbx_status s, const char* why);
-fbx_status launched();  // FBX_OK, or FBX_E_HIP with the text of the last launch's error
+// Around a call's launches: forgets errors that others left; FBX_OK, or FBX_E_HIP with the text of a launch's error.
+void launching();
+fbx_status launched();
 
 inline uint32_t size_of(fbx_dtype t) { return t == FBX_F32 ? 4u : 2u; }
 inline bool known(fbx_dtype t) { return t == FBX_F32 || t == FBX_F16 || t == FBX_BF16; }

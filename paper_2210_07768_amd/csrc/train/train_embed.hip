@@ -15,6 +15,8 @@ fbx_status refuse(fbx_status s, const char* why) {
   return s;
 }
 
+void launching() { (void)hipGetLastError(); }
+
 fbx_status launched() {
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? FBX_OK : refuse(FBX_E_HIP, hipGetErrorString(e));
@@ -169,6 +171,7 @@ extern "C" fbx_status fbx_embed_forward(const fbx_slot_view* slots, uint32_t n_s
   const uint64_t all = (uintptr_t)d_table | (uintptr_t)d_out | dim * e | table_stride * e | record_stride * e;
   uint32_t n = 16u / e;
   while (n > 1u && all % (n * e)) n /= 2u;
+  launching();
   EmbedArgs a{};
   a.table = d_table;
   a.n_records = n_records;

@@ -519,6 +519,7 @@ extern "C" fbx_status fbx_embed_backward(const fbx_slot_view* slots, uint32_t n_
   if (((uintptr_t)d_dtable | (uintptr_t)d_dout) % e) return refuse(FBX_E_ARG, "d_dtable and d_dout must be aligned to their elements");
   if (l.bytes && (!d_scratch || (uintptr_t)d_scratch % 256u)) return refuse(FBX_E_ARG, "d_scratch is NULL or not 256-byte aligned");
   if (scratch_bytes < l.bytes) return refuse(FBX_E_NOMEM, "scratch too small: fbx_embed_backward_scratch gives its size");
+  launching();
   const hipStream_t stream = (hipStream_t)hip_stream;
   char* scratch = (char*)d_scratch;
   uint32_t* keys[2] = {(uint32_t*)(scratch + l.keys[0]), (uint32_t*)(scratch + l.keys[1])};

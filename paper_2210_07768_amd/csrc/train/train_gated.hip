@@ -746,6 +746,7 @@ extern "C" fbx_status fbx_gated_forward(const fbx_gated* g, void* d_h, uint64_t 
   const hipStream_t stream = (hipStream_t)hip_stream;
   const Shape s = shape_of(g, false);
   if (!s.fits()) return refuse(FBX_E_ARG, "records x hidden is too large for one call");
+  launching();
   const void* from[3];
   uint64_t ld[3];
   operands(g, s, (char*)d_scratch, from, ld, stream);
@@ -789,6 +790,7 @@ extern "C" fbx_status fbx_gated_backward(const fbx_gated* g, const void* d_dh, u
   const Shape s = shape_of(g, true);
   if (!s.fits()) return refuse(FBX_E_ARG, "records x hidden is too large for one call");
   char* scratch = (char*)d_scratch;
+  launching();
   const void* from[3];
   uint64_t ld[3];
   operands(g, s, scratch, from, ld, stream);

@@ -81,7 +81,8 @@ def embed(slots, table, n_records: Optional[int] = None, mean: bool = False, out
     """Rows of ``table`` (rows x dim) for the signs of every slot, summed (or averaged) per record:
     n_records x slots x dim, zeros where a record has no signs.
 
-    slots: an ``ExtractResult``, or a sequence of its slots or of ``Signs`` (with n_records)."""
+    slots: an ``ExtractResult``, or a sequence of its slots or of ``Signs`` (with n_records).  Under autograd the signs are
+    read again by the backward pass: extract the next batch behind it, or into another workspace."""
     if table.requires_grad and torch.is_grad_enabled():
         if out is not None:
             _bad("out cannot take part in autograd")
