@@ -62,6 +62,12 @@ __global__ __launch_bounds__(256) void k_pairs(PairArgs) {
   }
 }
 
+// Workgroups go to the eight dies in turn; this gives each die a stretch of neighbouring tiles.
+__device__ __forceinline__ uint32_t tile_here() {
+  const uint32_t each = gridDim.x / 8u, more = gridDim.x % 8u, die = blockIdx.x % 8u;
+  return die * each + (die < more ? die : more) + blockIdx.x / 8u;
+}
+
 // Per tile of pairs, how many have each value of the digit; counts lie digit by digit.  (A wavefront has counters of its
 // own: the most frequent rows' digits are most of a tile's.)
 template <uint32_t kBits, uint32_t kItems>
@@ -70,7 +76,8 @@ __global__ __launch_bounds__(256) void k_digit_counts(const uint32_t* keys, uint
   __shared__ uint32_t h[4][kBins];
   for (uint32_t i = threadIdx.x; i < 4u * kBins; i += 256u) h[i / kBins][i % kBins] = 0u;
   __syncthreads();
-  const uint64_t at = (uint64_t)blockIdx.x * (256u * kItems);
+  const uint32_t tile = tile_here();
+  const uint64_t at = (uint64_t)tile * (256u * kItems);
   uint32_t k[kItems];
 #pragma unroll
   for (uint32_t i = 0; i < kItems; ++i) k[i] = at + i * 256u + threadIdx.x < n ? keys[at + i * 256u + threadIdx.x] : 0u;
@@ -78,7 +85,7 @@ __global__ __launch_bounds__(256) void k_digit_counts(const uint32_t* keys, uint
   for (uint32_t i = 0; i < kItems; ++i)
     if (at + i * 256u + threadIdx.x < n) atomicAdd(&h[threadIdx.x / 64u][(k[i] >> shift) % kBins], 1u);
   __syncthreads();
-  for (uint32_t d = threadIdx.x; d < kBins; d += 256u) counts[d * (uint64_t)n_tiles + blockIdx.x] = h[0][d] + h[1][d] + h[2][d] + h[3][d];
+  for (uint32_t d = threadIdx.x; d < kBins; d += 256u) counts[d * (uint64_t)n_tiles + tile] = h[0][d] + h[1][d] + h[2][d] + h[3][d];
 }
 
 // Inclusive sums over the workgroup's 256 lanes.
@@ -134,7 +141,8 @@ __global__ __launch_bounds__(256) void k_move_pairs(const uint32_t* keys, const 
   const uint32_t lane = threadIdx.x % 64u, wave = threadIdx.x / 64u;
   for (uint32_t i = threadIdx.x; i < 4u * kBins; i += 256u) seen[i / kBins][i % kBins] = 0u;
   __syncthreads();
-  const uint64_t at = (uint64_t)blockIdx.x * (256u * kItems) + wave * (kItems * 64u) + lane;
+  const uint32_t tile = tile_here();
+  const uint64_t at = (uint64_t)tile * (256u * kItems) + wave * (kItems * 64u) + lane;
   uint32_t k[kItems], f[kItems], rank[kItems];
 #pragma unroll
   for (uint32_t i = 0; i < kItems; ++i) {
@@ -178,7 +186,7 @@ __global__ __launch_bounds__(256) void k_move_pairs(const uint32_t* keys, const 
   for (uint32_t e = 0; e < kMine; ++e) {
     const uint32_t d = threadIdx.x * kMine + e;
     begin[d] = first;
-    to[d] = first_all + counts[d * (uint64_t)n_tiles + blockIdx.x];
+    to[d] = first_all + counts[d * (uint64_t)n_tiles + tile];
     first += mine[e];
     first_all += total[e];
   }
@@ -191,7 +199,7 @@ __global__ __launch_bounds__(256) void k_move_pairs(const uint32_t* keys, const 
       f_lds[p] = f[i];
     }
   __syncthreads();
-  const uint64_t first_pair = (uint64_t)blockIdx.x * (256u * kItems);
+  const uint64_t first_pair = (uint64_t)tile * (256u * kItems);
   const uint32_t here = n - first_pair < (256u * kItems) ? (uint32_t)(n - first_pair) : (256u * kItems);
   for (uint32_t i = threadIdx.x; i < here; i += 256u) {
     const uint32_t d = (k_lds[i] >> shift) % kBins, p = to[d] + i - begin[d];
@@ -275,7 +283,7 @@ __global__ __launch_bounds__(256) void k_sum_rows(SumArgs a) {
   uint32_t* key_of = lds;                                        // groups * kPad, then the one before and the one after
   uint32_t* from_of = lds + groups * kPad + 2u;                  // groups * kPad
   uint32_t* open = from_of + (kFirst ? groups * kPad : 0u);      // a group's flags: 1 began before it, 2 goes on after it, 4 all of it is one row's
-  float* shares = (float*)(open + groups);                       // groups x {head, tail} x columns
+  float* heads = (float*)(open + groups);                        // groups x columns
   const uint64_t b0 = (uint64_t)blockIdx.x * groups * kRun;
   const uint32_t here = a.n - b0 < groups * kRun ? (uint32_t)(a.n - b0) : groups * kRun;
   for (uint32_t i = threadIdx.x; i < groups * kRun; i += 256u) {
@@ -294,8 +302,7 @@ __global__ __launch_bounds__(256) void k_sum_rows(SumArgs a) {
   const uint32_t after = group + 1u < groups ? key_of[(group + 1u) * kPad] : ends[1];
   const uint32_t col = blockIdx.y * columns + mine * N;
   const bool in = col < a.dim;
-  float* head = shares + group * 2u * columns + mine * N;
-  float* tail = head + columns;
+  float* head = heads + group * columns + mine * N;
   auto write = [&](uint32_t row, const float (&sum)[N]) {
     if (row >= a.rows || !in) return;
     Pack<T, N> p;
@@ -350,11 +357,10 @@ __global__ __launch_bounds__(256) void k_sum_rows(SumArgs a) {
     }
   }
   const bool whole = began && goes_on;
-  if (began || goes_on) {
-    float* to = began ? head : tail;
+  if (began) {
 #pragma unroll
-    for (int j = 0; j < N; ++j) to[j] = sum[j];
-  } else {
+    for (int j = 0; j < N; ++j) head[j] = sum[j];
+  } else if (!goes_on) {
     write(key, sum);
   }
   if (mine == 0u) open[group] = (keys[0] == before && keys[0] != kNone ? 1u : 0u) | (goes_on ? 2u : 0u) | (whole ? 4u : 0u);
@@ -363,7 +369,7 @@ __global__ __launch_bounds__(256) void k_sum_rows(SumArgs a) {
   // Adds the heads from group g on to sum, up to the row's end; true: the row goes on after the workgroup.
   auto follow = [&](uint32_t g, float (&total)[N]) {
     for (; g < groups; ++g) {
-      const float* more = shares + g * 2u * columns + mine * N;
+      const float* more = heads + g * columns + mine * N;
 #pragma unroll
       for (int j = 0; j < N; ++j) total[j] += more[j];
       if (!(open[g] & 4u)) return false;
@@ -389,11 +395,8 @@ __global__ __launch_bounds__(256) void k_sum_rows(SumArgs a) {
     if (!(open[groups - 1u] & 2u) && mine == 0u && blockIdx.y == 0u) a.part_keys[2u * blockIdx.x + 1u] = kNone;
   }
   if (goes_on && !whole) {
-    float total[N];
-#pragma unroll
-    for (int j = 0; j < N; ++j) total[j] = tail[j];
-    if (follow(group + 1u, total)) leave(1u, last, total);
-    else write(last, total);
+    if (follow(group + 1u, sum)) leave(1u, last, sum);
+    else write(last, sum);
   }
 }
 
@@ -456,7 +459,7 @@ void sum_rows(SumArgs a, const Layout& l, char* scratch, uint64_t rows, hipStrea
     a.part_keys = last ? nullptr : (uint32_t*)(scratch + l.part_keys[side]);
     a.parts = last ? nullptr : (float*)(scratch + l.parts[side]);
     const dim3 grid((uint32_t)blocks, (uint32_t)ceil_div(a.dim, columns));
-    const uint32_t lds = 4u * ((first ? 2u : 1u) * groups * (kRun + 1u) + 2u + groups + groups * 2u * columns);
+    const uint32_t lds = 4u * ((first ? 2u : 1u) * groups * (kRun + 1u) + 2u + groups + groups * columns);
     if (first) hipLaunchKernelGGL((k_sum_rows<T, N, true>), grid, dim3(256), lds, stream, a);
     else hipLaunchKernelGGL((k_sum_rows<T, N, false>), grid, dim3(256), lds, stream, a);
     if (last) break;
