@@ -69,7 +69,9 @@ __device__ __forceinline__ uint32_t tile_here() {
 }
 
 // Per tile of pairs, how many have each value of the digit; counts lie digit by digit.  (A wavefront has counters of its
-// own: the most frequent rows' digits are most of a tile's.)
+// own, and its lanes that have the first one's digit are counted at once: the most frequent rows are next to each other after
+// the first pass.  13.1 M pairs, signs as frequent as 1 / rank: 16 us in every pass, against
+// 25 and 29 in the second and third.)
 template <uint32_t kBits, uint32_t kItems>
 __global__ __launch_bounds__(256) void k_digit_counts(const uint32_t* keys, uint32_t n, uint32_t shift, uint32_t n_tiles, uint32_t* counts) {
   constexpr uint32_t kBins = 1u << kBits;
@@ -82,8 +84,13 @@ __global__ __launch_bounds__(256) void k_digit_counts(const uint32_t* keys, uint
 #pragma unroll
   for (uint32_t i = 0; i < kItems; ++i) k[i] = at + i * 256u + threadIdx.x < n ? keys[at + i * 256u + threadIdx.x] : 0u;
 #pragma unroll
-  for (uint32_t i = 0; i < kItems; ++i)
-    if (at + i * 256u + threadIdx.x < n) atomicAdd(&h[threadIdx.x / 64u][(k[i] >> shift) % kBins], 1u);
+  for (uint32_t i = 0; i < kItems; ++i) {
+    if (at + i * 256u + threadIdx.x >= n) break;
+    const uint32_t d = (k[i] >> shift) % kBins, d0 = __builtin_amdgcn_readfirstlane(d);
+    const uint64_t same = __ballot(d == d0);
+    if (d != d0) atomicAdd(&h[threadIdx.x / 64u][d], 1u);
+    else if (__popcll(same & ((1ull << (threadIdx.x % 64u)) - 1ull)) == 0) atomicAdd(&h[threadIdx.x / 64u][d], (uint32_t)__popcll(same));
+  }
   __syncthreads();
   for (uint32_t d = threadIdx.x; d < kBins; d += 256u) counts[d * (uint64_t)n_tiles + tile] = h[0][d] + h[1][d] + h[2][d] + h[3][d];
 }
@@ -255,6 +262,14 @@ void sort_pass(uint32_t* const (&keys)[2], uint32_t* const (&from)[2], int side,
   hipLaunchKernelGGL((k_move_pairs<kBits, kItems>), dim3(n_tiles), dim3(256), 0, stream, keys[side], from[side], n, shift, n_tiles, counts, totals, keys[side ^ 1], from[side ^ 1]);
 }
 
+// Rows of the table up to the one of sorted term at - 1: the first row that belongs to what begins at term `at`.
+__device__ __forceinline__ uint32_t rows_before(const uint32_t* keys, uint32_t n, uint32_t rows, uint64_t at) {
+  if (!at) return 0u;
+  if (at >= n) return rows;
+  const uint32_t k = keys[at - 1u];
+  return k < rows ? k + 1u : rows;
+}
+
 struct SumArgs {
   const uint32_t* keys;       // ascending; kNone: no term
   const uint32_t* from;       // terms are rows of dout ...
@@ -266,6 +281,7 @@ struct SumArgs {
   float* parts;
   uint64_t record_stride, table_stride;
   uint32_t n, n_from, all_slots, rows, dim, lanes_log2, dense;  // dense: a record's rows of dout directly follow the last one's
+  uint32_t near;              // a workgroup zeroes its stretch of the table if that is no longer; 0: all zeroed before
 };
 
 // The sorted terms of a workgroup: 16 for every group of 2^lanes_log2 lanes, each lane N adjacent columns (blockIdx.y: which
@@ -273,7 +289,9 @@ struct SumArgs {
 // table; one that goes on is taken up by the group it begins in, which adds the next groups' shares of it; what
 // began before the workgroup or goes on after it is left to the next launch, which adds such sums up the same way (at most two a
 // workgroup, so three launches do for 10^8 terms).  kFirst: terms are rows of dout.
-// Bound by the rows of dout, which are fetched in lines of 128 bytes in the order of the keys.
+// Bound by the rows of dout, which are fetched in lines of 128 bytes in the order of the keys: 13.1 M terms of 32 bytes are 13.7 M
+// lines, 1.76 GB, of which a kernel that does nothing else fetches 6.4 TB/s, and their sums' rows: 376 us in all, whether four or six
+// workgroups are on a compute unit.  Whatever the loads' cache policy, a line is fetched whole; passing the caches by costs 60 us.
 template <class T, int N, bool kFirst>
 __global__ __launch_bounds__(256) void k_sum_rows(SumArgs a) {
   constexpr uint32_t kPad = kRun + 1;  // (a group's terms begin in another bank than the next one's)
@@ -290,6 +308,13 @@ __global__ __launch_bounds__(256) void k_sum_rows(SumArgs a) {
     const uint32_t at = i / kRun * kPad + i % kRun;
     key_of[at] = i < here ? a.keys[b0 + i] : kNone;
     if (kFirst) from_of[at] = i < here ? a.from[b0 + i] : 0u;
+  }
+  if (kFirst && a.near) {
+    const uint32_t begin = rows_before(a.keys, a.n, a.rows, b0), end = rows_before(a.keys, a.n, a.rows, b0 + groups * kRun);
+    const uint32_t c = blockIdx.y * columns + mine * N;
+    const Pack<T, N> zero{};
+    if (end > begin && end - begin <= a.near && c < a.dim)
+      for (uint32_t row = begin + group; row < end; row += groups) *(Pack<T, N>*)((T*)a.dtable + row * a.table_stride + c) = zero;
   }
   uint32_t* ends = key_of + groups * kPad;
   if (threadIdx.x == 0u) {
@@ -409,6 +434,38 @@ __global__ __launch_bounds__(256) void k_clear_rows(void* to, uint64_t rows, uin
     *(Pack<T, N>*)((T*)to + i / packs * stride + i % packs * N) = zero;
 }
 
+// Zeroes what the workgroups of k_sum_rows leave: stretches of the table, between the last rows of two of them, of more
+// than `near` rows.  All workgroups take a part of each.
+template <class T, int N>
+__global__ __launch_bounds__(256) void k_clear_far(SumArgs a, uint32_t each) {  // each: terms of a workgroup there
+  constexpr uint32_t kMine = 8;
+  __shared__ uint32_t begin[256 * kMine], end[256 * kMine], n_far;
+  const uint32_t packs = a.dim / N, blocks = (uint32_t)(((uint64_t)a.n + each - 1u) / each);
+  const Pack<T, N> zero{};
+  for (uint32_t b0 = 0; b0 < blocks; b0 += 256u * kMine) {
+    if (threadIdx.x == 0u) n_far = 0u;
+    __syncthreads();
+    const uint32_t b = b0 + threadIdx.x * kMine;
+    uint32_t at[kMine + 1];
+#pragma unroll
+    for (uint32_t e = 0; e <= kMine; ++e) at[e] = rows_before(a.keys, a.n, a.rows, (uint64_t)(b + e) * each);
+#pragma unroll
+    for (uint32_t e = 0; e < kMine; ++e)
+      if (b + e < blocks && at[e + 1] > at[e] && at[e + 1] - at[e] > a.near) {
+        const uint32_t i = atomicAdd(&n_far, 1u);
+        begin[i] = at[e];
+        end[i] = at[e + 1];
+      }
+    __syncthreads();
+    for (uint32_t f = 0; f < n_far; ++f) {
+      const uint64_t all = (uint64_t)(end[f] - begin[f]) * packs;
+      for (uint64_t i = (uint64_t)blockIdx.x * 256u + threadIdx.x; i < all; i += (uint64_t)gridDim.x * 256u)
+        *(Pack<T, N>*)((T*)a.dtable + (begin[f] + i / packs) * a.table_stride + i % packs * N) = zero;
+    }
+    __syncthreads();
+  }
+}
+
 // Where things lie in the scratch.
 struct Layout {
   uint64_t keys[2], from[2], counts, totals, share, part_keys[2], parts[2], bytes;
@@ -448,10 +505,19 @@ bool lay_out(Layout& l, uint64_t total, uint64_t n_records, uint32_t n_slots, ui
 
 template <class T, int N>
 void sum_rows(SumArgs a, const Layout& l, char* scratch, uint64_t rows, hipStream_t stream) {
-  const uint64_t packs = rows * (a.dim / N);
-  const uint32_t clear = (uint32_t)(ceil_div(packs, 256) < 16384 ? ceil_div(packs, 256) : 16384);
-  hipLaunchKernelGGL((k_clear_rows<T, N>), dim3(clear), dim3(256), 0, stream, a.dtable, rows, a.dim, a.table_stride);
   const uint32_t groups = 256u >> a.lanes_log2, columns = N << a.lanes_log2;
+  // Rows without terms.  Where most rows have some, a workgroup zeroes its own stretch before it writes its sums into it, so that
+  // memory sees whole lines, once (13.1 M terms, 10 M rows of 32 bytes: 680 us the whole gradient, against 712 with all rows zeroed
+  // first); where few have, stretches are long and unlike, and where there are few pairs it makes no difference.
+  if (a.n > kFewPairs && rows <= 2ull * a.n) {
+    a.near = 4u * groups * kRun;
+    // (each of its workgroups looks at all stretches' ends: with 2,048 of them that takes 35 us, with 128 two)
+    hipLaunchKernelGGL((k_clear_far<T, N>), dim3(128), dim3(256), 0, stream, a, groups * kRun);
+  } else {
+    const uint64_t packs = rows * (a.dim / N);
+    const uint32_t clear = (uint32_t)(ceil_div(packs, 256) < 16384 ? ceil_div(packs, 256) : 16384);
+    hipLaunchKernelGGL((k_clear_rows<T, N>), dim3(clear), dim3(256), 0, stream, a.dtable, rows, a.dim, a.table_stride);
+  }
   int side = 0;
   for (bool first = true; a.n; first = false) {
     const uint64_t blocks = ceil_div(a.n, groups * kRun);

@@ -142,6 +142,24 @@ def test_embed_backward_runs(signs, rows):
     assert np.array_equal(got.double().cpu().numpy(), want)
 
 
+@pytest.mark.parametrize("distinct", [1, 60, 3000, 1 << 20])
+@pytest.mark.parametrize("dim, pad, rows", [(4, 0, 540_000), (1, 2, 300_001), (16, 4, 270_011), (300, 0, 400_000), (300, 5, 540_001)])
+def test_embed_backward_many(dim, pad, rows, distinct):
+    """More pairs than half the rows, from rows that nearly all have terms to one row that has them all; sums of whole numbers
+    are exact, rows without terms are zero, and nothing is written beside them."""
+    n = 90_007
+    rng = np.random.default_rng(dim + distinct)
+    slots = _make_slots(rng, n, [1, 1, 1], distinct)
+    g = torch.Generator(device="cuda").manual_seed(distinct)
+    dout = torch.randint(-8, 9, (n, 3, dim), device="cuda", generator=g).float()
+    room = torch.full((rows, dim + pad), 7.0, device="cuda")
+    T.embed_backward(dout, _on_gpu(slots), rows, out=room[:, :dim])
+    want = torch.zeros(rows, dim, device="cuda")
+    for i, (v, _, _) in enumerate(slots):
+        want.index_add_(0, torch.from_numpy(_rows_of(v, rows)).cuda(), dout[:, i])
+    assert torch.equal(room[:, :dim], want) and bool((room[:, dim:] == 7.0).all())
+
+
 def test_embed_strides_and_outputs():
     rng = np.random.default_rng(5)
     slots = _make_slots(rng, 50, [1, "list", 2], 200)
