@@ -290,7 +290,7 @@ struct SumArgs {
 // began before the workgroup or goes on after it is left to the next launch, which adds such sums up the same way (at most two a
 // workgroup, so three launches do for 10^8 terms).  kFirst: terms are rows of dout.
 // Bound by the rows of dout, which are fetched in lines of 128 bytes in the order of the keys: 13.1 M terms of 32 bytes are 13.7 M
-// lines, 1.76 GB, of which a kernel that does nothing else fetches 6.4 TB/s, and their sums' rows: 376 us in all, whether four or six
+// lines, 1.76 GB, of which a kernel that does nothing else fetches 6.4 TB/s, and their sums' rows: 348 us in all, whether four or six
 // workgroups are on a compute unit.  Whatever the loads' cache policy, a line is fetched whole; passing the caches by costs 60 us.
 template <class T, int N, bool kFirst>
 __global__ __launch_bounds__(256) void k_sum_rows(SumArgs a) {
@@ -309,13 +309,8 @@ __global__ __launch_bounds__(256) void k_sum_rows(SumArgs a) {
     key_of[at] = i < here ? a.keys[b0 + i] : kNone;
     if (kFirst) from_of[at] = i < here ? a.from[b0 + i] : 0u;
   }
-  if (kFirst && a.near) {
-    const uint32_t begin = rows_before(a.keys, a.n, a.rows, b0), end = rows_before(a.keys, a.n, a.rows, b0 + groups * kRun);
-    const uint32_t c = blockIdx.y * columns + mine * N;
-    const Pack<T, N> zero{};
-    if (end > begin && end - begin <= a.near && c < a.dim)
-      for (uint32_t row = begin + group; row < end; row += groups) *(Pack<T, N>*)((T*)a.dtable + row * a.table_stride + c) = zero;
-  }
+  const uint32_t begin = kFirst && a.near ? rows_before(a.keys, a.n, a.rows, b0) : 0u;
+  const uint32_t end = kFirst && a.near ? rows_before(a.keys, a.n, a.rows, b0 + groups * kRun) : 0u;
   uint32_t* ends = key_of + groups * kPad;
   if (threadIdx.x == 0u) {
     ends[0] = b0 ? a.keys[b0 - 1u] : kNone;
@@ -361,6 +356,12 @@ __global__ __launch_bounds__(256) void k_sum_rows(SumArgs a) {
       } else {
         q[e] = *(const Pack<float, N>*)(a.terms + (b0 + group * kRun + i0 + e) * a.dim + col);
       }
+    }
+    if (kFirst && i0 == 0u && a.near) {  // (the terms asked for just now are awaited here too)
+      const Pack<T, N> zero{};
+      if (end > begin && end - begin <= a.near && in)
+        for (uint32_t row = begin + group; row < end; row += groups) *(Pack<T, N>*)((T*)a.dtable + row * a.table_stride + col) = zero;
+      __syncthreads();
     }
 #pragma unroll
     for (uint32_t e = 0; e < kAhead; ++e) {
@@ -437,12 +438,12 @@ __global__ __launch_bounds__(256) void k_clear_rows(void* to, uint64_t rows, uin
 // Zeroes what the workgroups of k_sum_rows leave: stretches of the table, between the last rows of two of them, of more
 // than `near` rows.  All workgroups take a part of each.
 template <class T, int N>
-__global__ __launch_bounds__(256) void k_clear_far(SumArgs a, uint32_t each) {  // each: terms of a workgroup there
+__global__ __launch_bounds__(1024) void k_clear_far(SumArgs a, uint32_t each) {  // each: terms of a workgroup there
   constexpr uint32_t kMine = 8;
-  __shared__ uint32_t begin[256 * kMine], end[256 * kMine], n_far;
+  __shared__ uint32_t begin[1024 * kMine], end[1024 * kMine], n_far;
   const uint32_t packs = a.dim / N, blocks = (uint32_t)(((uint64_t)a.n + each - 1u) / each);
   const Pack<T, N> zero{};
-  for (uint32_t b0 = 0; b0 < blocks; b0 += 256u * kMine) {
+  for (uint32_t b0 = 0; b0 < blocks; b0 += 1024u * kMine) {
     if (threadIdx.x == 0u) n_far = 0u;
     __syncthreads();
     const uint32_t b = b0 + threadIdx.x * kMine;
@@ -459,7 +460,7 @@ __global__ __launch_bounds__(256) void k_clear_far(SumArgs a, uint32_t each) {  
     __syncthreads();
     for (uint32_t f = 0; f < n_far; ++f) {
       const uint64_t all = (uint64_t)(end[f] - begin[f]) * packs;
-      for (uint64_t i = (uint64_t)blockIdx.x * 256u + threadIdx.x; i < all; i += (uint64_t)gridDim.x * 256u)
+      for (uint64_t i = (uint64_t)blockIdx.x * 1024u + threadIdx.x; i < all; i += (uint64_t)gridDim.x * 1024u)
         *(Pack<T, N>*)((T*)a.dtable + (begin[f] + i / packs) * a.table_stride + i % packs * N) = zero;
     }
     __syncthreads();
@@ -506,13 +507,14 @@ bool lay_out(Layout& l, uint64_t total, uint64_t n_records, uint32_t n_slots, ui
 template <class T, int N>
 void sum_rows(SumArgs a, const Layout& l, char* scratch, uint64_t rows, hipStream_t stream) {
   const uint32_t groups = 256u >> a.lanes_log2, columns = N << a.lanes_log2;
-  // Rows without terms.  Where most rows have some, a workgroup zeroes its own stretch before it writes its sums into it, so that
-  // memory sees whole lines, once (13.1 M terms, 10 M rows of 32 bytes: 680 us the whole gradient, against 712 with all rows zeroed
-  // first); where few have, stretches are long and unlike, and where there are few pairs it makes no difference.
+  // Rows without terms.  Where most rows have some, a workgroup zeroes its own stretch just before it writes its sums into it, while
+  // its first terms are on their way (13.1 M terms, 10 M rows of 32 bytes: 651 us the whole gradient, against 712 with all rows
+  // zeroed first, and 680 with the stretch zeroed before the terms are asked for: its lines have then left the cache); where few
+  // have, stretches are long and unlike, and where there are few pairs it makes no difference.
   if (a.n > kFewPairs && rows <= 2ull * a.n) {
     a.near = 4u * groups * kRun;
-    // (each of its workgroups looks at all stretches' ends: with 2,048 of them that takes 35 us, with 128 two)
-    hipLaunchKernelGGL((k_clear_far<T, N>), dim3(128), dim3(256), 0, stream, a, groups * kRun);
+    // (each of its workgroups looks at all stretches' ends: 64 large ones take 9 us for 6,400 stretches, 128 of 256 lanes 16)
+    hipLaunchKernelGGL((k_clear_far<T, N>), dim3(64), dim3(1024), 0, stream, a, groups * kRun);
   } else {
     const uint64_t packs = rows * (a.dim / N);
     const uint32_t clear = (uint32_t)(ceil_div(packs, 256) < 16384 ? ceil_div(packs, 256) : 16384);
