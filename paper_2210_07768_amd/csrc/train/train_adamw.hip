@@ -115,6 +115,9 @@ __device__ __forceinline__ void encode(uint8_t* codes, uint8_t* scale, const flo
 
 // A workgroup takes 2,048 elements of one tensor, a lane eight adjacent ones (so that four lanes hold a block of
 // 8-bit states).  P, G, C: types of weights, gradients, copies; kEight: states in 8 bits.
+// Bound by memory: 175 M weights in 32 bits with gradients and copies in 16 and states in 8 take 567 us, 16.1 bytes each at
+// 4.97 TB/s, what a copy reaches; 48 tensors of 0.53 M elements in all, in 32 bits,
+// 8 us, of which the kernel takes 6.5.
 template <class P, class G, class C, bool kEight, bool kCopy>
 __global__ __launch_bounds__(256) void k_adamw(AdamwArgs) {
 #pragma clang fp contract(off)

@@ -61,10 +61,11 @@ struct EmbedArgs {
 // lanes a (record, slot), slots side by side (a record's pooled rows are written whole lines at a time, past the caches,
 // which the table needs), each lane N adjacent columns, add the rows up in the order of the signs, four of
 // those behind the first on their way at once.
-// What bounds it is lines of 128 bytes fetched for shorter rows: 65,536 records of 164 slots, rows of 32 bytes in a table of
-// 320 MB: 317 us, 4.7 TB/s of such lines and results (5.0 is what a copy reaches).  Measured beside it: 32 records a
-// workgroup 403 (fewer workgroups at a time for the second stage to overlap the first's waits), two (record, slot)s in
-// hand 365, both 409; one sign behind the first at a time costs lists a third more.
+// What bounds it is lines of 128 bytes fetched for shorter rows, whatever the loads' cache policy: 65,536 records of 164 slots,
+// rows of 32 bytes in a table of 320 MB: 296 us for 1.42 GB of such lines and 0.34 GB of results, 6.0 TB/s (a kernel that does
+// nothing but fetch lines at random reaches 6.4).  In two launches, which took 317, other shapes took: 32 records a workgroup
+// 403 us (fewer workgroups at a time for the second stage to overlap the first's waits), two (record, slot)s in hand 365, both
+// 409; one sign behind the first at a time costs lists a third more.
 constexpr uint32_t kSigns = 4;
 template <class T, int N>
 __global__ __launch_bounds__(256) void k_embed(EmbedArgs) {

@@ -278,6 +278,12 @@ struct Split {
 // product).  C's rows come from A; its columns from B, which is the first side of the matrix instructions, so that a lane holds
 // four adjacent columns of a row.
 // kStages: steps whose tiles are in LDS or on their way there.
+// Bound by the matrix units where the product is large: 65,536 x 2,624 by 2 x 4,096 in bf16 takes 2.25 to 2.4 ms from card to card,
+// 1.17 to 1.25 PFLOP/s; they are busy 60 % of the cycles, at a clock that the power they draw keeps at 1.8 of 2.4 GHz, and reads from
+// LDS meet no bank conflict.  A library's product of the same two matrices, without the activation, reaches 1.37.  The three products
+// of a gradient of 16,384 records take 1.9 ms, 1.11 PFLOP/s, dh and both slopes moved in the first one's epilogue.  In 32 bits
+// 4,096 x 384 by 2 x 1,024 and back is 175 us, 110 of 154 TFLOP/s.  Measured and slower: 32 x 32 x 16 instructions (8 %),
+// four wavefronts of 128 x 128 (their sums do not fit the registers), workgroups that stay and take tile after tile (6 %).
 template <class T, Form kForm, int BM, int BN, int WM, int WN, int kStages>
 __global__ __launch_bounds__(WM * WN * 64) void k_mm(MmArgs p) {
 #ifdef __HIP_DEVICE_COMPILE__  // (the host's pass, which makes the launch stub of it, does not know the buffer's type)
@@ -457,7 +463,7 @@ __global__ __launch_bounds__(WM * WN * 64) void k_join(MmArgs p) {
 // Up to 16 records: the weights are read once, straight into the matrix units' registers, and bound it.  A workgroup takes
 // 16 columns of either product, its wavefronts a share of the depth each; their sums meet in LDS and are added in order.
 // kWhole: rows begin at, and are, whole 16-byte loads; else they are read element by element, which for so few records
-// costs less than a copy of the weights.
+// costs less than a copy of the weights.  One record, 2 x 4,096 x 1,536 in bf16: 5.6 us, 25 MB at 4.5 TB/s.
 constexpr int kFewWaves = 8;
 template <class T, bool kWhole>
 __global__ __launch_bounds__(kFewWaves * 64) void k_few(MmArgs p) {
