@@ -9,7 +9,7 @@ namespace {
 // Pairs of a lane when sorting; a workgroup has 256 lanes.  Sixteen put more pairs of one digit next to each other; four
 // make a pass shorter where there are too few pairs to fill the card (98,000 pairs: 10.8 us a pass and 6.4).
 constexpr uint32_t kManyItems = 16, kFewItems = 4, kFewPairs = 1u << 18;
-constexpr uint32_t kRun = 16, kAhead = 8;                          // sorted terms a group of lanes adds up, and has on their way
+constexpr uint32_t kRun = 8;  // sorted terms a group of lanes adds up, all on their way at once
 constexpr uint32_t kNone = 0xffffffffu;
 
 struct PairArgs {
@@ -286,14 +286,15 @@ struct SumArgs {
   uint32_t near;              // a workgroup zeroes its stretch of the table if that is no longer; 0: all zeroed before
 };
 
-// The sorted terms of a workgroup: 16 for every group of 2^lanes_log2 lanes, each lane N adjacent columns (blockIdx.y: which
+// The sorted terms of a workgroup: kRun for every group of 2^lanes_log2 lanes, each lane N adjacent columns (blockIdx.y: which
 // stretch of them).  A group adds its terms up one after the other.  A row that begins and ends in a group is written to the
 // table; one that goes on is taken up by the group it begins in, which adds the next groups' shares of it; what
 // began before the workgroup or goes on after it is left to the next launch, which adds such sums up the same way (at most two a
 // workgroup, so three launches do for 10^8 terms).  kFirst: terms are rows of dout.
 // Bound by the rows of dout, which are fetched in lines of 128 bytes in the order of the keys: 13.1 M terms of 32 bytes are 13.7 M
 // lines, 1.76 GB, of which a kernel that does nothing else fetches 6.4 TB/s, and their sums' rows: 348 us in all, whether four or six
-// workgroups are on a compute unit.  Whatever the loads' cache policy, a line is fetched whole; passing the caches by costs 60 us.
+// workgroups are on a compute unit, and whether a group has 8 or 16 terms (98,000 terms of 64 bytes: 41 us the whole gradient with 8,
+// 43.5 with 16, 44 with 4).  Whatever the loads' cache policy, a line is fetched whole; passing the caches by costs 60 us.
 template <class T, int N, bool kFirst>
 __global__ __launch_bounds__(256) void k_sum_rows(SumArgs a) {
   constexpr uint32_t kPad = kRun + 1;  // (a group's terms begin in another bank than the next one's)
@@ -335,54 +336,51 @@ __global__ __launch_bounds__(256) void k_sum_rows(SumArgs a) {
 
   float sum[N] = {};
   uint32_t key = keys[0];
-  bool began = key == before && key != kNone, first = true;  // the row at hand began before this group; it is the group's first
+  bool began = key == before && key != kNone;  // the row at hand began before this group
   const bool goes_on = last == after && last != kNone;
+  Pack<T, N> p[kRun] = {};
+  Pack<float, N> q[kRun] = {};
+  float w[kRun] = {};
 #pragma unroll
-  for (uint32_t i0 = 0; i0 < kRun; i0 += kAhead) {
-    Pack<T, N> p[kAhead] = {};
-    Pack<float, N> q[kAhead] = {};
-    float w[kAhead] = {};
+  for (uint32_t e = 0; e < kRun; ++e) {
+    if (!in || keys[e] == kNone) continue;
+    if (kFirst) {
+      const uint32_t from = from_of[group * kPad + e];
+      if (from >= a.n_from) continue;
+      uint64_t at = (uint64_t)from * a.dim;
+      if (!a.dense) {
+        const uint32_t r = from / a.all_slots;
+        at = r * a.record_stride + (uint64_t)(from - r * a.all_slots) * a.dim;
+      }
+      p[e] = *(const Pack<T, N>*)((const T*)a.dout + at + col);
+      w[e] = a.share ? a.share[from] : 1.f;
+    } else {
+      q[e] = *(const Pack<float, N>*)(a.terms + (b0 + group * kRun + e) * a.dim + col);
+    }
+  }
+  if (kFirst && a.near) {  // (the terms asked for just now are awaited here too)
+    const Pack<T, N> zero{};
+    if (end > begin && end - begin <= a.near && in)
+      for (uint32_t row = begin + group; row < end; row += groups) *(Pack<T, N>*)((T*)a.dtable + row * a.table_stride + col) = zero;
+    __syncthreads();
+  }
 #pragma unroll
-    for (uint32_t e = 0; e < kAhead; ++e) {
-      if (!in || keys[i0 + e] == kNone) continue;
-      if (kFirst) {
-        const uint32_t from = from_of[group * kPad + i0 + e];
-        if (from >= a.n_from) continue;
-        uint64_t at = (uint64_t)from * a.dim;
-        if (!a.dense) {
-          const uint32_t r = from / a.all_slots;
-          at = r * a.record_stride + (uint64_t)(from - r * a.all_slots) * a.dim;
-        }
-        p[e] = *(const Pack<T, N>*)((const T*)a.dout + at + col);
-        w[e] = a.share ? a.share[from] : 1.f;
+  for (uint32_t e = 0; e < kRun; ++e) {
+    const uint32_t k = keys[e];
+    if (k != key) {
+      if (began) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) head[j] = sum[j];
       } else {
-        q[e] = *(const Pack<float, N>*)(a.terms + (b0 + group * kRun + i0 + e) * a.dim + col);
+        write(key, sum);  // (kNone is no row)
       }
-    }
-    if (kFirst && i0 == 0u && a.near) {  // (the terms asked for just now are awaited here too)
-      const Pack<T, N> zero{};
-      if (end > begin && end - begin <= a.near && in)
-        for (uint32_t row = begin + group; row < end; row += groups) *(Pack<T, N>*)((T*)a.dtable + row * a.table_stride + col) = zero;
-      __syncthreads();
+      began = false;
+      key = k;
+#pragma unroll
+      for (int j = 0; j < N; ++j) sum[j] = 0.f;
     }
 #pragma unroll
-    for (uint32_t e = 0; e < kAhead; ++e) {
-      const uint32_t k = keys[i0 + e];
-      if (k != key) {
-        if (began) {
-#pragma unroll
-          for (int j = 0; j < N; ++j) head[j] = sum[j];
-        } else {
-          write(key, sum);  // (kNone is no row)
-        }
-        began = first = false;
-        key = k;
-#pragma unroll
-        for (int j = 0; j < N; ++j) sum[j] = 0.f;
-      }
-#pragma unroll
-      for (int j = 0; j < N; ++j) sum[j] += kFirst ? (a.share ? (float)p[e].v[j] * w[e] : (float)p[e].v[j]) : q[e].v[j];
-    }
+    for (int j = 0; j < N; ++j) sum[j] += kFirst ? (a.share ? (float)p[e].v[j] * w[e] : (float)p[e].v[j]) : q[e].v[j];
   }
   const bool whole = began && goes_on;
   if (began) {
@@ -475,6 +473,14 @@ struct Layout {
   uint32_t n, n_tiles, passes, bits, items;  // bits: of a pass's digit; items: pairs of a lane
 };
 
+// Lanes (a power of two) for a row's columns: as many as rows of whole 16 bytes take, whatever they are: in what order sums are
+// formed is not to follow from where a tensor lies.
+uint32_t lanes_of(uint32_t dim, uint32_t size) {
+  uint32_t log2 = 0;
+  while ((1u << log2) * (16u / size) < dim && log2 < 6u) ++log2;
+  return log2;
+}
+
 bool lay_out(Layout& l, uint64_t total, uint64_t n_records, uint32_t n_slots, uint64_t rows, uint32_t dim, bool mean) {
   if (total >> 32 || n_records * n_slots >> 32) return false;
   l.n = (uint32_t)total;
@@ -495,12 +501,13 @@ bool lay_out(Layout& l, uint64_t total, uint64_t n_records, uint32_t n_slots, ui
   l.counts = take(4ull * l.n_tiles << l.bits);
   l.totals = take(4ull << l.bits);
   l.share = take(mean ? 4 * n_records * n_slots : 0);
-  // (as many workgroups as there are where each has the fewest terms: a wavefront for each group)
-  uint64_t blocks = ceil_div(total, 4 * kRun);
+  // (as many workgroups as there are where each has the fewest terms: elements of 32 bits)
+  const uint32_t groups = 256u >> lanes_of(dim, 4);
+  uint64_t blocks = ceil_div(total, groups * kRun);
   for (int i = 0; i < 2; ++i) {
     l.part_keys[i] = take(4 * 2 * blocks);
     l.parts[i] = take(4ull * 2 * blocks * dim);
-    blocks = ceil_div(2 * blocks, 4 * kRun);
+    blocks = ceil_div(2 * blocks, groups * kRun);
   }
   l.bytes = at;
   return true;
@@ -647,9 +654,7 @@ extern "C" fbx_status fbx_embed_backward(const fbx_slot_view* slots, uint32_t n_
   a.all_slots = n_slots;
   a.rows = (uint32_t)rows;
   a.dim = dim;
-  // (as many lanes as rows of whole 16 bytes take, whatever they are: in what order sums are formed is not to follow from
-  // where a tensor lies)
-  while ((1u << a.lanes_log2) * (16u / e) < dim && a.lanes_log2 < 6u) ++a.lanes_log2;
+  a.lanes_log2 = lanes_of(dim, e);
   if (dtype == FBX_F32) sum_rows_by_width<float>(a, n, l, scratch, rows, stream);
   else if (dtype == FBX_F16) sum_rows_by_width<_Float16>(a, n, l, scratch, rows, stream);
   else sum_rows_by_width<__bf16>(a, n, l, scratch, rows, stream);
