@@ -292,7 +292,7 @@ struct SumArgs {
 // began before the workgroup or goes on after it is left to the next launch, which adds such sums up the same way (at most two a
 // workgroup, so three launches do for 10^8 terms).  kFirst: terms are rows of dout.
 // Bound by the rows of dout, which are fetched in lines of 128 bytes in the order of the keys: 13.1 M terms of 32 bytes are 13.7 M
-// lines, 1.76 GB, of which a kernel that does nothing else fetches 6.4 TB/s, and their sums' rows: 348 us in all, whether four or six
+// lines, 1.76 GB, of which a kernel that does nothing else fetches 6.4 TB/s, and their sums' rows: 349 us in all, whether four or six
 // workgroups are on a compute unit, and whether a group has 8 or 16 terms (98,000 terms of 64 bytes: 41 us the whole gradient with 8,
 // 43.5 with 16, 44 with 4).  Whatever the loads' cache policy, a line is fetched whole; passing the caches by costs 60 us.
 template <class T, int N, bool kFirst>
@@ -439,29 +439,29 @@ __global__ __launch_bounds__(256) void k_clear_rows(void* to, uint64_t rows, uin
 // than `near` rows.  All workgroups take a part of each.
 template <class T, int N>
 __global__ __launch_bounds__(1024) void k_clear_far(SumArgs a, uint32_t each) {  // each: terms of a workgroup there
-  constexpr uint32_t kMine = 8;
-  __shared__ uint32_t begin[1024 * kMine], end[1024 * kMine], n_far;
+  constexpr uint32_t kMine = 16;  // a lane's, which are looked at one by one only if they are far together
+  __shared__ uint32_t far[1024 * kMine], n_far;
   const uint32_t packs = a.dim / N, blocks = (uint32_t)(((uint64_t)a.n + each - 1u) / each);
   const Pack<T, N> zero{};
   for (uint32_t b0 = 0; b0 < blocks; b0 += 1024u * kMine) {
     if (threadIdx.x == 0u) n_far = 0u;
     __syncthreads();
     const uint32_t b = b0 + threadIdx.x * kMine;
-    uint32_t at[kMine + 1];
-#pragma unroll
-    for (uint32_t e = 0; e <= kMine; ++e) at[e] = rows_before(a.keys, a.n, a.rows, (uint64_t)(b + e) * each);
-#pragma unroll
-    for (uint32_t e = 0; e < kMine; ++e)
-      if (b + e < blocks && at[e + 1] > at[e] && at[e + 1] - at[e] > a.near) {
-        const uint32_t i = atomicAdd(&n_far, 1u);
-        begin[i] = at[e];
-        end[i] = at[e + 1];
+    const uint32_t first = rows_before(a.keys, a.n, a.rows, (uint64_t)b * each), last = rows_before(a.keys, a.n, a.rows, (uint64_t)(b + kMine) * each);
+    if (b < blocks && last > first && last - first > a.near) {
+      uint32_t begin = first;
+      for (uint32_t e = 0; e < kMine && b + e < blocks; ++e) {
+        const uint32_t end = rows_before(a.keys, a.n, a.rows, (uint64_t)(b + e + 1u) * each);
+        if (end > begin && end - begin > a.near) far[atomicAdd(&n_far, 1u)] = b + e;
+        begin = end;
       }
+    }
     __syncthreads();
     for (uint32_t f = 0; f < n_far; ++f) {
-      const uint64_t all = (uint64_t)(end[f] - begin[f]) * packs;
+      const uint32_t begin = rows_before(a.keys, a.n, a.rows, (uint64_t)far[f] * each), end = rows_before(a.keys, a.n, a.rows, (far[f] + 1ull) * each);
+      const uint64_t all = (uint64_t)(end - begin) * packs;
       for (uint64_t i = (uint64_t)blockIdx.x * 1024u + threadIdx.x; i < all; i += (uint64_t)gridDim.x * 1024u)
-        *(Pack<T, N>*)((T*)a.dtable + (begin[f] + i / packs) * a.table_stride + i % packs * N) = zero;
+        *(Pack<T, N>*)((T*)a.dtable + (begin + i / packs) * a.table_stride + i % packs * N) = zero;
     }
     __syncthreads();
   }
@@ -517,12 +517,12 @@ template <class T, int N>
 void sum_rows(SumArgs a, const Layout& l, char* scratch, uint64_t rows, hipStream_t stream) {
   const uint32_t groups = 256u >> a.lanes_log2, columns = N << a.lanes_log2;
   // Rows without terms.  Where most rows have some, a workgroup zeroes its own stretch just before it writes its sums into it, while
-  // its first terms are on their way (13.1 M terms, 10 M rows of 32 bytes: 651 us the whole gradient, against 712 with all rows
-  // zeroed first, and 680 with the stretch zeroed before the terms are asked for: its lines have then left the cache); where few
-  // have, stretches are long and unlike, and where there are few pairs it makes no difference.
+  // its first terms are on their way (13.1 M terms, 10 M rows of 32 bytes: 640 us the whole gradient, against 700 with all rows
+  // zeroed first; zeroed before the terms are asked for, the stretch's lines have left the cache when the sums come, which costs 20);
+  // where few have, stretches are long and unlike, and where there are few pairs it makes no difference.
   if (a.n > kFewPairs && rows <= 2ull * a.n) {
-    a.near = 4u * groups * kRun;
-    // (each of its workgroups looks at all stretches' ends: 64 large ones take 9 us for 6,400 stretches, 128 of 256 lanes 16)
+    a.near = 32u * groups * kRun;
+    // (each of its workgroups looks at the ends of all 16 stretches)
     hipLaunchKernelGGL((k_clear_far<T, N>), dim3(64), dim3(1024), 0, stream, a, groups * kRun);
   } else {
     const uint64_t packs = rows * (a.dim / N);
