@@ -44,7 +44,9 @@ const char* fbx_train_last_error(void);
  *                   zeros for a record without signs in that slot
  *
  *   slots      : HOST, n_slots entries: fbx_result.slots, or entries made by the caller (slot_id is ignored;
- *                n_values must be fixed_arity * n_records for fixed arity, offsets[n_records] for lists)
+ *                n_values must be fixed_arity * n_records for fixed arity, at least offsets[n_records] for lists.
+ *                A list slot's values before offsets[0] or from offsets[n_records] on belong to no record and are
+ *                left out: offsets + k of a slot of more records are the offsets of the records from k on)
  *   arrival_tile_records : fbx_result.arrival_tile_records, 0 for slots in record order
  *   d_table    : DEVICE, rows x dim, table_stride elements from row to row
  *   d_out      : DEVICE, n_records x (n_slots * dim), record_stride elements from record to record
@@ -63,7 +65,8 @@ fbx_status fbx_embed_forward(const fbx_slot_view* slots, uint32_t n_slots, uint6
  * w = 1, or 1 / (signs of that record in that slot) where mean is set.  All of dtable is written,
  * zeros where no sign leads.  A row's terms are ordered by slot, record and position; stretches of them are
  * added up in that order, and then the stretches' sums in theirs.
- * Arguments as above.  Limits also: fewer than 2^32 signs in all, n_records * n_slots < 2^32.
+ * Arguments as above.  Limits also: fewer than 2^32 values in all (those of no record count, for scratch and time
+ * too), n_records * n_slots < 2^32.
  * Errors: FBX_E_ARG, FBX_E_NOMEM (scratch too small), FBX_E_HIP.
  */
 fbx_status fbx_embed_backward_scratch(const fbx_slot_view* slots, uint32_t n_slots, uint64_t n_records,

@@ -24,12 +24,14 @@ struct PairArgs {
 // A workgroup 256 records of a slot: their signs' rows, and where each came from, at the signs' own positions.  A lane takes
 // a record's signs where there is one a record, or where records need not follow each other (arrival order); else lanes
 // take neighbouring signs and look up whose they are.  13.1 M signs: 56 us, their bytes and the pairs' at 3.8 TB/s.
+// Signs that no record's list holds (before the first one's, behind the last one's) have their place among the pairs too: as
+// terms from nowhere, which add zeros to the last row, so that sorting needs no key beyond the rows.
 __global__ __launch_bounds__(256) void k_pairs(PairArgs) {
   const PairArgs& a = launch_args<PairArgs>();
   __shared__ uint32_t ends[256];  // of the records' signs, from the first record's first on
   const SlotRef& s = a.slots[blockIdx.y];
   const uint64_t r0 = (uint64_t)blockIdx.x * 256u, r = r0 + threadIdx.x;
-  const uint32_t n = (uint32_t)(a.n_records - r0 < 256u ? a.n_records - r0 : 256u);
+  const uint32_t n = r0 >= a.n_records ? 0u : (uint32_t)(a.n_records - r0 < 256u ? a.n_records - r0 : 256u);
   const uint32_t first = (uint32_t)r0 * a.all_slots + a.first_slot + blockIdx.y;  // of the first record
   uint64_t b = 0;
   uint32_t c = 0;
@@ -45,6 +47,13 @@ __global__ __launch_bounds__(256) void k_pairs(PairArgs) {
     }
     return;
   }
+  const uint64_t held = s.offsets[0] < s.n_values ? s.offsets[0] : s.n_values, held_end = s.offsets[a.n_records] < s.n_values ? s.offsets[a.n_records] : s.n_values;
+  for (uint64_t i = r0 + threadIdx.x; i < held + (s.n_values - held_end); i += gridDim.x * 256ull) {
+    const uint64_t at = s.base + (i < held ? i : held_end + (i - held));
+    a.keys[at] = a.rows - 1u;
+    a.from[at] = kNone;
+  }
+  if (!n) return;
   const uint64_t begin = s.offsets[r0];
   if (threadIdx.x < n) ends[threadIdx.x] = (uint32_t)(b + c - begin);
   __syncthreads();
@@ -594,7 +603,7 @@ extern "C" fbx_status fbx_embed_backward(const fbx_slot_view* slots, uint32_t n_
   if (st != FBX_OK) return st;
   Layout l;
   if (!lay_out(l, total, n_records, n_slots, rows, dim, mean != 0)) return refuse(FBX_E_ARG, "2^32 signs, or records * slots, or more");
-  if (!d_dtable || (!d_dout && total)) return refuse(FBX_E_ARG, "d_dtable or d_dout is NULL");
+  if (!d_dtable || (!d_dout && total && n_records)) return refuse(FBX_E_ARG, "d_dtable or d_dout is NULL");
   const uint32_t e = size_of(dtype);
   if (((uintptr_t)d_dtable | (uintptr_t)d_dout) % e) return refuse(FBX_E_ARG, "d_dtable and d_dout must be aligned to their elements");
   if (l.bytes && (!d_scratch || (uintptr_t)d_scratch % 256u)) return refuse(FBX_E_ARG, "d_scratch is NULL or not 256-byte aligned");
@@ -617,6 +626,11 @@ extern "C" fbx_status fbx_embed_backward(const fbx_slot_view* slots, uint32_t n_
     p.all_slots = n_slots;
     p.rows = (uint32_t)rows;
     p.tile = arrival_tile_records;
+    uint64_t longest = 0;  // list
+    for (uint32_t i = 0; i < n_slots; ++i)
+      if (!slots[i].fixed_arity && slots[i].n_values > longest) longest = slots[i].n_values;
+    // (workgroups beyond those the records need, for signs that no record holds: none where a record has 16 signs or fewer)
+    const uint64_t blocks = ceil_div(n_records, 256), more = ceil_div(longest, 4096) < 1024 ? ceil_div(longest, 4096) : 1024;
     uint32_t base = 0;
     for (uint32_t s0 = 0; s0 < n_slots; s0 += kSlotsPerLaunch) {
       p.first_slot = s0;
@@ -625,7 +639,7 @@ extern "C" fbx_status fbx_embed_backward(const fbx_slot_view* slots, uint32_t n_
         p.slots[i] = slot_ref(slots[s0 + i], base);
         base += (uint32_t)slots[s0 + i].n_values;
       }
-      hipLaunchKernelGGL(k_pairs, dim3((uint32_t)ceil_div(n_records, 256), p.n_slots), dim3(256), 0, stream, p);
+      hipLaunchKernelGGL(k_pairs, dim3((uint32_t)(blocks > more ? blocks : more), p.n_slots), dim3(256), 0, stream, p);
     }
     if (l.n <= kRankPairs) {
       hipLaunchKernelGGL(k_rank_pairs, dim3((uint32_t)ceil_div(l.n, 4 * kRankEach)), dim3(256), 0, stream, keys[0], from[0], l.n, keys[1], from[1]);

@@ -27,7 +27,8 @@ BLOCK = 32   # elements that share a scale in 8-bit states
 
 
 class Signs(NamedTuple):
-    """One slot of signs; the slots of an ``ExtractResult`` have the same fields and can stand in its place."""
+    """One slot of signs; the slots of an ``ExtractResult`` have the same fields and can stand in its place.  Values that
+    the offsets leave out belong to no record: ``Signs(slot.values, slot.offsets[a:b + 1])`` are the records a to b - 1."""
     values: torch.Tensor                       # int64 or uint64
     offsets: Optional[torch.Tensor] = None     # n_records + 1; None: fixed_arity signs a record
     fixed_arity: int = 1                         # ignored where offsets are given

@@ -1,0 +1,67 @@
+"""The trainer's operators where a call's edges lie: lists cut out of longer ones, launches' limits, what autograd knows."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2210_07768_amd import binding as B
+from paper_2210_07768_amd import train as T
+
+pytestmark = pytest.mark.gpu
+TYPES = [torch.float32, torch.float16, torch.bfloat16]
+
+
+def _lists(rng, n, most, distinct):
+    """Values and offsets of a slot whose records have 0 .. most signs each."""
+    offsets = np.concatenate([[0], np.cumsum(rng.integers(0, most + 1, n))]).astype(np.int64)
+    pool = rng.integers(-(1 << 63), 1 << 63, size=distinct, dtype=np.int64)
+    return torch.from_numpy(pool[rng.integers(0, distinct, int(offsets[-1]))]).cuda(), torch.from_numpy(offsets).cuda()
+
+
+# ------------------------------------------------------------------ lists that leave values out
+@pytest.mark.parametrize("mean", [False, True])
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("n, most, rows", [(250, 8, 256), (250, 8, 1), (250, 8, 300), (20_000, 6, 4096), (20_000, 6, 5000), (20_000, 40, 1 << 18), (20_000, 40, 200_003),
+                                           (300, 3000, 70_001)])
+def test_gradient_of_a_window_of_records(n, most, rows, dtype, mean):
+    """Records a to b - 1 of longer slots, with room behind the last value: what the records' own signs alone give.  Sums of
+    whole numbers are exact.  Of means, terms and their places among the others are the same but for the last row's, whose
+    sum may be formed in another order: off by 2^-24 for each of its terms either way, and by the stored result's rounding."""
+    rng = np.random.default_rng(n + most + rows)
+    slots = [_lists(rng, n, most, 4000) for _ in range(2)]
+    one = torch.from_numpy(rng.integers(-(1 << 63), 1 << 63, size=n, dtype=np.int64)).cuda()
+    room = torch.from_numpy(rng.integers(-(1 << 63), 1 << 63, size=777, dtype=np.int64)).cuda()
+    longer = [torch.cat([v, room]) for v, _ in slots]
+    # (scratch of this size as a call leaves it: pairs that would all be taken for terms)
+    T.embed_backward(torch.ones(n, 3, 8, device="cuda", dtype=dtype), [T.Signs(longer[0], torch.cat([slots[0][1][:-1], slots[0][1][-1:] + 777])), T.Signs(longer[1], slots[1][1]),
+                                                                     T.Signs(one)], rows, mean=mean)
+    for a, b in ((0, n), (n // 3, n // 2), (n - 5, n), (0, 1), (7, 7)):
+        dout = torch.from_numpy(rng.integers(-8, 9, (b - a, 3, 8)).astype(np.float32)).to(dtype).cuda()
+        window = [T.Signs(v, o[a:b + 1]) for v, (_, o) in zip(longer, slots)] + [T.Signs(one[a:b])]
+        alone = [T.Signs(v[int(o[a]):int(o[b])].clone(), o[a:b + 1] - o[a]) for v, o in slots] + [T.Signs(one[a:b].clone())]
+        got, want = T.embed_backward(dout, window, rows, mean=mean), T.embed_backward(dout, alone, rows, mean=mean)
+        if mean:
+            assert torch.equal(got[:-1], want[:-1])
+            terms = sum(s.values.numel() for s in alone)
+            half = {torch.float32: 2.0 ** -24, torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}[dtype]
+            size = 8.0 * terms   # (at least the sum of the terms' magnitudes)
+            assert bool(((got[-1].double() - want[-1].double()).abs() <= 2 * terms * 2.0 ** -24 * size + 2 * half * want[-1].double().abs() + 2.0 ** -24).all())
+        else:
+            assert torch.equal(got, want)
+        assert torch.equal(got, T.embed_backward(dout, window, rows, mean=mean)), "the same inputs give the same bits"
+        table = torch.randn(rows, 8, device="cuda").to(dtype).requires_grad_()
+        pooled = T.embed(window, table, b - a, mean=mean)
+        assert torch.equal(pooled, T.embed(alone, table.detach(), b - a, mean=mean))
+        pooled.backward(dout)
+        assert torch.equal(table.grad, got)
+
+
+def test_gradient_of_few_records_with_much_left_out():
+    """One record in the middle of three million values, and no record at all."""
+    values = torch.arange(3_000_000, device="cuda")
+    dout = torch.full((1, 1, 4), 2.0, device="cuda")
+    for rows in (64, 1000, 2_000_000):
+        offsets = torch.tensor([1_234_567, 1_234_667], device="cuda")
+        want = T.embed_backward(dout, [T.Signs(values[1_234_567:1_234_667].clone(), offsets - 1_234_567)], rows)
+        assert float(want.sum()) == 800.0
+        assert torch.equal(T.embed_backward(dout, [T.Signs(values, offsets)], rows), want)
+        assert not T.embed_backward(dout[:0], [T.Signs(values, offsets[:1])], rows).any()
