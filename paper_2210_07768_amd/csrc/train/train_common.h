@@ -21,6 +21,9 @@ inline bool known(fbx_dtype t) { return t == FBX_F32 || t == FBX_F16 || t == FBX
 inline uint64_t round_up(uint64_t x, uint64_t to) { return (x + to - 1) / to * to; }
 inline uint64_t ceil_div(uint64_t x, uint64_t by) { return (x + by - 1) / by; }
 
+// The most workgroups a launch can have along x: it counts their lanes in 32 bits.
+constexpr uint64_t most_blocks(uint32_t lanes) { return 0xffffffffu / lanes; }
+
 // N adjacent elements, moved by one load or store.
 template <class T, int N>
 struct alignas(sizeof(T) * N) Pack {

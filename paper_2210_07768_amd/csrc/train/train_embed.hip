@@ -52,7 +52,7 @@ struct EmbedArgs {
   SlotRef slots[kSlotsPerLaunch];
   const void* table;
   void* out;                 // of the launch's first slot
-  uint64_t n_records, table_stride, record_stride;
+  uint64_t first_record, n_records, table_stride, record_stride;  // first_record: of the launch; n_records: in all
   uint32_t n_slots, each, rows, dim, tile, lanes_log2, mean;  // each: slots of a workgroup
 };
 
@@ -72,7 +72,7 @@ __global__ __launch_bounds__(256) void k_embed(EmbedArgs) {
   const EmbedArgs& a = launch_args<EmbedArgs>();
   __shared__ uint64_t begin[kTileSlots * (kTileRecords + 1)];
   __shared__ uint32_t count[kTileSlots * (kTileRecords + 1)], first[kTileSlots * (kTileRecords + 1)];
-  const uint64_t r0 = (uint64_t)blockIdx.x * kTileRecords;
+  const uint64_t r0 = a.first_record + (uint64_t)blockIdx.x * kTileRecords;
   const uint32_t s0 = blockIdx.y * a.each, n_slots = a.n_slots - s0 < a.each ? a.n_slots - s0 : a.each;
   const SlotRef* slots = a.slots + s0;
   const uint32_t n = (uint32_t)(a.n_records - r0 < kTileRecords ? a.n_records - r0 : kTileRecords);
@@ -131,7 +131,8 @@ __global__ __launch_bounds__(256) void k_embed(EmbedArgs) {
 
 template <class T, int N>
 void launch(const EmbedArgs& a, hipStream_t stream) {
-  hipLaunchKernelGGL((k_embed<T, N>), dim3((uint32_t)ceil_div(a.n_records, kTileRecords), (uint32_t)ceil_div(a.n_slots, a.each)), dim3(256), 0, stream, a);
+  const uint64_t blocks = ceil_div(a.n_records - a.first_record, kTileRecords), most = most_blocks(256);
+  hipLaunchKernelGGL((k_embed<T, N>), dim3((uint32_t)(blocks < most ? blocks : most), (uint32_t)ceil_div(a.n_slots, a.each)), dim3(256), 0, stream, a);
 }
 
 template <class T>
@@ -191,9 +192,11 @@ extern "C" fbx_status fbx_embed_forward(const fbx_slot_view* slots, uint32_t n_s
     for (uint32_t i = 0; i < a.n_slots; ++i) a.slots[i] = slot_ref(slots[s0 + i], 0u);
     a.out = (char*)d_out + (uint64_t)s0 * dim * e;
     const hipStream_t stream = (hipStream_t)hip_stream;
-    if (dtype == FBX_F32) launch_by_width<float>(a, n, stream);
-    else if (dtype == FBX_F16) launch_by_width<_Float16>(a, n, stream);
-    else launch_by_width<__bf16>(a, n, stream);
+    for (a.first_record = 0; a.first_record < n_records; a.first_record += most_blocks(256) * kTileRecords) {
+      if (dtype == FBX_F32) launch_by_width<float>(a, n, stream);
+      else if (dtype == FBX_F16) launch_by_width<_Float16>(a, n, stream);
+      else launch_by_width<__bf16>(a, n, stream);
+    }
   }
   return launched();
 }

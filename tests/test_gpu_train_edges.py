@@ -65,3 +65,25 @@ def test_gradient_of_few_records_with_much_left_out():
         assert float(want.sum()) == 800.0
         assert torch.equal(T.embed_backward(dout, [T.Signs(values, offsets)], rows), want)
         assert not T.embed_backward(dout[:0], [T.Signs(values, offsets[:1])], rows).any()
+
+
+# ------------------------------------------------------------------ what one launch cannot hold
+def _rows_of(values, rows):
+    """floor(mix64(sign) x rows / 2^64) in torch's signed integers."""
+    shr = lambda x, k: (x >> k) & ((1 << (64 - k)) - 1)  # noqa: E731
+    x = (values ^ shr(values, 30)) * (0xBF58476D1CE4E5B9 - (1 << 64))
+    x = (x ^ shr(x, 27)) * (0x94D049BB133111EB - (1 << 64))
+    x = x ^ shr(x, 31)
+    return (shr(x, 32) * rows + (((x & 0xFFFFFFFF) * rows) >> 32)) >> 32
+
+
+def test_more_records_than_a_launch_holds():
+    """2^28 records and some more (a launch's lanes are counted in 32 bits), a list slot's among them."""
+    n, rows = (1 << 28) + 1000, 30_011
+    table = torch.randn(rows, 1, device="cuda").to(torch.bfloat16)
+    values = torch.arange(n, device="cuda")
+    offsets = torch.arange(n + 1, device="cuda")
+    got = T.embed([T.Signs(values), T.Signs(values, offsets)], table, n)
+    for r0 in range(0, n, 1 << 25):
+        want = table[_rows_of(values[r0:r0 + (1 << 25)], rows)]
+        assert torch.equal(got[r0:r0 + (1 << 25), 0], want) and torch.equal(got[r0:r0 + (1 << 25), 1], want)
