@@ -66,7 +66,7 @@ fbx_status fbx_embed_forward(const fbx_slot_view* slots, uint32_t n_slots, uint6
  * zeros where no sign leads.  A row's terms are ordered by slot, record and position; stretches of them are
  * added up in that order, and then the stretches' sums in theirs.
  * Arguments as above.  Limits also: fewer than 2^32 values in all (those of no record count, for scratch and time
- * too), n_records * n_slots < 2^32.
+ * too), n_records * n_slots <= 2^32 - 256.
  * Errors: FBX_E_ARG, FBX_E_NOMEM (scratch too small), FBX_E_HIP.
  */
 fbx_status fbx_embed_backward_scratch(const fbx_slot_view* slots, uint32_t n_slots, uint64_t n_records,

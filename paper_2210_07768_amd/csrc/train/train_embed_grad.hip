@@ -291,7 +291,7 @@ struct SumArgs {
   uint32_t* part_keys;        // two a workgroup: a row that began before it, a row that goes on after it
   float* parts;
   uint64_t record_stride, table_stride;
-  uint32_t n, n_from, all_slots, rows, dim, lanes_log2, dense;  // dense: a record's rows of dout directly follow the last one's
+  uint32_t n, n_from, all_slots, rows, dim, lanes_log2, first_block, dense;  // first_block: of the launch; dense: a record's rows of dout directly follow the last one's
   uint32_t near;              // a workgroup zeroes its stretch of the table if that is no longer; 0: all zeroed before
 };
 
@@ -314,7 +314,8 @@ __global__ __launch_bounds__(256) void k_sum_rows(SumArgs a) {
   uint32_t* from_of = lds + groups * kPad + 2u;                  // groups * kPad
   uint32_t* open = from_of + (kFirst ? groups * kPad : 0u);      // a group's flags: 1 began before it, 2 goes on after it, 4 all of it is one row's
   float* heads = (float*)(open + groups);                        // groups x columns
-  const uint64_t b0 = (uint64_t)blockIdx.x * groups * kRun;
+  const uint32_t block = a.first_block + blockIdx.x;
+  const uint64_t b0 = (uint64_t)block * groups * kRun;
   const uint32_t here = a.n - b0 < groups * kRun ? (uint32_t)(a.n - b0) : groups * kRun;
   for (uint32_t i = threadIdx.x; i < groups * kRun; i += 256u) {
     const uint32_t at = i / kRun * kPad + i % kRun;
@@ -412,10 +413,10 @@ __global__ __launch_bounds__(256) void k_sum_rows(SumArgs a) {
     return true;
   };
   auto leave = [&](uint32_t which, uint32_t row, const float (&total)[N]) {
-    if (mine == 0u && blockIdx.y == 0u) a.part_keys[2u * blockIdx.x + which] = row;
+    if (mine == 0u && blockIdx.y == 0u) a.part_keys[2u * block + which] = row;
     if (in)
 #pragma unroll
-      for (int j = 0; j < N; ++j) a.parts[(2ull * blockIdx.x + which) * a.dim + col + j] = total[j];
+      for (int j = 0; j < N; ++j) a.parts[(2ull * block + which) * a.dim + col + j] = total[j];
   };
   const float none[N] = {};
   if (group == 0u && a.part_keys) {
@@ -425,9 +426,9 @@ __global__ __launch_bounds__(256) void k_sum_rows(SumArgs a) {
       if (follow(0u, total)) leave(1u, row, none);
       leave(0u, row, total);
     } else if (mine == 0u && blockIdx.y == 0u) {
-      a.part_keys[2u * blockIdx.x] = kNone;
+      a.part_keys[2u * block] = kNone;
     }
-    if (!(open[groups - 1u] & 2u) && mine == 0u && blockIdx.y == 0u) a.part_keys[2u * blockIdx.x + 1u] = kNone;
+    if (!(open[groups - 1u] & 2u) && mine == 0u && blockIdx.y == 0u) a.part_keys[2u * block + 1u] = kNone;
   }
   if (goes_on && !whole) {
     if (follow(group + 1u, sum)) leave(1u, last, sum);
@@ -491,7 +492,7 @@ uint32_t lanes_of(uint32_t dim, uint32_t size) {
 }
 
 bool lay_out(Layout& l, uint64_t total, uint64_t n_records, uint32_t n_slots, uint64_t rows, uint32_t dim, bool mean) {
-  if (total >> 32 || n_records * n_slots >> 32) return false;
+  if (total >> 32 || n_records * n_slots > most_blocks(256) * 256) return false;  // (k_pairs has a lane for a record)
   l.n = (uint32_t)total;
   l.items = total <= kFewPairs ? kFewItems : kManyItems;
   l.n_tiles = (uint32_t)ceil_div(total, 256u * l.items);
@@ -544,10 +545,13 @@ void sum_rows(SumArgs a, const Layout& l, char* scratch, uint64_t rows, hipStrea
     const bool last = blocks == 1;
     a.part_keys = last ? nullptr : (uint32_t*)(scratch + l.part_keys[side]);
     a.parts = last ? nullptr : (float*)(scratch + l.parts[side]);
-    const dim3 grid((uint32_t)blocks, (uint32_t)ceil_div(a.dim, columns));
     const uint32_t lds = 4u * ((first ? 2u : 1u) * groups * (kRun + 1u) + 2u + groups + groups * columns);
-    if (first) hipLaunchKernelGGL((k_sum_rows<T, N, true>), grid, dim3(256), lds, stream, a);
-    else hipLaunchKernelGGL((k_sum_rows<T, N, false>), grid, dim3(256), lds, stream, a);
+    for (uint64_t b = 0; b < blocks; b += most_blocks(256)) {
+      const dim3 grid((uint32_t)(blocks - b < most_blocks(256) ? blocks - b : most_blocks(256)), (uint32_t)ceil_div(a.dim, columns));
+      a.first_block = (uint32_t)b;
+      if (first) hipLaunchKernelGGL((k_sum_rows<T, N, true>), grid, dim3(256), lds, stream, a);
+      else hipLaunchKernelGGL((k_sum_rows<T, N, false>), grid, dim3(256), lds, stream, a);
+    }
     if (last) break;
     a.keys = a.part_keys;
     a.terms = a.parts;
@@ -586,7 +590,7 @@ extern "C" fbx_status fbx_embed_backward_scratch(const fbx_slot_view* slots, uin
     total += slots[i].n_values;
   }
   Layout l;
-  if (!lay_out(l, total, n_records, n_slots, rows, dim, mean != 0)) return refuse(FBX_E_ARG, "2^32 signs, or records * slots, or more");
+  if (!lay_out(l, total, n_records, n_slots, rows, dim, mean != 0)) return refuse(FBX_E_ARG, "2^32 signs or more, or records * slots above 2^32 - 256");
   *bytes = l.bytes;
   return FBX_OK;
 }
@@ -602,7 +606,7 @@ extern "C" fbx_status fbx_embed_backward(const fbx_slot_view* slots, uint32_t n_
   const fbx_status st = check_slots(slots, n_slots, n_records, arrival_tile_records, &total);
   if (st != FBX_OK) return st;
   Layout l;
-  if (!lay_out(l, total, n_records, n_slots, rows, dim, mean != 0)) return refuse(FBX_E_ARG, "2^32 signs, or records * slots, or more");
+  if (!lay_out(l, total, n_records, n_slots, rows, dim, mean != 0)) return refuse(FBX_E_ARG, "2^32 signs or more, or records * slots above 2^32 - 256");
   if (!d_dtable || (!d_dout && total && n_records)) return refuse(FBX_E_ARG, "d_dtable or d_dout is NULL");
   const uint32_t e = size_of(dtype);
   if (((uintptr_t)d_dtable | (uintptr_t)d_dout) % e) return refuse(FBX_E_ARG, "d_dtable and d_dout must be aligned to their elements");

@@ -87,3 +87,14 @@ def test_more_records_than_a_launch_holds():
     for r0 in range(0, n, 1 << 25):
         want = table[_rows_of(values[r0:r0 + (1 << 25)], rows)]
         assert torch.equal(got[r0:r0 + (1 << 25), 0], want) and torch.equal(got[r0:r0 + (1 << 25), 1], want)
+
+
+def test_more_terms_than_a_launch_holds():
+    """2^29 signs and some more whose rows take 64 lanes each: every row's sum is how often signs lead to it."""
+    n, arity, rows, dim = 65_536, 8193, 300, 129
+    values = torch.arange(n * arity, device="cuda")
+    count = torch.zeros(rows, dtype=torch.int64, device="cuda")
+    for at in range(0, n * arity, 1 << 26):
+        count += torch.bincount(_rows_of(values[at:at + (1 << 26)], rows), minlength=rows)
+    got = T.embed_backward(torch.ones(n, 1, dim, device="cuda"), [T.Signs(values, None, arity)], rows)
+    assert int(count.max()) < 1 << 24 and torch.equal(got, count.float().unsqueeze(1).expand(rows, dim))
