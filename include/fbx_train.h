@@ -81,7 +81,8 @@ fbx_status fbx_embed_backward(const fbx_slot_view* slots, uint32_t n_slots, uint
  * product in one kernel.  x: records x inputs; Wg, Wu: hidden x inputs; h: records x hidden; all of
  * one type.  No value between x and h is rounded to fewer than 32 bits.
  *   act: silu a / (1 + e^-a); gelu a Phi(a), Phi by erf; relu max(a, 0), slope 0 at 0; sigmoid 1 / (1 + e^-a)
- * Limits: records < 2^31, 1 <= inputs, hidden <= 2^20, strides < 2^22.
+ * Limits: records < 2^31, 1 <= inputs, hidden <= 2^20, strides < 2^22; and so few tiles of 256 x 256 elements in each product
+ * (records x 2 hidden; of the gradient also records x inputs and 2 hidden x inputs) that a launch holds them: below 2^23 - 4096.
  */
 typedef enum { FBX_ACT_SILU = 0, FBX_ACT_GELU = 1, FBX_ACT_RELU = 2, FBX_ACT_SIGMOID = 3 } fbx_act;
 typedef struct {

@@ -553,7 +553,8 @@ __global__ __launch_bounds__(256) void k_pad_rows(PadArgs a) {
 struct Cut {
   uint32_t size;  // 0: tiles of 256 x 256, 1: 128 x 128, 2: 64 x 64
   uint32_t row_tiles, column_tiles, steps, shared, shares;
-  uint64_t parts_bytes() const { return (uint64_t)shared * shares * kSide[size] * kSide[size] * 4; }
+  uint64_t parts_bytes() const { return shared ? (uint64_t)shared * shares * kSide[size] * kSide[size] * 4 : 0; }
+  static constexpr uint32_t lanes(uint32_t size) { return size ? 256 : 512; }  // of a workgroup
   static constexpr uint32_t kSide[3] = {256, 128, 64};
 };
 constexpr uint32_t Cut::kSide[3];
@@ -564,18 +565,22 @@ constexpr uint32_t Cut::kSide[3];
 // in tiles of 128 and 2.4 in tiles of 64), small ones begin sooner and leave fewer compute units idle; products of 32-bit numbers are bound by the matrix
 // units at every size.  Tiles that do not fill the card another time can be shared out by steps, which
 // costs a launch and their sums' way through memory: a write and a read at 5 TB/s.
+// size kNoCut: more tiles of any size than a launch has workgroups.
+constexpr uint32_t kNoCut = 3;
 Cut cut(uint64_t rows, uint64_t columns, uint64_t steps, bool single) {
   struct Cost { uint32_t at_once; double begin, lone, full; };
   constexpr Cost kCost[2][3] = {{{1, 8, 1.4, 1.6}, {2, 5.5, 0.5, 0.95}, {2, 3.5, 0.22, 0.3}}, {{1, 10, 7.0, 7.0}, {2, 6, 1.95, 3.9}, {4, 3, 0.55, 2.15}}};
   constexpr uint32_t kUnits = 256;  // compute units
   constexpr double kJoin = 3.5, kBytes = 2 / 5e6;
   Cut best{};
+  best.size = kNoCut;
   double least = 0;
   if (!steps) steps = 1;
   for (uint32_t size = 0; size < 3; ++size) {
     const Cost& c = kCost[single][size];
     const uint64_t side = Cut::kSide[size], row_tiles = ceil_div(rows, side), column_tiles = ceil_div(columns, side), tiles = row_tiles * column_tiles;
     const uint64_t slots = kUnits * c.at_once, rest = tiles % slots;
+    if (tiles + 16 * slots > most_blocks(Cut::lanes(size))) continue;
     for (uint32_t n = 1; n <= 16 && (n == 1 || (rest && 4 * n <= steps)); ++n) {
       const uint64_t groups = rest * n, busy = ceil_div(groups < slots ? groups : slots, kUnits);
       const double step = c.full * busy / c.at_once;
@@ -652,12 +657,7 @@ struct Shape {
   bool pad[3];                 // x, w_gate, w_up
   uint64_t at[3], slopes, parts, bytes;
   Cut forward, inputs, weights;
-  bool fits() const {  // a grid's limit
-    const Cut all[3] = {forward, inputs, weights};
-    for (const Cut& c : all)
-      if ((uint64_t)c.row_tiles * c.column_tiles >> 31) return false;
-    return true;
-  }
+  bool fits() const { return forward.size != kNoCut && inputs.size != kNoCut && weights.size != kNoCut; }
 };
 
 Shape shape_of(const fbx_gated* g, bool backward) {

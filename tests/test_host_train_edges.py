@@ -2,7 +2,7 @@
 import ctypes
 
 from paper_2210_07768_amd import binding as B
-from test_host_train import _library, _slot, _why
+from test_host_train import _gated, _library, _slot, _why
 
 
 def test_embed_backward_refuses_more_records_than_a_launch_holds():
@@ -12,3 +12,13 @@ def test_embed_backward_refuses_more_records_than_a_launch_holds():
     assert scratch((1 << 32) - 256, 1) == B.OK and scratch((1 << 31) - 128, 2) == B.OK
     assert scratch((1 << 32) - 255, 1) == B.E_ARG and "2^32 - 256" in _why()
     assert scratch((1 << 31) - 127, 2) == B.E_ARG
+
+
+def test_gated_refuses_more_tiles_than_a_launch_holds():
+    """2^25 tiles of 512 lanes each, which are counted in 32 bits: of the forward product, or of one of the gradient's alone."""
+    L = _library()
+    wide = _gated(records=1 << 24, inputs=8, hidden=1 << 16, ld_x=8, ld_w_gate=8, ld_w_up=8)
+    assert L.fbx_gated_forward(wide, 4096, 1 << 16, 1 << 20, 1 << 62, None) == B.E_ARG and "too large" in _why()
+    for inputs, hidden in ((8, 1 << 16), (1 << 17, 8)):
+        g = _gated(records=1 << 24, inputs=inputs, hidden=hidden, ld_x=inputs, ld_w_gate=inputs, ld_w_up=inputs)
+        assert L.fbx_gated_backward(g, 4096, hidden, 4096, inputs, 4096, inputs, 4096, inputs, 1 << 20, 1 << 62, None) == B.E_ARG and "too large" in _why()
