@@ -129,10 +129,11 @@ fbx_status fbx_gated_backward(const fbx_gated* g, const void* d_dh, uint64_t ld_
  *   mix64(mix64(mix64(seed + step) + t) + i / 2).  A value that is not finite makes its block NaN.
  *   All zero bytes are the state before the first step.
  *
- *   tensors    : HOST, n_tensors entries; elements of a tensor are adjacent
+ *   tensors    : HOST, n_tensors entries; elements of a tensor are adjacent; at most FBX_ADAMW_MOST of them in one
  *   copy       : DEVICE or NULL: receives the new weights in copy_dtype as well (for weights kept in f32)
  * Errors: FBX_E_ARG, FBX_E_HIP.
  */
+#define FBX_ADAMW_MOST 34359736320ull /* 2^35 - 2048 */
 typedef struct {
   void* d_param;
   const void* d_grad;

@@ -10,6 +10,7 @@ namespace {
 constexpr uint32_t kTensorsPerLaunch = 128;  // (10 KB of arguments)
 constexpr uint32_t kEach = 8;                 // elements of a lane
 constexpr uint32_t kBlock = 256 * kEach;      // elements of a workgroup
+static_assert(FBX_ADAMW_MOST == most_blocks(256) * kBlock, "a tensor is within one launch");
 
 struct AdamwArgs {
   fbx_adamw_tensor t[kTensorsPerLaunch];
@@ -208,7 +209,7 @@ extern "C" fbx_status fbx_adamw_step(const fbx_adamw* h, const fbx_adamw_tensor*
     const fbx_adamw_tensor& t = tensors[i];
     if (!t.n) continue;
     if (!t.d_param || !t.d_grad || !t.d_m || !t.d_v || (eight && (!t.d_m_scale || !t.d_v_scale))) return refuse(FBX_E_ARG, "a tensor lacks its weights, gradient or state");
-    if (t.n >> 40) return refuse(FBX_E_ARG, "a tensor has 2^40 elements or more");
+    if (t.n > FBX_ADAMW_MOST) return refuse(FBX_E_ARG, "a tensor has more than 2^35 - 2048 elements");
     if ((uintptr_t)t.d_param % ps || (uintptr_t)t.d_grad % gs || (!eight && ((uintptr_t)t.d_m | (uintptr_t)t.d_v) % 4u)) return refuse(FBX_E_ARG, "a tensor is not aligned to its elements");
     if (t.d_copy && (h->copy_dtype == FBX_F32 || !known(h->copy_dtype) || h->param_dtype != FBX_F32 || (uintptr_t)t.d_copy % 2u))
       return refuse(FBX_E_ARG, "a copy is in f16 or bf16, of weights in f32");
@@ -241,7 +242,7 @@ extern "C" fbx_status fbx_adamw_step(const fbx_adamw* h, const fbx_adamw_tensor*
   for (uint32_t i = 0; i < n_tensors; ++i) {
     if (!tensors[i].n) continue;
     const uint64_t blocks = ceil_div(tensors[i].n, kBlock);
-    if (a.n == kTensorsPerLaunch || (a.n && a.first_block[a.n] + blocks > 0x7fffffffull)) flush();
+    if (a.n == kTensorsPerLaunch || (a.n && a.first_block[a.n] + blocks > most_blocks(256))) flush();
     a.t[a.n] = tensors[i];
     a.key[a.n] = mix64(key + i);
     a.first_block[a.n + 1] = a.first_block[a.n] + (uint32_t)blocks;

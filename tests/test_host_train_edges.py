@@ -2,7 +2,7 @@
 import ctypes
 
 from paper_2210_07768_amd import binding as B
-from test_host_train import _gated, _library, _slot, _why
+from test_host_train import TENSOR, AdamwArgs, _gated, _library, _slot, _why
 
 
 def test_embed_backward_refuses_more_records_than_a_launch_holds():
@@ -22,3 +22,10 @@ def test_gated_refuses_more_tiles_than_a_launch_holds():
     for inputs, hidden in ((8, 1 << 16), (1 << 17, 8)):
         g = _gated(records=1 << 24, inputs=inputs, hidden=hidden, ld_x=inputs, ld_w_gate=inputs, ld_w_up=inputs)
         assert L.fbx_gated_backward(g, 4096, hidden, 4096, inputs, 4096, inputs, 4096, inputs, 1 << 20, 1 << 62, None) == B.E_ARG and "too large" in _why()
+
+
+def test_adamw_refuses_more_elements_than_a_launch_holds():
+    """2,048 elements a workgroup of 256 lanes, lanes counted in 32 bits; nothing is enqueued for the tensors before it."""
+    h = AdamwArgs(0, 0, 0, 32, 1, 1e-3, 0.9, 0.999, 1e-8, 0.0, 1.0, 0)
+    tensors = TENSOR.pack(4096, 4096, 4096, 4096, 0, 0, 0, 8) + TENSOR.pack(4096, 4096, 4096, 4096, 0, 0, 0, (1 << 35) - 2047)
+    assert _library().fbx_adamw_step(h, tensors, 2, None) == B.E_ARG and "2^35" in _why()
