@@ -128,11 +128,16 @@ fbx_status fbx_gated_backward(const fbx_gated* g, const void* d_dh, uint64_t ld_
  *   tensor t takes 16 bits (m: from bit 0, sqrt(v): from bit 16; 32 higher for odd i) of
  *   mix64(mix64(mix64(seed + step) + t) + i / 2).  A value that is not finite makes its block NaN.
  *   All zero bytes are the state before the first step.
+ *   m and sqrt(v) are rounded independently of each other, so sqrt(v) can become 0 beside an m that does not; a gradient of 0
+ *   then moves that weight by lr * m / eps, thousands of times lr.  With FBX_ADAMW_KEEP_ROOTS a sqrt(v) above 0
+ *   that would be coded as 0 is coded as 1, the smallest code above it, and nothing else changes.
+ * state_bits = 8 | FBX_ADAMW_KEEP_ROOTS: what a training run is to use, from its first step on.
  *
  *   tensors    : HOST, n_tensors entries; elements of a tensor are adjacent; at most FBX_ADAMW_MOST of them in one
  *   copy       : DEVICE or NULL: receives the new weights in copy_dtype as well (for weights kept in f32)
  * Errors: FBX_E_ARG, FBX_E_HIP.
  */
+#define FBX_ADAMW_KEEP_ROOTS 0x100u
 #define FBX_ADAMW_MOST 34359736320ull /* 2^35 - 2048 */
 typedef struct {
   void* d_param;

@@ -16,7 +16,7 @@ struct AdamwArgs {
   fbx_adamw_tensor t[kTensorsPerLaunch];
   uint64_t key[kTensorsPerLaunch];            // of the tensor's random bits
   uint32_t first_block[kTensorsPerLaunch + 1];
-  uint32_t n;
+  uint32_t n, least_root;                     // least_root: the least code of a sqrt(v) above 0
   float keep, step_size, beta1, beta2, one_beta1, one_beta2, root_scale, eps, grad_scale;
 };
 
@@ -77,9 +77,10 @@ __device__ __forceinline__ void decode(float (&to)[kEach], const uint8_t* codes,
   }
 }
 
-// Eight codes of a block of 32, which four neighbouring lanes hold, and its scale.  random16(i): 16 random bits.
+// Eight codes of a block of 32, which four neighbouring lanes hold, and its scale.  random16(i): 16 random bits; least: the
+// code, 0 or 1, of what is above 0 and would be rounded to 0.
 template <class Random>
-__device__ __forceinline__ void encode(uint8_t* codes, uint8_t* scale, const float (&x)[kEach], uint32_t n, bool wide, Random random16) {
+__device__ __forceinline__ void encode(uint8_t* codes, uint8_t* scale, const float (&x)[kEach], uint32_t n, bool wide, uint32_t least, Random random16) {
   uint32_t top = 0u;  // (magnitudes compare as integers, NaN above infinity above the rest)
 #pragma unroll
   for (uint32_t i = 0; i < kEach; ++i) {
@@ -102,7 +103,7 @@ __device__ __forceinline__ void encode(uint8_t* codes, uint8_t* scale, const flo
     const float t = a * __uint_as_float((uint32_t)(130 - ee) << 23);  // in units of the code's last place
     const uint32_t q = (uint32_t)floorf(t + (float)random16(i) * (1.f / 65536.f));
     const uint32_t code = b == 255u ? 127u : q + ((uint32_t)(ee + 6) << 3) + (y < 0.f ? 128u : 0u);
-    w[i / 4] |= code << (8 * (i % 4));
+    w[i / 4] |= (code == 0u && x[i] > 0.f ? least : code) << (8 * (i % 4));
   }
   if (wide) {
     *(Pack<uint32_t, 2>*)codes = Pack<uint32_t, 2>{{w[0], w[1]}};
@@ -160,8 +161,8 @@ __global__ __launch_bounds__(256) void k_adamw(AdamwArgs) {
     uint64_t bits[kEach / 2];
 #pragma unroll
     for (uint32_t i = 0; i < kEach / 2; ++i) bits[i] = mix64(a.key[lo] + at / 2u + i);
-    encode((uint8_t*)t.d_m + at, t.d_m_scale + at / 32u, m, n, wide, [&](uint32_t i) { return (uint32_t)(bits[i / 2] >> (32 * (i % 2))) & 0xffffu; });
-    encode((uint8_t*)t.d_v + at, t.d_v_scale + at / 32u, root, n, wide, [&](uint32_t i) { return (uint32_t)(bits[i / 2] >> (32 * (i % 2) + 16)) & 0xffffu; });
+    encode((uint8_t*)t.d_m + at, t.d_m_scale + at / 32u, m, n, wide, 0u, [&](uint32_t i) { return (uint32_t)(bits[i / 2] >> (32 * (i % 2))) & 0xffffu; });
+    encode((uint8_t*)t.d_v + at, t.d_v_scale + at / 32u, root, n, wide, a.least_root, [&](uint32_t i) { return (uint32_t)(bits[i / 2] >> (32 * (i % 2) + 16)) & 0xffffu; });
   } else {
     store((float*)t.d_m + at, m, n, wide);
     store((float*)t.d_v + at, v, n, wide);
@@ -177,9 +178,9 @@ void launch(const AdamwArgs& a, bool eight, hipStream_t stream) {
 
 template <class P, class G>
 void launch_by_copy(const AdamwArgs& a, const fbx_adamw& h, bool copy, hipStream_t stream) {
-  if (!copy) launch<P, G, float, false>(a, h.state_bits == 8u, stream);
-  else if (h.copy_dtype == FBX_F16) launch<P, G, _Float16, true>(a, h.state_bits == 8u, stream);
-  else launch<P, G, __bf16, true>(a, h.state_bits == 8u, stream);
+  if (!copy) launch<P, G, float, false>(a, h.state_bits != 32u, stream);
+  else if (h.copy_dtype == FBX_F16) launch<P, G, _Float16, true>(a, h.state_bits != 32u, stream);
+  else launch<P, G, __bf16, true>(a, h.state_bits != 32u, stream);
 }
 
 template <class P>
@@ -198,11 +199,12 @@ using namespace fbx::train;
 extern "C" fbx_status fbx_adamw_step(const fbx_adamw* h, const fbx_adamw_tensor* tensors, uint32_t n_tensors, void* hip_stream) {
   if (!h || (!tensors && n_tensors)) return refuse(FBX_E_ARG, "h or tensors is NULL");
   if (!known(h->param_dtype) || !known(h->grad_dtype)) return refuse(FBX_E_ARG, "unknown dtype");
-  if (h->state_bits != 8u && h->state_bits != 32u) return refuse(FBX_E_ARG, "state_bits must be 8 or 32");
+  if (h->state_bits != 8u && h->state_bits != 32u && h->state_bits != (8u | FBX_ADAMW_KEEP_ROOTS))
+    return refuse(FBX_E_ARG, "state_bits must be 8 (also with FBX_ADAMW_KEEP_ROOTS) or 32");
   if (!h->step) return refuse(FBX_E_ARG, "step counts from 1");
   if (!(h->beta1 >= 0 && h->beta1 < 1 && h->beta2 >= 0 && h->beta2 < 1)) return refuse(FBX_E_ARG, "beta1 and beta2 must be in [0, 1)");
   if (!(h->eps >= 0) || !isfinite(h->lr) || !isfinite(h->weight_decay) || isnan(h->grad_scale)) return refuse(FBX_E_ARG, "lr, eps, weight_decay or grad_scale is not a number that makes sense");
-  const bool eight = h->state_bits == 8u;
+  const bool eight = h->state_bits != 32u;
   const uint32_t ps = size_of(h->param_dtype), gs = size_of(h->grad_dtype);
   bool copy = false, any = false;
   for (uint32_t i = 0; i < n_tensors; ++i) {
@@ -221,6 +223,7 @@ extern "C" fbx_status fbx_adamw_step(const fbx_adamw* h, const fbx_adamw_tensor*
   for (uint32_t i = 0; copy && i < n_tensors; ++i)
     if (tensors[i].n && !tensors[i].d_copy) return refuse(FBX_E_ARG, "either all tensors have a copy or none");
   AdamwArgs a{};
+  a.least_root = h->state_bits & FBX_ADAMW_KEEP_ROOTS ? 1u : 0u;
   a.keep = (float)(1.0 - h->lr * h->weight_decay);
   a.step_size = (float)(h->lr / (1.0 - pow(h->beta1, (double)h->step)));
   a.beta1 = (float)h->beta1;

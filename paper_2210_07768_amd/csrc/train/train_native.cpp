@@ -309,13 +309,14 @@ struct List {
   const at::Tensor& operator[](Py_ssize_t i) const { return tensor(PySequence_Fast_GET_ITEM(seq, i), "an entry of a list"); }
 };
 
-// adamw(params, grads, m, v, m_scale, v_scale, copies, step, lr, beta1, beta2, eps, weight_decay, grad_scale, seed)
+// adamw(params, grads, m, v, m_scale, v_scale, copies, step, lr, beta1, beta2, eps, weight_decay, grad_scale, seed, keep_roots)
 PyObject* adamw(PyObject*, PyObject* args) {
   PyObject* lists[7];
   fbx_adamw h{};
   unsigned long long step, seed;
-  if (!PyArg_ParseTuple(args, "OOOOOOOKddddddK", &lists[0], &lists[1], &lists[2], &lists[3], &lists[4], &lists[5], &lists[6], &step, &h.lr, &h.beta1, &h.beta2, &h.eps,
-                        &h.weight_decay, &h.grad_scale, &seed))
+  int keep_roots;
+  if (!PyArg_ParseTuple(args, "OOOOOOOKddddddKp", &lists[0], &lists[1], &lists[2], &lists[3], &lists[4], &lists[5], &lists[6], &step, &h.lr, &h.beta1, &h.beta2, &h.eps,
+                        &h.weight_decay, &h.grad_scale, &seed, &keep_roots))
     return nullptr;
   return guarded([&]() -> PyObject* {
     const List p(lists[0]), grad(lists[1]), m(lists[2]), v(lists[3]), m_scale(lists[4]), v_scale(lists[5]), copy(lists[6]);
@@ -325,7 +326,7 @@ PyObject* adamw(PyObject*, PyObject* args) {
       if (l->seq && l->size() != n) bad("params, grads, states and copies must be lists of one length");
     if (!n) Py_RETURN_NONE;
     const bool eight = m_scale.seq;
-    h.state_bits = eight ? 8 : 32;
+    h.state_bits = !eight ? 32 : keep_roots ? 8 | FBX_ADAMW_KEEP_ROOTS : 8;
     h.step = step;
     h.seed = seed;
     h.param_dtype = code(p[0]);

@@ -154,20 +154,22 @@ class _Gated(torch.autograd.Function):
 # ------------------------------------------------------------------ AdamW
 def adamw(params: Sequence, grads: Sequence, m: Sequence, v: Sequence, m_scale: Optional[Sequence] = None, v_scale: Optional[Sequence] = None,
           copies: Optional[Sequence] = None, *, step: int, lr: float = 1e-3, betas: Tuple[float, float] = (0.9, 0.999), eps: float = 1e-8,
-          weight_decay: float = 1e-2, grad_scale: float = 1.0, seed: int = 0):
+          weight_decay: float = 1e-2, grad_scale: float = 1.0, seed: int = 0, keep_roots: bool = False):
     """One AdamW step over all tensors, in place (the formulas, the 8-bit states and their random rounding: fbx_adamw_step
     in ``include/fbx_train.h``).  All weights are of one type, and so are all gradients.
 
     m, v: float32 tensors of the weights' sizes, or, with m_scale and v_scale, their codes (float8_e4m3fn or uint8) with
     ceil(n / 32) scales each (float8_e8m0fnu or uint8).  copies: float16 or bfloat16 tensors that receive the new weights
-    too.  step counts from 1; seed: of the random rounding, the same for all steps."""
-    _load().adamw(params, grads, m, v, m_scale, v_scale, copies, step, lr, betas[0], betas[1], eps, weight_decay, grad_scale, seed & ((1 << 64) - 1))
+    too.  step counts from 1; seed: of the random rounding, the same for all steps.  keep_roots, for 8-bit states: a sqrt(v) above
+    0 is never rounded to 0.  Without it a weight can be moved by lr * m / eps, thousands of times lr, where gradients of
+    very unlike size share a block of 32: a training run sets it, as ``AdamW`` does."""
+    _load().adamw(params, grads, m, v, m_scale, v_scale, copies, step, lr, betas[0], betas[1], eps, weight_decay, grad_scale, seed & ((1 << 64) - 1), keep_roots)
 
 
 class AdamW:
     """Keeps the states of a list of weights and steps them all at once from their ``.grad``.
 
-    bits: 32 or 8, of a state.  copies: a list of float16 or bfloat16 tensors, one for each weight (float32 then), that
+    bits: 32 or 8, of a state (8: with ``keep_roots``, see ``adamw``).  copies: a list of float16 or bfloat16 tensors, one for each weight (float32 then), that
     follow the weights: what the kernels of a model in 16 bits read."""
 
     def __init__(self, params, lr: float = 1e-3, betas: Tuple[float, float] = (0.9, 0.999), eps: float = 1e-8, weight_decay: float = 1e-2,
@@ -203,7 +205,7 @@ class AdamW:
             pick = lambda x: None if x is None else [x[i] for i in at]  # noqa: E731
             adamw(pick(self.params), pick(grads), pick(self.m), pick(self.v), pick(self.m_scale), pick(self.v_scale), pick(self.copies),
                   step=self.step_count, lr=self.lr if lr is None else lr, betas=self.betas, eps=self.eps, weight_decay=self.weight_decay,
-                  grad_scale=grad_scale, seed=self.seed + (k << 32))
+                  grad_scale=grad_scale, seed=self.seed + (k << 32), keep_roots=True)
 
     def zero_grad(self):
         for p in self.params:

@@ -98,3 +98,41 @@ def test_more_terms_than_a_launch_holds():
         count += torch.bincount(_rows_of(values[at:at + (1 << 26)], rows), minlength=rows)
     got = T.embed_backward(torch.ones(n, 1, dim, device="cuda"), [T.Signs(values, None, arity)], rows)
     assert int(count.max()) < 1 << 24 and torch.equal(got, count.float().unsqueeze(1).expand(rows, dim))
+
+
+# ------------------------------------------------------------------ AdamW
+def test_adamw_8_bit_states_of_unlike_rows():
+    """A table's rows whose gradients differ by orders of magnitude, most of them not hit in most steps.  No history of gradients
+    moves a weight by more than (1 - beta1) / sqrt((1 - beta2) (1 - beta1^2 / beta2)) = 7.3 times lr (Cauchy-Schwarz on the
+    two averages; the bias corrections only lower it); twice that leaves room for the states' rounding."""
+    rows, dim = 4096, 16
+    for sigma in (2.0, 4.0):
+        g = torch.Generator(device="cuda").manual_seed(1)
+        scale = 7e-3 * torch.exp(sigma * torch.randn(rows, 1, device="cuda", generator=g))
+        often = torch.arange(1, rows + 1, device="cuda").float().rsqrt().unsqueeze(1)
+        p = torch.zeros(rows, dim, device="cuda")
+        opt = T.AdamW([p], lr=1.0, weight_decay=0.0, bits=8, seed=7)
+        most = torch.zeros((), device="cuda")
+        for _ in range(300):
+            grad = torch.randn(rows, dim, device="cuda", generator=g) * scale * (torch.rand(rows, 1, device="cuda", generator=g) < often)
+            p.zero_()
+            opt.step([grad])
+            most = torch.maximum(most, p.abs().max())
+        assert float(most) < 2 * 7.3
+
+
+@pytest.mark.parametrize("n", [1, 31, 33, 5000, 70_001])
+def test_adamw_kept_roots_change_nothing_else(n):
+    """The same step with and without: only codes 0 of a sqrt(v) above 0 differ, and they are 1."""
+    g = torch.Generator(device="cuda").manual_seed(n)
+    r = lambda: torch.randn(n, device="cuda", generator=g) * 10.0 ** torch.randint(-8, 1, (n,), device="cuda", generator=g)  # noqa: E731
+    grad, p = r(), torch.randn(n, device="cuda", generator=g)
+    grad[n // 2:] *= torch.rand(n - n // 2, device="cuda", generator=g) < 0.5
+    sides = []
+    for keep in (False, True):
+        s = [p.clone(), *(torch.zeros(n, dtype=torch.uint8, device="cuda") for _ in range(2)), *(torch.zeros(-(-n // 32), dtype=torch.uint8, device="cuda") for _ in range(2))]
+        T.adamw([s[0]], [grad], [s[1]], [s[2]], [s[3]], [s[4]], step=1, seed=5, keep_roots=keep)
+        sides.append(s)
+    (p0, m0, v0, ms0, vs0), (p1, m1, v1, ms1, vs1) = sides
+    assert torch.equal(p0, p1) and torch.equal(m0, m1) and torch.equal(ms0, ms1) and torch.equal(vs0, vs1)
+    assert torch.equal(v1, torch.where((v0 == 0) & (grad * grad * 0.001 > 0), 1, v0)) and (n < 5000 or bool(((v0 == 0) & (v1 == 1)).any()))
