@@ -309,14 +309,14 @@ struct List {
   const at::Tensor& operator[](Py_ssize_t i) const { return tensor(PySequence_Fast_GET_ITEM(seq, i), "an entry of a list"); }
 };
 
-// adamw(params, grads, m, v, m_scale, v_scale, copies, step, lr, beta1, beta2, eps, weight_decay, grad_scale, seed, keep_roots)
+// adamw(params, grads, m, v, m_scale, v_scale, copies, step, lr, beta1, beta2, eps, weight_decay, grad_scale, seed, keep_roots, check_only)
 PyObject* adamw(PyObject*, PyObject* args) {
   PyObject* lists[7];
   fbx_adamw h{};
   unsigned long long step, seed;
-  int keep_roots;
-  if (!PyArg_ParseTuple(args, "OOOOOOOKddddddKp", &lists[0], &lists[1], &lists[2], &lists[3], &lists[4], &lists[5], &lists[6], &step, &h.lr, &h.beta1, &h.beta2, &h.eps,
-                        &h.weight_decay, &h.grad_scale, &seed, &keep_roots))
+  int keep_roots, check_only;
+  if (!PyArg_ParseTuple(args, "OOOOOOOKddddddKpp", &lists[0], &lists[1], &lists[2], &lists[3], &lists[4], &lists[5], &lists[6], &step, &h.lr, &h.beta1, &h.beta2, &h.eps,
+                        &h.weight_decay, &h.grad_scale, &seed, &keep_roots, &check_only))
     return nullptr;
   return guarded([&]() -> PyObject* {
     const List p(lists[0]), grad(lists[1]), m(lists[2]), v(lists[3]), m_scale(lists[4]), v_scale(lists[5]), copy(lists[6]);
@@ -360,9 +360,13 @@ PyObject* adamw(PyObject*, PyObject* args) {
         t.d_v_scale = static_cast<uint8_t*>(same(v_scale[i]));
       }
       if (copy.seq) t.d_copy = same(copy[i]);
+      // (what the library refuses too, but of one list at a time)
+      if (size && copy.seq && (h.copy_dtype == FBX_F32 || h.param_dtype != FBX_F32)) bad("a copy is in float16 or bfloat16, of weights in float32");
+      if (static_cast<uint64_t>(size) > FBX_ADAMW_MOST) bad("a tensor has more than 2^35 - 2048 elements");
       t.n = size;
     }
     on_gpu(p[0]);
+    if (check_only) Py_RETURN_NONE;
     const c10::DeviceGuard guard(where);
     check(g.adamw_step(&h, all.data(), static_cast<uint32_t>(n), stream_of(p[0])));
     for (Py_ssize_t i = 0; i < n; ++i) {  // (autograd then knows that they changed)

@@ -163,7 +163,7 @@ def adamw(params: Sequence, grads: Sequence, m: Sequence, v: Sequence, m_scale: 
     too.  step counts from 1; seed: of the random rounding, the same for all steps.  keep_roots, for 8-bit states: a sqrt(v) above
     0 is never rounded to 0.  Without it a weight can be moved by lr * m / eps, thousands of times lr, where gradients of
     very unlike size share a block of 32: a training run sets it, as ``AdamW`` does."""
-    _load().adamw(params, grads, m, v, m_scale, v_scale, copies, step, lr, betas[0], betas[1], eps, weight_decay, grad_scale, seed & ((1 << 64) - 1), keep_roots)
+    _load().adamw(params, grads, m, v, m_scale, v_scale, copies, step, lr, betas[0], betas[1], eps, weight_decay, grad_scale, seed & ((1 << 64) - 1), keep_roots, False)
 
 
 class AdamW:
@@ -192,7 +192,8 @@ class AdamW:
 
     @torch.no_grad()
     def step(self, grads: Optional[Sequence] = None, grad_scale: float = 1.0, lr: Optional[float] = None):
-        """grads: one for each weight, instead of their .grad.  Weights without a gradient stay as they are."""
+        """grads: one for each weight, instead of their .grad.  Weights without a gradient stay as they are.  All weights are
+        stepped, or, where something is refused, none."""
         grads = [p.grad for p in self.params] if grads is None else list(grads)
         if len(grads) != len(self.params):
             _bad("one gradient for each weight")
@@ -200,12 +201,15 @@ class AdamW:
         for i, (p, g) in enumerate(zip(self.params, grads)):
             if g is not None:
                 kinds.setdefault((p.dtype, g.dtype, p.device), []).append(i)
+        pick = lambda x, at: None if x is None else [x[i] for i in at]  # noqa: E731
+        calls = [[*(pick(x, at) for x in (self.params, grads, self.m, self.v, self.m_scale, self.v_scale, self.copies)), self.step_count + 1,
+                  self.lr if lr is None else lr, *self.betas, self.eps, self.weight_decay, grad_scale, (self.seed + (k << 32)) & ((1 << 64) - 1), True]
+                 for k, at in enumerate(kinds.values())]
+        step = _load().adamw
+        for check_only in (True, False) if len(calls) > 1 else (False,):   # (nothing is stepped if a later list is refused)
+            for call in calls:
+                step(*call, check_only)
         self.step_count += 1
-        for k, at in enumerate(kinds.values()):
-            pick = lambda x: None if x is None else [x[i] for i in at]  # noqa: E731
-            adamw(pick(self.params), pick(grads), pick(self.m), pick(self.v), pick(self.m_scale), pick(self.v_scale), pick(self.copies),
-                  step=self.step_count, lr=self.lr if lr is None else lr, betas=self.betas, eps=self.eps, weight_decay=self.weight_decay,
-                  grad_scale=grad_scale, seed=self.seed + (k << 32), keep_roots=True)
 
     def zero_grad(self):
         for p in self.params:

@@ -136,3 +136,30 @@ def test_adamw_kept_roots_change_nothing_else(n):
     (p0, m0, v0, ms0, vs0), (p1, m1, v1, ms1, vs1) = sides
     assert torch.equal(p0, p1) and torch.equal(m0, m1) and torch.equal(ms0, ms1) and torch.equal(vs0, vs1)
     assert torch.equal(v1, torch.where((v0 == 0) & (grad * grad * 0.001 > 0), 1, v0)) and (n < 5000 or bool(((v0 == 0) & (v1 == 1)).any()))
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("wrong", ["strided gradient", "copies of 16-bit weights", "state of another size", "lr"])
+def test_adamw_class_steps_all_weights_or_none(wrong, bits):
+    """Two lists by type, of which the second is refused: nothing has moved, and the step that follows is the first one."""
+    make = lambda: [torch.full((40,), 0.5, device="cuda"), torch.full((6, 6), 0.25, device="cuda").to(torch.bfloat16)]  # noqa: E731
+    grads = lambda: [torch.full((40,), 0.1, device="cuda"), torch.arange(36, device="cuda").view(6, 6).to(torch.bfloat16)]  # noqa: E731
+    a, b = make(), make()
+    opt, fresh = T.AdamW(a, bits=bits), T.AdamW(b, bits=bits)
+    g, lr, kept = grads(), None, opt.m[1]
+    if wrong == "strided gradient":
+        g[1] = g[1].t()
+    elif wrong == "copies of 16-bit weights":
+        opt.copies = [torch.zeros_like(w, dtype=torch.bfloat16) for w in a]
+    elif wrong == "state of another size":
+        opt.m[1] = kept[:-1]
+    else:
+        lr = float("nan")
+    with pytest.raises(B.FbxError):
+        opt.step(g, lr=lr)
+    assert opt.step_count == 0 and all(torch.equal(x, y) for x, y in zip(a, make()))
+    assert not any(bool(t.any()) for t in opt.m + opt.v)
+    opt.copies, opt.m[1] = None, kept
+    opt.step(grads())
+    fresh.step(grads())
+    assert opt.step_count == 1 and all(torch.equal(x, y) for x, y in zip(a + opt.m + opt.v, b + fresh.m + fresh.v))
