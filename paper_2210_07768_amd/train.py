@@ -170,7 +170,7 @@ class AdamW:
     """Keeps the states of a list of weights and steps them all at once from their ``.grad``.
 
     bits: 32 or 8, of a state (8: with ``keep_roots``, see ``adamw``).  copies: a list of float16 or bfloat16 tensors, one for each weight (float32 then), that
-    follow the weights: what the kernels of a model in 16 bits read."""
+    follow the weights: what the kernels of a model in 16 bits read.  A weight's steps count from its first gradient."""
 
     def __init__(self, params, lr: float = 1e-3, betas: Tuple[float, float] = (0.9, 0.999), eps: float = 1e-8, weight_decay: float = 1e-2,
                  bits: int = 32, seed: int = 0, copies: Optional[List] = None):
@@ -182,6 +182,7 @@ class AdamW:
             _bad("one copy for each weight")
         self.lr, self.betas, self.eps, self.weight_decay, self.bits, self.seed = lr, betas, eps, weight_decay, bits, seed
         self.step_count = 0
+        self.steps = [0] * len(self.params)   # of each weight: its bias corrections are of the gradients it had
         kind = torch.uint8 if bits == 8 else torch.float32
         state = lambda p, n, dtype: torch.zeros(n, dtype=dtype, device=p.device)  # noqa: E731
         self.m, self.v = ([state(p, p.numel(), kind) for p in self.params] for _ in range(2))
@@ -200,15 +201,18 @@ class AdamW:
         kinds = {}
         for i, (p, g) in enumerate(zip(self.params, grads)):
             if g is not None:
-                kinds.setdefault((p.dtype, g.dtype, p.device), []).append(i)
+                kinds.setdefault((p.dtype, g.dtype, p.device, self.steps[i]), []).append(i)
         pick = lambda x, at: None if x is None else [x[i] for i in at]  # noqa: E731
-        calls = [[*(pick(x, at) for x in (self.params, grads, self.m, self.v, self.m_scale, self.v_scale, self.copies)), self.step_count + 1,
+        calls = [[*(pick(x, at) for x in (self.params, grads, self.m, self.v, self.m_scale, self.v_scale, self.copies)), self.steps[at[0]] + 1,
                   self.lr if lr is None else lr, *self.betas, self.eps, self.weight_decay, grad_scale, (self.seed + (k << 32)) & ((1 << 64) - 1), True]
                  for k, at in enumerate(kinds.values())]
         step = _load().adamw
         for check_only in (True, False) if len(calls) > 1 else (False,):   # (nothing is stepped if a later list is refused)
             for call in calls:
                 step(*call, check_only)
+        for at in kinds.values():
+            for i in at:
+                self.steps[i] += 1
         self.step_count += 1
 
     def zero_grad(self):
@@ -216,13 +220,14 @@ class AdamW:
             p.grad = None
 
     def state_dict(self) -> dict:
-        return {"step": self.step_count, "seed": self.seed, "bits": self.bits,
+        return {"step": self.step_count, "steps": tuple(self.steps), "seed": self.seed, "bits": self.bits,
                 **{k: getattr(self, k) for k in ("m", "v", "m_scale", "v_scale")}}
 
     def load_state_dict(self, state: dict):
         if state["bits"] != self.bits or len(state["m"]) != len(self.m):
             _bad("the states are of another kind")
         self.step_count, self.seed = state["step"], state["seed"]
+        self.steps = list(state.get("steps", [state["step"]] * len(self.m)))   # (states saved without: all weights took all steps)
         for k in ("m", "v", "m_scale", "v_scale"):
             for mine, theirs in zip(getattr(self, k) or (), state[k] or ()):
                 mine.copy_(theirs)

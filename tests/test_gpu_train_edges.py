@@ -163,3 +163,28 @@ def test_adamw_class_steps_all_weights_or_none(wrong, bits):
     opt.step(grads())
     fresh.step(grads())
     assert opt.step_count == 1 and all(torch.equal(x, y) for x, y in zip(a + opt.m + opt.v, b + fresh.m + fresh.v))
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_adamw_class_counts_each_weights_own_steps(bits):
+    """A weight whose first gradient comes later than the others' moves as if the optimizer were new, also behind a saved and
+    loaded state; a state saved without the weights' counts gives all of them the optimizer's."""
+    make = lambda: [torch.full((70,), 0.5, device="cuda"), torch.full((50,), 0.25, device="cuda"), torch.ones(5, device="cuda")]  # noqa: E731
+    g = torch.Generator(device="cuda").manual_seed(0)
+    first = torch.randn(50, device="cuda", generator=g)
+    a = make()
+    opt = T.AdamW(a, lr=0.1, bits=bits)
+    for _ in range(6):
+        opt.step([torch.randn(70, device="cuda", generator=g), None, None])
+    saved = {k: [t.clone() for t in x] if isinstance(x, list) else x for k, x in opt.state_dict().items()}
+    for o in (opt, T.AdamW([w.clone() for w in a], lr=0.1, bits=bits)):
+        o.load_state_dict(saved)
+        alone = make()[1]
+        T.AdamW([alone], lr=0.1, bits=bits).step([first])
+        mine = [w.clone() for w in a]
+        o.params = mine
+        o.step([torch.ones(70, device="cuda"), first, None])
+        assert torch.equal(mine[1], alone) and torch.equal(mine[2], a[2]) and o.step_count == 7 and list(o.steps) == [7, 1, 0]
+        old = {k: x for k, x in o.state_dict().items() if k != "steps"}
+        o.load_state_dict(old)
+        assert list(o.steps) == [7, 7, 7]
