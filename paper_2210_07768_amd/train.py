@@ -224,10 +224,19 @@ class AdamW:
                 **{k: getattr(self, k) for k in ("m", "v", "m_scale", "v_scale")}}
 
     def load_state_dict(self, state: dict):
-        if state["bits"] != self.bits or len(state["m"]) != len(self.m):
+        if state["bits"] != self.bits:
             _bad("the states are of another kind")
-        self.step_count, self.seed = state["step"], state["seed"]
-        self.steps = list(state.get("steps", [state["step"]] * len(self.m)))   # (states saved without: all weights took all steps)
-        for k in ("m", "v", "m_scale", "v_scale"):
-            for mine, theirs in zip(getattr(self, k) or (), state[k] or ()):
+        names = ("m", "v", "m_scale", "v_scale") if self.bits == 8 else ("m", "v")
+        steps = list(state.get("steps", [state["step"]] * len(self.m)))   # (states saved without: all weights took all steps)
+        if len(steps) != len(self.m):
+            _bad("the states are of another number of weights")
+        for k in names:   # (all of them before any is copied)
+            if state.get(k) is None or len(state[k]) != len(self.m):
+                _bad(f"{k}: the states are of another kind or number of weights")
+            for mine, theirs in zip(getattr(self, k), state[k]):
+                if mine.shape != theirs.shape or mine.dtype != theirs.dtype:
+                    _bad(f"{k}: a state is {tuple(theirs.shape)}, {theirs.dtype}, and its weight's {tuple(mine.shape)}, {mine.dtype}")
+        for k in names:
+            for mine, theirs in zip(getattr(self, k), state[k]):
                 mine.copy_(theirs)
+        self.step_count, self.seed, self.steps = state["step"], state["seed"], steps

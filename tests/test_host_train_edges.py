@@ -1,7 +1,11 @@
 """The trainer's operators without a GPU: what lies beyond a launch is refused before any work."""
 import ctypes
 
+import pytest
+import torch
+
 from paper_2210_07768_amd import binding as B
+from paper_2210_07768_amd import train as T
 from test_host_train import TENSOR, AdamwArgs, _gated, _library, _slot, _why
 
 
@@ -29,3 +33,39 @@ def test_adamw_refuses_more_elements_than_a_launch_holds():
     h = AdamwArgs(0, 0, 0, 32, 1, 1e-3, 0.9, 0.999, 1e-8, 0.0, 1.0, 0)
     tensors = TENSOR.pack(4096, 4096, 4096, 4096, 0, 0, 0, 8) + TENSOR.pack(4096, 4096, 4096, 4096, 0, 0, 0, (1 << 35) - 2047)
     assert _library().fbx_adamw_step(h, tensors, 2, None) == B.E_ARG and "2^35" in _why()
+
+
+def _optimizer(sizes, bits):
+    opt = T.AdamW([torch.zeros(n) for n in sizes], bits=bits)
+    for k, x in enumerate((opt.m, opt.v, opt.m_scale or [], opt.v_scale or [])):
+        for t in x:
+            t.fill_(k + 1)
+    return opt
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_adamw_loads_only_states_of_its_weights(bits):
+    """A state that would have to be spread over a weight, cut, or taken for another kind is refused, and nothing is loaded."""
+    def change(**to):
+        return {**_optimizer([40, 33], bits).state_dict(), "step": 9, "steps": (9, 9), "seed": 4, **to}
+
+    one, short = [torch.zeros(1, dtype=t.dtype) for t in _optimizer([40, 33], bits).m], _optimizer([40], bits)
+    refused = [change(m=one), change(v=one), change(m=short.m), change(v=short.v), change(m=[t.double() for t in _optimizer([40, 33], bits).m]), change(v=None),
+               change(steps=(9,)), change(bits=40 - bits), _optimizer([33, 40], bits).state_dict()]
+    if bits == 8:
+        refused += [change(m_scale=None), change(v_scale=None, m_scale=None), change(v_scale=short.v_scale), change(m_scale=[t[:1] for t in _optimizer([40, 33], bits).m_scale])]
+    for state in refused:
+        opt, same = _optimizer([40, 33], bits), _optimizer([40, 33], bits)
+        for t in opt.m + opt.v + (opt.m_scale or []) + (opt.v_scale or []):
+            t.add_(10)
+        for t in same.m + same.v + (same.m_scale or []) + (same.v_scale or []):
+            t.add_(10)
+        with pytest.raises(B.FbxError) as e:
+            opt.load_state_dict(state)
+        assert e.value.status == B.E_ARG
+        mine, kept = opt.state_dict(), same.state_dict()
+        assert all(torch.equal(x, y) for k in ("m", "v", "m_scale", "v_scale") for x, y in zip(mine[k] or [], kept[k] or []))
+        assert (mine["step"], mine["seed"], mine["steps"]) == (0, 0, (0, 0))
+    opt = _optimizer([40, 33], bits)
+    opt.load_state_dict(change())
+    assert opt.step_count == 9 and opt.steps == [9, 9] and opt.seed == 4
