@@ -64,6 +64,12 @@ const at::Tensor& tensor(PyObject* o, const char* name) {
   if (!THPVariable_Check(o)) bad(std::string(name) + " must be a tensor");
   return THPVariable_Unpack(o);
 }
+// A tensor whose gradient a call may take part in.  A tangent (forward mode) would be lost without a word.
+const at::Tensor& input(PyObject* o, const char* name) {
+  const at::Tensor& t = tensor(o, name);
+  if (t._fw_grad(0).defined()) bad(std::string(name) + ": derivatives in forward mode are not supported");
+  return t;
+}
 fbx_dtype code(const at::Tensor& t) {
   const auto s = t.scalar_type();
   if (s == at::kFloat) return FBX_F32;
@@ -171,7 +177,7 @@ PyObject* embed(PyObject*, PyObject* args) {
   int mean;
   if (!PyArg_ParseTuple(args, "OOLIpO", &slots_o, &table_o, &n_records, &tile, &mean, &out_o)) return nullptr;
   return guarded([&] {
-    const at::Tensor& table = tensor(table_o, "table");
+    const at::Tensor& table = input(table_o, "table");
     const fbx_dtype dtype = code(table);
     const int64_t rows = table.dim() == 2 ? table.size(0) : 0, dim = table.dim() == 2 ? table.size(1) : 0;
     const uint64_t stride = matrix(table, "table");
@@ -203,7 +209,7 @@ PyObject* embed_backward(PyObject*, PyObject* args) {
   int mean;
   if (!PyArg_ParseTuple(args, "OOILpO", &dout_o, &slots_o, &tile, &rows, &mean, &out_o)) return nullptr;
   return guarded([&] {
-    at::Tensor dout = tensor(dout_o, "dout");
+    at::Tensor dout = input(dout_o, "dout");
     const fbx_dtype dtype = code(dout);
     if (dout.dim() != 3) bad("dout must have three dimensions");
     const int64_t n_records = dout.size(0), n_slots = dout.size(1), dim = dout.size(2);
@@ -228,7 +234,7 @@ struct Block {
   fbx_gated a{};
   const at::Tensor &x, &w_gate, &w_up;
 
-  Block(PyObject* x_o, PyObject* gate_o, PyObject* up_o, int act) : x(tensor(x_o, "x")), w_gate(tensor(gate_o, "w_gate")), w_up(tensor(up_o, "w_up")) {
+  Block(PyObject* x_o, PyObject* gate_o, PyObject* up_o, int act) : x(input(x_o, "x")), w_gate(input(gate_o, "w_gate")), w_up(input(up_o, "w_up")) {
     a.dtype = code(x);
     a.ld_x = matrix(x, "x");
     const int64_t hidden = w_gate.dim() == 2 ? w_gate.size(0) : 0;
@@ -272,7 +278,7 @@ PyObject* gated_backward(PyObject*, PyObject* args) {
   if (!PyArg_ParseTuple(args, "OOOOipp", &dh_o, &x, &gate, &up, &act, &need_dx, &need_dw)) return nullptr;
   return guarded([&]() -> PyObject* {
     const Block b(x, gate, up, act);
-    const at::Tensor& dh = tensor(dh_o, "dh");
+    const at::Tensor& dh = input(dh_o, "dh");
     const uint64_t ld_dh = matrix(dh, "dh", &b.x, b.a.records, b.a.hidden), k = b.a.inputs;
     on_gpu(b.x);
     const c10::DeviceGuard guard(b.x.device());

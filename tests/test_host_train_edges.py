@@ -69,3 +69,21 @@ def test_adamw_loads_only_states_of_its_weights(bits):
     opt = _optimizer([40, 33], bits)
     opt.load_state_dict(change())
     assert opt.step_count == 9 and opt.steps == [9, 9] and opt.seed == 4
+
+
+def test_forward_mode_is_refused():
+    """A tangent that the operators cannot carry on is no reason to return a result without one."""
+    from torch.autograd import forward_ad
+
+    x, w, s = torch.zeros(4, 6), torch.zeros(5, 6), [T.Signs(torch.zeros(4, dtype=torch.int64))]
+    with forward_ad.dual_level():
+        dual = lambda t: forward_ad.make_dual(t, torch.ones_like(t))  # noqa: E731
+        for call in (lambda: T.embed(s, dual(x), 4), lambda: T.embed_backward(dual(x.view(4, 1, 6)), s, 10), lambda: T.gated(dual(x), w, w), lambda: T.gated(x, dual(w), w),
+                     lambda: T.gated(x, w, dual(w)), lambda: T.gated_backward(dual(torch.zeros(4, 5)), x, w, w), lambda: T.gated_backward(torch.zeros(4, 5), dual(x), w, w)):
+            with pytest.raises(B.FbxError) as e:
+                call()
+            assert e.value.status == B.E_ARG and "forward mode" in str(e.value)
+        for call in (lambda: T.embed(s, dual(x.clone().requires_grad_()), 4), lambda: T.gated(x, dual(w.clone().requires_grad_()), w)):
+            with pytest.raises(RuntimeError):   # (torch's own error, or the operator's)
+                call()
+    assert "GPU" in str(pytest.raises(B.FbxError, T.gated, x, w, w).value)
