@@ -5,6 +5,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/GradMode.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <string>
@@ -103,6 +104,17 @@ uint64_t matrix(const at::Tensor& t, const char* name, const at::Tensor* like = 
   return t.stride(0);
 }
 
+// A tensor given for a result, like torch's own `out`: it has no history of its own.
+const at::Tensor& result(PyObject* o) {
+  const at::Tensor& t = tensor(o, "out");
+  if (t.requires_grad() && c10::GradMode::is_enabled()) bad("out cannot take part in autograd");
+  return t;
+}
+// Autograd then knows that it changed.
+void changed(const at::Tensor& t) {
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 at::Tensor scratch(uint64_t bytes, const at::Tensor& like) {
   return bytes ? at::empty({static_cast<int64_t>(bytes)}, like.options().dtype(at::kByte).memory_format(c10::nullopt)) : at::Tensor();
 }
@@ -189,7 +201,7 @@ PyObject* embed(PyObject*, PyObject* args) {
     if (out_o == Py_None) {
       out = at::empty({n_records, slots.n, dim}, table.options());
     } else {
-      out = tensor(out_o, "out");
+      out = result(out_o);
       if (out.dim() != 3 || out.size(0) != n_records || out.size(1) != slots.n || out.size(2) != dim || out.scalar_type() != table.scalar_type() || out.device() != table.device())
         bad("out must be n_records x slots x dim with the table's type and device");
       if ((dim > 1 && out.stride(2) != 1) || (slots.n > 1 && out.stride(1) != dim)) bad("out: a record's rows must be adjacent");
@@ -197,6 +209,7 @@ PyObject* embed(PyObject*, PyObject* args) {
     const uint64_t record_stride = n_records > 1 ? out.stride(0) : slots.n * dim;
     check(g.embed_forward(slots.views, slots.n, n_records, tile, table.data_ptr(), rows, static_cast<uint32_t>(dim), stride, dtype, mean, out.data_ptr(), record_stride,
                           stream_of(table)));
+    if (out_o != Py_None) changed(out);
     return wrap(std::move(out));
   });
 }
@@ -219,13 +232,14 @@ PyObject* embed_backward(PyObject*, PyObject* args) {
     on_gpu(dout);
     const c10::DeviceGuard guard(dout.device());
     if ((dim > 1 && dout.stride(2) != 1) || (n_slots > 1 && dout.stride(1) != dim) || (n_records > 1 && dout.stride(0) < n_slots * dim)) dout = dout.contiguous();
-    at::Tensor out = out_o == Py_None ? at::empty({rows, dim}, dout.options()) : tensor(out_o, "out");
+    at::Tensor out = out_o == Py_None ? at::empty({rows, dim}, dout.options()) : result(out_o);
     const uint64_t stride = matrix(out, "out", &dout, rows, dim);
     uint64_t need = 0;
     check(g.embed_backward_scratch(slots.views, slots.n, n_records, rows, static_cast<uint32_t>(dim), mean, &need));
     const at::Tensor s = scratch(need, dout);
     check(g.embed_backward(slots.views, slots.n, n_records, tile, dout.data_ptr(), n_records > 1 ? dout.stride(0) : n_slots * dim, rows, static_cast<uint32_t>(dim), stride,
                            dtype, mean, out.data_ptr(), pointer(s), need, stream_of(dout)));
+    if (out_o != Py_None) changed(out);
     return wrap(std::move(out));
   });
 }
@@ -258,7 +272,7 @@ PyObject* gated(PyObject*, PyObject* args) {
   if (!PyArg_ParseTuple(args, "OOOiO", &x, &gate, &up, &act, &out_o)) return nullptr;
   return guarded([&] {
     const Block b(x, gate, up, act);
-    if (out_o != Py_None) matrix(tensor(out_o, "out"), "out", &b.x, b.a.records, b.a.hidden);
+    if (out_o != Py_None) matrix(result(out_o), "out", &b.x, b.a.records, b.a.hidden);
     on_gpu(b.x);
     const c10::DeviceGuard guard(b.x.device());
     at::Tensor out = out_o == Py_None ? at::empty({static_cast<int64_t>(b.a.records), b.a.hidden}, b.x.options()) : tensor(out_o, "out");
@@ -267,6 +281,7 @@ PyObject* gated(PyObject*, PyObject* args) {
     check(g.gated_scratch(&b.a, 0, &need));
     const at::Tensor s = scratch(need, b.x);
     check(g.gated_forward(&b.a, out.data_ptr(), ld, pointer(s), need, stream_of(b.x)));
+    if (out_o != Py_None) changed(out);
     return wrap(std::move(out));
   });
 }
@@ -375,10 +390,9 @@ PyObject* adamw(PyObject*, PyObject* args) {
     if (check_only) Py_RETURN_NONE;
     const c10::DeviceGuard guard(where);
     check(g.adamw_step(&h, all.data(), static_cast<uint32_t>(n), stream_of(p[0])));
-    for (Py_ssize_t i = 0; i < n; ++i) {  // (autograd then knows that they changed)
+    for (Py_ssize_t i = 0; i < n; ++i)
       for (const List* l : {&p, &m, &v, &m_scale, &v_scale, &copy})
-        if (l->seq && !(*l)[i].is_inference()) (*l)[i].unsafeGetTensorImpl()->bump_version();
-    }
+        if (l->seq) changed((*l)[i]);
     Py_RETURN_NONE;
   });
 }

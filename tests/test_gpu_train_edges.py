@@ -188,3 +188,24 @@ def test_adamw_class_counts_each_weights_own_steps(bits):
         old = {k: x for k, x in o.state_dict().items() if k != "steps"}
         o.load_state_dict(old)
         assert list(o.steps) == [7, 7, 7]
+
+
+# ------------------------------------------------------------------ what autograd knows
+def test_results_written_into_a_tensor_are_noted():
+    """A tensor that autograd saved and that then takes a result is found changed; one with a history of its own is refused."""
+    x, w = torch.randn(8, 6, device="cuda"), torch.randn(5, 6, device="cuda")
+    signs, table = [T.Signs(torch.arange(8, device="cuda"))], torch.randn(20, 3, device="cuda")
+    for shape, call in (((8, 5), lambda out: T.gated(x, w, w, out=out)), ((8, 1, 3), lambda out: T.embed(signs, table, 8, out=out)),
+                        ((20, 3), lambda out: T.embed_backward(torch.ones(8, 1, 3, device="cuda"), signs, 20, out=out))):
+        room = torch.ones(shape, device="cuda")
+        factor = torch.ones(shape, device="cuda", requires_grad=True)
+        product = (factor * room).sum()
+        assert call(room).data_ptr() == room.data_ptr()
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            product.backward()
+        with pytest.raises(B.FbxError):
+            call(factor)
+        with pytest.raises(B.FbxError):
+            call(factor * 2)
+        with torch.no_grad():
+            assert torch.equal(call(factor), room)
