@@ -270,6 +270,7 @@ class Plan:
     def extract_raw(self, raw_ptr: int, raw_len: int, off_ptr: int, n_records: int, stream: int = 0) -> Result:
         res = Result()
         st = lib().fbx_extract(self._h, raw_ptr, raw_len, off_ptr, n_records, stream, ctypes.byref(res))
+        _native.wrote(self._ws)
         if st != OK:
             err = FbxError(st, lib().fbx_last_error(self._h).decode())
             err.required_bytes = res.arena_high_water if st == E_NOMEM else 0
@@ -284,6 +285,8 @@ class Plan:
             stream = _current_stream()
         (st, n_records, n_values, malformed, high_water, n_layers, tile_launches, arrival, note,
          table) = _native.extract(self._h.value or 0, d_raw, d_rec_off, stream, out_buffer)
+        home = self._ws if out_buffer is None else out_buffer
+        _native.wrote(home)
         if st != OK:
             err = FbxError(st, note)
             err.required_bytes = high_water if st == E_NOMEM else 0
@@ -293,7 +296,6 @@ class Plan:
         out.arena_high_water, out.n_layers, out.tile_launches, out.arrival_tile_records = high_water, n_layers, tile_launches, arrival
         out.note = note
         # (the library's slot table is overwritten by the next call: these are copies)
-        home = self._ws if out_buffer is None else out_buffer
         out._table = (table, home, home.data_ptr(), n_records + 1)
         return out
 

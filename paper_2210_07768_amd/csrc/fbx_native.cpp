@@ -227,6 +227,13 @@ PyObject* extract(PyObject*, PyObject* args) {
                        st == FBX_OK ? static_cast<Py_ssize_t>(r.n_slots * sizeof(fbx_slot_view)) : static_cast<Py_ssize_t>(0));
 }
 
+// wrote(buffer): the library wrote to a tensor's memory, which torch does not see; what was saved of it, or of a view, can be
+// found changed from then on.  (None, and arrays that are not torch's: nothing to note.)
+PyObject* wrote(PyObject*, PyObject* o) {
+  if (THPVariable_Check(o) && !THPVariable_Unpack(o).is_inference()) THPVariable_Unpack(o).unsafeGetTensorImpl()->bump_version();
+  Py_RETURN_NONE;
+}
+
 // bind(address of fbx_extract, of fbx_extract_static, of fbx_last_error): the library itself is loaded by the binding
 PyObject* bind(PyObject*, PyObject* args) {
   unsigned long long a, b, c;
@@ -240,6 +247,7 @@ PyObject* bind(PyObject*, PyObject* args) {
 PyMethodDef methods[] = {{"bind", bind, METH_VARARGS, nullptr},
                          {"extract", extract, METH_VARARGS, nullptr},
                          {"slots", slots, METH_VARARGS, nullptr},
+                         {"wrote", wrote, METH_O, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

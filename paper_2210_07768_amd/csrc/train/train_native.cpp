@@ -124,6 +124,20 @@ PyObject* wrap(at::Tensor t) {
   return THPVariable_Wrap(std::move(t));
 }
 
+struct Held {
+  PyObject* o;
+  ~Held() { Py_XDECREF(o); }
+};
+// A slot's k-th part (a new reference): an attribute, or an entry of a tuple.
+PyObject* part_of(PyObject* slot, int k) {
+  PyObject* const names[4] = {g_values, g_offsets, g_arity, g_ends};
+  const bool tuple = PyTuple_Check(slot) && PyTuple_GET_SIZE(slot) == 4;
+  PyObject* o = tuple ? PyTuple_GET_ITEM(slot, k) : PyObject_GetAttr(slot, names[k]);
+  if (!o) throw PythonError{};
+  if (tuple) Py_INCREF(o);
+  return o;
+}
+
 // The slots of a call: the library's own table as bytes, or a sequence of objects with values, offsets, fixed_arity and
 // tile_ends (a tuple has them in this order).
 struct Slots {
@@ -139,21 +153,11 @@ struct Slots {
     }
     PyObject* seq = PySequence_Fast(o, "slots must be an ExtractResult or a sequence");
     if (!seq) throw PythonError{};
-    struct Held {
-      PyObject* o;
-      ~Held() { Py_XDECREF(o); }
-    } held{seq};
+    const Held held{seq};
     own.resize(PySequence_Fast_GET_SIZE(seq));
     for (size_t i = 0; i < own.size(); ++i) {
       PyObject* s = PySequence_Fast_GET_ITEM(seq, i);
-      const bool tuple = PyTuple_Check(s) && PyTuple_GET_SIZE(s) == 4;
-      Held part[4];
-      PyObject* names[4] = {g_values, g_offsets, g_arity, g_ends};
-      for (int k = 0; k < 4; ++k) {
-        part[k].o = tuple ? PyTuple_GET_ITEM(s, k) : PyObject_GetAttr(s, names[k]);
-        if (!part[k].o) throw PythonError{};
-        if (tuple) Py_INCREF(part[k].o);
-      }
+      const Held part[4] = {{part_of(s, 0)}, {part_of(s, 1)}, {part_of(s, 2)}, {part_of(s, 3)}};
       if (part[3].o != Py_None) bad("slots in arrival order are taken as a whole ExtractResult");
       fbx_slot_view& v = own[i] = fbx_slot_view{};
       const at::Tensor& values = whole(part[0].o, device, "a slot's values must be contiguous 64-bit integers on the table's device");
@@ -180,6 +184,26 @@ struct Slots {
     return t;
   }
 };
+
+// versions(tensor, or a sequence of slots): grows whenever torch, or a call of this library's binding, has written to what was given.
+PyObject* versions(PyObject*, PyObject* o) {
+  return guarded([&]() -> PyObject* {
+    auto version = [](PyObject* t) -> unsigned long long {
+      if (!THPVariable_Check(t) || THPVariable_Unpack(t).is_inference()) return 0;
+      return THPVariable_Unpack(t).unsafeGetTensorImpl()->version_counter().current_version();
+    };
+    if (THPVariable_Check(o)) return PyLong_FromUnsignedLongLong(version(o));
+    const Held seq{PySequence_Fast(o, "slots must be an ExtractResult or a sequence")};
+    if (!seq.o) throw PythonError{};
+    unsigned long long sum = 0;
+    for (Py_ssize_t i = 0; i < PySequence_Fast_GET_SIZE(seq.o); ++i)
+      for (int k = 0; k < 2; ++k) {
+        const Held array{part_of(PySequence_Fast_GET_ITEM(seq.o, i), k)};
+        sum += version(array.o);
+      }
+    return PyLong_FromUnsignedLongLong(sum);
+  });
+}
 
 // embed(slots, table, n_records, tile, mean, out)
 PyObject* embed(PyObject*, PyObject* args) {
@@ -415,6 +439,7 @@ PyObject* bind(PyObject*, PyObject* args) {
 
 PyMethodDef methods[] = {{"bind", bind, METH_VARARGS, nullptr},
                          {"embed", embed, METH_VARARGS, nullptr},
+                         {"versions", versions, METH_O, nullptr},
                          {"embed_backward", embed_backward, METH_VARARGS, nullptr},
                          {"gated", gated, METH_VARARGS, nullptr},
                          {"gated_backward", gated_backward, METH_VARARGS, nullptr},

@@ -83,7 +83,8 @@ def embed(slots, table, n_records: Optional[int] = None, mean: bool = False, out
     n_records x slots x dim, zeros where a record has no signs.
 
     slots: an ``ExtractResult``, or a sequence of its slots or of ``Signs`` (with n_records).  Under autograd the signs are
-    read again by the backward pass: extract the next batch behind it, or into another workspace."""
+    read again by the backward pass: extract the next batch behind it, or into another workspace.  It is refused where torch
+    or a ``Plan``'s call has written to them, or to the workspace they lie in, since."""
     if table.requires_grad and torch.is_grad_enabled():
         if out is not None:
             _bad("out cannot take part in autograd")
@@ -122,15 +123,25 @@ def gated_backward(dh, x, w_gate, w_up, act: str = "silu", need_dx: bool = True,
     return _load().gated_backward(dh, x, w_gate, w_up, _act(act), need_dx, need_dw)
 
 
+def _versions(slots) -> int:
+    if isinstance(slots, ExtractResult):
+        return 0 if slots._table is None else _load().versions(slots._table[1])
+    return _load().versions(slots)
+
+
 class _Embed(torch.autograd.Function):
     @staticmethod
     def forward(ctx, table, slots, n_records, mean):
-        ctx.slots, ctx.rows, ctx.mean = slots, table.shape[0], mean
-        return _embed_forward(slots, table, n_records, mean, None)
+        ctx.slots, ctx.rows, ctx.mean = slots if isinstance(slots, ExtractResult) else tuple(slots), table.shape[0], mean
+        pooled = _embed_forward(slots, table, n_records, mean, None)
+        ctx.versions = _versions(ctx.slots)
+        return pooled
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dout):
+        if _versions(ctx.slots) != ctx.versions:
+            _bad("the signs were written to after embed had read them: their gradient would be another batch's")
         return embed_backward(dout, ctx.slots, ctx.rows, ctx.mean), None, None, None
 
 

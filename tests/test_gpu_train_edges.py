@@ -209,3 +209,49 @@ def test_results_written_into_a_tensor_are_noted():
             call(factor * 2)
         with torch.no_grad():
             assert torch.equal(call(factor), room)
+
+
+def test_signs_that_changed_before_their_gradient_are_refused():
+    """The backward pass reads the signs again: after another extraction into their workspace, or any other write to them, it
+    would give another batch's gradient."""
+    from paper_2210_07768_amd import workloads as W
+
+    w = W.get(1, 600)
+    batches = [[torch.from_numpy(np.asarray(t).copy()).cuda() for t in (raw, off.astype(np.int64))] for raw, off in (w.generate(k * 600, 600) for k in range(2))]
+    plan = B.Plan(w.spec)
+    table = torch.randn(1000, 4, device="cuda", requires_grad=True)
+    want = None
+    for static in (False, True):
+        into = lambda: torch.empty(1 << 24, dtype=torch.uint8, device="cuda") if static else None  # noqa: E731
+        if not static:
+            _, ws = B.extract_with_retry(plan, *batches[0])
+        for again in (False, True):
+            room = into()
+            result = plan.extract(*batches[0], out_buffer=room)
+            pooled = [T.embed(result, table), T.embed([result.slots[i] for i in result.slot_ids], table, 600)]
+            if again:
+                plan.extract(*batches[1], out_buffer=room)
+                for p in pooled:
+                    with pytest.raises(B.FbxError, match="written to"):
+                        p.sum().backward()
+                continue
+            if static:
+                plan.extract(*batches[1], out_buffer=into())   # (elsewhere)
+            for p in pooled:
+                table.grad = None
+                p.sum().backward()
+                want = table.grad if want is None else want
+                assert torch.equal(table.grad, want)
+    plan.close()
+    values, offsets = torch.arange(12, device="cuda"), torch.tensor([0, 3, 3, 9], device="cuda")
+    for write in (lambda: values.add_(1), lambda: offsets[1:2].zero_()):
+        pooled = T.embed([T.Signs(values[:3]), T.Signs(values, offsets)], table, 3)
+        write()
+        with pytest.raises(B.FbxError, match="written to"):
+            pooled.sum().backward()
+    slots = [T.Signs(values[:3])]
+    pooled = T.embed(slots, table, 3)
+    slots[0] = T.Signs(values[3:6])   # (the list is the caller's)
+    table.grad = None
+    pooled.sum().backward()
+    assert torch.equal(table.grad, T.embed_backward(torch.ones(3, 1, 4, device="cuda"), [T.Signs(values[:3])], 1000))
