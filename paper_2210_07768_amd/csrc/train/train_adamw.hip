@@ -172,8 +172,8 @@ __global__ __launch_bounds__(256) void k_adamw(AdamwArgs) {
 template <class P, class G, class C, bool kCopy>
 void launch(const AdamwArgs& a, bool eight, hipStream_t stream) {
   const dim3 grid(a.first_block[a.n]);
-  if (eight) hipLaunchKernelGGL((k_adamw<P, G, C, true, kCopy>), grid, dim3(256), 0, stream, a);
-  else hipLaunchKernelGGL((k_adamw<P, G, C, false, kCopy>), grid, dim3(256), 0, stream, a);
+  if (eight) launch_on(stream, k_adamw<P, G, C, true, kCopy>, grid, dim3(256), 0, a);
+  else launch_on(stream, k_adamw<P, G, C, false, kCopy>, grid, dim3(256), 0, a);
 }
 
 template <class P, class G>
@@ -219,7 +219,6 @@ extern "C" fbx_status fbx_adamw_step(const fbx_adamw* h, const fbx_adamw_tensor*
     any = true;
   }
   if (!any) return FBX_OK;
-  launching();
   for (uint32_t i = 0; copy && i < n_tensors; ++i)
     if (tensors[i].n && !tensors[i].d_copy) return refuse(FBX_E_ARG, "either all tensors have a copy or none");
   AdamwArgs a{};

@@ -5,6 +5,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "fbx_train.h"
 
 namespace fbx {
@@ -12,9 +14,15 @@ namespace train {
 
 // Notes why a call fails and returns `s`.
 fbx_status refuse(fbx_status s, const char* why);
-// Around a call's launches: forgets errors that others left; FBX_OK, or FBX_E_HIP with the text of a launch's error.
-void launching();
+// A call's launches: each by `launch_on`, which notes the thread's first that fails; then `launched` gives FBX_OK, or FBX_E_HIP
+// with the text of that one's error.  Errors that others left with the runtime stay there for them.
+void note(hipError_t e);
 fbx_status launched();
+template <class... P>
+void launch_on(hipStream_t stream, void (*kernel)(P...), dim3 grid, dim3 block, uint32_t lds, const std::enable_if_t<true, P>&... args) {
+  void* at[] = {const_cast<void*>(static_cast<const void*>(&args))...};
+  note(hipLaunchKernel((const void*)kernel, grid, block, at, lds, stream));
+}
 
 inline uint32_t size_of(fbx_dtype t) { return t == FBX_F32 ? 4u : 2u; }
 inline bool known(fbx_dtype t) { return t == FBX_F32 || t == FBX_F16 || t == FBX_BF16; }

@@ -8,6 +8,7 @@ namespace train {
 
 namespace {
 thread_local char g_error[256];
+thread_local hipError_t g_launch = hipSuccess;
 }
 
 fbx_status refuse(fbx_status s, const char* why) {
@@ -15,11 +16,16 @@ fbx_status refuse(fbx_status s, const char* why) {
   return s;
 }
 
-void launching() { (void)hipGetLastError(); }
+void note(hipError_t e) {
+  if (e != hipSuccess && g_launch == hipSuccess) g_launch = e;
+}
 
 fbx_status launched() {
-  const hipError_t e = hipGetLastError();
-  return e == hipSuccess ? FBX_OK : refuse(FBX_E_HIP, hipGetErrorString(e));
+  const hipError_t e = g_launch;
+  if (e == hipSuccess) return FBX_OK;
+  g_launch = hipSuccess;
+  (void)hipGetLastError();  // (it is reported here)
+  return refuse(FBX_E_HIP, hipGetErrorString(e));
 }
 
 fbx_status check_slots(const fbx_slot_view* slots, uint32_t n_slots, uint64_t n_records, uint32_t tile, uint64_t* total) {
@@ -132,7 +138,7 @@ __global__ __launch_bounds__(256) void k_embed(EmbedArgs) {
 template <class T, int N>
 void launch(const EmbedArgs& a, hipStream_t stream) {
   const uint64_t blocks = ceil_div(a.n_records - a.first_record, kTileRecords), most = most_blocks(256);
-  hipLaunchKernelGGL((k_embed<T, N>), dim3((uint32_t)(blocks < most ? blocks : most), (uint32_t)ceil_div(a.n_slots, a.each)), dim3(256), 0, stream, a);
+  launch_on(stream, k_embed<T, N>, dim3((uint32_t)(blocks < most ? blocks : most), (uint32_t)ceil_div(a.n_slots, a.each)), dim3(256), 0, a);
 }
 
 template <class T>
@@ -173,7 +179,6 @@ extern "C" fbx_status fbx_embed_forward(const fbx_slot_view* slots, uint32_t n_s
   const uint64_t all = (uintptr_t)d_table | (uintptr_t)d_out | dim * e | table_stride * e | record_stride * e;
   uint32_t n = 16u / e;
   while (n > 1u && all % (n * e)) n /= 2u;
-  launching();
   EmbedArgs a{};
   a.table = d_table;
   a.n_records = n_records;

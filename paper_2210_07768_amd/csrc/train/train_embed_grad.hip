@@ -268,9 +268,9 @@ __global__ __launch_bounds__(256) void k_rank_pairs(const uint32_t* keys, const 
 template <uint32_t kBits, uint32_t kItems>
 void sort_pass(uint32_t* const (&keys)[2], uint32_t* const (&from)[2], int side, uint32_t n, uint32_t shift, uint32_t n_tiles, uint32_t* counts, uint32_t* totals,
                hipStream_t stream) {
-  hipLaunchKernelGGL((k_digit_counts<kBits, kItems>), dim3(n_tiles), dim3(256), 0, stream, keys[side], n, shift, n_tiles, counts);
-  hipLaunchKernelGGL(k_digit_sums, dim3(1u << kBits), dim3(256), 0, stream, counts, n_tiles, totals);
-  hipLaunchKernelGGL((k_move_pairs<kBits, kItems>), dim3(n_tiles), dim3(256), 0, stream, keys[side], from[side], n, shift, n_tiles, counts, totals, keys[side ^ 1], from[side ^ 1]);
+  launch_on(stream, k_digit_counts<kBits, kItems>, dim3(n_tiles), dim3(256), 0, keys[side], n, shift, n_tiles, counts);
+  launch_on(stream, k_digit_sums, dim3(1u << kBits), dim3(256), 0, counts, n_tiles, totals);
+  launch_on(stream, k_move_pairs<kBits, kItems>, dim3(n_tiles), dim3(256), 0, keys[side], from[side], n, shift, n_tiles, counts, totals, keys[side ^ 1], from[side ^ 1]);
 }
 
 // Rows of the table up to the one of sorted term at - 1: the first row that belongs to what begins at term `at`.
@@ -533,11 +533,11 @@ void sum_rows(SumArgs a, const Layout& l, char* scratch, uint64_t rows, hipStrea
   if (a.n > kFewPairs && rows <= 2ull * a.n) {
     a.near = 32u * groups * kRun;
     // (each of its workgroups looks at the ends of all 16 stretches)
-    hipLaunchKernelGGL((k_clear_far<T, N>), dim3(64), dim3(1024), 0, stream, a, groups * kRun);
+    launch_on(stream, k_clear_far<T, N>, dim3(64), dim3(1024), 0, a, groups * kRun);
   } else {
     const uint64_t packs = rows * (a.dim / N);
     const uint32_t clear = (uint32_t)(ceil_div(packs, 256) < 16384 ? ceil_div(packs, 256) : 16384);
-    hipLaunchKernelGGL((k_clear_rows<T, N>), dim3(clear), dim3(256), 0, stream, a.dtable, rows, a.dim, a.table_stride);
+    launch_on(stream, k_clear_rows<T, N>, dim3(clear), dim3(256), 0, a.dtable, rows, a.dim, a.table_stride);
   }
   int side = 0;
   for (bool first = true; a.n; first = false) {
@@ -549,8 +549,8 @@ void sum_rows(SumArgs a, const Layout& l, char* scratch, uint64_t rows, hipStrea
     for (uint64_t b = 0; b < blocks; b += most_blocks(256)) {
       const dim3 grid((uint32_t)(blocks - b < most_blocks(256) ? blocks - b : most_blocks(256)), (uint32_t)ceil_div(a.dim, columns));
       a.first_block = (uint32_t)b;
-      if (first) hipLaunchKernelGGL((k_sum_rows<T, N, true>), grid, dim3(256), lds, stream, a);
-      else hipLaunchKernelGGL((k_sum_rows<T, N, false>), grid, dim3(256), lds, stream, a);
+      if (first) launch_on(stream, k_sum_rows<T, N, true>, grid, dim3(256), lds, a);
+      else launch_on(stream, k_sum_rows<T, N, false>, grid, dim3(256), lds, a);
     }
     if (last) break;
     a.keys = a.part_keys;
@@ -612,7 +612,6 @@ extern "C" fbx_status fbx_embed_backward(const fbx_slot_view* slots, uint32_t n_
   if (((uintptr_t)d_dtable | (uintptr_t)d_dout) % e) return refuse(FBX_E_ARG, "d_dtable and d_dout must be aligned to their elements");
   if (l.bytes && (!d_scratch || (uintptr_t)d_scratch % 256u)) return refuse(FBX_E_ARG, "d_scratch is NULL or not 256-byte aligned");
   if (scratch_bytes < l.bytes) return refuse(FBX_E_NOMEM, "scratch too small: fbx_embed_backward_scratch gives its size");
-  launching();
   const hipStream_t stream = (hipStream_t)hip_stream;
   char* scratch = (char*)d_scratch;
   uint32_t* keys[2] = {(uint32_t*)(scratch + l.keys[0]), (uint32_t*)(scratch + l.keys[1])};
@@ -643,10 +642,10 @@ extern "C" fbx_status fbx_embed_backward(const fbx_slot_view* slots, uint32_t n_
         p.slots[i] = slot_ref(slots[s0 + i], base);
         base += (uint32_t)slots[s0 + i].n_values;
       }
-      hipLaunchKernelGGL(k_pairs, dim3((uint32_t)(blocks > more ? blocks : more), p.n_slots), dim3(256), 0, stream, p);
+      launch_on(stream, k_pairs, dim3((uint32_t)(blocks > more ? blocks : more), p.n_slots), dim3(256), 0, p);
     }
     if (l.n <= kRankPairs) {
-      hipLaunchKernelGGL(k_rank_pairs, dim3((uint32_t)ceil_div(l.n, 4 * kRankEach)), dim3(256), 0, stream, keys[0], from[0], l.n, keys[1], from[1]);
+      launch_on(stream, k_rank_pairs, dim3((uint32_t)ceil_div(l.n, 4 * kRankEach)), dim3(256), 0, keys[0], from[0], l.n, keys[1], from[1]);
       side = 1;
     }
     for (uint32_t pass = 0; l.n > kRankPairs && pass < l.passes; ++pass, side ^= 1) {

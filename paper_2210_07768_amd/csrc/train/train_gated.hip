@@ -597,8 +597,8 @@ Cut cut(uint64_t rows, uint64_t columns, uint64_t steps, bool single) {
 
 template <class T, Form kForm, int BM, int BN, int WM, int WN, int kStages>
 void launch(const MmArgs& p, uint32_t shared, hipStream_t stream) {
-  hipLaunchKernelGGL((k_mm<T, kForm, BM, BN, WM, WN, kStages>), dim3(p.whole + shared * p.shares), dim3(WM * WN * 64), 0, stream, p);
-  if (shared) hipLaunchKernelGGL((k_join<T, kForm, BM, BN, WM, WN>), dim3(shared, BM / WM / 16), dim3(WM * WN * 64), 0, stream, p);
+  launch_on(stream, k_mm<T, kForm, BM, BN, WM, WN, kStages>, dim3(p.whole + shared * p.shares), dim3(WM * WN * 64), 0, p);
+  if (shared) launch_on(stream, k_join<T, kForm, BM, BN, WM, WN>, dim3(shared, BM / WM / 16), dim3(WM * WN * 64), 0, p);
 }
 template <class T, Form kForm>
 void launch_by_size(const MmArgs& p, const Cut& c, hipStream_t stream) {
@@ -622,8 +622,8 @@ void launch_by_type(MmArgs& p, const Cut& c, fbx_dtype t, char* parts, hipStream
 template <class T>
 void launch_few(const MmArgs& p, bool whole, hipStream_t stream) {
   const dim3 grid((uint32_t)ceil_div(p.columns, 16));
-  if (whole) hipLaunchKernelGGL((k_few<T, true>), grid, dim3(kFewWaves * 64), 0, stream, p);
-  else hipLaunchKernelGGL((k_few<T, false>), grid, dim3(kFewWaves * 64), 0, stream, p);
+  if (whole) launch_on(stream, k_few<T, true>, grid, dim3(kFewWaves * 64), 0, p);
+  else launch_on(stream, k_few<T, false>, grid, dim3(kFewWaves * 64), 0, p);
 }
 void launch_few_by_type(const MmArgs& p, fbx_dtype t, bool whole, hipStream_t stream) {
   if (t == FBX_F32) launch_few<float>(p, whole, stream);
@@ -723,8 +723,8 @@ void operands(const fbx_gated* g, const Shape& s, char* scratch, const void* (&f
   while (a.lanes_log2 < 8u && (s.lanes << a.lanes_log2) < s.wide) ++a.lanes_log2;
   const uint64_t blocks = ceil_div(most, 256u >> a.lanes_log2);
   const dim3 grid((uint32_t)(blocks < 65536 ? blocks : 65536), n);
-  if (s.size == 4u) hipLaunchKernelGGL(k_pad_rows<float>, grid, dim3(256), 0, stream, a);
-  else hipLaunchKernelGGL(k_pad_rows<_Float16>, grid, dim3(256), 0, stream, a);
+  if (s.size == 4u) launch_on(stream, k_pad_rows<float>, grid, dim3(256), 0, a);
+  else launch_on(stream, k_pad_rows<_Float16>, grid, dim3(256), 0, a);
 }
 
 bool four_at_a_time(const void* p, uint64_t ld, uint32_t size) { return (uintptr_t)p % (4 * size) == 0 && ld % 4 == 0; }
@@ -761,7 +761,6 @@ extern "C" fbx_status fbx_gated_forward(const fbx_gated* g, void* d_h, uint64_t 
   const hipStream_t stream = (hipStream_t)hip_stream;
   const Shape s = shape_of(g, false);
   if (!s.fits()) return refuse(FBX_E_ARG, "records x hidden is too large for one call");
-  launching();
   const void* from[3];
   uint64_t ld[3];
   operands(g, s, (char*)d_scratch, from, ld, stream);
@@ -805,7 +804,6 @@ extern "C" fbx_status fbx_gated_backward(const fbx_gated* g, const void* d_dh, u
   const Shape s = shape_of(g, true);
   if (!s.fits()) return refuse(FBX_E_ARG, "records x hidden is too large for one call");
   char* scratch = (char*)d_scratch;
-  launching();
   const void* from[3];
   uint64_t ld[3];
   operands(g, s, scratch, from, ld, stream);

@@ -255,3 +255,27 @@ def test_signs_that_changed_before_their_gradient_are_refused():
     table.grad = None
     pooled.sum().backward()
     assert torch.equal(table.grad, T.embed_backward(torch.ones(3, 1, 4, device="cuda"), [T.Signs(values[:3])], 1000))
+
+
+# ------------------------------------------------------------------ the runtime's errors
+def test_errors_that_others_left_stay_theirs():
+    """A call succeeds beside an error that something else left with the HIP runtime, and leaves it there to be found."""
+    import ctypes
+
+    path = next(line.split()[-1] for line in open("/proc/self/maps") if "libamdhip64" in line)
+    hip = ctypes.CDLL(path)
+    x, w, out = torch.randn(40, 8, device="cuda"), torch.randn(6, 8, device="cuda"), torch.zeros(40, 6, device="cuda")
+    signs, table, pooled, grad = [T.Signs(torch.arange(40, device="cuda"))], torch.randn(20, 4, device="cuda"), torch.zeros(40, 1, 4, device="cuda"), torch.zeros(20, 4, device="cuda")
+    p, m, v, ones = *(torch.zeros(9, device="cuda") for _ in range(3)), torch.ones(9, device="cuda")   # (torch looks for errors when it computes)
+    calls = (lambda: T.gated(x, w, w, out=out), lambda: T.embed(signs, table, 40, out=pooled), lambda: T.embed_backward(pooled, signs, 20, out=grad),
+             lambda: T.adamw([p], [ones], [m], [v], step=1))
+    for call in calls:
+        call()
+    for call in calls:
+        hip.hipGetLastError()
+        assert hip.hipSetDevice(12345) == hip.hipPeekAtLastError() == 101   # (no such device)
+        call()
+        assert hip.hipPeekAtLastError() == 101
+        assert hip.hipGetLastError() == 101
+    torch.cuda.synchronize()
+    assert bool((grad != 0).any()) and bool((p != 0).all())
