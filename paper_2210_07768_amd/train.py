@@ -174,6 +174,8 @@ def adamw(params: Sequence, grads: Sequence, m: Sequence, v: Sequence, m_scale: 
     too.  step counts from 1; seed: of the random rounding, the same for all steps.  keep_roots, for 8-bit states: a sqrt(v) above
     0 is never rounded to 0.  Without it a weight can be moved by lr * m / eps, thousands of times lr, where gradients of
     very unlike size share a block of 32: a training run sets it, as ``AdamW`` does."""
+    if step < 1:
+        _bad("step counts from 1")
     _load().adamw(params, grads, m, v, m_scale, v_scale, copies, step, lr, betas[0], betas[1], eps, weight_decay, grad_scale, seed & ((1 << 64) - 1), keep_roots, False)
 
 

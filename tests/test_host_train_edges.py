@@ -87,3 +87,11 @@ def test_forward_mode_is_refused():
             with pytest.raises(RuntimeError):   # (torch's own error, or the operator's)
                 call()
     assert "GPU" in str(pytest.raises(B.FbxError, T.gated, x, w, w).value)
+
+
+@pytest.mark.parametrize("step", [0, -1, -(1 << 63)])
+def test_adamw_steps_count_from_one(step):
+    x = torch.zeros(4, 6)
+    with pytest.raises(B.FbxError) as e:
+        T.adamw([x], [x], [x], [x], step=step)
+    assert e.value.status == B.E_ARG and "step" in str(e.value)
