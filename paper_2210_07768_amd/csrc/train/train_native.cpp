@@ -248,7 +248,6 @@ PyObject* embed_backward(PyObject*, PyObject* args) {
   return guarded([&] {
     at::Tensor dout = input(dout_o, "dout");
     const fbx_dtype dtype = code(dout);
-    if (dout.dim() != 3) bad("dout must have three dimensions");
     const int64_t n_records = dout.size(0), n_slots = dout.size(1), dim = dout.size(2);
     const Slots slots(slots_o, n_records, dout.device());
     if (slots.n != n_slots) bad("dout must have as many slots as there are");

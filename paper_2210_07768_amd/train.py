@@ -57,6 +57,12 @@ def _bad(why: str):
     raise FbxError(_b.E_ARG, why)
 
 
+def _tensors(**given):
+    for name, t in given.items():
+        if not isinstance(t, torch.Tensor):
+            _bad(f"{name} must be a tensor")
+
+
 # ------------------------------------------------------------------ rows of a table, pooled
 def _table_of(slots, device, n_records: Optional[int]):
     """(slots as the native part takes them, records, records of a tile in arrival order)."""
@@ -85,6 +91,7 @@ def embed(slots, table, n_records: Optional[int] = None, mean: bool = False, out
     slots: an ``ExtractResult``, or a sequence of its slots or of ``Signs`` (with n_records).  Under autograd the signs are
     read again by the backward pass: extract the next batch behind it, or into another workspace.  It is refused where torch
     or a ``Plan``'s call has written to them, or to the workspace they lie in, since."""
+    _tensors(table=table)
     if table.requires_grad and torch.is_grad_enabled():
         if out is not None:
             _bad("out cannot take part in autograd")
@@ -95,6 +102,9 @@ def embed(slots, table, n_records: Optional[int] = None, mean: bool = False, out
 def embed_backward(dout, slots, rows: int, mean: bool = False, out=None):
     """The gradient of ``embed`` with respect to its table: rows x dim, of dout's type; dout: n_records x slots x dim.
     All rows are written.  The same inputs give the same bits."""
+    _tensors(dout=dout)
+    if dout.dim() != 3:
+        _bad("dout must have three dimensions")
     slots, _, tile = _table_of(slots, dout.device, dout.shape[0])
     return _load().embed_backward(dout, slots, tile, rows, mean, out)
 
@@ -110,6 +120,7 @@ def _act(act: str) -> int:
 def gated(x, w_gate, w_up, act: str = "silu", out=None):
     """act(x w_gate^T) * (x w_up^T) in one kernel: x records x inputs, weights hidden x inputs, result records x hidden.
     act: silu, gelu, relu or sigmoid."""
+    _tensors(x=x, w_gate=w_gate, w_up=w_up)
     if (x.requires_grad or w_gate.requires_grad or w_up.requires_grad) and torch.is_grad_enabled():
         if out is not None:
             _bad("out cannot take part in autograd")

@@ -95,3 +95,13 @@ def test_adamw_steps_count_from_one(step):
     with pytest.raises(B.FbxError) as e:
         T.adamw([x], [x], [x], [x], step=step)
     assert e.value.status == B.E_ARG and "step" in str(e.value)
+
+
+def test_what_is_no_tensor_is_refused():
+    x, w, s = torch.zeros(4, 6), torch.zeros(5, 6), [T.Signs(torch.zeros(4, dtype=torch.int64))]
+    for call in (lambda: T.embed(s, None, 4), lambda: T.embed(s, x.numpy(), 4), lambda: T.embed_backward(None, s, 4), lambda: T.embed_backward(torch.tensor(1.0), s, 4),
+                 lambda: T.embed_backward(torch.zeros(4), s, 4), lambda: T.gated(None, w, w), lambda: T.gated(x, [1.0], w), lambda: T.gated(x, w, 3),
+                 lambda: T.gated_backward(None, x, w, w), lambda: T.gated_backward(torch.zeros(4, 5), x, w, "w"), lambda: T.adamw([x], [None], [x], [x], step=1)):
+        with pytest.raises(B.FbxError) as e:
+            call()
+        assert e.value.status == B.E_ARG
