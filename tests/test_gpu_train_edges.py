@@ -279,3 +279,32 @@ def test_errors_that_others_left_stay_theirs():
         assert hip.hipGetLastError() == 101
     torch.cuda.synchronize()
     assert bool((grad != 0).any()) and bool((p != 0).all())
+
+
+# ------------------------------------------------------------------ the ways a large gradient goes
+@pytest.mark.parametrize("mean", [False, True])
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("dim, pad, rows, distinct", [(16, 0, 70_001, 1 << 20), (16, 0, 200_003, 3000), (5, 3, 300, 1 << 20), (16, 8, 262_144, 1 << 20), (8, 0, 540_000, 1 << 20), (300, 0, 130_003, 3000),
+                                                      (33, 7, 600_011, 1 << 20), (16, 0, 2_000_003, 1 << 20), (2, 2, 1, 1 << 20)])
+def test_gradient_of_many_terms(dim, pad, rows, distinct, dtype, mean):
+    """Some 350,000 terms: digits of eight and of nine bits, tables most of whose rows have terms and tables where few have, in
+    every type.  Lists of 0, 1, 2 or 4 signs, so that whole numbers' sums, and those of their halves and quarters, are exact in
+    32 bits (below 2^24 quarters each); what is stored is the nearest of its type."""
+    n = 90_007
+    rng = np.random.default_rng(dim + rows)
+    pool = torch.from_numpy(rng.integers(-(1 << 63), 1 << 63, size=distinct, dtype=np.int64)).cuda()
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    signs = lambda k: pool[(torch.rand(k, device="cuda", generator=g, dtype=torch.float64) ** 3 * distinct).long()]  # noqa: E731
+    lens = torch.tensor([0, 1, 2, 4], device="cuda")[torch.randint(0, 4, (2, n), device="cuda", generator=g)]
+    offsets = torch.nn.functional.pad(lens.cumsum(1), (1, 0))
+    slots = [T.Signs(signs(n)), *(T.Signs(signs(int(o[-1])), o.contiguous()) for o in offsets)]
+    assert sum(s.values.numel() for s in slots) > 1 << 18
+    dout = torch.randint(-4, 5, (n, 3, dim), device="cuda", generator=g).to(dtype)
+    room = torch.full((rows, dim + pad), 7.0, device="cuda", dtype=dtype)
+    T.embed_backward(dout, slots, rows, mean=mean, out=room[:, :dim])
+    want = torch.zeros(rows, dim, device="cuda", dtype=torch.float64)
+    for i, s in enumerate(slots):
+        owner = torch.arange(n, device="cuda") if s.offsets is None else torch.repeat_interleave(torch.arange(n, device="cuda"), lens[i - 1])
+        share = 1.0 if s.offsets is None or not mean else 1.0 / lens[i - 1][owner].double().unsqueeze(1)
+        want.index_add_(0, _rows_of(s.values, rows), dout[:, i].double()[owner] * share)
+    assert torch.equal(room[:, :dim], want.float().to(dtype)) and bool((room[:, dim:] == 7.0).all())
