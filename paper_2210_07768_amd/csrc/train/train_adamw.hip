@@ -78,7 +78,8 @@ __device__ __forceinline__ void decode(float (&to)[kEach], const uint8_t* codes,
 }
 
 // Eight codes of a block of 32, which four neighbouring lanes hold, and its scale.  random16(i): 16 random bits; least: the
-// code, 0 or 1, of what is above 0 and would be rounded to 0.
+// code, 0 or 1, of what is above 0 and would be rounded to 0 (1 for sqrt(v): rounded independently of m, it could become 0
+// beside an m that does not, and the next update be m / eps).
 template <class Random>
 __device__ __forceinline__ void encode(uint8_t* codes, uint8_t* scale, const float (&x)[kEach], uint32_t n, bool wide, uint32_t least, Random random16) {
   uint32_t top = 0u;  // (magnitudes compare as integers, NaN above infinity above the rest)
@@ -117,9 +118,9 @@ __device__ __forceinline__ void encode(uint8_t* codes, uint8_t* scale, const flo
 
 // A workgroup takes 2,048 elements of one tensor, a lane eight adjacent ones (so that four lanes hold a block of
 // 8-bit states).  P, G, C: types of weights, gradients, copies; kEight: states in 8 bits.
-// Bound by memory: 175 M weights in 32 bits with gradients and copies in 16 and states in 8 take 567 us, 16.1 bytes each at
-// 4.97 TB/s, what a copy reaches; 48 tensors of 0.53 M elements in all, in 32 bits,
-// 8 us, of which the kernel takes 6.5.
+// Bound by memory: 175 M weights in 32 bits with gradients and copies in 16 and states in 8 take 567 to 579 us, 16.1 bytes each at
+// 4.87 to 4.97 TB/s, what a copy reaches; 48 tensors of 0.53 M elements in all, in 32 bits,
+// 8 to 9.3 us, of which the kernel takes 6.5.
 template <class P, class G, class C, bool kEight, bool kCopy>
 __global__ __launch_bounds__(256) void k_adamw(AdamwArgs) {
 #pragma clang fp contract(off)

@@ -39,6 +39,9 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 //   kSlopes   the same product;  c: a row of da, then of du, each `half` elements wide (zeros beyond columns)
 //   kInputs   A = the rows kSlopes wrote, B = the weights, read along their rows;  c: dx
 //   kWeights  A = those rows and B = x, both read along their rows (depth: the records);  c, c2: dWg, dWu
+// da and du are rounded to the block's type on their way: they are operands of the next two products, and matrix instructions of
+// 32-bit operands have a ninth of the rate of those of 16 (154 of 1,370 TFLOP/s).  The gradients' relative error against 64 bits is 1.4 times that of
+// one rounding at the end: 2.9e-4 to 2.1e-4 in f16 (1,000 x 411 by 2 x 773), 2.3e-3 to 1.7e-3 in bf16 (16,384 x 2,624 by 2 x 4,096).
 enum Form { kForward, kSlopes, kInputs, kWeights };
 
 struct MmArgs {
@@ -278,10 +281,10 @@ struct Split {
 // product).  C's rows come from A; its columns from B, which is the first side of the matrix instructions, so that a lane holds
 // four adjacent columns of a row.
 // kStages: steps whose tiles are in LDS or on their way there.
-// Bound by the matrix units where the product is large: 65,536 x 2,624 by 2 x 4,096 in bf16 takes 2.25 to 2.4 ms from card to card,
-// 1.17 to 1.25 PFLOP/s; they are busy 60 % of the cycles, at a clock that the power they draw keeps at 1.8 of 2.4 GHz, and reads from
+// Bound by the matrix units where the product is large: 65,536 x 2,624 by 2 x 4,096 in bf16 takes 2.25 to 2.42 ms from card to card,
+// 1.16 to 1.25 PFLOP/s; they are busy 60 % of the cycles, at a clock that the power they draw keeps at 1.8 of 2.4 GHz, and reads from
 // LDS meet no bank conflict.  A library's product of the same two matrices, without the activation, reaches 1.37.  The three products
-// of a gradient of 16,384 records take 1.9 ms, 1.11 PFLOP/s, dh and both slopes moved in the first one's epilogue.  In 32 bits
+// of a gradient of 16,384 records take 1.9 to 2.0 ms, 1.05 to 1.11 PFLOP/s, dh and both slopes moved in the first one's epilogue.  In 32 bits
 // 4,096 x 384 by 2 x 1,024 and back is 175 us, 110 of 154 TFLOP/s.  Measured and slower: 32 x 32 x 16 instructions (8 %),
 // workgroups that stay and take tile after tile (6 %), four wavefronts of 128 x 128, which read a third less from LDS (compiled,
 // their sums are moved from register to register; with the instructions written out and loads spread among them the

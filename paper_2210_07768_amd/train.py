@@ -130,7 +130,8 @@ def gated(x, w_gate, w_up, act: str = "silu", out=None):
 
 def gated_backward(dh, x, w_gate, w_up, act: str = "silu", need_dx: bool = True, need_dw: bool = True):
     """Gradients of ``gated`` with respect to x, w_gate and w_up (None for those not needed), of their type.  The
-    projections are computed again, not kept."""
+    projections are computed again, not kept; their gradients are rounded to that type between the products (in float16 one
+    beyond its range becomes infinite: scale the loss)."""
     return _load().gated_backward(dh, x, w_gate, w_up, _act(act), need_dx, need_dw)
 
 
