@@ -264,4 +264,7 @@ class AdamW:
         for k in names:
             for mine, theirs in zip(getattr(self, k), state[k]):
                 mine.copy_(theirs)
+        if self.bits == 8:   # (states of steps without keep_roots)
+            for m, v in zip(self.m, self.v):
+                v.masked_fill_((v == 0) & ((m & 127) != 0), 1)
         self.step_count, self.seed, self.steps = state["step"], state["seed"], steps

@@ -105,3 +105,13 @@ def test_what_is_no_tensor_is_refused():
         with pytest.raises(B.FbxError) as e:
             call()
         assert e.value.status == B.E_ARG
+
+
+def test_adamw_loads_states_whose_roots_were_not_kept():
+    """A code 0 of sqrt(v) beside a code of m that is not 0, of either sign: 1 from then on; nothing else changes."""
+    saved = T.AdamW([torch.zeros(40)], bits=8).state_dict()
+    saved["m"][0][:6] = torch.tensor([0, 128, 1, 129, 5, 255], dtype=torch.uint8)
+    saved["v"][0][4:6] = torch.tensor([9, 127], dtype=torch.uint8)
+    opt = T.AdamW([torch.zeros(40)], bits=8)
+    opt.load_state_dict(saved)
+    assert torch.equal(opt.m[0], saved["m"][0]) and opt.v[0].tolist() == [0, 0, 1, 1, 9, 127] + [0] * 34
