@@ -1,0 +1,721 @@
+// Orthogonalised matrices by Newton-Schulz products, and the update step that takes them.
+//
+// A list of matrices goes through the same launches together: sizes, two for each matrix's norm and its parts of 16 bits, and
+// three products a step.  Matrices with more rows than columns are transposed when they are split and when the result
+// leaves, so that every X is m x n, m <= n.
+//
+// Numbers of 32 bits are held as two of f16, the second what the first leaves, of which matrix instructions take the first
+// (or, exact, first by first, first by second and second by first).  f16 and not bf16: three more bits at the same rate.  Why two
+// parts where products are of the first alone: an update's small singular values grow by a each step, 485 times over five, and
+// so does what rounding X leaves in their directions, unless a X is taken of the whole X; the rounding of a product's operands
+// stays within the directions that the product has.  Measured against 64 bits (a matrix of 8 large directions and a hundredth of
+// noise, 384 x 1,024): 3.7e-2 with X in one part, 3.3e-4 with two.
+#include "train_tiles.h"
+
+#include <float.h>
+#include <math.h>
+
+#include <vector>
+
+namespace fbx {
+namespace train {
+namespace {
+
+typedef _Float16 f16;
+constexpr uint32_t kMatrices = 32;        // of a launch
+constexpr uint32_t kDepth = kStepBytes / sizeof(f16);
+constexpr uint32_t kMostPartials = 512;   // of a matrix's sum of squares
+constexpr int kX = 14;                    // X is held times 2^14, but for the first
+
+// One matrix of a launch: what it is made of, where its result goes, and its scratch.
+struct Matrix {
+  const void* u;                          // the matrix, or a gradient
+  float* m;                               // a gradient's momentum, or null
+  void *out, *copy;                       // the result, or the weights
+  uint64_t ld_u, ld_out;
+  char* scratch;
+  float step;                             // the result's factor (lr times the matrix's, or 1)
+  uint32_t rows, columns;                 // of what is given
+  uint32_t tall, m_side, n_side, wide_m, wide_n;  // of X: m x n; rows of either side made up to whole steps of depth
+  uint32_t chunk, partials;               // elements whose squares a workgroup adds up; workgroups
+  uint32_t exact;                         // products of both parts
+  uint32_t at_norm, at_x, at_a;           // places in scratch, in units of 256 bytes (a, then b)
+
+  __device__ f16* x(uint32_t turn, uint32_t part) const { return (f16*)(scratch + (uint64_t)at_x * 256u) + (uint64_t)(turn * 2u + part) * m_side * wide_n; }
+  __device__ f16* a(uint32_t part) const { return (f16*)(scratch + (uint64_t)at_a * 256u) + (uint64_t)part * m_side * wide_m; }
+  __device__ f16* b(uint32_t part) const { return a(2u + part); }
+  __device__ double* squares() const { return (double*)(scratch + (uint64_t)at_norm * 256u); }
+  __device__ float* factor() const { return (float*)(squares() + kMostPartials); }   // X = what is held first, times this
+};
+
+struct List {
+  Matrix of[kMatrices];
+  uint32_t first[kMatrices + 1];          // the first workgroup (or tile) of each
+  uint32_t n;
+
+  __device__ uint32_t find(uint32_t block) const {
+    uint32_t lo = 0u, hi = n;
+    while (hi - lo > 1u) {
+      const uint32_t mid = (lo + hi) / 2u;
+      if (first[mid] <= block) lo = mid;
+      else hi = mid;
+    }
+    return lo;
+  }
+};
+
+struct PrepareArgs {
+  List list;
+  uint32_t in, given;                     // types: of the matrix or gradient; given: there is momentum
+  uint32_t nesterov;
+  float momentum, grad_scale;
+  double eps;
+};
+
+__device__ __forceinline__ float element(const void* p, uint64_t i, uint32_t type) {
+  return type == FBX_F32 ? ((const float*)p)[i] : type == FBX_F16 ? (float)((const f16*)p)[i] : (float)((const __bf16*)p)[i];
+}
+
+// Sums of squares, in 64 bits so that they stay within range whatever the gradient's size; momentum is brought up to date.
+// A workgroup adds up `chunk` elements.
+__global__ __launch_bounds__(256) void k_measure(PrepareArgs) {
+  const PrepareArgs& p = launch_args<PrepareArgs>();
+  const uint32_t which = same(p.list.find(blockIdx.x));
+  const Matrix& t = p.list.of[which];
+  const uint32_t part = blockIdx.x - p.list.first[which];
+  const uint64_t all = (uint64_t)t.rows * t.columns, from = (uint64_t)part * t.chunk, to = from + t.chunk < all ? from + t.chunk : all;
+  double sum = 0;
+  for (uint64_t i = from + threadIdx.x; i < to; i += 256u) {
+    float u;
+    if (p.given) {
+#pragma clang fp contract(off)
+      const float g = element(t.u, i, p.in) * p.grad_scale, m = t.m[i] * p.momentum + g;
+      t.m[i] = m;
+      u = p.nesterov ? g + m * p.momentum : m;
+    } else {
+      const uint64_t r = t.ld_u == t.columns ? 0u : i / t.columns;
+      u = element(t.u, i + r * (t.ld_u - t.columns), p.in);
+    }
+    sum += (double)u * u;
+  }
+  __shared__ double sums[256];
+  sums[threadIdx.x] = sum;
+  __syncthreads();
+  for (uint32_t d = 128; d; d /= 2u) {
+    if (threadIdx.x < d) sums[threadIdx.x] += sums[threadIdx.x + d];
+    __syncthreads();
+  }
+  if (threadIdx.x == 0u) t.squares()[part] = sums[0];
+}
+
+// The matrix's parts of 16 bits, times the power of two that brings its norm into [2^13, 2^14): one times 2^14 for the
+// steps that follow, and the factor that makes X of it.  A workgroup takes 64 x 64 elements of X (zeros beyond them).
+constexpr uint32_t kSquare = 64;
+__global__ __launch_bounds__(256) void k_split(PrepareArgs) {
+  const PrepareArgs& p = launch_args<PrepareArgs>();
+  const uint32_t which = same(p.list.find(blockIdx.x));
+  const Matrix& t = p.list.of[which];
+  const uint32_t tile = blockIdx.x - p.list.first[which], across = t.wide_n / kSquare, r0 = tile / across * kSquare, c0 = tile % across * kSquare;
+  __shared__ double sums[256];
+  __shared__ float turned[kSquare][kSquare + 1];
+  double sum = 0;
+  for (uint32_t i = threadIdx.x; i < t.partials; i += 256u) sum += t.squares()[i];
+  sums[threadIdx.x] = sum;
+  const uint32_t lane = threadIdx.x % 64u, wave = threadIdx.x / 64u;
+  // rows of what is given: those of X, or its columns
+  const uint32_t row0 = t.tall ? c0 : r0, column = (t.tall ? r0 : c0) + lane;
+  float u[kSquare / 4];
+#pragma unroll
+  for (uint32_t k = 0; k < kSquare / 4; ++k) {
+    const uint32_t row = row0 + wave + 4u * k;
+    u[k] = 0.f;
+    if (row >= t.rows || column >= t.columns) continue;
+    if (p.given) {
+#pragma clang fp contract(off)
+      const uint64_t i = (uint64_t)row * t.columns + column;
+      const float m = t.m[i];
+      u[k] = p.nesterov ? element(t.u, i, p.in) * p.grad_scale + m * p.momentum : m;
+    } else {
+      u[k] = element(t.u, row * t.ld_u + column, p.in);
+    }
+  }
+  __syncthreads();
+  for (uint32_t d = 128; d; d /= 2u) {
+    if (threadIdx.x < d) sums[threadIdx.x] += sums[threadIdx.x + d];
+    __syncthreads();
+  }
+  const double norm = sqrt(sums[0]);
+  int k2 = 0;
+  if (norm > 0 && norm <= DBL_MAX) {
+    int e;
+    (void)frexp(norm, &e);   // norm in [2^(e - 1), 2^e)
+    k2 = kX - e;
+  }
+  if (tile == 0u && threadIdx.x == 0u) *t.factor() = norm == 0 ? 0.f : norm <= DBL_MAX ? (float)(1.0 / ldexp(norm + p.eps, k2)) : __builtin_nanf("");
+  if (t.tall) {
+#pragma unroll
+    for (uint32_t k = 0; k < kSquare / 4; ++k) turned[wave + 4u * k][lane] = u[k];
+    __syncthreads();
+#pragma unroll
+    for (uint32_t k = 0; k < kSquare / 4; ++k) u[k] = turned[lane][wave + 4u * k];
+  }
+#pragma unroll
+  for (uint32_t k = 0; k < kSquare / 4; ++k) {
+    const uint32_t r = r0 + wave + 4u * k;
+    if (r >= t.m_side) continue;
+    const uint64_t at = (uint64_t)r * t.wide_n + c0 + lane;
+    const float v = ldexpf(u[k], k2);
+    const f16 high = (f16)v;
+    t.x(0, 0)[at] = high;
+    t.x(0, 1)[at] = (f16)(v - (float)high);
+  }
+}
+
+// One launch's products, of every matrix of the list:
+//   kGram     A = X X^T
+//   kPolynom  B = b A + c A A (A is its own transpose)
+//   kNext     X = a X + B X, into the other of two places
+//   kLast     the same, and it leaves as the result, or goes into the weights
+enum Form { kGram, kPolynom, kNext, kLast };
+struct ProductArgs {
+  List list;
+  uint32_t turn;                          // which X is read
+  uint32_t begins;                        // X is what k_split left
+  float keep, sum;                        // C = keep (what is there) + sum (the product), but for the scale of the first X
+  uint32_t out, copy, weights;            // kLast: types; the result goes into weights
+  float decay;                            // of them: 1 - lr weight_decay
+};
+
+struct Halves {
+  f16 high[4], low[4];
+  __device__ explicit Halves(f32x4 v) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      high[e] = (f16)v[e];
+      low[e] = (f16)(v[e] - (float)high[e]);
+    }
+  }
+};
+__device__ __forceinline__ f32x4 whole(const f16* high, const f16* low) {
+  const Pack<f16, 4> h = *(const Pack<f16, 4>*)high;
+  f32x4 v = {(float)h.v[0], (float)h.v[1], (float)h.v[2], (float)h.v[3]};
+  if (low) {
+    const Pack<f16, 4> l = *(const Pack<f16, 4>*)low;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] += (float)l.v[e];
+  }
+  return v;
+}
+
+// BM x BN of C a workgroup, its WM x WN wavefronts side by side.  C's rows come from A; its columns from B, which is the first side
+// of the matrix instructions, so that a lane holds four adjacent columns of a row.  Of a symmetric C tiles on and below the
+// diagonal are worked out, and stored on either side of it.
+template <Form kForm, int BM, int BN, int WM, int WN, int kStages>
+__global__ __launch_bounds__(WM * WN * 64) void k_product(ProductArgs) {
+#ifdef __HIP_DEVICE_COMPILE__
+  constexpr bool kTwin = kForm == kGram || kForm == kPolynom;
+  constexpr int kWaves = WM * WN, kRows = BM / WM, kCols = BN / WN, kMF = kRows / 16, kNF = kCols / 16;
+  typedef Tile<f16, BM, kWaves, false> TileA;
+  typedef Tile<f16, BN, kWaves, !kTwin> TileB;
+  __shared__ alignas(1024) char a0[BM * kStepBytes], b0[BN * kStepBytes], a1[BM * kStepBytes], b1[BN * kStepBytes];
+  __shared__ alignas(1024) char a2[kStages > 2 ? BM * kStepBytes : 16], b2[kStages > 2 ? BN * kStepBytes : 16];
+  __shared__ alignas(1024) char a3[kStages > 2 ? BM * kStepBytes : 16], b3[kStages > 2 ? BN * kStepBytes : 16];
+  const ProductArgs& p = launch_args<ProductArgs>();
+  const uint32_t lane = threadIdx.x % 64u, wave = same(threadIdx.x / 64u), wm = wave % WM, wn = wave / WM;
+  uint32_t at;
+  {  // workgroups go to the eight dies in turn: each die takes a stretch of the tiles
+    const uint32_t n = gridDim.x, each = n / 8u, more = n % 8u, die = blockIdx.x % 8u;
+    at = die * each + (die < more ? die : more) + blockIdx.x / 8u;
+  }
+  const uint32_t which = same(p.list.find(at));
+  const Matrix& t = p.list.of[which];
+  at -= p.list.first[which];
+  uint32_t row0, col0;
+  if (kTwin) {  // the i-th row of tiles has i + 1
+    uint32_t i = (uint32_t)((__builtin_sqrtf(8.f * (float)at + 1.f) - 1.f) * 0.5f);
+    while (i * (i + 1u) / 2u > at) --i;
+    while ((i + 1u) * (i + 2u) / 2u <= at) ++i;
+    row0 = same(i * BM);
+    col0 = same((at - i * (i + 1u) / 2u) * BN);
+  } else {      // eight row tiles wide, down the columns
+    const uint32_t row_tiles = (t.m_side + BM - 1u) / BM, column_tiles = (t.n_side + BN - 1u) / BN;
+    const uint32_t band = at / (8u * column_tiles), in_band = at - band * 8u * column_tiles, high = row_tiles - band * 8u < 8u ? row_tiles - band * 8u : 8u;
+    row0 = same((band * 8u + in_band % high) * BM);
+    col0 = same(in_band / high * BN);
+  }
+  const uint32_t m_side = same(t.m_side), wide_a = same(kForm == kGram ? t.wide_n : t.wide_m), wide_b = same(kForm == kPolynom ? t.wide_m : t.wide_n);
+  const uint64_t ld_a = wide_a * 2u, ld_b = wide_b * 2u;
+  const uint32_t each = wide_a / kDepth, end = t.exact ? 3u * each : each;   // steps: of one product of parts, of all
+  const char* of_a = (const char*)(kForm == kGram ? t.x(p.turn, 0) : kForm == kPolynom ? t.a(0) : t.b(0));
+  const char* of_b = (const char*)(kForm == kPolynom ? t.a(0) : t.x(p.turn, 0));
+  const uint64_t part_a = (uint64_t)m_side * ld_a, part_b = (uint64_t)m_side * ld_b;
+  of_a += (uint64_t)row0 * ld_a;
+  of_b += kTwin ? (uint64_t)col0 * ld_b : (uint64_t)col0 * 2u;
+  TileA ta;
+  TileB tb;
+  ta.begin(wave, lane, ld_a, 0);
+  tb.begin(wave, lane, ld_b, wide_b - col0);
+  // (behind the last step: of nothing, so that every step's loads are as many)
+  auto load = [&](char* to_a, char* to_b, uint32_t s) {
+    const bool none = s >= end;
+    const uint32_t pair = s >= 2u * each ? 2u : s >= each ? 1u : 0u, k = s - pair * each;  // first by first, first by second, second by first
+    const char *a = of_a + (pair == 2u ? part_a : 0u), *b = of_b + (pair == 1u ? part_b : 0u);
+    const uint32_t left = wide_a - k * kDepth;
+    ta.load((lds_char*)to_a, a + (uint64_t)k * kStepBytes, ld_a, none ? 0u : m_side - row0, left, left * 2u, wave);
+    if (kTwin) tb.load((lds_char*)to_b, b + (uint64_t)k * kStepBytes, ld_b, none ? 0u : m_side - col0, left, left * 2u, wave);
+    else tb.load((lds_char*)to_b, b + (uint64_t)k * kDepth * ld_b, ld_b, none || m_side <= k * kDepth ? 0u : m_side - k * kDepth, 0, (wide_b - col0) * 2u, wave);
+  };
+
+  // Two halves of a step's depth in turn: while one is multiplied out of registers the other's rows are read from LDS.
+  // A step's barrier lies between the halves: behind it the next step's tile is there and nobody reads this step's any more, so
+  // the loads of the step kStages later go there.
+  f32x4 sum[kMF][kNF] = {};
+  typename Frag<f16>::type fa[2][kMF], fb[2][kNF];
+  auto read = [&](int part, const char* in_a, const char* in_b) {
+#pragma unroll
+    for (int i = 0; i < kMF; ++i) fa[part][i] = TileA::read((const lds_char*)in_a, wm * kRows + i * 16, part, lane);
+#pragma unroll
+    for (int j = 0; j < kNF; ++j) fb[part][j] = TileB::read((const lds_char*)in_b, wn * kCols + j * 16, part, lane);
+  };
+  auto multiply = [&](int part) {
+#pragma unroll
+    for (int j = 0; j < kNF; ++j)
+#pragma unroll
+      for (int i = 0; i < kMF; ++i) sum[i][j] = mma(fb[part][j], fa[part][i], sum[i][j]);
+  };
+  auto arrived = [](auto steps) {
+    constexpr int n = decltype(steps)::value * (TileA::kLoads + TileB::kLoads);
+    static_assert(n < 64, "");
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt((n & 15) | (n >> 4) << 14 | 0x0070);  // (vmcnt n, lgkmcnt 0)
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto step = [&](char* at_a, char* at_b, const char* next_a, const char* next_b, uint32_t s) {
+    read(1, at_a, at_b);
+    multiply(0);
+    arrived(Kind<kStages - 2>());
+    load(at_a, at_b, s + kStages);
+    __builtin_amdgcn_sched_barrier(0);
+    read(0, next_a, next_b);  // (behind the last step: what is there, unused)
+    multiply(1);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  load(a0, b0, 0);
+  load(a1, b1, 1);
+  if constexpr (kStages == 4) {
+    load(a2, b2, 2);
+    load(a3, b3, 3);
+  }
+  arrived(Kind<kStages - 1>());
+  read(0, a0, b0);
+  if constexpr (kStages == 4) {
+    for (uint32_t s = 0;; s += 4) {
+      step(a0, b0, a1, b1, s);
+      if (s + 1 >= end) break;
+      step(a1, b1, a2, b2, s + 1);
+      if (s + 2 >= end) break;
+      step(a2, b2, a3, b3, s + 2);
+      if (s + 3 >= end) break;
+      step(a3, b3, a0, b0, s + 3);
+      if (s + 4 >= end) break;
+    }
+  } else {
+    for (uint32_t s = 0; s < end; s += 2) {
+      step(a0, b0, a1, b1, s);
+      if (s + 1 < end) step(a1, b1, a0, b0, s + 1);
+    }
+  }
+  arrived(Kind<0>());  // (nothing is to land in LDS that may be another workgroup's by then)
+
+  // The first X is held times 1 / f, every other one times 2^14.
+  const float f = p.begins ? *t.factor() : 1.f;
+  const float keep = p.keep * (kForm == kPolynom ? 1.f : f), product = p.sum * (kForm == kGram ? f * f : kForm == kPolynom ? 1.f : f);
+#pragma unroll
+  for (int i = 0; i < kMF; ++i) {
+    const uint32_t r = row0 + wm * kRows + i * 16 + lane % 16u;
+#pragma unroll
+    for (int j = 0; j < kNF; ++j) {
+      const uint32_t c = col0 + wn * kCols + j * 16 + lane / 16u * 4u;
+      if constexpr (kTwin) {
+        f32x4 v = sum[i][j] * product;
+        f16 *high = kForm == kGram ? t.a(0) : t.b(0), *low = kForm == kGram ? t.a(1) : t.b(1);
+        const uint64_t to = (uint64_t)r * t.wide_m + c;
+        if (r < m_side && c < t.wide_m) {
+          if (kForm == kPolynom) v += whole(t.a(0) + to, t.exact ? t.a(1) + to : nullptr) * keep;
+          const Halves w(v);
+          *(Pack<f16, 4>*)(high + to) = Pack<f16, 4>{{w.high[0], w.high[1], w.high[2], w.high[3]}};
+          if (t.exact) *(Pack<f16, 4>*)(low + to) = Pack<f16, 4>{{w.low[0], w.low[1], w.low[2], w.low[3]}};
+          if (row0 != col0) {
+#pragma unroll
+            for (uint32_t e = 0; e < 4u; ++e) {   // (c is below the diagonal's tile: within the rows)
+              high[(uint64_t)(c + e) * t.wide_m + r] = w.high[e];
+              if (t.exact) low[(uint64_t)(c + e) * t.wide_m + r] = w.low[e];
+            }
+          }
+        } else if (row0 != col0 && r < t.wide_m) {  // (columns beyond the last row's: zeros)
+#pragma unroll
+          for (uint32_t e = 0; e < 4u; ++e) {
+            high[(uint64_t)(c + e) * t.wide_m + r] = (f16)0.f;
+            if (t.exact) low[(uint64_t)(c + e) * t.wide_m + r] = (f16)0.f;
+          }
+        }
+      } else {
+        if (r >= m_side || c >= t.wide_n) continue;
+        const uint64_t from = (uint64_t)r * t.wide_n + c;
+        f32x4 v = whole(t.x(p.turn, 0) + from, t.x(p.turn, 1) + from);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = v[e] * keep + sum[i][j][e] * product;
+        if constexpr (kForm == kNext) {
+          const Halves w(v);
+          *(Pack<f16, 4>*)(t.x(p.turn ^ 1u, 0) + from) = Pack<f16, 4>{{w.high[0], w.high[1], w.high[2], w.high[3]}};
+          *(Pack<f16, 4>*)(t.x(p.turn ^ 1u, 1) + from) = Pack<f16, 4>{{w.low[0], w.low[1], w.low[2], w.low[3]}};
+        } else {
+#pragma unroll
+          for (uint32_t e = 0; e < 4u; ++e) {
+            if (c + e >= t.n_side) continue;
+            const uint64_t to = t.tall ? (uint64_t)(c + e) * t.ld_out + r : (uint64_t)r * t.ld_out + c + e;
+            float o = v[e] * t.step;
+            if (p.weights) o = element(t.out, to, p.out) * p.decay - o;
+            if (p.out == FBX_F32) ((float*)t.out)[to] = o;
+            else if (p.out == FBX_F16) ((f16*)t.out)[to] = (f16)o;
+            else ((__bf16*)t.out)[to] = (__bf16)o;
+            if (t.copy && p.copy == FBX_F16) ((f16*)t.copy)[to] = (f16)o;
+            else if (t.copy) ((__bf16*)t.copy)[to] = (__bf16)o;
+          }
+        }
+      }
+    }
+  }
+#endif
+}
+
+// The steps' scales: A is held times 2^a, B times 2^b, so that no first part reaches f16's end (65,504).
+struct Step {
+  double a, b, c;
+  int at_a, at_b;
+};
+constexpr double kFull = 57344;   // (with an eighth to spare for what rounding adds)
+// Bounds of the singular values before each step, from 1 on; how far they can go follows from the coefficients.
+const char* plan(const fbx_ortho* h, std::vector<Step>* steps) {
+  double most = 1;
+  for (uint32_t i = 0; i < h->steps; ++i) {
+    Step s{};
+    s.a = h->coefficients[3 * i];
+    s.b = h->coefficients[3 * i + 1];
+    s.c = h->coefficients[3 * i + 2];
+    if (!isfinite(s.a) || !isfinite(s.b) || !isfinite(s.c)) return "coefficients must be finite";
+    double next = 0, polynom = 0;
+    constexpr int kPlaces = 2048;
+    for (int k = 0; k <= kPlaces; ++k) {
+      const double v = most * k / kPlaces, q = v * v * (s.b + s.c * v * v);
+      next = fmax(next, fabs(v * (s.a + q)));
+      polynom = fmax(polynom, fabs(q));
+    }
+    // (between two places a polynomial of the fifth degree moves by less than this)
+    const double slack = (fabs(s.a) + 3 * fabs(s.b) * most * most + 5 * fabs(s.c) * most * most * most * most) * most / kPlaces;
+    next += slack;
+    polynom += 2 * slack;
+    auto scale = [](double top) {
+      int e = kX;
+      while (e > -kX && ldexp(top, e) > kFull) --e;
+      return e;
+    };
+    s.at_a = scale(most * most);
+    s.at_b = scale(fmax(polynom, 1e-3));
+    if (polynom > 256 || (i + 1 < h->steps && next > 3)) return "coefficients: a step takes singular values beyond 3, or its polynomial beyond 256";
+    most = fmax(next * 1.01, 0.25);
+    steps->push_back(s);
+  }
+  return nullptr;
+}
+
+// A list of matrices as both calls see it.
+struct Whole {
+  const fbx_ortho* h;
+  fbx_dtype in, out, copy;
+  bool weights;
+  float nesterov, momentum, grad_scale, decay;
+  std::vector<Matrix> all;
+};
+
+// Tiles of 256 x 256 read least from LDS, smaller ones begin sooner and leave fewer compute units idle; the times are those that
+// the gated block's products were measured to take (microseconds: a workgroup's begin and each step, alone on a compute unit or among
+// as many as fit one).
+struct Size { uint32_t side, at_once; double begin, lone, full; };
+constexpr Size kSizes[3] = {{256, 1, 8, 1.4, 1.6}, {128, 2, 5.5, 0.5, 0.95}, {64, 2, 3.5, 0.22, 0.3}};
+uint64_t tiles_of(const Matrix& t, Form form, uint32_t side) {
+  const uint64_t rows = ceil_div(t.m_side, side);
+  return form == kGram || form == kPolynom ? rows * (rows + 1) / 2 : rows * ceil_div(t.n_side, side);
+}
+uint32_t choose(const Matrix* t, uint32_t n, Form form) {
+  uint32_t best = 2;
+  double least = 0;
+  for (uint32_t i = 0; i < 3; ++i) {
+    const Size& s = kSizes[i];
+    double tiles = 0, steps = 0, longest = 0;
+    for (uint32_t k = 0; k < n; ++k) {
+      const double count = (double)tiles_of(t[k], form, s.side), depth = (double)(form == kGram ? t[k].wide_n : t[k].wide_m) / kDepth * (t[k].exact ? 3 : 1);
+      tiles += count;
+      steps += count * depth;
+      longest = fmax(longest, depth);
+    }
+    if (tiles >= most_blocks(512)) continue;
+    const double slots = 256.0 * s.at_once, rounds = floor(tiles / slots), rest = tiles - rounds * slots, mean = steps / tiles;
+    const double busy = ceil(fmin(rest, slots) / 256.0), step = fmax(s.lone, s.full * busy / s.at_once);
+    const double takes = rounds * (s.begin + mean * s.full) + (rest > 0 ? s.begin + (rounds > 0 ? mean : longest) * step : 0);
+    if (!least || takes < least) {
+      least = takes;
+      best = i;
+    }
+  }
+  return best;
+}
+
+template <Form kForm>
+void multiply(ProductArgs& p, hipStream_t stream) {
+  const uint32_t size = choose(p.list.of, p.list.n, kForm), side = kSizes[size].side;
+  for (uint32_t i = 0; i < p.list.n; ++i) p.list.first[i + 1] = p.list.first[i] + (uint32_t)tiles_of(p.list.of[i], kForm, side);
+  const dim3 grid(p.list.first[p.list.n]);
+  if (size == 0) launch_on(stream, k_product<kForm, 256, 256, 2, 4, 2>, grid, dim3(512), 0, p);
+  else if (size == 1) launch_on(stream, k_product<kForm, 128, 128, 2, 2, 2>, grid, dim3(256), 0, p);
+  else launch_on(stream, k_product<kForm, 64, 64, 2, 2, 4>, grid, dim3(256), 0, p);
+}
+
+// Left to this, products are of both parts where results keep more than bf16 does, and for small matrices: their products take little
+// beside their launches, and their roundings average out less.  Error against 64 bits, results in bf16 (whose own rounding is
+// 1.7e-3), products of first parts: 199 x 164 3.2e-3, 48 x 16 2.8e-3, 2,624 x 4,096 1.7e-3.
+constexpr uint32_t kSmall = 256;
+uint32_t is_exact(const Matrix& t, uint32_t asked, fbx_dtype out) {
+  return asked != FBX_EXACT_BY_SIZE ? asked : out != FBX_BF16 || (t.rows < t.columns ? t.rows : t.columns) <= kSmall;
+}
+
+// Where a matrix's parts lie in its scratch; its size.
+uint64_t lay_out(Matrix& t, uint32_t rows, uint32_t columns) {
+  t.rows = rows;
+  t.columns = columns;
+  t.tall = rows > columns;
+  t.m_side = t.tall ? columns : rows;
+  t.n_side = t.tall ? rows : columns;
+  t.wide_m = (uint32_t)round_up(t.m_side, kDepth);
+  t.wide_n = (uint32_t)round_up(t.n_side, kDepth);
+  const uint64_t all = (uint64_t)rows * columns;
+  t.chunk = (uint32_t)round_up(ceil_div(all, kMostPartials), 2048);
+  t.partials = (uint32_t)ceil_div(all, t.chunk);
+  uint64_t at = 0;
+  auto take = [&](uint64_t bytes) {
+    const uint64_t was = at;
+    at = round_up(at + bytes, 256);
+    return (uint32_t)(was / 256);
+  };
+  t.at_norm = take(kMostPartials * 8 + 8);
+  t.at_x = take(4ull * t.m_side * t.wide_n * sizeof(f16));
+  t.at_a = take(4ull * t.m_side * t.wide_m * sizeof(f16));
+  return at;
+}
+
+// Matrices go together until there are kMatrices of them or their scratch is more than this: by then they fill the card.
+constexpr uint64_t kTogether = 1ull << 30;
+struct Batch { uint32_t from, to; uint64_t bytes; };
+std::vector<Batch> batches(std::vector<Matrix>& all) {
+  std::vector<Batch> b;
+  for (uint32_t i = 0; i < all.size(); ++i) {
+    const uint64_t bytes = lay_out(all[i], all[i].rows, all[i].columns);
+    if (b.empty() || b.back().to - b.back().from == kMatrices || b.back().bytes + bytes > kTogether) b.push_back({i, i, 0});
+    b.back().to = i + 1;
+    b.back().bytes += bytes;
+  }
+  return b;
+}
+uint64_t scratch_of(std::vector<Matrix>& all) {
+  uint64_t most = 0;
+  for (const Batch& b : batches(all)) most = b.bytes > most ? b.bytes : most;
+  return most;
+}
+
+void run(Whole& w, const std::vector<Step>& steps, char* scratch, hipStream_t stream) {
+  for (const Batch& b : batches(w.all)) {
+    PrepareArgs q{};
+    ProductArgs p{};
+    q.list.n = p.list.n = b.to - b.from;
+    char* at = scratch;
+    for (uint32_t i = 0; i < q.list.n; ++i) {
+      Matrix& t = q.list.of[i] = w.all[b.from + i];
+      t.scratch = at;
+      at += lay_out(t, t.rows, t.columns);
+      p.list.of[i] = t;
+    }
+    q.in = w.in;
+    q.given = q.list.of[0].m != nullptr;
+    q.nesterov = w.nesterov != 0;
+    q.momentum = w.momentum;
+    q.grad_scale = w.grad_scale;
+    q.eps = w.h->eps;
+    for (uint32_t i = 0; i < q.list.n; ++i) q.list.first[i + 1] = q.list.first[i] + q.list.of[i].partials;
+    launch_on(stream, k_measure, dim3(q.list.first[q.list.n]), dim3(256), 0, q);
+    for (uint32_t i = 0; i < q.list.n; ++i) q.list.first[i + 1] = q.list.first[i] + (uint32_t)(ceil_div(q.list.of[i].m_side, kSquare) * (q.list.of[i].wide_n / kSquare));
+    launch_on(stream, k_split, dim3(q.list.first[q.list.n]), dim3(256), 0, q);
+    p.out = w.out;
+    p.copy = w.copy;
+    p.weights = w.weights;
+    p.decay = w.decay;
+    for (size_t i = 0; i < steps.size(); ++i) {
+      const Step& s = steps[i];
+      const double x = i ? ldexp(1, kX) : 1, a = ldexp(1, s.at_a), bb = ldexp(1, s.at_b), next = i + 1 < steps.size() ? ldexp(1, kX) : 1;
+      p.turn = i & 1u;
+      p.begins = i == 0;
+      p.keep = 0;
+      p.sum = (float)(a / (x * x));
+      multiply<kGram>(p, stream);
+      p.keep = (float)(s.b * bb / a);
+      p.sum = (float)(s.c * bb / (a * a));
+      multiply<kPolynom>(p, stream);
+      p.keep = (float)(s.a * next / x);
+      p.sum = (float)(next / (bb * x));
+      if (i + 1 < steps.size()) multiply<kNext>(p, stream);
+      else multiply<kLast>(p, stream);
+    }
+  }
+}
+
+fbx_status check(const fbx_ortho* h, std::vector<Step>* steps) {
+  if (!h->steps || h->steps > 64) return refuse(FBX_E_ARG, "steps must be 1 .. 64");
+  if (h->exact > FBX_EXACT_BY_SIZE) return refuse(FBX_E_ARG, "exact must be 0, 1 or FBX_EXACT_BY_SIZE");
+  if (!h->coefficients) return refuse(FBX_E_ARG, "coefficients is NULL");
+  if (!(h->eps >= 1e-30 && h->eps <= 1e30)) return refuse(FBX_E_ARG, "eps must be 1e-30 .. 1e30");
+  const char* why = plan(h, steps);
+  return why ? refuse(FBX_E_ARG, why) : FBX_OK;
+}
+fbx_status check_sides(uint32_t rows, uint32_t columns) {
+  return !rows || !columns || rows > FBX_ORTHO_MOST || columns > FBX_ORTHO_MOST ? refuse(FBX_E_ARG, "rows and columns must be 1 .. FBX_ORTHO_MOST") : FBX_OK;
+}
+fbx_status check_scratch(const void* d_scratch, uint64_t bytes, uint64_t need) {
+  if (need && (!d_scratch || (uintptr_t)d_scratch % 256u)) return refuse(FBX_E_ARG, "d_scratch is NULL or not 256-byte aligned");
+  return bytes < need ? refuse(FBX_E_NOMEM, "scratch too small: the scratch function gives its size") : FBX_OK;
+}
+template <class M>
+fbx_status sides(const M* matrices, uint32_t n, std::vector<Matrix>* all) {
+  if (!matrices && n) return refuse(FBX_E_ARG, "matrices is NULL");
+  for (uint32_t i = 0; i < n; ++i) {
+    const fbx_status st = check_sides(matrices[i].rows, matrices[i].columns);
+    if (st != FBX_OK) return st;
+    Matrix t{};
+    t.rows = matrices[i].rows;
+    t.columns = matrices[i].columns;
+    all->push_back(t);
+  }
+  return FBX_OK;
+}
+// (no exception may leave a call)
+template <class F>
+fbx_status guarded(F f) {
+  try {
+    return f();
+  } catch (...) {
+    return refuse(FBX_E_NOMEM, "out of host memory");
+  }
+}
+
+}  // namespace
+}  // namespace train
+}  // namespace fbx
+
+using namespace fbx::train;
+
+extern "C" fbx_status fbx_ortho_scratch(const fbx_ortho* h, const fbx_ortho_matrix* matrices, uint32_t n, uint64_t* bytes) {
+  return guarded([&] {
+    if (!h || !bytes) return refuse(FBX_E_ARG, "h or bytes is NULL");
+    std::vector<Matrix> all;
+    const fbx_status st = sides(matrices, n, &all);
+    if (st == FBX_OK) *bytes = scratch_of(all);
+    return st;
+  });
+}
+
+extern "C" fbx_status fbx_orthogonalise(const fbx_ortho* h, const fbx_ortho_matrix* matrices, uint32_t n, void* d_scratch, uint64_t scratch_bytes, void* hip_stream) {
+  return guarded([&] {
+    if (!h) return refuse(FBX_E_ARG, "h is NULL");
+    Whole w{};
+    std::vector<Step> steps;
+    if (!known(h->in) || !known(h->out)) return refuse(FBX_E_ARG, "unknown dtype");
+    fbx_status st = check(h, &steps);
+    if (st == FBX_OK) st = sides(matrices, n, &w.all);
+    if (st != FBX_OK) return st;
+    for (uint32_t i = 0; i < n; ++i) {
+      const fbx_ortho_matrix& m = matrices[i];
+      Matrix& t = w.all[i];
+      if (!m.d_u || !m.d_out) return refuse(FBX_E_ARG, "a matrix or its result is NULL");
+      if ((uintptr_t)m.d_u % size_of(h->in) || (uintptr_t)m.d_out % size_of(h->out)) return refuse(FBX_E_ARG, "a matrix is not aligned to its elements");
+      if (m.ld_u < m.columns || m.ld_out < m.columns || (m.ld_u | m.ld_out) >> 40) return refuse(FBX_E_ARG, "a stride is smaller than columns, or 2^40 or more");
+      t.u = m.d_u;
+      t.ld_u = m.ld_u;
+      t.out = m.d_out;
+      t.ld_out = m.ld_out;
+      t.step = 1.f;
+      t.exact = is_exact(t, h->exact, h->out);
+    }
+    st = check_scratch(d_scratch, scratch_bytes, scratch_of(w.all));
+    if (st != FBX_OK || !n) return st;
+    w.h = h;
+    w.in = h->in;
+    w.out = h->out;
+    run(w, steps, (char*)d_scratch, (hipStream_t)hip_stream);
+    return launched();
+  });
+}
+
+extern "C" fbx_status fbx_muon_scratch(const fbx_muon* h, const fbx_muon_matrix* matrices, uint32_t n, uint64_t* bytes) {
+  return guarded([&] {
+    if (!h || !bytes) return refuse(FBX_E_ARG, "h or bytes is NULL");
+    std::vector<Matrix> all;
+    const fbx_status st = sides(matrices, n, &all);
+    if (st == FBX_OK) *bytes = scratch_of(all);
+    return st;
+  });
+}
+
+extern "C" fbx_status fbx_muon_step(const fbx_muon* h, const fbx_muon_matrix* matrices, uint32_t n, void* d_scratch, uint64_t scratch_bytes, void* hip_stream) {
+  return guarded([&] {
+    if (!h) return refuse(FBX_E_ARG, "h is NULL");
+    Whole w{};
+    std::vector<Step> steps;
+    if (!known(h->param_dtype) || !known(h->grad_dtype)) return refuse(FBX_E_ARG, "unknown dtype");
+    if (!(h->momentum >= 0 && h->momentum < 1)) return refuse(FBX_E_ARG, "momentum must be in [0, 1)");
+    if (!isfinite((float)h->lr) || !isfinite((float)h->weight_decay) || !isfinite((float)h->grad_scale)) return refuse(FBX_E_ARG, "lr, weight_decay and grad_scale must be finite");
+    fbx_status st = check(&h->ortho, &steps);
+    if (st == FBX_OK) st = sides(matrices, n, &w.all);
+    if (st != FBX_OK) return st;
+    bool copy = false;
+    for (uint32_t i = 0; i < n; ++i) copy |= matrices[i].d_copy != nullptr;
+    for (uint32_t i = 0; i < n; ++i) {
+      const fbx_muon_matrix& m = matrices[i];
+      Matrix& t = w.all[i];
+      if (!m.d_param || !m.d_grad || !m.d_m) return refuse(FBX_E_ARG, "a matrix lacks its weights, gradient or momentum");
+      if ((uintptr_t)m.d_param % size_of(h->param_dtype) || (uintptr_t)m.d_grad % size_of(h->grad_dtype) || (uintptr_t)m.d_m % 4u) return refuse(FBX_E_ARG, "a matrix is not aligned to its elements");
+      if (m.d_copy && (h->copy_dtype == FBX_F32 || !known(h->copy_dtype) || h->param_dtype != FBX_F32 || (uintptr_t)m.d_copy % 2u))
+        return refuse(FBX_E_ARG, "a copy is in f16 or bf16, of weights in f32");
+      if (copy && !m.d_copy) return refuse(FBX_E_ARG, "either all matrices have a copy or none");
+      if (!isfinite((float)(h->lr * m.factor))) return refuse(FBX_E_ARG, "factor must be finite");
+      t.u = m.d_grad;
+      t.m = (float*)m.d_m;
+      t.out = m.d_param;
+      t.copy = m.d_copy;
+      t.ld_u = t.ld_out = m.columns;
+      t.step = (float)(h->lr * m.factor);
+      t.exact = is_exact(t, h->ortho.exact, h->param_dtype);
+    }
+    st = check_scratch(d_scratch, scratch_bytes, scratch_of(w.all));
+    if (st != FBX_OK || !n) return st;
+    w.h = &h->ortho;
+    w.in = h->grad_dtype;
+    w.out = h->param_dtype;
+    w.copy = h->copy_dtype;
+    w.weights = true;
+    w.nesterov = h->nesterov != 0;
+    w.momentum = (float)h->momentum;
+    w.grad_scale = (float)h->grad_scale;
+    w.decay = (float)(1.0 - h->lr * h->weight_decay);
+    run(w, steps, (char*)d_scratch, (hipStream_t)hip_stream);
+    return launched();
+  });
+}

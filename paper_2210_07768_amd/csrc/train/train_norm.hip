@@ -1,0 +1,799 @@
+// The norm of rows before a block (`norm`), what joins a block's result to the residual stream, with the next block's norm
+// (`join`), and their gradients.
+#include "train_common.h"
+
+#include <float.h>
+#include <math.h>
+
+namespace fbx {
+namespace train {
+namespace {
+
+constexpr uint32_t kPack = 8;                 // adjacent elements of a lane
+constexpr uint32_t kMostLanes = 1024;         // of a row, and of a workgroup
+static_assert(FBX_NORM_MOST == 2 * kMostLanes * kPack, "a row is held by a workgroup's registers");
+
+// Eight adjacent elements in whole loads, wherever they begin: a row that is aligned to its elements only is read and
+// written four to sixteen bytes a lane like any other (the hardware takes such addresses), so odd widths and strides need no
+// form of their own.
+template <class X>
+struct Raw {
+  X v[kPack];
+};
+template <class X>
+__device__ __forceinline__ Raw<X> fetch(const X* row, uint32_t c, uint32_t n) {
+  Raw<X> r = {};
+  if (n == kPack) {
+    __builtin_memcpy(&r, row + c, sizeof r);
+  } else {
+#pragma unroll
+    for (uint32_t e = 0; e < kPack; ++e)
+      if (e < n) r.v[e] = row[c + e];
+  }
+  return r;
+}
+template <class X>
+__device__ __forceinline__ void put(X* row, uint32_t c, uint32_t n, const float (&from)[kPack]) {
+  Raw<X> r;
+#pragma unroll
+  for (uint32_t e = 0; e < kPack; ++e) r.v[e] = (X)from[e];
+  if (n == kPack) {
+    __builtin_memcpy(row + c, &r, sizeof r);
+  } else {
+#pragma unroll
+    for (uint32_t e = 0; e < kPack; ++e)
+      if (e < n) row[c + e] = r.v[e];
+  }
+}
+
+// A workgroup's lanes: `slots` rows at a time, `lanes` to a row: a power of two up to 64, or whole wavefronts.
+struct Group {
+  uint32_t lanes, slot, mine, waves;
+  float* shared;   // two times what a reduction leaves there, in turn
+  uint32_t turn;
+
+  __device__ Group(uint32_t lanes_, float* shared_) : lanes(lanes_), slot(threadIdx.x / lanes_), mine(threadIdx.x % lanes_), waves(lanes_ / 64u), shared(shared_), turn(0) {}
+
+  // Sums over a row's lanes, in all of them.  Every lane of the workgroup takes part.
+  template <int kN>
+  __device__ __forceinline__ void sum(float (&v)[kN]) {
+#ifdef __HIP_DEVICE_COMPILE__
+    auto moved = [](float x, auto control) { return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(control)::value, 15, 15, true)); };
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      if (lanes > 1u) v[i] += moved(v[i], std::integral_constant<int, 0xb1>());    // lane ^ 1
+      if (lanes > 2u) v[i] += moved(v[i], std::integral_constant<int, 0x4e>());    // lane ^ 2
+      if (lanes > 4u) v[i] += moved(v[i], std::integral_constant<int, 0x141>());   // 7 - lane, of eight: the other four
+      if (lanes > 8u) v[i] += moved(v[i], std::integral_constant<int, 0x140>());   // 15 - lane, of sixteen: the other eight
+      if (lanes > 16u) {  // (both give each lane the sums of both halves)
+        const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[i]), __float_as_uint(v[i]), false, false);
+        const uint32_t one = p[0], other = p[1];
+        v[i] = __uint_as_float(one) + __uint_as_float(other);
+      }
+      if (lanes > 32u) {
+        const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[i]), __float_as_uint(v[i]), false, false);
+        const uint32_t one = p[0], other = p[1];
+        v[i] = __uint_as_float(one) + __uint_as_float(other);
+      }
+    }
+#endif
+    if (waves <= 1u) return;
+    // (a wavefront that writes here for the next reduction but one has met all others at the next one's barrier, behind their reads)
+    float* at = shared + turn * (kMostLanes / 64u) * kMostSums;
+    turn ^= 1u;
+    const uint32_t wave = threadIdx.x / 64u;
+    if (threadIdx.x % 64u == 0u)
+#pragma unroll
+      for (int i = 0; i < kN; ++i) at[wave * kN + i] = v[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kN; ++i) v[i] = 0.f;
+    for (uint32_t w = slot * waves; w < (slot + 1u) * waves; ++w)
+#pragma unroll
+      for (int i = 0; i < kN; ++i) v[i] += at[w * kN + i];
+  }
+  static constexpr uint32_t kMostSums = 4;
+  static constexpr uint32_t kShared = 2 * (kMostLanes / 64) * kMostSums;
+};
+
+// A row's packs of this lane: pack j begins at column (j * lanes + mine) * 8, and n[j] of its elements exist.
+template <int kN>
+struct Columns {
+  uint32_t c[kN], n[kN];
+  __device__ Columns(const Group& g, uint32_t dim) {
+#pragma unroll
+    for (int j = 0; j < kN; ++j) {
+      c[j] = (j * g.lanes + g.mine) * kPack;
+      n[j] = c[j] >= dim ? 0u : dim - c[j] < kPack ? dim - c[j] : kPack;
+    }
+  }
+};
+template <int kN>
+using Row = float[kN][kPack];
+
+template <class X, int kN>
+__device__ __forceinline__ void fetch_row(Raw<X> (&to)[kN], const X* row, const Columns<kN>& at, bool in) {
+#pragma unroll
+  for (int j = 0; j < kN; ++j) to[j] = fetch(row, at.c[j], in ? at.n[j] : 0u);
+}
+template <class X, int kN>
+__device__ __forceinline__ void widen(Row<kN>& to, const Raw<X> (&from)[kN]) {
+#pragma unroll
+  for (int j = 0; j < kN; ++j)
+#pragma unroll
+    for (uint32_t e = 0; e < kPack; ++e) to[j][e] = (float)from[j].v[e];
+}
+template <class X, int kN>
+__device__ __forceinline__ void put_row(X* row, const Row<kN>& from, const Columns<kN>& at, bool in) {
+#pragma unroll
+  for (int j = 0; j < kN; ++j) put(row, at.c[j], in ? at.n[j] : 0u, from[j]);
+}
+// A vector of weights, in the block's type or 32 bits; `none` where there is none.
+template <class T, int kN>
+__device__ __forceinline__ void fetch_vector(Row<kN>& to, const void* from, bool single, const Columns<kN>& at, float none) {
+#pragma unroll
+  for (int j = 0; j < kN; ++j) {
+    if (!from) {
+#pragma unroll
+      for (uint32_t e = 0; e < kPack; ++e) to[j][e] = none;
+    } else if (single) {
+      const Raw<float> r = fetch((const float*)from, at.c[j], at.n[j]);
+#pragma unroll
+      for (uint32_t e = 0; e < kPack; ++e) to[j][e] = r.v[e];
+    } else {
+      const Raw<T> r = fetch((const T*)from, at.c[j], at.n[j]);
+#pragma unroll
+      for (uint32_t e = 0; e < kPack; ++e) to[j][e] = (float)r.v[e];
+    }
+  }
+}
+
+// v becomes (v - mean) / sqrt(variance + eps), or v / sqrt(mean square + eps); returns 1 / sqrt.  Means and squares are taken
+// of the row in registers, the squares behind the mean: sums of squares less a squared mean would lose what a large mean hides.
+template <int kN>
+__device__ __forceinline__ float normalise(Row<kN>& v, Group& g, const Columns<kN>& at, bool layer, float one_dim, float eps) {
+  float s[1];
+  if (layer) {
+    s[0] = 0.f;
+#pragma unroll
+    for (int j = 0; j < kN; ++j)
+#pragma unroll
+      for (uint32_t e = 0; e < kPack; ++e) s[0] += v[j][e];
+    g.sum(s);
+    const float mean = s[0] * one_dim;
+#pragma unroll
+    for (int j = 0; j < kN; ++j)
+#pragma unroll
+      for (uint32_t e = 0; e < kPack; ++e) v[j][e] = e < at.n[j] ? v[j][e] - mean : 0.f;
+  }
+  s[0] = 0.f;
+#pragma unroll
+  for (int j = 0; j < kN; ++j)
+#pragma unroll
+    for (uint32_t e = 0; e < kPack; ++e) s[0] += v[j][e] * v[j][e];
+  g.sum(s);
+  const float inverse = 1.f / __builtin_sqrtf(s[0] * one_dim + eps);
+#pragma unroll
+  for (int j = 0; j < kN; ++j)
+#pragma unroll
+    for (uint32_t e = 0; e < kPack; ++e) v[j][e] *= inverse;
+  return inverse;
+}
+
+// p, the gradient of normalised rows, becomes that of what they were made from: inverse (p - mean p - unit mean(p unit)), the
+// first mean for a layer's norm only.  more: another sum over the row that is wanted too.
+template <int kN>
+__device__ __forceinline__ void denormalise(Row<kN>& p, const Row<kN>& unit, float inverse, Group& g, bool layer, float one_dim, float& more) {
+  float s[3] = {0.f, 0.f, more};
+#pragma unroll
+  for (int j = 0; j < kN; ++j)
+#pragma unroll
+    for (uint32_t e = 0; e < kPack; ++e) {
+      s[0] += p[j][e] * unit[j][e];
+      s[1] += p[j][e];
+    }
+  g.sum(s);
+  const float along = s[0] * one_dim, mean = layer ? s[1] * one_dim : 0.f;
+#pragma unroll
+  for (int j = 0; j < kN; ++j)
+#pragma unroll
+    for (uint32_t e = 0; e < kPack; ++e) p[j][e] = inverse * (p[j][e] - mean - unit[j][e] * along);
+  more = s[2];
+}
+
+// Every sum of columns of a workgroup, its rows in a fixed order: those of a wavefront by halves, then wavefront by wavefront
+// (or row by row, where a row has more than one); shared: `wide` floats a sum.
+template <int kSums, int kN>
+__device__ __forceinline__ void leave_sums(Row<kN> (&sums)[kSums], float* to, uint32_t wide, const Group& g, const Columns<kN>& at, uint32_t slots, float* shared) {
+  for (uint32_t d = g.lanes; d < 64u; d *= 2u)
+#pragma unroll
+    for (int i = 0; i < kSums; ++i)
+#pragma unroll
+      for (int j = 0; j < kN; ++j)
+#pragma unroll
+        for (uint32_t e = 0; e < kPack; ++e) sums[i][j][e] += __shfl_xor(sums[i][j][e], d, 64);
+  const uint32_t turns = g.waves ? slots : blockDim.x / 64u, mine = g.waves ? g.slot : threadIdx.x / 64u;
+  const bool first = g.waves || threadIdx.x % 64u < g.lanes;   // (of the lanes that hold the same sums now)
+  for (uint32_t s = 0; s < turns; ++s) {
+    if (mine == s && first)
+#pragma unroll
+      for (int i = 0; i < kSums; ++i)
+#pragma unroll
+        for (int j = 0; j < kN; ++j) {
+          if (!at.n[j]) continue;
+          Pack<float, kPack> v;
+          float* held = shared + i * wide + at.c[j];
+#pragma unroll
+          for (uint32_t e = 0; e < kPack; ++e) v.v[e] = sums[i][j][e] + (s ? held[e] : 0.f);
+          if (s + 1u < turns) *(Pack<float, kPack>*)held = v;
+          else *(Pack<float, kPack>*)(to + i * wide + at.c[j]) = v;
+        }
+    if (s + 1u < turns) __syncthreads();
+  }
+}
+
+struct NormArgs {
+  const void *x, *weight, *dy;
+  void *out, *dx;
+  float* sums;                      // of a gradient: a row of `wide` floats a workgroup
+  uint64_t ld_x, ld_out, ld_dy, ld_dx, rows;
+  uint32_t dim, wide, lanes, slots;
+  uint32_t layer, single;           // single: vectors are in 32 bits
+  float eps, one_dim;
+};
+
+// R: of the residual stream; T: of the result.
+// Bound by memory.
+template <class R, class T, int kN>
+__global__ __launch_bounds__(kMostLanes) void k_norm(NormArgs p) {
+  __shared__ float shared[Group::kShared];
+  Group g(p.lanes, shared);
+  const Columns<kN> at(g, p.dim);
+  Row<kN> weight;
+  fetch_vector<T>(weight, p.weight, p.single, at, 1.f);
+  for (uint64_t r0 = (uint64_t)blockIdx.x * p.slots; r0 < p.rows; r0 += (uint64_t)gridDim.x * p.slots) {
+    const uint64_t r = r0 + g.slot;
+    const bool in = r < p.rows;
+    Raw<R> raw[kN];
+    Row<kN> v;
+    fetch_row(raw, (const R*)p.x + r * p.ld_x, at, in);
+    widen(v, raw);
+    normalise(v, g, at, p.layer, p.one_dim, p.eps);
+#pragma unroll
+    for (int j = 0; j < kN; ++j)
+#pragma unroll
+      for (uint32_t e = 0; e < kPack; ++e) v[j][e] *= weight[j][e];
+    put_row((T*)p.out + r * p.ld_out, v, at, in);
+  }
+}
+
+template <class R, class T, int kN>
+__global__ __launch_bounds__(kMostLanes) void k_norm_grad(NormArgs p) {
+  __shared__ float shared[Group::kShared];
+  extern __shared__ __attribute__((aligned(32))) float columns[];
+  Group g(p.lanes, shared);
+  const Columns<kN> at(g, p.dim);
+  Row<kN> weight, sums[1] = {};
+  fetch_vector<T>(weight, p.weight, p.single, at, 1.f);
+  for (uint64_t r0 = (uint64_t)blockIdx.x * p.slots; r0 < p.rows; r0 += (uint64_t)gridDim.x * p.slots) {
+    const uint64_t r = r0 + g.slot;
+    const bool in = r < p.rows;
+    Raw<R> raw_x[kN];
+    Raw<T> raw_dy[kN];
+    Row<kN> unit, d;
+    fetch_row(raw_x, (const R*)p.x + r * p.ld_x, at, in);
+    fetch_row(raw_dy, (const T*)p.dy + r * p.ld_dy, at, in);
+    widen(unit, raw_x);
+    const float inverse = normalise(unit, g, at, p.layer, p.one_dim, p.eps);
+    widen(d, raw_dy);
+#pragma unroll
+    for (int j = 0; j < kN; ++j)
+#pragma unroll
+      for (uint32_t e = 0; e < kPack; ++e) {
+        sums[0][j][e] += d[j][e] * unit[j][e];
+        d[j][e] *= weight[j][e];
+      }
+    if (p.dx) {
+      float none = 0.f;
+      denormalise(d, unit, inverse, g, p.layer, p.one_dim, none);
+      put_row((R*)p.dx + r * p.ld_dx, d, at, in);
+    }
+  }
+  if (p.sums) leave_sums(sums, p.sums + (uint64_t)blockIdx.x * p.wide, p.wide, g, at, p.slots, columns);
+}
+
+struct JoinArgs {
+  const void *x, *y, *gate, *weight, *scale, *next_weight, *dout, *dnext;
+  void *out, *next, *dx, *dy, *dgate;
+  float* sums;                      // of a gradient: two rows of `wide` floats a workgroup
+  uint64_t ld_x, ld_y, ld_gate, ld_out, ld_next, ld_dout, ld_dnext, ld_dx, ld_dy, ld_dgate, rows;
+  uint32_t dim, wide, lanes, slots;
+  uint32_t layer, single, post, then, each, sigmoid;  // each: a gate for each element, not one a row
+  float eps, one_dim, number;       // number: the scale, where it is no vector
+};
+
+// e^-a by the hardware's exponential and reciprocal (one unit in the last place each).
+__device__ __forceinline__ float logistic(float a) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(a * -1.4426950408889634f)); }
+
+// act(gate) of this lane's elements: of a row's one gate, of its own, or 1.
+template <class T, int kN>
+__device__ __forceinline__ void fetch_gate(Raw<T> (&to)[kN], const JoinArgs& p, uint64_t r, const Columns<kN>& at, bool in) {
+  if (p.each) {
+    fetch_row(to, (const T*)p.gate + r * p.ld_gate, at, in && p.gate);
+  } else {
+    const T one = in && p.gate ? ((const T*)p.gate)[r * p.ld_gate] : (T)0.f;
+#pragma unroll
+    for (int j = 0; j < kN; ++j)
+#pragma unroll
+      for (uint32_t e = 0; e < kPack; ++e) to[j].v[e] = one;
+  }
+}
+template <class T>
+__device__ __forceinline__ float open(T z, const JoinArgs& p) {
+  return !p.gate ? 1.f : p.sigmoid ? logistic((float)z) : (float)z;
+}
+
+// Bound by memory.
+template <class R, class T, int kN>
+__global__ __launch_bounds__(kMostLanes) void k_join(JoinArgs p) {
+  __shared__ float shared[Group::kShared];
+  Group g(p.lanes, shared);
+  const Columns<kN> at(g, p.dim);
+  Row<kN> weight, scale, next_weight;
+  fetch_vector<T>(weight, p.weight, p.single, at, 1.f);
+  fetch_vector<T>(scale, p.scale, p.single, at, p.number);
+  fetch_vector<T>(next_weight, p.next_weight, p.single, at, 1.f);
+#pragma unroll
+  for (int j = 0; j < kN; ++j)
+#pragma unroll
+    for (uint32_t e = 0; e < kPack; ++e) weight[j][e] *= scale[j][e];
+  for (uint64_t r0 = (uint64_t)blockIdx.x * p.slots; r0 < p.rows; r0 += (uint64_t)gridDim.x * p.slots) {
+    const uint64_t r = r0 + g.slot;
+    const bool in = r < p.rows;
+    Raw<R> raw_x[kN];
+    Raw<T> raw_y[kN], raw_gate[kN];
+    fetch_row(raw_y, (const T*)p.y + r * p.ld_y, at, in);
+    fetch_gate(raw_gate, p, r, at, in);
+    fetch_row(raw_x, (const R*)p.x + r * p.ld_x, at, in);
+    Row<kN> v;
+    widen(v, raw_y);
+    if (p.post) normalise(v, g, at, p.layer, p.one_dim, p.eps);
+#pragma unroll
+    for (int j = 0; j < kN; ++j)
+#pragma unroll
+      for (uint32_t e = 0; e < kPack; ++e) v[j][e] = (float)raw_x[j].v[e] + open(raw_gate[j].v[e], p) * weight[j][e] * v[j][e];
+    put_row((R*)p.out + r * p.ld_out, v, at, in);
+    if (p.then) {
+#pragma unroll
+      for (int j = 0; j < kN; ++j)
+#pragma unroll
+        for (uint32_t e = 0; e < kPack; ++e)
+          if (e >= at.n[j]) v[j][e] = 0.f;
+      normalise(v, g, at, p.layer, p.one_dim, p.eps);
+#pragma unroll
+      for (int j = 0; j < kN; ++j)
+#pragma unroll
+        for (uint32_t e = 0; e < kPack; ++e) v[j][e] *= next_weight[j][e];
+      put_row((T*)p.next + r * p.ld_next, v, at, in);
+    }
+  }
+}
+
+template <class R, class T, int kN>
+__global__ __launch_bounds__(kMostLanes) void k_join_grad(JoinArgs p) {
+  __shared__ float shared[Group::kShared];
+  extern __shared__ __attribute__((aligned(32))) float columns[];
+  Group g(p.lanes, shared);
+  const Columns<kN> at(g, p.dim);
+  Row<kN> weight, next_weight, sums[2] = {};
+  {
+    Row<kN> scale;
+    fetch_vector<T>(weight, p.weight, p.single, at, 1.f);
+    fetch_vector<T>(scale, p.scale, p.single, at, p.number);
+    fetch_vector<T>(next_weight, p.next_weight, p.single, at, 1.f);
+#pragma unroll
+    for (int j = 0; j < kN; ++j)
+#pragma unroll
+      for (uint32_t e = 0; e < kPack; ++e) weight[j][e] *= scale[j][e];
+  }
+  for (uint64_t r0 = (uint64_t)blockIdx.x * p.slots; r0 < p.rows; r0 += (uint64_t)gridDim.x * p.slots) {
+    const uint64_t r = r0 + g.slot;
+    const bool in = r < p.rows;
+    Raw<R> raw_x[kN], raw_dout[kN];
+    Raw<T> raw_y[kN], raw_gate[kN], raw_dnext[kN];
+    fetch_row(raw_y, (const T*)p.y + r * p.ld_y, at, in);
+    fetch_gate(raw_gate, p, r, at, in);
+    if (p.then) {
+      fetch_row(raw_x, (const R*)p.x + r * p.ld_x, at, in);
+      fetch_row(raw_dnext, (const T*)p.dnext + r * p.ld_dnext, at, in);
+    }
+    fetch_row(raw_dout, (const R*)p.dout + r * p.ld_dout, at, in && p.dout);
+    Row<kN> unit, d;
+    widen(unit, raw_y);
+    float inverse = 1.f;
+    if (p.post) inverse = normalise(unit, g, at, p.layer, p.one_dim, p.eps);
+    widen(d, raw_dout);
+    if (p.then) {
+      Row<kN> after, q;
+      widen(q, raw_dnext);
+#pragma unroll
+      for (int j = 0; j < kN; ++j)
+#pragma unroll
+        for (uint32_t e = 0; e < kPack; ++e)
+          after[j][e] = e < at.n[j] ? (float)raw_x[j].v[e] + open(raw_gate[j].v[e], p) * weight[j][e] * unit[j][e] : 0.f;
+      const float after_inverse = normalise(after, g, at, p.layer, p.one_dim, p.eps);
+#pragma unroll
+      for (int j = 0; j < kN; ++j)
+#pragma unroll
+        for (uint32_t e = 0; e < kPack; ++e) {
+          sums[1][j][e] += q[j][e] * after[j][e];
+          q[j][e] *= next_weight[j][e];
+        }
+      float none = 0.f;
+      denormalise(q, after, after_inverse, g, p.layer, p.one_dim, none);
+#pragma unroll
+      for (int j = 0; j < kN; ++j)
+#pragma unroll
+        for (uint32_t e = 0; e < kPack; ++e) d[j][e] += q[j][e];
+    }
+    if (p.dx) put_row((R*)p.dx + r * p.ld_dx, d, at, in);
+    // from here on: the gradient of what was added to x
+    Row<kN> dgate;
+    float all = 0.f;
+#pragma unroll
+    for (int j = 0; j < kN; ++j)
+#pragma unroll
+      for (uint32_t e = 0; e < kPack; ++e) {
+        if (e >= at.n[j]) d[j][e] = 0.f;
+        const float a = open(raw_gate[j].v[e], p), through = d[j][e] * unit[j][e], slope = through * weight[j][e];
+        sums[0][j][e] += through * a;
+        all += slope;
+        dgate[j][e] = p.sigmoid ? slope * a * (1.f - a) : slope;
+        d[j][e] *= weight[j][e] * a;
+      }
+    if (p.post) {
+      denormalise(d, unit, inverse, g, p.layer, p.one_dim, all);
+    } else if (p.gate && !p.each) {
+      float s[1] = {all};
+      g.sum(s);
+      all = s[0];
+    }
+    if (p.dy) put_row((T*)p.dy + r * p.ld_dy, d, at, in);
+    if (!p.dgate) continue;
+    if (p.each) {
+      put_row((T*)p.dgate + r * p.ld_dgate, dgate, at, in);
+    } else if (in && g.mine == 0u) {
+      const float a = open(raw_gate[0].v[0], p);
+      ((T*)p.dgate)[r * p.ld_dgate] = (T)(p.sigmoid ? all * a * (1.f - a) : all);
+    }
+  }
+  if (p.sums) leave_sums(sums, p.sums + (uint64_t)blockIdx.x * 2u * p.wide, p.wide, g, at, p.slots, columns);
+}
+
+// Adds up the workgroups' sums of columns, in their order, and makes gradients of them: of the first, times the scale, the
+// weight's; times the weight, the scale's; of the second the next weight's.
+struct SumArgs {
+  const float* sums;
+  const void *weight, *scale;
+  void *first, *second, *third;
+  uint32_t dim, wide, rows, n_sums;
+  uint32_t single, half;            // half: vectors that are not in 32 bits are in f16, not bf16
+  float number;
+};
+constexpr uint32_t kStrips = 16;
+__global__ __launch_bounds__(64 * kStrips) void k_sum_columns(SumArgs p) {
+  __shared__ float shared[kStrips][64];
+  const uint32_t lane = threadIdx.x % 64u, strip = threadIdx.x / 64u, c = blockIdx.x * 64u + lane, which = blockIdx.y;
+  const uint32_t each = (p.rows + kStrips - 1u) / kStrips, from = strip * each, to = from + each < p.rows ? from + each : p.rows;
+  float s = 0.f;
+  if (c < p.dim) {
+    const float* in = p.sums + which * p.wide + c;
+    const uint64_t step = (uint64_t)p.n_sums * p.wide;
+#pragma unroll 8
+    for (uint32_t r = from; r < to; ++r) s += in[r * step];
+  }
+  shared[strip][lane] = s;
+  __syncthreads();
+  if (strip || c >= p.dim) return;
+  s = 0.f;
+#pragma unroll
+  for (uint32_t i = 0; i < kStrips; ++i) s += shared[i][lane];
+  auto get = [&](const void* v, float none) { return !v ? none : p.single ? ((const float*)v)[c] : p.half ? (float)((const _Float16*)v)[c] : (float)((const __bf16*)v)[c]; };
+  auto set = [&](void* v, float x) {
+    if (!v) return;
+    if (p.single) ((float*)v)[c] = x;
+    else if (p.half) ((_Float16*)v)[c] = (_Float16)x;
+    else ((__bf16*)v)[c] = (__bf16)x;
+  };
+  if (which) {
+    set(p.third, s);
+  } else {
+    set(p.first, s * get(p.scale, p.number));
+    set(p.second, s * get(p.weight, 1.f));
+  }
+}
+
+// How rows go to lanes: `packs` of a lane, lanes of a row, rows a workgroup holds at a time, workgroups.
+struct Layout {
+  uint32_t packs, lanes, slots, blocks;
+  uint32_t threads() const { return lanes * slots; }
+};
+Layout lay_out(uint64_t rows, uint32_t dim, bool backward) {
+  Layout l;
+  const uint32_t packs = (uint32_t)ceil_div(dim, kPack);
+  l.packs = packs > kMostLanes ? 2 : 1;
+  const uint32_t need = (uint32_t)ceil_div(packs, l.packs);
+  l.lanes = 1;
+  while (l.lanes < need && l.lanes < 64u) l.lanes *= 2u;
+  if (need > 64u) l.lanes = (uint32_t)round_up(need, 64);
+  const uint32_t target = backward ? 512 : 256;
+  l.slots = l.lanes < target ? target / l.lanes : 1u;
+  while (l.lanes * l.slots % 64u) ++l.slots;
+  const uint64_t blocks = ceil_div(rows, l.slots), most = backward ? 512 : 2048;
+  l.blocks = (uint32_t)(blocks < most ? blocks : most);
+  return l;
+}
+
+uint32_t wide_of(uint32_t dim) { return (uint32_t)round_up(dim, kPack); }
+
+fbx_status check_types(fbx_dtype stream, fbx_dtype block, fbx_dtype vectors) {
+  if (!known(stream) || !known(block) || !known(vectors)) return refuse(FBX_E_ARG, "unknown dtype");
+  if (stream != block && stream != FBX_F32) return refuse(FBX_E_ARG, "the stream is of the block's type or f32");
+  if (vectors != block && vectors != FBX_F32) return refuse(FBX_E_ARG, "vectors are of the block's type or f32");
+  return FBX_OK;
+}
+fbx_status check_sizes(uint64_t records, uint32_t dim, fbx_norm_kind kind, double eps) {
+  if (records >> 40) return refuse(FBX_E_ARG, "records must be below 2^40");
+  if (!dim || dim > FBX_NORM_MOST) return refuse(FBX_E_ARG, "dim must be 1 .. FBX_NORM_MOST");
+  if (kind != FBX_NORM_RMS && kind != FBX_NORM_LAYER) return refuse(FBX_E_ARG, "unknown kind");
+  if (!((float)eps >= FLT_MIN && (float)eps <= FLT_MAX)) return refuse(FBX_E_ARG, "eps must be a positive number of 32 bits");
+  return FBX_OK;
+}
+// A matrix of `columns` elements a row.
+fbx_status check_matrix(const void* p, uint64_t ld, uint64_t columns, fbx_dtype t, uint64_t records, const char* null, const char* why) {
+  if (!p && records) return refuse(FBX_E_ARG, null);
+  if ((uintptr_t)p % size_of(t)) return refuse(FBX_E_ARG, "a matrix is not aligned to its elements");
+  if (ld < columns || ld >> 40) return refuse(FBX_E_ARG, why);
+  return FBX_OK;
+}
+fbx_status check_vectors(fbx_dtype t, uintptr_t all) {
+  return all % size_of(t) ? refuse(FBX_E_ARG, "a vector is not aligned to its elements") : FBX_OK;
+}
+fbx_status check_scratch(const void* d_scratch, uint64_t bytes, uint64_t need) {
+  if (need && (!d_scratch || (uintptr_t)d_scratch % 256u)) return refuse(FBX_E_ARG, "d_scratch is NULL or not 256-byte aligned");
+  return bytes < need ? refuse(FBX_E_NOMEM, "scratch too small: the scratch function gives its size") : FBX_OK;
+}
+
+fbx_status check(const fbx_norm* h) {
+  if (!h) return refuse(FBX_E_ARG, "h is NULL");
+  fbx_status st = check_types(h->stream, h->block, h->vectors);
+  if (st == FBX_OK) st = check_sizes(h->records, h->dim, h->kind, h->eps);
+  return st;
+}
+fbx_status check(const fbx_join* h) {
+  if (!h) return refuse(FBX_E_ARG, "h is NULL");
+  fbx_status st = check_types(h->stream, h->block, h->vectors);
+  if (st == FBX_OK) st = check_sizes(h->records, h->dim, h->kind, h->eps);
+  if (st != FBX_OK) return st;
+  if (h->gate_act != FBX_GATE_NONE && h->gate_act != FBX_GATE_SIGMOID) return refuse(FBX_E_ARG, "unknown gate_act");
+  if (h->d_gate && h->gate_columns != 1 && h->gate_columns != h->dim) return refuse(FBX_E_ARG, "gate_columns must be 1 or dim");
+  if (!h->post && h->d_weight) return refuse(FBX_E_ARG, "a weight is the norm's: none without post");
+  if (!isfinite((float)h->scale)) return refuse(FBX_E_ARG, "scale must be a finite number of 32 bits");
+  return FBX_OK;
+}
+
+template <template <class, class, int> class K, class A>
+void launch(const A& p, const Layout& l, fbx_dtype stream, fbx_dtype block, uint32_t lds, hipStream_t on) {
+  const dim3 grid(l.blocks), threads(l.threads());
+  auto go = [&](auto packs) {
+    constexpr int n = decltype(packs)::value;
+    if (stream == FBX_F32 && block == FBX_F32) launch_on(on, K<float, float, n>::kernel, grid, threads, lds, p);
+    else if (stream == FBX_F32 && block == FBX_F16) launch_on(on, K<float, _Float16, n>::kernel, grid, threads, lds, p);
+    else if (stream == FBX_F32) launch_on(on, K<float, __bf16, n>::kernel, grid, threads, lds, p);
+    else if (stream == FBX_F16) launch_on(on, K<_Float16, _Float16, n>::kernel, grid, threads, lds, p);
+    else launch_on(on, K<__bf16, __bf16, n>::kernel, grid, threads, lds, p);
+  };
+  if (l.packs == 1) go(std::integral_constant<int, 1>());
+  else go(std::integral_constant<int, 2>());
+}
+template <class R, class T, int kN> struct Norm { static constexpr auto kernel = k_norm<R, T, kN>; };
+template <class R, class T, int kN> struct NormGrad { static constexpr auto kernel = k_norm_grad<R, T, kN>; };
+template <class R, class T, int kN> struct Join { static constexpr auto kernel = k_join<R, T, kN>; };
+template <class R, class T, int kN> struct JoinGrad { static constexpr auto kernel = k_join_grad<R, T, kN>; };
+
+void sum_columns(SumArgs& s, uint32_t dim, uint32_t blocks, uint32_t n_sums, fbx_dtype vectors, hipStream_t stream) {
+  s.dim = dim;
+  s.wide = wide_of(dim);
+  s.rows = blocks;
+  s.n_sums = n_sums;
+  s.single = vectors == FBX_F32;
+  s.half = vectors == FBX_F16;
+  launch_on(stream, k_sum_columns, dim3((uint32_t)ceil_div(dim, 64), n_sums), dim3(64 * kStrips), 0, s);
+}
+
+NormArgs args_of(const fbx_norm* h, const Layout& l) {
+  NormArgs p{};
+  p.x = h->d_x;
+  p.ld_x = h->ld_x;
+  p.weight = h->d_weight;
+  p.rows = h->records;
+  p.dim = h->dim;
+  p.wide = wide_of(h->dim);
+  p.lanes = l.lanes;
+  p.slots = l.slots;
+  p.layer = h->kind == FBX_NORM_LAYER;
+  p.single = h->vectors == FBX_F32;
+  p.eps = (float)h->eps;
+  p.one_dim = (float)(1.0 / h->dim);
+  return p;
+}
+JoinArgs args_of(const fbx_join* h, const Layout& l) {
+  JoinArgs p{};
+  p.x = h->d_x;
+  p.ld_x = h->ld_x;
+  p.y = h->d_y;
+  p.ld_y = h->ld_y;
+  p.gate = h->d_gate;
+  p.ld_gate = h->ld_gate;
+  p.weight = h->d_weight;
+  p.scale = h->d_scale;
+  p.next_weight = h->d_next_weight;
+  p.rows = h->records;
+  p.dim = h->dim;
+  p.wide = wide_of(h->dim);
+  p.lanes = l.lanes;
+  p.slots = l.slots;
+  p.layer = h->kind == FBX_NORM_LAYER;
+  p.single = h->vectors == FBX_F32;
+  p.post = h->post != 0;
+  p.each = h->gate_columns != 1;
+  p.sigmoid = h->gate_act == FBX_GATE_SIGMOID;
+  p.eps = (float)h->eps;
+  p.one_dim = (float)(1.0 / h->dim);
+  p.number = (float)h->scale;
+  return p;
+}
+uint32_t lds_of(const Layout& l, uint32_t dim, uint32_t sums) { return l.slots > 1 ? wide_of(dim) * sums * 4u : 0u; }
+uint64_t sums_bytes(uint64_t records, uint32_t dim, uint32_t sums) { return round_up((uint64_t)lay_out(records, dim, true).blocks * wide_of(dim) * sums * 4u, 256); }
+
+}  // namespace
+}  // namespace train
+}  // namespace fbx
+
+using namespace fbx::train;
+
+extern "C" fbx_status fbx_norm_forward(const fbx_norm* h, void* d_out, uint64_t ld_out, void* hip_stream) {
+  fbx_status st = check(h);
+  if (st == FBX_OK) st = check_matrix(h->d_x, h->ld_x, h->dim, h->stream, h->records, "d_x is NULL", "ld_x is smaller than dim, or 2^40 or more");
+  if (st == FBX_OK) st = check_matrix(d_out, ld_out, h->dim, h->block, h->records, "d_out is NULL", "ld_out is smaller than dim, or 2^40 or more");
+  if (st == FBX_OK) st = check_vectors(h->vectors, (uintptr_t)h->d_weight);
+  if (st != FBX_OK || !h->records) return st;
+  const Layout l = lay_out(h->records, h->dim, false);
+  NormArgs p = args_of(h, l);
+  p.out = d_out;
+  p.ld_out = ld_out;
+  launch<Norm>(p, l, h->stream, h->block, 0, (hipStream_t)hip_stream);
+  return launched();
+}
+
+extern "C" fbx_status fbx_norm_scratch(const fbx_norm* h, uint64_t* bytes) {
+  const fbx_status st = check(h);
+  if (st != FBX_OK) return st;
+  if (!bytes) return refuse(FBX_E_ARG, "bytes is NULL");
+  *bytes = sums_bytes(h->records, h->dim, 1);
+  return FBX_OK;
+}
+
+extern "C" fbx_status fbx_norm_backward(const fbx_norm* h, const void* d_dy, uint64_t ld_dy, void* d_dx, uint64_t ld_dx, void* d_dweight, void* d_scratch,
+                                        uint64_t scratch_bytes, void* hip_stream) {
+  fbx_status st = check(h);
+  if (st == FBX_OK) st = check_matrix(h->d_x, h->ld_x, h->dim, h->stream, h->records, "d_x is NULL", "ld_x is smaller than dim, or 2^40 or more");
+  if (st == FBX_OK) st = check_matrix(d_dy, ld_dy, h->dim, h->block, h->records, "d_dy is NULL", "ld_dy is smaller than dim, or 2^40 or more");
+  if (st == FBX_OK && d_dx) st = check_matrix(d_dx, ld_dx, h->dim, h->stream, h->records, "", "ld_dx is smaller than dim, or 2^40 or more");
+  if (st == FBX_OK) st = check_vectors(h->vectors, (uintptr_t)h->d_weight | (uintptr_t)d_dweight);
+  if (st == FBX_OK && d_dweight) st = check_scratch(d_scratch, scratch_bytes, sums_bytes(h->records, h->dim, 1));
+  if (st != FBX_OK) return st;
+  if (!d_dx && !d_dweight) return FBX_OK;
+  const hipStream_t stream = (hipStream_t)hip_stream;
+  const Layout l = lay_out(h->records, h->dim, true);
+  if (h->records) {
+    NormArgs p = args_of(h, l);
+    p.dy = d_dy;
+    p.ld_dy = ld_dy;
+    p.dx = d_dx;
+    p.ld_dx = ld_dx;
+    p.sums = d_dweight ? (float*)d_scratch : nullptr;
+    launch<NormGrad>(p, l, h->stream, h->block, lds_of(l, h->dim, 1), stream);
+  }
+  if (d_dweight) {
+    SumArgs s{};
+    s.sums = (const float*)d_scratch;
+    s.first = d_dweight;
+    s.number = 1.f;
+    sum_columns(s, h->dim, l.blocks, 1, h->vectors, stream);
+  }
+  return launched();
+}
+
+extern "C" fbx_status fbx_join_forward(const fbx_join* h, void* d_out, uint64_t ld_out, void* d_next, uint64_t ld_next, void* hip_stream) {
+  fbx_status st = check(h);
+  if (st == FBX_OK) st = check_matrix(h->d_x, h->ld_x, h->dim, h->stream, h->records, "d_x is NULL", "ld_x is smaller than dim, or 2^40 or more");
+  if (st == FBX_OK) st = check_matrix(h->d_y, h->ld_y, h->dim, h->block, h->records, "d_y is NULL", "ld_y is smaller than dim, or 2^40 or more");
+  if (st == FBX_OK && h->d_gate) st = check_matrix(h->d_gate, h->ld_gate, h->gate_columns, h->block, h->records, "", "ld_gate is smaller than gate_columns, or 2^40 or more");
+  if (st == FBX_OK) st = check_matrix(d_out, ld_out, h->dim, h->stream, h->records, "d_out is NULL", "ld_out is smaller than dim, or 2^40 or more");
+  if (st == FBX_OK && d_next) st = check_matrix(d_next, ld_next, h->dim, h->block, h->records, "", "ld_next is smaller than dim, or 2^40 or more");
+  if (st == FBX_OK) st = check_vectors(h->vectors, (uintptr_t)h->d_weight | (uintptr_t)h->d_scale | (uintptr_t)h->d_next_weight);
+  if (st != FBX_OK || !h->records) return st;
+  const Layout l = lay_out(h->records, h->dim, false);
+  JoinArgs p = args_of(h, l);
+  p.out = d_out;
+  p.ld_out = ld_out;
+  p.next = d_next;
+  p.ld_next = ld_next;
+  p.then = d_next != nullptr;
+  launch<Join>(p, l, h->stream, h->block, 0, (hipStream_t)hip_stream);
+  return launched();
+}
+
+extern "C" fbx_status fbx_join_scratch(const fbx_join* h, uint64_t* bytes) {
+  const fbx_status st = check(h);
+  if (st != FBX_OK) return st;
+  if (!bytes) return refuse(FBX_E_ARG, "bytes is NULL");
+  *bytes = sums_bytes(h->records, h->dim, 2);
+  return FBX_OK;
+}
+
+extern "C" fbx_status fbx_join_backward(const fbx_join* h, const fbx_join_gradients* g, void* d_scratch, uint64_t scratch_bytes, void* hip_stream) {
+  fbx_status st = check(h);
+  if (st != FBX_OK) return st;
+  if (!g) return refuse(FBX_E_ARG, "g is NULL");
+  const uint64_t n = h->records;
+  if (!g->d_dout && !g->d_dnext && n) return refuse(FBX_E_ARG, "d_dout and d_dnext are both NULL");
+  const bool then = g->d_dnext != nullptr, sums = g->d_dweight || g->d_dscale || g->d_dnext_weight;
+  st = check_matrix(h->d_y, h->ld_y, h->dim, h->block, n, "d_y is NULL", "ld_y is smaller than dim, or 2^40 or more");
+  if (st == FBX_OK && then) st = check_matrix(h->d_x, h->ld_x, h->dim, h->stream, n, "d_x is NULL", "ld_x is smaller than dim, or 2^40 or more");
+  if (st == FBX_OK && h->d_gate) st = check_matrix(h->d_gate, h->ld_gate, h->gate_columns, h->block, n, "", "ld_gate is smaller than gate_columns, or 2^40 or more");
+  if (st == FBX_OK && g->d_dout) st = check_matrix(g->d_dout, g->ld_dout, h->dim, h->stream, n, "", "ld_dout is smaller than dim, or 2^40 or more");
+  if (st == FBX_OK && then) st = check_matrix(g->d_dnext, g->ld_dnext, h->dim, h->block, n, "", "ld_dnext is smaller than dim, or 2^40 or more");
+  if (st == FBX_OK && g->d_dx) st = check_matrix(g->d_dx, g->ld_dx, h->dim, h->stream, n, "", "ld_dx is smaller than dim, or 2^40 or more");
+  if (st == FBX_OK && g->d_dy) st = check_matrix(g->d_dy, g->ld_dy, h->dim, h->block, n, "", "ld_dy is smaller than dim, or 2^40 or more");
+  if (st == FBX_OK && g->d_dgate) {
+    if (!h->d_gate) return refuse(FBX_E_ARG, "a gate's gradient without a gate");
+    st = check_matrix(g->d_dgate, g->ld_dgate, h->gate_columns, h->block, n, "", "ld_dgate is smaller than gate_columns, or 2^40 or more");
+  }
+  if (st == FBX_OK)
+    st = check_vectors(h->vectors, (uintptr_t)h->d_weight | (uintptr_t)h->d_scale | (uintptr_t)h->d_next_weight | (uintptr_t)g->d_dweight | (uintptr_t)g->d_dscale | (uintptr_t)g->d_dnext_weight);
+  if (st == FBX_OK && sums) st = check_scratch(d_scratch, scratch_bytes, sums_bytes(n, h->dim, 2));
+  if (st != FBX_OK) return st;
+  if (!g->d_dx && !g->d_dy && !g->d_dgate && !sums) return FBX_OK;
+  const hipStream_t stream = (hipStream_t)hip_stream;
+  const Layout l = lay_out(n, h->dim, true);
+  if (n) {
+    JoinArgs p = args_of(h, l);
+    p.dout = g->d_dout;
+    p.ld_dout = g->ld_dout;
+    p.dnext = g->d_dnext;
+    p.ld_dnext = g->ld_dnext;
+    p.dx = g->d_dx;
+    p.ld_dx = g->ld_dx;
+    p.dy = g->d_dy;
+    p.ld_dy = g->ld_dy;
+    p.dgate = g->d_dgate;
+    p.ld_dgate = g->ld_dgate;
+    p.then = then;
+    p.sums = sums ? (float*)d_scratch : nullptr;
+    launch<JoinGrad>(p, l, h->stream, h->block, lds_of(l, h->dim, 2), stream);
+  }
+  if (sums) {
+    SumArgs s{};
+    s.sums = (const float*)d_scratch;
+    s.weight = h->d_weight;
+    s.scale = h->d_scale;
+    s.number = (float)h->scale;
+    s.first = g->d_dweight;
+    s.second = g->d_dscale;
+    s.third = g->d_dnext_weight;
+    sum_columns(s, h->dim, l.blocks, 2, h->vectors, stream);
+  }
+  return launched();
+}
