@@ -159,6 +159,163 @@ typedef struct {
 fbx_status fbx_adamw_step(const fbx_adamw* h, const fbx_adamw_tensor* tensors, uint32_t n_tensors,
                           void* hip_stream);
 
+/*
+ * Norms of rows: of a row v of dim elements
+ *   N(v) = v / sqrt(mean(v^2) + eps)              FBX_NORM_RMS
+ *   N(v) = (v - m) / sqrt(mean((v - m)^2) + eps), m = mean(v)     FBX_NORM_LAYER
+ * in 32 bits; rows whose squares leave the range of 32 bits are the caller's to scale.
+ *
+ *   stream  : type of the residual stream (x, and what is added to it); the block's, or FBX_F32
+ *   block   : type of what a block reads and returns
+ *   vectors : type of weights and scales, of dim adjacent elements each; the block's, or FBX_F32
+ *   eps     : above 0
+ * Limits: 1 <= dim <= FBX_NORM_MOST, records and strides < 2^40.
+ *
+ * fbx_norm_forward: out = N(x) * weight, rounded to the block's type (weight NULL: 1)
+ * fbx_norm_backward, given dy of the block's type: dx, of the stream's type, and dweight, of the vectors';
+ *   either may be NULL.  Scratch is for dweight.
+ * Errors: FBX_E_ARG, FBX_E_NOMEM, FBX_E_HIP.
+ */
+#define FBX_NORM_MOST 16384u
+typedef enum { FBX_NORM_RMS = 0, FBX_NORM_LAYER = 1 } fbx_norm_kind;
+typedef struct {
+  uint64_t records;
+  uint32_t dim;
+  fbx_norm_kind kind;
+  fbx_dtype stream, block, vectors;
+  double eps;
+  const void* d_x;      /* DEVICE, of the stream's type */
+  const void* d_weight; /* DEVICE or NULL */
+  uint64_t ld_x;
+} fbx_norm;
+fbx_status fbx_norm_forward(const fbx_norm* h, void* d_out, uint64_t ld_out, void* hip_stream);
+fbx_status fbx_norm_scratch(const fbx_norm* h, uint64_t* bytes);
+fbx_status fbx_norm_backward(const fbx_norm* h, const void* d_dy, uint64_t ld_dy, void* d_dx, uint64_t ld_dx,
+                             void* d_dweight, void* d_scratch, uint64_t scratch_bytes, void* hip_stream);
+
+/*
+ * What joins a block's result y to the residual stream x, with the norm that the next block begins with:
+ *   out  = x + scale * act(gate) * N(y) * weight      (post = 0: y in the place of N(y) * weight)
+ *   next = N(out) * next_weight                       (of out before it is rounded)
+ *   gate   : DEVICE or NULL (1): of the block's type, gate_columns = 1 (a gate a record) or dim (one an element)
+ *   act    : FBX_GATE_NONE: the gate as it is; FBX_GATE_SIGMOID: 1 / (1 + e^-gate)
+ *   d_scale: DEVICE or NULL: then `scale`, for all elements
+ *   d_weight, d_next_weight: DEVICE or NULL (1)
+ * Types and limits as for fbx_norm; x, out, their gradients are of the stream's type, y, gate, next and theirs of the block's,
+ * gradients of vectors of the vectors'.
+ *
+ * fbx_join_forward: d_next may be NULL: not computed.
+ * fbx_join_backward: from d_dout and d_dnext (one of them may be NULL: zero; without d_dnext x is not read) whichever
+ *   gradients are not NULL.  Between x and a gradient nothing is rounded to fewer than 32 bits.  Scratch is for the vectors'
+ *   gradients.
+ * Errors: FBX_E_ARG, FBX_E_NOMEM, FBX_E_HIP.
+ */
+typedef enum { FBX_GATE_NONE = 0, FBX_GATE_SIGMOID = 1 } fbx_gate_act;
+typedef struct {
+  uint64_t records;
+  uint32_t dim;
+  fbx_norm_kind kind;
+  fbx_dtype stream, block, vectors;
+  fbx_gate_act gate_act;
+  uint32_t gate_columns;
+  int post;
+  double eps, scale;
+  const void* d_x;
+  const void* d_y;
+  const void* d_gate;
+  const void* d_weight;
+  const void* d_scale;
+  const void* d_next_weight;
+  uint64_t ld_x, ld_y, ld_gate;
+} fbx_join;
+typedef struct {
+  const void* d_dout;
+  const void* d_dnext;
+  void* d_dx;
+  void* d_dy;
+  void* d_dgate;
+  void* d_dweight;
+  void* d_dscale;
+  void* d_dnext_weight;
+  uint64_t ld_dout, ld_dnext, ld_dx, ld_dy, ld_dgate;
+} fbx_join_gradients;
+fbx_status fbx_join_forward(const fbx_join* h, void* d_out, uint64_t ld_out, void* d_next, uint64_t ld_next,
+                            void* hip_stream);
+fbx_status fbx_join_scratch(const fbx_join* h, uint64_t* bytes);
+fbx_status fbx_join_backward(const fbx_join* h, const fbx_join_gradients* g, void* d_scratch,
+                             uint64_t scratch_bytes, void* hip_stream);
+
+/*
+ * Orthogonalised matrices.  Of a matrix U with at most as many rows as columns (of others: of its transpose, and the result's
+ * transpose)
+ *   X = U / (|U| + eps), |U| the root of the sum of its elements' squares
+ *   for each of `steps` triples (a, b, c):  A = X X^T,  B = b A + c A^2,  X = a X + B X
+ * the Newton-Schulz iteration of Muon, whose singular values end near 1 for its coefficients
+ * (3.4445, -4.7750, 2.0315), five times.  A matrix of zeros stays one; one with an element that is not finite becomes NaN.
+ *
+ * Precision: X, A and B are held in two parts of 16 bits, the second what the first leaves (22 bits in all), scaled so that no
+ * first part overflows; sums are in 32 bits.
+ *   exact = 1: products are of both parts of both sides (all but second by second): errors like those of
+ *     products in 32 bits.
+ *   exact = 0: products are of first parts, a third of the work; a X is of both.  The result's error is that of
+ *     rounding it to bf16: about 1.7e-3 of its size, twice that for small matrices.
+ *   exact = FBX_EXACT_BY_SIZE: 0 for results in bf16 of matrices of more than 256 rows and columns, else 1.
+ *
+ *   coefficients : HOST, steps triples
+ *   matrices     : HOST, n entries; elements of a row are adjacent; results may not overlap
+ * Limits: 1 <= rows, columns <= FBX_ORTHO_MOST; 1 <= steps <= 64; coefficients whose iteration takes a singular value from
+ * [0, 1] above 3, or b s^2 + c s^4 of one beyond 256, are refused.
+ * Errors: FBX_E_ARG, FBX_E_NOMEM, FBX_E_HIP.
+ */
+#define FBX_ORTHO_MOST 65536u
+#define FBX_EXACT_BY_SIZE 2u
+typedef struct {
+  const void* d_u;
+  void* d_out;
+  uint64_t ld_u, ld_out;
+  uint32_t rows, columns;
+} fbx_ortho_matrix;
+typedef struct {
+  fbx_dtype in, out;
+  uint32_t exact, steps;
+  const double* coefficients;
+  double eps;
+} fbx_ortho;
+fbx_status fbx_ortho_scratch(const fbx_ortho* h, const fbx_ortho_matrix* matrices, uint32_t n, uint64_t* bytes);
+fbx_status fbx_orthogonalise(const fbx_ortho* h, const fbx_ortho_matrix* matrices, uint32_t n, void* d_scratch,
+                             uint64_t scratch_bytes, void* hip_stream);
+
+/*
+ * fbx_muon_step — one step of Muon over all matrices of a list, in place:
+ *   g = grad_scale * grad
+ *   m = momentum * m + g
+ *   u = g + momentum * m   (nesterov; else m)
+ *   p = p (1 - lr weight_decay) - lr factor O(u)
+ * O as fbx_orthogonalise makes it, of `ortho` (whose `in` and `out` are ignored; the weights' type stands for `out`); p rounded to its type once.
+ *   d_m    : DEVICE, floats
+ *   d_copy : DEVICE or NULL: receives the new weights in copy_dtype as well (for weights kept in f32)
+ *   factor : of the matrix: an orthogonal matrix's elements have a mean square of 1 / max(rows, columns)
+ * Elements of a matrix are adjacent.
+ * Errors: FBX_E_ARG, FBX_E_NOMEM, FBX_E_HIP.
+ */
+typedef struct {
+  void* d_param;
+  const void* d_grad;
+  void* d_m;
+  void* d_copy;
+  uint32_t rows, columns;
+  double factor;
+} fbx_muon_matrix;
+typedef struct {
+  fbx_ortho ortho;
+  fbx_dtype param_dtype, grad_dtype, copy_dtype;
+  int nesterov;
+  double lr, momentum, weight_decay, grad_scale;
+} fbx_muon;
+fbx_status fbx_muon_scratch(const fbx_muon* h, const fbx_muon_matrix* matrices, uint32_t n, uint64_t* bytes);
+fbx_status fbx_muon_step(const fbx_muon* h, const fbx_muon_matrix* matrices, uint32_t n, void* d_scratch,
+                         uint64_t scratch_bytes, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

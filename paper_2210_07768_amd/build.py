@@ -14,8 +14,9 @@ NATIVE_SOURCE = os.path.join(CSRC, "fbx_native.cpp")
 TRAIN_NATIVE = os.path.join(_HERE, "_train.so")     # the same for the trainer's operators
 TRAIN_NATIVE_SOURCE = os.path.join(CSRC, "train", "train_native.cpp")
 SOURCES = ["fbx_plan.cpp", "fbx_api.cpp", "fbx_jit.cpp", "fbx_support.hip", "fbx_walk.hip", "fbx_tile.hip", "fbx_clean.hip",
-           "train/train_embed.hip", "train/train_embed_grad.hip", "train/train_gated.hip", "train/train_adamw.hip"]
-HEADERS = ["fbx_internal.h", "fbx_device.h", "fbx_arena.h", "fbx_lists.h", "fbx_split.h", "train/train_common.h",
+           "train/train_embed.hip", "train/train_embed_grad.hip", "train/train_gated.hip", "train/train_adamw.hip",
+           "train/train_norm.hip", "train/train_muon.hip"]
+HEADERS = ["fbx_internal.h", "fbx_device.h", "fbx_arena.h", "fbx_lists.h", "fbx_split.h", "train/train_common.h", "train/train_tiles.h",
            os.path.join(_ROOT, "include", "fbx_train.h"), os.path.join(_ROOT, "include", "fbx.h")]
 
 

@@ -6,8 +6,10 @@
 
 #include <ATen/ATen.h>
 #include <c10/core/GradMode.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
 #include <string>
 #include <vector>
 
@@ -24,6 +26,16 @@ struct {
   decltype(&fbx_gated_forward) gated_forward;
   decltype(&fbx_gated_backward) gated_backward;
   decltype(&fbx_adamw_step) adamw_step;
+  decltype(&fbx_norm_forward) norm_forward;
+  decltype(&fbx_norm_scratch) norm_scratch;
+  decltype(&fbx_norm_backward) norm_backward;
+  decltype(&fbx_join_forward) join_forward;
+  decltype(&fbx_join_scratch) join_scratch;
+  decltype(&fbx_join_backward) join_backward;
+  decltype(&fbx_ortho_scratch) ortho_scratch;
+  decltype(&fbx_orthogonalise) orthogonalise;
+  decltype(&fbx_muon_scratch) muon_scratch;
+  decltype(&fbx_muon_step) muon_step;
 } g;
 PyObject *g_error = nullptr, *g_stream = nullptr;  // FbxError; torch's function from a device to its current stream
 PyObject* g_memory = nullptr;  // torch.OutOfMemoryError
@@ -420,12 +432,382 @@ PyObject* adamw(PyObject*, PyObject* args) {
   });
 }
 
-// bind(FbxError, torch.OutOfMemoryError, stream function, addresses of the library's functions in the order of `g`)
+fbx_dtype code_of(PyObject* dtype, fbx_dtype none) {
+  if (dtype == Py_None) return none;
+  if (!THPDtype_Check(dtype)) bad("dtype must be a torch.dtype");
+  const auto s = reinterpret_cast<THPDtype*>(dtype)->scalar_type;
+  if (s == at::kFloat) return FBX_F32;
+  if (s == at::kHalf) return FBX_F16;
+  if (s == at::kBFloat16) return FBX_BF16;
+  bad(std::string(c10::toString(s)) + ": float32, float16 and bfloat16 are supported");
+}
+at::ScalarType type_of(fbx_dtype t) { return t == FBX_F32 ? at::kFloat : t == FBX_F16 ? at::kHalf : at::kBFloat16; }
+const at::Tensor* maybe(PyObject* o, const char* name) { return o == Py_None ? nullptr : &input(o, name); }
+
+// Rows of a batch: n x columns, on the device of the others.
+uint64_t rows_of(const at::Tensor& t, const char* name, fbx_dtype type, const at::Tensor& like, int64_t n, int64_t columns) {
+  if (t.device() != like.device()) bad(std::string(name) + " must be on the device of the others");
+  if (code(t) != type) bad(std::string(name) + " must be of type " + c10::toString(type_of(type)));
+  return matrix(t, name, nullptr, n, columns);
+}
+// A gradient as autograd gives it may be one element seen many times.
+at::Tensor gradient_rows(const at::Tensor& t) {
+  const bool fine = t.dim() != 2 || ((t.size(1) <= 1 || t.stride(1) == 1) && (t.size(0) <= 1 || t.stride(0) >= t.size(1)));
+  return fine ? t : t.contiguous();
+}
+// Vectors of weights: of dim elements, of one type.
+struct Vectors {
+  const at::Tensor& like;
+  int64_t dim;
+  bool any = false;
+  fbx_dtype type = FBX_F32;
+  const void* operator()(const at::Tensor* t, const char* name) {
+    if (!t) return nullptr;
+    if (t->dim() != 1 || t->size(0) != dim || !t->is_contiguous()) bad(std::string(name) + " must be a vector of " + std::to_string(dim) + " adjacent elements");
+    if (t->device() != like.device()) bad(std::string(name) + " must be on the device of the others");
+    const fbx_dtype c = code(*t);
+    if (any && c != type) bad("weights and scales must be of one type");
+    any = true;
+    type = c;
+    return t->data_ptr();
+  }
+};
+uint32_t width(const at::Tensor& x, const char* name) {
+  if (x.dim() != 2) bad(std::string(name) + " must have two dimensions");
+  if (x.size(1) < 1 || x.size(1) > FBX_NORM_MOST) bad(std::string(name) + " must have 1 .. " + std::to_string(FBX_NORM_MOST) + " columns");
+  return static_cast<uint32_t>(x.size(1));
+}
+
+struct NormCall {
+  fbx_norm a{};
+  const at::Tensor& x;
+  const at::Tensor* weight;
+  NormCall(PyObject* x_o, PyObject* weight_o, PyObject* dtype, int kind, double eps) : x(input(x_o, "x")), weight(maybe(weight_o, "weight")) {
+    a.stream = code(x);
+    a.block = code_of(dtype, a.stream);
+    a.dim = width(x, "x");
+    a.records = x.size(0);
+    a.kind = static_cast<fbx_norm_kind>(kind);
+    a.eps = eps;
+    a.ld_x = matrix(x, "x");
+    Vectors v{x, x.size(1)};
+    a.d_weight = v(weight, "weight");
+    a.vectors = v.type;
+    a.d_x = on_gpu(x);
+  }
+};
+
+// norm(x, weight, dtype, kind, eps, out)
+PyObject* norm(PyObject*, PyObject* args) {
+  PyObject *x, *weight, *dtype, *out_o;
+  int kind;
+  double eps;
+  if (!PyArg_ParseTuple(args, "OOOidO", &x, &weight, &dtype, &kind, &eps, &out_o)) return nullptr;
+  return guarded([&] {
+    const NormCall c(x, weight, dtype, kind, eps);
+    if (out_o != Py_None) rows_of(result(out_o), "out", c.a.block, c.x, c.a.records, c.a.dim);
+    const c10::DeviceGuard guard(c.x.device());
+    at::Tensor out = out_o == Py_None ? at::empty({c.x.size(0), c.x.size(1)}, c.x.options().dtype(type_of(c.a.block)).memory_format(c10::nullopt)) : tensor(out_o, "out");
+    check(g.norm_forward(&c.a, out.data_ptr(), matrix(out, "out"), stream_of(c.x)));
+    if (out_o != Py_None) changed(out);
+    return wrap(std::move(out));
+  });
+}
+
+// norm_backward(dy, x, weight, kind, eps, need_dx, need_dw)
+PyObject* norm_backward(PyObject*, PyObject* args) {
+  PyObject *dy_o, *x, *weight;
+  int kind, need_dx, need_dw;
+  double eps;
+  if (!PyArg_ParseTuple(args, "OOOidpp", &dy_o, &x, &weight, &kind, &eps, &need_dx, &need_dw)) return nullptr;
+  return guarded([&]() -> PyObject* {
+    NormCall c(x, weight, Py_None, kind, eps);
+    const at::Tensor dy = gradient_rows(input(dy_o, "dy"));
+    c.a.block = code(dy);
+    const uint64_t ld_dy = rows_of(dy, "dy", c.a.block, c.x, c.a.records, c.a.dim);
+    const c10::DeviceGuard guard(c.x.device());
+    at::Tensor dx, dw;
+    if (need_dx) dx = at::empty({c.x.size(0), c.x.size(1)}, c.x.options());
+    if (need_dw && c.weight) dw = at::empty({c.x.size(1)}, c.weight->options());
+    uint64_t need = 0;
+    if (dw.defined()) check(g.norm_scratch(&c.a, &need));
+    const at::Tensor s = scratch(need, c.x);
+    check(g.norm_backward(&c.a, dy.data_ptr(), ld_dy, pointer(dx), c.a.dim, pointer(dw), pointer(s), need, stream_of(c.x)));
+    PyObject* out = PyTuple_New(2);
+    if (!out) throw PythonError{};
+    PyTuple_SET_ITEM(out, 0, wrap(std::move(dx)));
+    PyTuple_SET_ITEM(out, 1, wrap(std::move(dw)));
+    return out;
+  });
+}
+
+struct JoinCall {
+  fbx_join a{};
+  const at::Tensor &x, &y;
+  const at::Tensor *weight, *gate, *scale = nullptr, *next_weight;
+  // what: x, y, weight, gate, scale, next_weight
+  JoinCall(PyObject* const* what, int post, int gate_act, int kind, double eps)
+      : x(input(what[0], "x")), y(input(what[1], "y")), weight(maybe(what[2], "weight")), gate(maybe(what[3], "gate")), next_weight(maybe(what[5], "next_weight")) {
+    a.stream = code(x);
+    a.block = code(y);
+    if (a.stream != a.block && a.stream != FBX_F32) bad("x must be of y's type or float32");
+    a.dim = width(x, "x");
+    a.records = x.size(0);
+    a.kind = static_cast<fbx_norm_kind>(kind);
+    a.gate_act = static_cast<fbx_gate_act>(gate_act);
+    a.post = post;
+    a.eps = eps;
+    a.ld_x = matrix(x, "x");
+    a.ld_y = rows_of(y, "y", a.block, x, a.records, a.dim);
+    a.gate_columns = a.dim;
+    if (gate) {
+      if (gate->dim() == 2 && gate->size(1) == 1) a.gate_columns = 1;
+      a.ld_gate = rows_of(*gate, "gate", a.block, x, a.records, a.gate_columns);
+      a.d_gate = gate->data_ptr();
+    }
+    Vectors v{x, x.size(1)};
+    a.d_weight = v(weight, "weight");
+    if (THPVariable_Check(what[4])) {
+      scale = &input(what[4], "scale");
+      a.d_scale = v(scale, "scale");
+    } else {
+      a.scale = PyFloat_AsDouble(what[4]);
+      if (a.scale == -1.0 && PyErr_Occurred()) throw PythonError{};
+    }
+    a.d_next_weight = v(next_weight, "next_weight");
+    a.vectors = v.type;
+    a.d_y = y.data_ptr();
+    a.d_x = on_gpu(x);
+  }
+};
+
+// join(x, y, weight, gate, scale, next_weight, post, then, gate_act, kind, eps, out, out_next)
+PyObject* join(PyObject*, PyObject* args) {
+  PyObject *what[6], *out_o[2];
+  int post, then, gate_act, kind;
+  double eps;
+  if (!PyArg_ParseTuple(args, "OOOOOOppiidOO", &what[0], &what[1], &what[2], &what[3], &what[4], &what[5], &post, &then, &gate_act, &kind, &eps, &out_o[0], &out_o[1])) return nullptr;
+  return guarded([&]() -> PyObject* {
+    const JoinCall c(what, post, gate_act, kind, eps);
+    if (!then && (c.next_weight || out_o[1] != Py_None)) bad("next_weight and out_next are of the next norm: none without then");
+    const fbx_dtype types[2] = {c.a.stream, c.a.block};
+    at::Tensor out[2];
+    for (int i = 0; i < 2; ++i)
+      if (out_o[i] != Py_None) rows_of(result(out_o[i]), i ? "out_next" : "out", types[i], c.x, c.a.records, c.a.dim);
+    const c10::DeviceGuard guard(c.x.device());
+    for (int i = 0; i < 1 + then; ++i)
+      out[i] = out_o[i] == Py_None ? at::empty({c.x.size(0), c.x.size(1)}, c.x.options().dtype(type_of(types[i])).memory_format(c10::nullopt)) : tensor(out_o[i], "out");
+    check(g.join_forward(&c.a, out[0].data_ptr(), matrix(out[0], "out"), pointer(out[1]), then ? matrix(out[1], "out_next") : 0, stream_of(c.x)));
+    for (int i = 0; i < 2; ++i)
+      if (out_o[i] != Py_None) changed(out[i]);
+    if (!then) return wrap(std::move(out[0]));
+    PyObject* both = PyTuple_New(2);
+    if (!both) throw PythonError{};
+    for (int i = 0; i < 2; ++i) PyTuple_SET_ITEM(both, i, wrap(std::move(out[i])));
+    return both;
+  });
+}
+
+// join_backward(dout, dnext, x, y, weight, gate, scale, next_weight, post, gate_act, kind, eps, need): the gradients of x, y, weight,
+// gate, scale and next_weight, those whose bit of need is set and that there are
+PyObject* join_backward(PyObject*, PyObject* args) {
+  PyObject *given[2], *what[6];
+  int post, gate_act, kind;
+  unsigned int need;
+  double eps;
+  if (!PyArg_ParseTuple(args, "OOOOOOOOpiidI", &given[0], &given[1], &what[0], &what[1], &what[2], &what[3], &what[4], &what[5], &post, &gate_act, &kind, &eps, &need)) return nullptr;
+  return guarded([&]() -> PyObject* {
+    const JoinCall c(what, post, gate_act, kind, eps);
+    if (given[0] == Py_None && given[1] == Py_None) bad("dout or dnext is needed");
+    fbx_join_gradients d{};
+    at::Tensor in[2];
+    const c10::DeviceGuard guard(c.x.device());
+    for (int i = 0; i < 2; ++i)
+      if (given[i] != Py_None) {
+        in[i] = gradient_rows(input(given[i], i ? "dnext" : "dout"));
+        (i ? d.ld_dnext : d.ld_dout) = rows_of(in[i], i ? "dnext" : "dout", i ? c.a.block : c.a.stream, c.x, c.a.records, c.a.dim);
+      }
+    // (of no records: there is nothing to point to, but what is given counts)
+    d.d_dout = pointer(in[0]);
+    d.d_dnext = pointer(in[1]);
+    const at::Tensor* of[6] = {&c.x, &c.y, c.weight, c.gate, c.scale, c.next_weight};
+    at::Tensor out[6];
+    for (int i = 0; i < 6; ++i)
+      if (of[i] && need >> i & 1u) out[i] = at::empty(of[i]->sizes(), of[i]->options());
+    d.d_dx = pointer(out[0]);
+    d.d_dy = pointer(out[1]);
+    d.d_dweight = pointer(out[2]);
+    d.d_dgate = pointer(out[3]);
+    d.d_dscale = pointer(out[4]);
+    d.d_dnext_weight = pointer(out[5]);
+    d.ld_dx = d.ld_dy = c.a.dim;
+    d.ld_dgate = c.a.gate_columns;
+    uint64_t bytes = 0;
+    if (d.d_dweight || d.d_dscale || d.d_dnext_weight) check(g.join_scratch(&c.a, &bytes));
+    const at::Tensor s = scratch(bytes, c.x);
+    check(g.join_backward(&c.a, &d, pointer(s), bytes, stream_of(c.x)));
+    PyObject* all = PyTuple_New(6);
+    if (!all) throw PythonError{};
+    for (int i = 0; i < 6; ++i) PyTuple_SET_ITEM(all, i, wrap(std::move(out[i])));
+    return all;
+  });
+}
+
+// The steps' coefficients: a flat sequence of numbers, three for each.
+std::vector<double> numbers(PyObject* o) {
+  const Held seq{PySequence_Fast(o, "coefficients must be a sequence of numbers")};
+  if (!seq.o) throw PythonError{};
+  std::vector<double> v(PySequence_Fast_GET_SIZE(seq.o));
+  for (size_t i = 0; i < v.size(); ++i) {
+    v[i] = PyFloat_AsDouble(PySequence_Fast_GET_ITEM(seq.o, i));
+    if (v[i] == -1.0 && PyErr_Occurred()) throw PythonError{};
+  }
+  return v;
+}
+void sides_fit(const at::Tensor& t, const char* name) {
+  if (t.dim() != 2) bad(std::string(name) + " must have two dimensions");
+  if (t.size(0) > FBX_ORTHO_MOST || t.size(1) > FBX_ORTHO_MOST) bad(std::string(name) + " must have at most " + std::to_string(FBX_ORTHO_MOST) + " rows and columns");
+}
+
+// orthogonalise(matrices, outs, dtype, exact, coefficients, eps): the results, a list
+PyObject* orthogonalise(PyObject*, PyObject* args) {
+  PyObject *in_o, *out_o, *dtype, *coefficients;
+  int exact;
+  fbx_ortho h{};
+  if (!PyArg_ParseTuple(args, "OOOiOd", &in_o, &out_o, &dtype, &exact, &coefficients, &h.eps)) return nullptr;
+  return guarded([&]() -> PyObject* {
+    const List in(in_o), given(out_o);
+    if (!in.seq) bad("matrices must be a list");
+    const Py_ssize_t n = in.size();
+    if (given.seq && given.size() != n) bad("one result for each matrix");
+    std::vector<double> steps = numbers(coefficients);
+    h.steps = static_cast<uint32_t>(steps.size() / 3);
+    h.coefficients = steps.data();
+    const Held all{PyList_New(n)};
+    if (!all.o) throw PythonError{};
+    if (!n) return Py_NewRef(all.o);
+    const at::Tensor& like = in[0];
+    h.in = code(like);
+    h.out = code_of(dtype, h.in);
+    h.exact = exact < 0 ? FBX_EXACT_BY_SIZE : exact;   // (below 0: nothing was asked for)
+    std::vector<fbx_ortho_matrix> list;
+    std::vector<at::Tensor> out(n);
+    std::vector<const void*> seen;
+    for (Py_ssize_t i = 0; i < n; ++i) {
+      const at::Tensor& t = in[i];
+      if (t._fw_grad(0).defined() || (t.requires_grad() && c10::GradMode::is_enabled())) bad("orthogonalise has no derivative");
+      sides_fit(t, "a matrix");
+      if (t.scalar_type() != like.scalar_type() || t.device() != like.device()) bad("matrices must be of one type and on one device");
+      matrix(t, "a matrix");
+      on_gpu(t);
+      if (given.seq) {
+        out[i] = result(PySequence_Fast_GET_ITEM(given.seq, i));
+        rows_of(out[i], "out", h.out, like, t.size(0), t.size(1));
+        if (out[i].numel()) seen.push_back(out[i].data_ptr());
+      }
+    }
+    std::sort(seen.begin(), seen.end());
+    if (std::adjacent_find(seen.begin(), seen.end()) != seen.end()) bad("a result is given twice");
+    const c10::DeviceGuard guard(like.device());
+    for (Py_ssize_t i = 0; i < n; ++i) {
+      const at::Tensor& t = in[i];
+      if (!given.seq) out[i] = at::empty({t.size(0), t.size(1)}, t.options().dtype(type_of(h.out)).memory_format(c10::nullopt));
+      if (t.numel())
+        list.push_back({t.data_ptr(), out[i].data_ptr(), matrix(t, "a matrix"), matrix(out[i], "out"), static_cast<uint32_t>(t.size(0)), static_cast<uint32_t>(t.size(1))});
+    }
+    uint64_t need = 0;
+    check(g.ortho_scratch(&h, list.data(), static_cast<uint32_t>(list.size()), &need));
+    const at::Tensor s = scratch(need, like);
+    check(g.orthogonalise(&h, list.data(), static_cast<uint32_t>(list.size()), pointer(s), need, stream_of(like)));
+    for (Py_ssize_t i = 0; i < n; ++i) {
+      if (given.seq) changed(out[i]);
+      PyList_SET_ITEM(all.o, i, wrap(std::move(out[i])));
+    }
+    return Py_NewRef(all.o);
+  });
+}
+
+// muon(params, grads, momenta, copies, factors, lr, momentum, nesterov, weight_decay, grad_scale, exact, coefficients, eps, check_only)
+PyObject* muon(PyObject*, PyObject* args) {
+  PyObject *lists[4], *factors, *coefficients;
+  int nesterov, exact, check_only;
+  fbx_muon h{};
+  if (!PyArg_ParseTuple(args, "OOOOOddpddiOdp", &lists[0], &lists[1], &lists[2], &lists[3], &factors, &h.lr, &h.momentum, &nesterov, &h.weight_decay, &h.grad_scale, &exact, &coefficients,
+                        &h.ortho.eps, &check_only))
+    return nullptr;
+  return guarded([&]() -> PyObject* {
+    const List p(lists[0]), grad(lists[1]), m(lists[2]), copy(lists[3]);
+    if (!p.seq || !grad.seq || !m.seq) bad("params, grads and momenta must be lists");
+    const Py_ssize_t n = p.size();
+    for (const List* l : {&grad, &m, &copy})
+      if (l->seq && l->size() != n) bad("params, grads, momenta and copies must be lists of one length");
+    const std::vector<double> factor = numbers(factors);
+    if (static_cast<Py_ssize_t>(factor.size()) != n) bad("one factor for each matrix");
+    std::vector<double> steps = numbers(coefficients);
+    h.ortho.steps = static_cast<uint32_t>(steps.size() / 3);
+    h.ortho.coefficients = steps.data();
+    if (!n) Py_RETURN_NONE;
+    h.param_dtype = code(p[0]);
+    h.grad_dtype = code(grad[0]);
+    h.copy_dtype = copy.seq ? code(copy[0]) : FBX_F32;
+    h.nesterov = nesterov;
+    h.ortho.exact = exact < 0 ? FBX_EXACT_BY_SIZE : exact;
+    const at::Device where = p[0].device();
+    std::vector<const void*> seen;
+    auto same = [&](const at::Tensor& t, bool written) {
+      if (t.device() != where || !t.is_contiguous()) bad("all matrices must be contiguous and on one device");
+      if (written && t.numel()) seen.push_back(t.data_ptr());
+      return t.data_ptr();
+    };
+    std::vector<fbx_muon_matrix> all;
+    for (Py_ssize_t i = 0; i < n; ++i) {
+      fbx_muon_matrix t{};
+      sides_fit(p[i], "a matrix of weights");
+      if (p[i].scalar_type() != p[0].scalar_type() || grad[i].scalar_type() != grad[0].scalar_type() || (copy.seq && copy[i].scalar_type() != copy[0].scalar_type()))
+        bad("all weights are of one type, and so are all gradients and all copies");
+      if (grad[i].sizes() != p[i].sizes() || m[i].numel() != p[i].numel() || (copy.seq && copy[i].numel() != p[i].numel())) bad("a gradient, momentum or copy is not of its weights' size");
+      if (m[i].scalar_type() != at::kFloat) bad("momenta are float32");
+      if (copy.seq && (h.copy_dtype == FBX_F32 || h.param_dtype != FBX_F32)) bad("a copy is in float16 or bfloat16, of weights in float32");
+      t.d_param = same(p[i], true);
+      t.d_grad = same(grad[i], false);
+      t.d_m = same(m[i], true);
+      if (copy.seq) t.d_copy = same(copy[i], true);
+      t.rows = static_cast<uint32_t>(p[i].size(0));
+      t.columns = static_cast<uint32_t>(p[i].size(1));
+      t.factor = factor[i];
+      if (p[i].numel()) all.push_back(t);
+    }
+    std::sort(seen.begin(), seen.end());
+    if (std::adjacent_find(seen.begin(), seen.end()) != seen.end()) bad("a matrix, momentum or copy is given twice");
+    on_gpu(p[0]);
+    uint64_t need = 0;
+    check(g.muon_scratch(&h, all.data(), static_cast<uint32_t>(all.size()), &need));
+    if (check_only) Py_RETURN_NONE;
+    const c10::DeviceGuard guard(where);
+    const at::Tensor s = scratch(need, p[0]);
+    check(g.muon_step(&h, all.data(), static_cast<uint32_t>(all.size()), pointer(s), need, stream_of(p[0])));
+    for (Py_ssize_t i = 0; i < n; ++i)
+      for (const List* l : {&p, &m, &copy})
+        if (l->seq) changed((*l)[i]);
+    Py_RETURN_NONE;
+  });
+}
+
+// bind(FbxError, torch.OutOfMemoryError, stream function, a tuple of the addresses of the library's functions in the order of `g`)
 PyObject* bind(PyObject*, PyObject* args) {
-  PyObject *error, *memory, *stream;
-  unsigned long long at[8];
-  if (!PyArg_ParseTuple(args, "OOOKKKKKKKK", &error, &memory, &stream, &at[0], &at[1], &at[2], &at[3], &at[4], &at[5], &at[6], &at[7])) return nullptr;
-  static_assert(sizeof g == sizeof at, "eight pointers");
+  PyObject *error, *memory, *stream, *addresses;
+  if (!PyArg_ParseTuple(args, "OOOO!", &error, &memory, &stream, &PyTuple_Type, &addresses)) return nullptr;
+  constexpr Py_ssize_t kAll = sizeof g / sizeof(void*);
+  if (PyTuple_GET_SIZE(addresses) != kAll) {
+    PyErr_SetString(PyExc_RuntimeError, "the binding is of another library");
+    return nullptr;
+  }
+  unsigned long long at[kAll];
+  for (Py_ssize_t i = 0; i < kAll; ++i) {
+    at[i] = PyLong_AsUnsignedLongLong(PyTuple_GET_ITEM(addresses, i));
+    if (PyErr_Occurred()) return nullptr;
+  }
+  static_assert(sizeof g == sizeof at, "all are pointers");
   memcpy(&g, at, sizeof g);
   Py_INCREF(error);
   Py_INCREF(memory);
@@ -443,6 +825,12 @@ PyMethodDef methods[] = {{"bind", bind, METH_VARARGS, nullptr},
                          {"gated", gated, METH_VARARGS, nullptr},
                          {"gated_backward", gated_backward, METH_VARARGS, nullptr},
                          {"adamw", adamw, METH_VARARGS, nullptr},
+                         {"norm", norm, METH_VARARGS, nullptr},
+                         {"norm_backward", norm_backward, METH_VARARGS, nullptr},
+                         {"join", join, METH_VARARGS, nullptr},
+                         {"join_backward", join_backward, METH_VARARGS, nullptr},
+                         {"orthogonalise", orthogonalise, METH_VARARGS, nullptr},
+                         {"muon", muon, METH_VARARGS, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_train", "The native part of the trainer's binding.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -148,42 +148,46 @@ __device__ __forceinline__ void fetch_vector(Row<kN>& to, const void* from, bool
   }
 }
 
-// v becomes (v - mean) / sqrt(variance + eps), or v / sqrt(mean square + eps); returns 1 / sqrt.  Means and squares are taken
-// of the row in registers, the squares behind the mean: sums of squares less a squared mean would lose what a large mean hides.
+// v becomes (v - mean) / sqrt(variance + eps), or v / sqrt(mean square + eps); returns 1 / sqrt.  Squares are taken behind the mean:
+// sums of squares less a squared mean would lose what a large mean hides.  What rounding left of the mean is found beside them
+// and taken off too, so that a row of one large number is one of zeros.
 template <int kN>
-__device__ __forceinline__ float normalise(Row<kN>& v, Group& g, const Columns<kN>& at, bool layer, float one_dim, float eps) {
-  float s[1];
+__device__ __forceinline__ float normalise(Row<kN>& v, Group& g, const Columns<kN>& at, bool layer, float dim, float eps) {
+  float s[2] = {0.f, 0.f};
   if (layer) {
-    s[0] = 0.f;
+    float all[1] = {0.f};
 #pragma unroll
     for (int j = 0; j < kN; ++j)
 #pragma unroll
-      for (uint32_t e = 0; e < kPack; ++e) s[0] += v[j][e];
-    g.sum(s);
-    const float mean = s[0] * one_dim;
+      for (uint32_t e = 0; e < kPack; ++e) all[0] += v[j][e];
+    g.sum(all);
+    const float mean = all[0] / dim;
 #pragma unroll
     for (int j = 0; j < kN; ++j)
 #pragma unroll
-      for (uint32_t e = 0; e < kPack; ++e) v[j][e] = e < at.n[j] ? v[j][e] - mean : 0.f;
+      for (uint32_t e = 0; e < kPack; ++e) {
+        v[j][e] = e < at.n[j] ? v[j][e] - mean : 0.f;
+        s[1] += v[j][e];
+      }
   }
-  s[0] = 0.f;
 #pragma unroll
   for (int j = 0; j < kN; ++j)
 #pragma unroll
     for (uint32_t e = 0; e < kPack; ++e) s[0] += v[j][e] * v[j][e];
   g.sum(s);
-  const float inverse = 1.f / __builtin_sqrtf(s[0] * one_dim + eps);
+  const float rest = s[1] / dim, square = s[0] / dim - rest * rest;
+  const float inverse = 1.f / __builtin_sqrtf((square > 0.f || square != square ? square : 0.f) + eps);
 #pragma unroll
   for (int j = 0; j < kN; ++j)
 #pragma unroll
-    for (uint32_t e = 0; e < kPack; ++e) v[j][e] *= inverse;
+    for (uint32_t e = 0; e < kPack; ++e) v[j][e] = layer && e >= at.n[j] ? 0.f : (v[j][e] - rest) * inverse;
   return inverse;
 }
 
 // p, the gradient of normalised rows, becomes that of what they were made from: inverse (p - mean p - unit mean(p unit)), the
 // first mean for a layer's norm only.  more: another sum over the row that is wanted too.
 template <int kN>
-__device__ __forceinline__ void denormalise(Row<kN>& p, const Row<kN>& unit, float inverse, Group& g, bool layer, float one_dim, float& more) {
+__device__ __forceinline__ void denormalise(Row<kN>& p, const Row<kN>& unit, float inverse, Group& g, bool layer, float dim, float& more) {
   float s[3] = {0.f, 0.f, more};
 #pragma unroll
   for (int j = 0; j < kN; ++j)
@@ -193,7 +197,7 @@ __device__ __forceinline__ void denormalise(Row<kN>& p, const Row<kN>& unit, flo
       s[1] += p[j][e];
     }
   g.sum(s);
-  const float along = s[0] * one_dim, mean = layer ? s[1] * one_dim : 0.f;
+  const float along = s[0] / dim, mean = layer ? s[1] / dim : 0.f;
 #pragma unroll
   for (int j = 0; j < kN; ++j)
 #pragma unroll
@@ -239,7 +243,7 @@ struct NormArgs {
   uint64_t ld_x, ld_out, ld_dy, ld_dx, rows;
   uint32_t dim, wide, lanes, slots;
   uint32_t layer, single;           // single: vectors are in 32 bits
-  float eps, one_dim;
+  float eps, whole;                 // whole: dim
 };
 
 // R: of the residual stream; T: of the result.
@@ -258,7 +262,7 @@ __global__ __launch_bounds__(kMostLanes) void k_norm(NormArgs p) {
     Row<kN> v;
     fetch_row(raw, (const R*)p.x + r * p.ld_x, at, in);
     widen(v, raw);
-    normalise(v, g, at, p.layer, p.one_dim, p.eps);
+    normalise(v, g, at, p.layer, p.whole, p.eps);
 #pragma unroll
     for (int j = 0; j < kN; ++j)
 #pragma unroll
@@ -284,7 +288,7 @@ __global__ __launch_bounds__(kMostLanes) void k_norm_grad(NormArgs p) {
     fetch_row(raw_x, (const R*)p.x + r * p.ld_x, at, in);
     fetch_row(raw_dy, (const T*)p.dy + r * p.ld_dy, at, in);
     widen(unit, raw_x);
-    const float inverse = normalise(unit, g, at, p.layer, p.one_dim, p.eps);
+    const float inverse = normalise(unit, g, at, p.layer, p.whole, p.eps);
     widen(d, raw_dy);
 #pragma unroll
     for (int j = 0; j < kN; ++j)
@@ -295,7 +299,7 @@ __global__ __launch_bounds__(kMostLanes) void k_norm_grad(NormArgs p) {
       }
     if (p.dx) {
       float none = 0.f;
-      denormalise(d, unit, inverse, g, p.layer, p.one_dim, none);
+      denormalise(d, unit, inverse, g, p.layer, p.whole, none);
       put_row((R*)p.dx + r * p.ld_dx, d, at, in);
     }
   }
@@ -309,7 +313,7 @@ struct JoinArgs {
   uint64_t ld_x, ld_y, ld_gate, ld_out, ld_next, ld_dout, ld_dnext, ld_dx, ld_dy, ld_dgate, rows;
   uint32_t dim, wide, lanes, slots;
   uint32_t layer, single, post, then, each, sigmoid;  // each: a gate for each element, not one a row
-  float eps, one_dim, number;       // number: the scale, where it is no vector
+  float eps, whole, number;         // whole: dim; number: the scale, where it is no vector
 };
 
 // e^-a by the hardware's exponential and reciprocal (one unit in the last place each).
@@ -357,7 +361,7 @@ __global__ __launch_bounds__(kMostLanes) void k_join(JoinArgs p) {
     fetch_row(raw_x, (const R*)p.x + r * p.ld_x, at, in);
     Row<kN> v;
     widen(v, raw_y);
-    if (p.post) normalise(v, g, at, p.layer, p.one_dim, p.eps);
+    if (p.post) normalise(v, g, at, p.layer, p.whole, p.eps);
 #pragma unroll
     for (int j = 0; j < kN; ++j)
 #pragma unroll
@@ -369,7 +373,7 @@ __global__ __launch_bounds__(kMostLanes) void k_join(JoinArgs p) {
 #pragma unroll
         for (uint32_t e = 0; e < kPack; ++e)
           if (e >= at.n[j]) v[j][e] = 0.f;
-      normalise(v, g, at, p.layer, p.one_dim, p.eps);
+      normalise(v, g, at, p.layer, p.whole, p.eps);
 #pragma unroll
       for (int j = 0; j < kN; ++j)
 #pragma unroll
@@ -411,7 +415,7 @@ __global__ __launch_bounds__(kMostLanes) void k_join_grad(JoinArgs p) {
     Row<kN> unit, d;
     widen(unit, raw_y);
     float inverse = 1.f;
-    if (p.post) inverse = normalise(unit, g, at, p.layer, p.one_dim, p.eps);
+    if (p.post) inverse = normalise(unit, g, at, p.layer, p.whole, p.eps);
     widen(d, raw_dout);
     if (p.then) {
       Row<kN> after, q;
@@ -421,7 +425,7 @@ __global__ __launch_bounds__(kMostLanes) void k_join_grad(JoinArgs p) {
 #pragma unroll
         for (uint32_t e = 0; e < kPack; ++e)
           after[j][e] = e < at.n[j] ? (float)raw_x[j].v[e] + open(raw_gate[j].v[e], p) * weight[j][e] * unit[j][e] : 0.f;
-      const float after_inverse = normalise(after, g, at, p.layer, p.one_dim, p.eps);
+      const float after_inverse = normalise(after, g, at, p.layer, p.whole, p.eps);
 #pragma unroll
       for (int j = 0; j < kN; ++j)
 #pragma unroll
@@ -430,7 +434,7 @@ __global__ __launch_bounds__(kMostLanes) void k_join_grad(JoinArgs p) {
           q[j][e] *= next_weight[j][e];
         }
       float none = 0.f;
-      denormalise(q, after, after_inverse, g, p.layer, p.one_dim, none);
+      denormalise(q, after, after_inverse, g, p.layer, p.whole, none);
 #pragma unroll
       for (int j = 0; j < kN; ++j)
 #pragma unroll
@@ -452,7 +456,7 @@ __global__ __launch_bounds__(kMostLanes) void k_join_grad(JoinArgs p) {
         d[j][e] *= weight[j][e] * a;
       }
     if (p.post) {
-      denormalise(d, unit, inverse, g, p.layer, p.one_dim, all);
+      denormalise(d, unit, inverse, g, p.layer, p.whole, all);
     } else if (p.gate && !p.each) {
       float s[1] = {all};
       g.sum(s);
@@ -624,7 +628,7 @@ NormArgs args_of(const fbx_norm* h, const Layout& l) {
   p.layer = h->kind == FBX_NORM_LAYER;
   p.single = h->vectors == FBX_F32;
   p.eps = (float)h->eps;
-  p.one_dim = (float)(1.0 / h->dim);
+  p.whole = (float)h->dim;
   return p;
 }
 JoinArgs args_of(const fbx_join* h, const Layout& l) {
@@ -649,7 +653,7 @@ JoinArgs args_of(const fbx_join* h, const Layout& l) {
   p.each = h->gate_columns != 1;
   p.sigmoid = h->gate_act == FBX_GATE_SIGMOID;
   p.eps = (float)h->eps;
-  p.one_dim = (float)(1.0 / h->dim);
+  p.whole = (float)h->dim;
   p.number = (float)h->scale;
   return p;
 }

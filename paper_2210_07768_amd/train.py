@@ -21,9 +21,15 @@ from .binding import ExtractResult, FbxError
 EXPORTS = [
     "fbx_train_last_error", "fbx_embed_forward", "fbx_embed_backward_scratch", "fbx_embed_backward",
     "fbx_gated_scratch", "fbx_gated_forward", "fbx_gated_backward", "fbx_adamw_step",
+    "fbx_norm_forward", "fbx_norm_scratch", "fbx_norm_backward", "fbx_join_forward", "fbx_join_scratch", "fbx_join_backward",
+    "fbx_ortho_scratch", "fbx_orthogonalise", "fbx_muon_scratch", "fbx_muon_step",
 ]
 ACTS = {"silu": 0, "gelu": 1, "relu": 2, "sigmoid": 3}
+KINDS = {"rms": 0, "layer": 1}           # of a norm
+GATES = {"none": 0, "sigmoid": 1}
+NEWTON_SCHULZ = (3.4445, -4.7750, 2.0315)   # takes singular values from (0, 1] to near 1 in five steps
 BLOCK = 32   # elements that share a scale in 8-bit states
+NORM_MOST = 16384   # elements of a row that is normed
 
 
 class Signs(NamedTuple):
@@ -48,7 +54,7 @@ def _load():
         from . import _train as N
 
         N.bind(FbxError, torch.OutOfMemoryError, torch._C._cuda_getCurrentRawStream,
-               *(ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in EXPORTS))
+               tuple(ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in EXPORTS))
         _native = N
     return _native
 
@@ -172,6 +178,226 @@ class _Gated(torch.autograd.Function):
         need = ctx.needs_input_grad
         dx, dw_gate, dw_up = gated_backward(dh, *ctx.saved_tensors, ctx.act, need_dx=need[0], need_dw=need[1] or need[2])
         return dx, dw_gate if need[1] else None, dw_up if need[2] else None, None
+
+
+# ------------------------------------------------------------------ norms, and what joins a block to its stream
+def _code(given, of: dict, name: str) -> int:
+    code = of.get(given) if isinstance(given, str) else None
+    if code is None:
+        _bad(f"{name} must be one of {', '.join(of)}")
+    return code
+
+
+def _asks(*tensors) -> bool:
+    return torch.is_grad_enabled() and any(isinstance(t, torch.Tensor) and t.requires_grad for t in tensors)
+
+
+def norm(x, weight=None, kind: str = "rms", eps: float = 1e-6, dtype=None, out=None):
+    """Rows of x brought to unit size, times weight: x / sqrt(mean(x^2) + eps) (kind "rms"), or the same of x less its mean
+    ("layer").  x: records x dim; weight: dim elements, of the result's type or float32; dtype: of the result: x's, or, where x is
+    float32, float16 or bfloat16."""
+    _tensors(x=x)
+    if _asks(x, weight):
+        if out is not None:
+            _bad("out cannot take part in autograd")
+        return _Norm.apply(x, weight, kind, eps, dtype)
+    return _load().norm(x, weight, dtype, _code(kind, KINDS, "kind"), eps, out)
+
+
+def norm_backward(dy, x, weight=None, kind: str = "rms", eps: float = 1e-6, need_dx: bool = True, need_dw: bool = True):
+    """Gradients of ``norm`` with respect to x and weight (None for those not needed or not there), of their types; dy: of the
+    result's type.  The same inputs give the same bits."""
+    _tensors(dy=dy, x=x)
+    return _load().norm_backward(dy, x, weight, _code(kind, KINDS, "kind"), eps, need_dx, need_dw)
+
+
+def join(x, y, weight=None, gate=None, scale=1.0, next_weight=None, *, post: bool = True, then: Optional[bool] = None, gate_act: str = "sigmoid",
+         kind: str = "rms", eps: float = 1e-6, out=None, out_next=None):
+    """Joins a block's result y to the residual stream x, in one kernel: x + scale * act(gate) * norm(y, weight), and with it
+    the norm that the next block begins with.  Returns the stream, or, where ``then`` is true (by default, if there is a next_weight), the
+    stream and norm(stream, next_weight), which is taken of the stream before it is rounded.
+
+    x, y: records x dim; x: of y's type or float32, and so is the stream returned; what is normed is of y's.
+    weight, next_weight, scale: dim elements, all of y's type or all float32; scale may be a number.
+    gate: records x dim, or records x 1, of y's type; gate_act: "sigmoid", or "none" where it is to be taken as it is.
+    post: false leaves out y's norm (and has no weight): x + scale * act(gate) * y."""
+    _tensors(x=x, y=y)
+    then = next_weight is not None if then is None else bool(then)
+    if _asks(x, y, weight, gate, scale, next_weight):
+        if out is not None or out_next is not None:
+            _bad("out and out_next cannot take part in autograd")
+        return _Join.apply(x, y, weight, gate, scale, next_weight, post, then, gate_act, kind, eps)
+    return _load().join(x, y, weight, gate, scale, next_weight, post, then, _code(gate_act, GATES, "gate_act"), _code(kind, KINDS, "kind"), eps, out, out_next)
+
+
+class JoinGradients(NamedTuple):
+    """Of ``join``'s inputs; None for those not asked for or not there."""
+    dx: Optional[torch.Tensor]
+    dy: Optional[torch.Tensor]
+    dweight: Optional[torch.Tensor]
+    dgate: Optional[torch.Tensor]
+    dscale: Optional[torch.Tensor]
+    dnext_weight: Optional[torch.Tensor]
+
+
+def join_backward(dout, dnext, x, y, weight=None, gate=None, scale=1.0, next_weight=None, *, post: bool = True, then: Optional[bool] = None,
+                  gate_act: str = "sigmoid", kind: str = "rms", eps: float = 1e-6, need: Optional[Sequence[str]] = None) -> JoinGradients:
+    """Gradients of ``join`` given those of what it returns: dout of the stream's type, dnext of y's (either may be None: zero).
+    need: the names of the inputs whose gradients are wanted (all of them).  The stream is worked out again, not kept.  The same inputs give
+    the same bits."""
+    _tensors(x=x, y=y)
+    then = next_weight is not None if then is None else bool(then)
+    if not then and (dnext is not None or next_weight is not None):
+        _bad("dnext and next_weight are of the next norm: none without then")
+    names = ("x", "y", "weight", "gate", "scale", "next_weight")
+    if need is not None and not set(need) <= set(names):
+        _bad(f"need must be names of {', '.join(names)}")
+    wanted = sum(1 << i for i, name in enumerate(names) if need is None or name in need)
+    return JoinGradients(*_load().join_backward(dout, dnext, x, y, weight, gate, scale, next_weight, post, _code(gate_act, GATES, "gate_act"),
+                                                _code(kind, KINDS, "kind"), eps, wanted))
+
+
+class _Norm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, kind, eps, dtype):
+        ctx.save_for_backward(x, weight)
+        ctx.how = (kind, eps)
+        return _load().norm(x, weight, dtype, _code(kind, KINDS, "kind"), eps, None)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        dx, dweight = norm_backward(dy, *ctx.saved_tensors, *ctx.how, need_dx=ctx.needs_input_grad[0], need_dw=ctx.needs_input_grad[1])
+        return dx, dweight, None, None, None
+
+
+class _Join(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, y, weight, gate, scale, next_weight, post, then, gate_act, kind, eps):
+        number = None if isinstance(scale, torch.Tensor) else scale
+        ctx.save_for_backward(x, y, weight, gate, None if number is not None else scale, next_weight)
+        ctx.number, ctx.how = number, dict(post=post, then=then, gate_act=gate_act, kind=kind, eps=eps)
+        ctx.set_materialize_grads(False)
+        return _load().join(x, y, weight, gate, scale, next_weight, post, then, _code(gate_act, GATES, "gate_act"), _code(kind, KINDS, "kind"), eps, None, None)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dout, dnext=None):
+        if dout is None and dnext is None:
+            return (None,) * 11
+        x, y, weight, gate, scale, next_weight = ctx.saved_tensors
+        need = [name for name, wanted in zip(("x", "y", "weight", "gate", "scale", "next_weight"), ctx.needs_input_grad) if wanted]
+        if dnext is None and "next_weight" in need:   # (what it is multiplied with was not used)
+            need.remove("next_weight")
+        d = join_backward(dout, dnext, x, y, weight, gate, scale if ctx.number is None else ctx.number, next_weight, **ctx.how, need=need)
+        return (*d, None, None, None, None, None)
+
+
+# ------------------------------------------------------------------ orthogonalised updates
+def _steps(steps: int, coefficients) -> List[float]:
+    """The coefficients of every step, one behind the other."""
+    rows = list(coefficients)
+    if rows and not hasattr(rows[0], "__len__"):
+        rows = [rows] * steps
+    if steps < 1 or len(rows) != steps or any(len(r) != 3 for r in rows):
+        _bad("coefficients must be three numbers, or three for each of the steps (of which there is one at least)")
+    return [float(c) for r in rows for c in r]
+
+
+def orthogonalise(x, steps: int = 5, coefficients=NEWTON_SCHULZ, eps: float = 1e-7, dtype=None, exact: Optional[bool] = None, out=None):
+    """A matrix, or each of a list of them, with its singular values brought near 1 by Newton-Schulz products (the formulas:
+    fbx_orthogonalise in ``include/fbx_train.h``).  All matrices of a list go through the same launches.
+
+    coefficients: three numbers, or three for each step.  dtype: of the results (the matrices').  exact: products of 32-bit accuracy, of three
+    times the work; by default for all but results in bfloat16 of matrices of more than 256 rows and columns, whose products are then in
+    half precision, with an error of about that of the results' rounding.  out: a tensor, or a list of them.  Without derivative."""
+    one = isinstance(x, torch.Tensor)
+    if out is not None and one != isinstance(out, torch.Tensor):
+        _bad("out must be a tensor for a tensor, and a list for a list")
+    got = _load().orthogonalise([x] if one else x, None if out is None else [out] if one else out, dtype, -1 if exact is None else int(bool(exact)), _steps(steps, coefficients), eps)
+    return got[0] if one else got
+
+
+ADJUST = {"rms": lambda rows, columns: 0.2 * max(rows, columns) ** 0.5,          # elements of a fifth of lr, as an Adam step's are
+          "spectral": lambda rows, columns: max(1.0, rows / max(columns, 1)) ** 0.5, "none": lambda rows, columns: 1.0}
+
+
+def _factors(adjust: str, params) -> List[float]:
+    if adjust not in ADJUST:
+        _bad(f"adjust must be one of {', '.join(ADJUST)}")
+    for p in params:
+        if not isinstance(p, torch.Tensor) or p.dim() != 2:
+            _bad("weights must be tensors of two dimensions")
+    return [ADJUST[adjust](*p.shape) for p in params]
+
+
+def muon(params: Sequence, grads: Sequence, momenta: Sequence, copies: Optional[Sequence] = None, *, lr: float = 2e-3, momentum: float = 0.95, nesterov: bool = True,
+         weight_decay: float = 1e-2, grad_scale: float = 1.0, adjust: str = "rms", steps: int = 5, coefficients=NEWTON_SCHULZ, eps: float = 1e-7,
+         exact: Optional[bool] = None):
+    """One step of Muon over all matrices, in place (the formulas: fbx_muon_step in ``include/fbx_train.h``): the momentum takes the
+    gradient in, and the weights move by the orthogonalised momentum (nesterov: the gradient and momentum times it).
+
+    momenta: float32, of the weights' sizes; copies: float16 or bfloat16 tensors that receive float32 weights too.  All weights are of one type, and
+    so are all gradients.  adjust: what the update is multiplied by, "rms" 0.2 sqrt(max(rows, columns)), "spectral" sqrt(max(1, rows / columns)),
+    "none" 1.  exact: see ``orthogonalise`` (the weights' type decides)."""
+    params = list(params)
+    _load().muon(params, grads, momenta, copies, _factors(adjust, params), lr, momentum, nesterov, weight_decay, grad_scale, -1 if exact is None else int(bool(exact)),
+                 _steps(steps, coefficients), eps, False)
+
+
+class Muon:
+    """Keeps the momenta of a list of matrices and steps them all at once from their ``.grad``; vectors and tables are ``AdamW``'s.
+
+    copies: a list of float16 or bfloat16 tensors, one for each weight (float32 then), that follow the weights.  The other arguments: see ``muon``."""
+
+    def __init__(self, params, lr: float = 2e-3, momentum: float = 0.95, nesterov: bool = True, weight_decay: float = 1e-2, adjust: str = "rms", steps: int = 5,
+                 coefficients=NEWTON_SCHULZ, eps: float = 1e-7, exact: Optional[bool] = None, copies: Optional[List] = None):
+        self.params = list(params)
+        self.copies = None if copies is None else list(copies)
+        if self.copies is not None and len(self.copies) != len(self.params):
+            _bad("one copy for each weight")
+        self.lr, self.momentum, self.nesterov, self.weight_decay, self.eps = lr, momentum, nesterov, weight_decay, eps
+        self.exact = -1 if exact is None else int(bool(exact))
+        self.coefficients, self.factors = _steps(steps, coefficients), _factors(adjust, self.params)
+        self.step_count = 0
+        self.m = [torch.zeros(p.shape, dtype=torch.float32, device=p.device) for p in self.params]
+
+    @torch.no_grad()
+    def step(self, grads: Optional[Sequence] = None, grad_scale: float = 1.0, lr: Optional[float] = None):
+        """grads: one for each weight, instead of their .grad.  Weights without a gradient stay as they are.  All weights are
+        stepped, or, where something is refused, none."""
+        grads = [p.grad for p in self.params] if grads is None else list(grads)
+        if len(grads) != len(self.params):
+            _bad("one gradient for each weight")
+        kinds = {}
+        for i, (p, g) in enumerate(zip(self.params, grads)):
+            if g is not None:
+                kinds.setdefault((p.dtype, g.dtype, p.device), []).append(i)
+        pick = lambda x, at: None if x is None else [x[i] for i in at]  # noqa: E731
+        calls = [[*(pick(x, at) for x in (self.params, grads, self.m, self.copies, self.factors)), self.lr if lr is None else lr, self.momentum, self.nesterov,
+                  self.weight_decay, grad_scale, self.exact, self.coefficients, self.eps] for at in kinds.values()]
+        step = _load().muon
+        for check_only in (True, False) if len(calls) > 1 else (False,):   # (nothing is stepped if a later list is refused)
+            for call in calls:
+                step(*call, check_only)
+        self.step_count += 1
+
+    def zero_grad(self):
+        for p in self.params:
+            p.grad = None
+
+    def state_dict(self) -> dict:
+        return {"step": self.step_count, "m": self.m}
+
+    def load_state_dict(self, state: dict):
+        if len(state["m"]) != len(self.m):
+            _bad("the states are of another number of weights")
+        for mine, theirs in zip(self.m, state["m"]):   # (all of them before any is copied)
+            if mine.shape != theirs.shape or mine.dtype != theirs.dtype:
+                _bad(f"m: a state is {tuple(theirs.shape)}, {theirs.dtype}, and its weight's {tuple(mine.shape)}, {mine.dtype}")
+        for mine, theirs in zip(self.m, state["m"]):
+            mine.copy_(theirs)
+        self.step_count = state["step"]
 
 
 # ------------------------------------------------------------------ AdamW
