@@ -10,43 +10,24 @@ namespace train {
 namespace {
 
 constexpr uint32_t kPack = 8;                 // adjacent elements of a lane
-constexpr uint32_t kMostLanes = 1024;         // of a row, and of a workgroup
-static_assert(FBX_NORM_MOST == 2 * kMostLanes * kPack, "a row is held by a workgroup's registers");
+constexpr uint32_t kMostLanes = 512;          // of a row, and of a workgroup
+constexpr int kMostPacks = 4;                 // of a lane
+static_assert(FBX_NORM_MOST == kMostPacks * kMostLanes * kPack, "a row is held by a workgroup's registers");
 
-// Eight adjacent elements in whole loads, wherever they begin: a row that is aligned to its elements only is read and
-// written four to sixteen bytes a lane like any other (the hardware takes such addresses), so odd widths and strides need no
-// form of their own.
+// Eight adjacent elements, in whole loads and stores wherever they begin: a row that is aligned to its elements only is moved
+// sixteen bytes a lane like any other (the hardware takes such addresses), so odd widths and strides need no form of their own.
 template <class X>
 struct Raw {
   X v[kPack];
 };
-template <class X>
-__device__ __forceinline__ Raw<X> fetch(const X* row, uint32_t c, uint32_t n) {
-  Raw<X> r = {};
-  if (n == kPack) {
-    __builtin_memcpy(&r, row + c, sizeof r);
-  } else {
-#pragma unroll
-    for (uint32_t e = 0; e < kPack; ++e)
-      if (e < n) r.v[e] = row[c + e];
-  }
-  return r;
-}
-template <class X>
-__device__ __forceinline__ void put(X* row, uint32_t c, uint32_t n, const float (&from)[kPack]) {
-  Raw<X> r;
-#pragma unroll
-  for (uint32_t e = 0; e < kPack; ++e) r.v[e] = (X)from[e];
-  if (n == kPack) {
-    __builtin_memcpy(row + c, &r, sizeof r);
-  } else {
-#pragma unroll
-    for (uint32_t e = 0; e < kPack; ++e)
-      if (e < n) row[c + e] = r.v[e];
-  }
-}
 
-// A workgroup's lanes: `slots` rows at a time, `lanes` to a row: a power of two up to 64, or whole wavefronts.
+// How a row lies in lanes: fewer than 8 elements in one lane, up to 64 packs in less than a wavefront, more in whole wavefronts, 1, 2 or 4 to
+// a lane.
+enum Shape { kTiny1, kNarrow1, kWide1, kWide2, kWide4 };
+constexpr int packs_of(Shape s) { return s == kWide4 ? 4 : s == kWide2 ? 2 : 1; }
+
+// A workgroup's lanes: `slots` rows at a time, `lanes` to a row: a power of two below 64, or whole wavefronts (kWide).
+template <bool kWide>
 struct Group {
   uint32_t lanes, slot, mine, waves;
   float* shared;   // two times what a reduction leaves there, in turn
@@ -58,181 +39,243 @@ struct Group {
   template <int kN>
   __device__ __forceinline__ void sum(float (&v)[kN]) {
 #ifdef __HIP_DEVICE_COMPILE__
-    auto moved = [](float x, auto control) { return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(control)::value, 15, 15, true)); };
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
-      if (lanes > 1u) v[i] += moved(v[i], std::integral_constant<int, 0xb1>());    // lane ^ 1
-      if (lanes > 2u) v[i] += moved(v[i], std::integral_constant<int, 0x4e>());    // lane ^ 2
-      if (lanes > 4u) v[i] += moved(v[i], std::integral_constant<int, 0x141>());   // 7 - lane, of eight: the other four
-      if (lanes > 8u) v[i] += moved(v[i], std::integral_constant<int, 0x140>());   // 15 - lane, of sixteen: the other eight
-      if (lanes > 16u) {  // (both give each lane the sums of both halves)
+      v[i] = sixteen(v[i], kWide ? 64u : lanes);
+      if (kWide || lanes > 16u) {  // (both give each lane the sums of both halves)
         const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[i]), __float_as_uint(v[i]), false, false);
         const uint32_t one = p[0], other = p[1];
         v[i] = __uint_as_float(one) + __uint_as_float(other);
       }
-      if (lanes > 32u) {
+      if (kWide || lanes > 32u) {
         const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[i]), __float_as_uint(v[i]), false, false);
         const uint32_t one = p[0], other = p[1];
         v[i] = __uint_as_float(one) + __uint_as_float(other);
       }
     }
 #endif
-    if (waves <= 1u) return;
+    if (!kWide || waves == 1u) return;
     // (a wavefront that writes here for the next reduction but one has met all others at the next one's barrier, behind their reads)
-    float* at = shared + turn * (kMostLanes / 64u) * kMostSums;
+    float* at = shared + turn * kWaves * kMostSums;
     turn ^= 1u;
-    const uint32_t wave = threadIdx.x / 64u;
-    if (threadIdx.x % 64u == 0u)
+    const uint32_t wave = threadIdx.x / 64u, lane = threadIdx.x % 64u;
+    if (lane == 0u)
 #pragma unroll
-      for (int i = 0; i < kN; ++i) at[wave * kN + i] = v[i];
+      for (int i = 0; i < kN; ++i) at[i * kWaves + wave] = v[i];
     __syncthreads();
+    // the row's wavefronts' sums, one a lane of sixteen
 #pragma unroll
-    for (int i = 0; i < kN; ++i) v[i] = 0.f;
-    for (uint32_t w = slot * waves; w < (slot + 1u) * waves; ++w)
+    for (int i = 0; i < kN; ++i) v[i] = lane % 16u < waves ? at[i * kWaves + slot * waves + lane % 16u] : 0.f;
 #pragma unroll
-      for (int i = 0; i < kN; ++i) v[i] += at[w * kN + i];
+    for (int i = 0; i < kN; ++i) v[i] = sixteen(v[i], 64u);
   }
-  static constexpr uint32_t kMostSums = 4;
-  static constexpr uint32_t kShared = 2 * (kMostLanes / 64) * kMostSums;
+  // Sums over 2, 4, 8 or 16 neighbouring lanes, as many as `n` reaches.
+  __device__ __forceinline__ static float sixteen(float v, uint32_t n) {
+#ifdef __HIP_DEVICE_COMPILE__
+    auto moved = [](float x, auto control) { return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(control)::value, 15, 15, true)); };
+    if (n > 1u) v += moved(v, std::integral_constant<int, 0xb1>());    // lane ^ 1
+    if (n > 2u) v += moved(v, std::integral_constant<int, 0x4e>());    // lane ^ 2
+    if (n > 4u) v += moved(v, std::integral_constant<int, 0x141>());   // 7 - lane, of eight: the other four
+    if (n > 8u) v += moved(v, std::integral_constant<int, 0x140>());   // 15 - lane, of sixteen: the other eight
+#endif
+    return v;
+  }
+  static constexpr uint32_t kMostSums = 3, kWaves = kMostLanes / 64;
+  static constexpr uint32_t kShared = 2 * kWaves * kMostSums;
 };
 
-// A row's packs of this lane: pack j begins at column (j * lanes + mine) * 8, and n[j] of its elements exist.
-template <int kN>
+// A row's packs of this lane.  Pack j begins at column (j * lanes + mine) * 8, or, where it would reach beyond the row, as much
+// earlier as makes it end there: its first `skip` elements are another pack's, which it works out and stores like that one, but leaves out
+// of sums.  A pack behind the row is all another's (skip = 8).  So no lane's loads depend on a condition: where they did, the compiler
+// waited for them at once, and none were on their way while a row was worked on.  Rows of fewer than 8 elements (kTiny) are moved one by
+// one, behind `skip` places that hold nothing.
+template <int kN, bool kTiny>
 struct Columns {
-  uint32_t c[kN], n[kN];
-  __device__ Columns(const Group& g, uint32_t dim) {
+  int32_t c[kN];
+  uint32_t skip[kN];
+  bool ragged;   // the row is no whole number of packs
+  template <class G>
+  __device__ Columns(const G& g, uint32_t dim) {
+    ragged = dim % kPack != 0u;
 #pragma unroll
     for (int j = 0; j < kN; ++j) {
-      c[j] = (j * g.lanes + g.mine) * kPack;
-      n[j] = c[j] >= dim ? 0u : dim - c[j] < kPack ? dim - c[j] : kPack;
+      const uint32_t from = (j * g.lanes + g.mine) * kPack, over = from + kPack > dim ? from + kPack - dim : 0u;
+      c[j] = (int32_t)(from - over);
+      skip[j] = over < kPack ? over : kPack;
     }
+  }
+  __device__ bool owns(int j) const { return skip[j] < kPack; }
+  // The sum of f(j, e) over this lane's elements.
+  template <class F>
+  __device__ __forceinline__ float sum(F f) const {
+    float s = 0.f;
+    if (!ragged) {
+#pragma unroll
+      for (int j = 0; j < kN; ++j) {
+        float t = 0.f;
+#pragma unroll
+        for (uint32_t e = 0; e < kPack; ++e) t += f(j, e);
+        s += owns(j) ? t : 0.f;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < kN; ++j)
+#pragma unroll
+        for (uint32_t e = 0; e < kPack; ++e) s += e >= skip[j] ? f(j, e) : 0.f;
+    }
+    return s;
   }
 };
 template <int kN>
 using Row = float[kN][kPack];
-
-template <class X, int kN>
-__device__ __forceinline__ void fetch_row(Raw<X> (&to)[kN], const X* row, const Columns<kN>& at, bool in) {
-#pragma unroll
-  for (int j = 0; j < kN; ++j) to[j] = fetch(row, at.c[j], in ? at.n[j] : 0u);
-}
-template <class X, int kN>
-__device__ __forceinline__ void widen(Row<kN>& to, const Raw<X> (&from)[kN]) {
+template <int kN, class F>
+__device__ __forceinline__ void each(F f) {
 #pragma unroll
   for (int j = 0; j < kN; ++j)
 #pragma unroll
-    for (uint32_t e = 0; e < kPack; ++e) to[j][e] = (float)from[j].v[e];
+    for (uint32_t e = 0; e < kPack; ++e) f(j, e);
 }
-template <class X, int kN>
-__device__ __forceinline__ void put_row(X* row, const Row<kN>& from, const Columns<kN>& at, bool in) {
-#pragma unroll
-  for (int j = 0; j < kN; ++j) put(row, at.c[j], in ? at.n[j] : 0u, from[j]);
-}
-// A vector of weights, in the block's type or 32 bits; `none` where there is none.
-template <class T, int kN>
-__device__ __forceinline__ void fetch_vector(Row<kN>& to, const void* from, bool single, const Columns<kN>& at, float none) {
+
+template <class X, int kN, bool kTiny>
+__device__ __forceinline__ void fetch_row(Raw<X> (&to)[kN], const X* row, const Columns<kN, kTiny>& at) {
 #pragma unroll
   for (int j = 0; j < kN; ++j) {
-    if (!from) {
-#pragma unroll
-      for (uint32_t e = 0; e < kPack; ++e) to[j][e] = none;
-    } else if (single) {
-      const Raw<float> r = fetch((const float*)from, at.c[j], at.n[j]);
-#pragma unroll
-      for (uint32_t e = 0; e < kPack; ++e) to[j][e] = r.v[e];
+    if (!kTiny) {
+      __builtin_memcpy(&to[j], row + at.c[j], sizeof to[j]);
     } else {
-      const Raw<T> r = fetch((const T*)from, at.c[j], at.n[j]);
 #pragma unroll
-      for (uint32_t e = 0; e < kPack; ++e) to[j][e] = (float)r.v[e];
+      for (uint32_t e = 0; e < kPack; ++e) to[j].v[e] = e >= at.skip[j] ? row[at.c[j] + (int32_t)e] : (X)0.f;
     }
+  }
+}
+template <class X, int kN, bool kTiny>
+__device__ __forceinline__ void put_row(X* row, const Row<kN>& from, const Columns<kN, kTiny>& at, bool in) {
+#pragma unroll
+  for (int j = 0; j < kN; ++j) {
+    if (!in || !at.owns(j)) continue;
+    Raw<X> r;
+#pragma unroll
+    for (uint32_t e = 0; e < kPack; ++e) r.v[e] = (X)from[j][e];
+    if (!kTiny) {
+      __builtin_memcpy(row + at.c[j], &r, sizeof r);
+    } else {
+#pragma unroll
+      for (uint32_t e = 0; e < kPack; ++e)
+        if (e >= at.skip[j]) row[at.c[j] + (int32_t)e] = r.v[e];
+    }
+  }
+}
+template <class X, int kN>
+__device__ __forceinline__ void widen(Row<kN>& to, const Raw<X> (&from)[kN]) {
+  each<kN>([&](int j, uint32_t e) { to[j][e] = (float)from[j].v[e]; });
+}
+// A vector of weights, in the block's type or 32 bits; `none` where there is none.
+template <class T, int kN, bool kTiny>
+__device__ __forceinline__ void fetch_vector(Row<kN>& to, const void* from, bool single, const Columns<kN, kTiny>& at, float none) {
+  if (!from) {
+    each<kN>([&](int j, uint32_t e) { to[j][e] = none; });
+  } else if (single) {
+    Raw<float> r[kN];
+    fetch_row(r, (const float*)from, at);
+    widen(to, r);
+  } else {
+    Raw<T> r[kN];
+    fetch_row(r, (const T*)from, at);
+    widen(to, r);
   }
 }
 
 // v becomes (v - mean) / sqrt(variance + eps), or v / sqrt(mean square + eps); returns 1 / sqrt.  Squares are taken behind the mean:
 // sums of squares less a squared mean would lose what a large mean hides.  What rounding left of the mean is found beside them
 // and taken off too, so that a row of one large number is one of zeros.
-template <int kN>
-__device__ __forceinline__ float normalise(Row<kN>& v, Group& g, const Columns<kN>& at, bool layer, float dim, float eps) {
-  float s[2] = {0.f, 0.f};
+template <int kN, bool kTiny, class G>
+__device__ __forceinline__ float normalise(Row<kN>& v, G& g, const Columns<kN, kTiny>& at, bool layer, float dim, float eps) {
+  float square;
   if (layer) {
-    float all[1] = {0.f};
-#pragma unroll
-    for (int j = 0; j < kN; ++j)
-#pragma unroll
-      for (uint32_t e = 0; e < kPack; ++e) all[0] += v[j][e];
+    float all[1] = {at.sum([&](int j, uint32_t e) { return v[j][e]; })};
     g.sum(all);
     const float mean = all[0] / dim;
-#pragma unroll
-    for (int j = 0; j < kN; ++j)
-#pragma unroll
-      for (uint32_t e = 0; e < kPack; ++e) {
-        v[j][e] = e < at.n[j] ? v[j][e] - mean : 0.f;
-        s[1] += v[j][e];
-      }
+    each<kN>([&](int j, uint32_t e) { v[j][e] -= mean; });
+    float s[2] = {at.sum([&](int j, uint32_t e) { return v[j][e] * v[j][e]; }), at.sum([&](int j, uint32_t e) { return v[j][e]; })};
+    g.sum(s);
+    const float rest = s[1] / dim;
+    each<kN>([&](int j, uint32_t e) { v[j][e] -= rest; });
+    square = s[0] / dim - rest * rest;
+    if (square < 0.f) square = 0.f;
+  } else {
+    float s[1] = {at.sum([&](int j, uint32_t e) { return v[j][e] * v[j][e]; })};
+    g.sum(s);
+    square = s[0] / dim;
   }
-#pragma unroll
-  for (int j = 0; j < kN; ++j)
-#pragma unroll
-    for (uint32_t e = 0; e < kPack; ++e) s[0] += v[j][e] * v[j][e];
-  g.sum(s);
-  const float rest = s[1] / dim, square = s[0] / dim - rest * rest;
-  const float inverse = 1.f / __builtin_sqrtf((square > 0.f || square != square ? square : 0.f) + eps);
-#pragma unroll
-  for (int j = 0; j < kN; ++j)
-#pragma unroll
-    for (uint32_t e = 0; e < kPack; ++e) v[j][e] = layer && e >= at.n[j] ? 0.f : (v[j][e] - rest) * inverse;
+  const float inverse = 1.f / __builtin_sqrtf(square + eps);
+  each<kN>([&](int j, uint32_t e) { v[j][e] *= inverse; });
   return inverse;
 }
 
 // p, the gradient of normalised rows, becomes that of what they were made from: inverse (p - mean p - unit mean(p unit)), the
-// first mean for a layer's norm only.  more: another sum over the row that is wanted too.
-template <int kN>
-__device__ __forceinline__ void denormalise(Row<kN>& p, const Row<kN>& unit, float inverse, Group& g, bool layer, float dim, float& more) {
-  float s[3] = {0.f, 0.f, more};
-#pragma unroll
-  for (int j = 0; j < kN; ++j)
-#pragma unroll
-    for (uint32_t e = 0; e < kPack; ++e) {
-      s[0] += p[j][e] * unit[j][e];
-      s[1] += p[j][e];
-    }
-  g.sum(s);
-  const float along = s[0] / dim, mean = layer ? s[1] / dim : 0.f;
-#pragma unroll
-  for (int j = 0; j < kN; ++j)
-#pragma unroll
-    for (uint32_t e = 0; e < kPack; ++e) p[j][e] = inverse * (p[j][e] - mean - unit[j][e] * along);
-  more = s[2];
+// first mean for a layer's norm only.  more: another sum over the row, where it is wanted too.
+template <int kN, bool kTiny, class G>
+__device__ __forceinline__ void denormalise(Row<kN>& p, const Row<kN>& unit, float inverse, G& g, const Columns<kN, kTiny>& at, bool layer, float dim, bool wanted, float& more) {
+  float along = at.sum([&](int j, uint32_t e) { return p[j][e] * unit[j][e]; }), mean = 0.f;
+  if (layer || wanted) {
+    float s[3] = {along, at.sum([&](int j, uint32_t e) { return p[j][e]; }), more};
+    g.sum(s);
+    along = s[0];
+    mean = layer ? s[1] / dim : 0.f;
+    more = s[2];
+  } else {
+    float s[1] = {along};
+    g.sum(s);
+    along = s[0];
+  }
+  along *= inverse / dim;
+  mean *= inverse;
+  each<kN>([&](int j, uint32_t e) { p[j][e] = p[j][e] * inverse - mean - unit[j][e] * along; });
 }
 
 // Every sum of columns of a workgroup, its rows in a fixed order: those of a wavefront by halves, then wavefront by wavefront
-// (or row by row, where a row has more than one); shared: `wide` floats a sum.
-template <int kSums, int kN>
-__device__ __forceinline__ void leave_sums(Row<kN> (&sums)[kSums], float* to, uint32_t wide, const Group& g, const Columns<kN>& at, uint32_t slots, float* shared) {
-  for (uint32_t d = g.lanes; d < 64u; d *= 2u)
-#pragma unroll
-    for (int i = 0; i < kSums; ++i)
-#pragma unroll
-      for (int j = 0; j < kN; ++j)
-#pragma unroll
-        for (uint32_t e = 0; e < kPack; ++e) sums[i][j][e] += __shfl_xor(sums[i][j][e], d, 64);
-  const uint32_t turns = g.waves ? slots : blockDim.x / 64u, mine = g.waves ? g.slot : threadIdx.x / 64u;
-  const bool first = g.waves || threadIdx.x % 64u < g.lanes;   // (of the lanes that hold the same sums now)
-  for (uint32_t s = 0; s < turns; ++s) {
-    if (mine == s && first)
+// (or row by row, where a row has more than one).  shared: a line of `wide` floats for each sum and wavefront (or row).
+template <int kSums, int kN, bool kWide, bool kTiny>
+__device__ __forceinline__ void leave_sums(Row<kN> (&sums)[kSums], float* to, uint32_t wide, const Group<kWide>& g, const Columns<kN, kTiny>& at, uint32_t slots, float* shared) {
+  if (!kWide)
+    for (uint32_t d = g.lanes; d < 64u; d *= 2u)
 #pragma unroll
       for (int i = 0; i < kSums; ++i)
 #pragma unroll
-        for (int j = 0; j < kN; ++j) {
-          if (!at.n[j]) continue;
-          Pack<float, kPack> v;
-          float* held = shared + i * wide + at.c[j];
+        for (int j = 0; j < kN; ++j)
 #pragma unroll
-          for (uint32_t e = 0; e < kPack; ++e) v.v[e] = sums[i][j][e] + (s ? held[e] : 0.f);
-          if (s + 1u < turns) *(Pack<float, kPack>*)held = v;
-          else *(Pack<float, kPack>*)(to + i * wide + at.c[j]) = v;
+          for (uint32_t e = 0; e < kPack; ++e) sums[i][j][e] += __shfl_xor(sums[i][j][e], d, 64);
+  const uint32_t lines = kWide ? slots : blockDim.x / 64u, line = kWide ? g.slot : threadIdx.x / 64u;
+  const bool first = kWide || threadIdx.x % 64u < g.lanes;   // (of the lanes that hold the same sums now)
+  // (LDS and memory are written apart, and no pointer is made that lies before either: `c` may be below 0)
+  auto leave = [&](float* into, uint32_t base) {
+#pragma unroll
+    for (int i = 0; i < kSums; ++i)
+#pragma unroll
+      for (int j = 0; j < kN; ++j) {
+        if (!at.owns(j) || !first) continue;
+        if (at.skip[j] == 0u) {
+          Pack<float, kPack> v;
+#pragma unroll
+          for (uint32_t e = 0; e < kPack; ++e) v.v[e] = sums[i][j][e];
+          *(Pack<float, kPack>*)(into + base + i * wide + (uint32_t)at.c[j]) = v;
+        } else {
+#pragma unroll
+          for (uint32_t e = 0; e < kPack; ++e)
+            if (e >= at.skip[j]) into[base + i * wide + (uint32_t)(at.c[j] + (int32_t)e)] = sums[i][j][e];
         }
-    if (s + 1u < turns) __syncthreads();
+      }
+  };
+  if (lines == 1u) {
+    leave(to, 0u);
+    return;
+  }
+  leave(shared, line * wide * kSums);
+  __syncthreads();
+  for (uint32_t c = threadIdx.x; c < wide * kSums; c += blockDim.x) {
+    float v = shared[c];
+    for (uint32_t l = 1; l < lines; ++l) v += shared[l * wide * kSums + c];
+    to[c] = v;
   }
 }
 
@@ -246,62 +289,73 @@ struct NormArgs {
   float eps, whole;                 // whole: dim
 };
 
-// R: of the residual stream; T: of the result.
+// R: of the residual stream; T: of the result.  A row's loads are on their way while the one before it is worked on, but for rows that
+// leave no registers for it (kAhead).
 // Bound by memory.
-template <class R, class T, int kN>
+template <int kN>
+constexpr bool kAhead = kN == 1;
+
+template <class R, class T, Shape kShape>
 __global__ __launch_bounds__(kMostLanes) void k_norm(NormArgs p) {
-  __shared__ float shared[Group::kShared];
-  Group g(p.lanes, shared);
-  const Columns<kN> at(g, p.dim);
+  constexpr int kN = packs_of(kShape);
+  constexpr bool kWide = kShape >= kWide1, kTiny = kShape == kTiny1;
+  __shared__ float shared[Group<kWide>::kShared];
+  Group<kWide> g(p.lanes, shared);
+  const Columns<kN, kTiny> at(g, p.dim);
+
   Row<kN> weight;
   fetch_vector<T>(weight, p.weight, p.single, at, 1.f);
-  for (uint64_t r0 = (uint64_t)blockIdx.x * p.slots; r0 < p.rows; r0 += (uint64_t)gridDim.x * p.slots) {
-    const uint64_t r = r0 + g.slot;
-    const bool in = r < p.rows;
-    Raw<R> raw[kN];
+  const uint64_t stride = (uint64_t)gridDim.x * p.slots, last = p.rows - 1u;
+  uint64_t r = (uint64_t)blockIdx.x * p.slots + g.slot;
+  Raw<R> raw[kN];
+  auto get = [&](uint64_t r) { fetch_row(raw, (const R*)p.x + (r < last ? r : last) * p.ld_x, at); };
+  get(r);
+  for (uint64_t r0 = (uint64_t)blockIdx.x * p.slots; r0 < p.rows; r0 += stride, r += stride) {
     Row<kN> v;
-    fetch_row(raw, (const R*)p.x + r * p.ld_x, at, in);
     widen(v, raw);
+    if (kAhead<kN>) get(r + stride);
     normalise(v, g, at, p.layer, p.whole, p.eps);
-#pragma unroll
-    for (int j = 0; j < kN; ++j)
-#pragma unroll
-      for (uint32_t e = 0; e < kPack; ++e) v[j][e] *= weight[j][e];
-    put_row((T*)p.out + r * p.ld_out, v, at, in);
+    each<kN>([&](int j, uint32_t e) { v[j][e] *= weight[j][e]; });
+    put_row((T*)p.out + r * p.ld_out, v, at, r < p.rows);
+    if (!kAhead<kN>) get(r + stride);
   }
 }
 
-template <class R, class T, int kN>
+template <class R, class T, Shape kShape>
 __global__ __launch_bounds__(kMostLanes) void k_norm_grad(NormArgs p) {
-  __shared__ float shared[Group::kShared];
+  constexpr int kN = packs_of(kShape);
+  constexpr bool kWide = kShape >= kWide1, kTiny = kShape == kTiny1;
+  __shared__ float shared[Group<kWide>::kShared];
   extern __shared__ __attribute__((aligned(32))) float columns[];
-  Group g(p.lanes, shared);
-  const Columns<kN> at(g, p.dim);
+  Group<kWide> g(p.lanes, shared);
+  const Columns<kN, kTiny> at(g, p.dim);
+
   Row<kN> weight, sums[1] = {};
   fetch_vector<T>(weight, p.weight, p.single, at, 1.f);
-  for (uint64_t r0 = (uint64_t)blockIdx.x * p.slots; r0 < p.rows; r0 += (uint64_t)gridDim.x * p.slots) {
-    const uint64_t r = r0 + g.slot;
-    const bool in = r < p.rows;
-    Raw<R> raw_x[kN];
-    Raw<T> raw_dy[kN];
+  const uint64_t stride = (uint64_t)gridDim.x * p.slots, last = p.rows - 1u;
+  uint64_t r = (uint64_t)blockIdx.x * p.slots + g.slot;
+  Raw<R> raw_x[kN];
+  Raw<T> raw_dy[kN];
+  auto get = [&](uint64_t r) {
+    const uint64_t there = r < last ? r : last;
+    fetch_row(raw_x, (const R*)p.x + there * p.ld_x, at);
+    fetch_row(raw_dy, (const T*)p.dy + there * p.ld_dy, at);
+  };
+  get(r);
+  for (uint64_t r0 = (uint64_t)blockIdx.x * p.slots; r0 < p.rows; r0 += stride, r += stride) {
     Row<kN> unit, d;
-    fetch_row(raw_x, (const R*)p.x + r * p.ld_x, at, in);
-    fetch_row(raw_dy, (const T*)p.dy + r * p.ld_dy, at, in);
     widen(unit, raw_x);
-    const float inverse = normalise(unit, g, at, p.layer, p.whole, p.eps);
     widen(d, raw_dy);
-#pragma unroll
-    for (int j = 0; j < kN; ++j)
-#pragma unroll
-      for (uint32_t e = 0; e < kPack; ++e) {
-        sums[0][j][e] += d[j][e] * unit[j][e];
-        d[j][e] *= weight[j][e];
-      }
+    if (kAhead<kN>) get(r + stride);
+    const float inverse = normalise(unit, g, at, p.layer, p.whole, p.eps);
+    if (r < p.rows) each<kN>([&](int j, uint32_t e) { sums[0][j][e] += d[j][e] * unit[j][e]; });
     if (p.dx) {
       float none = 0.f;
-      denormalise(d, unit, inverse, g, p.layer, p.whole, none);
-      put_row((R*)p.dx + r * p.ld_dx, d, at, in);
+      each<kN>([&](int j, uint32_t e) { d[j][e] *= weight[j][e]; });
+      denormalise(d, unit, inverse, g, at, p.layer, p.whole, false, none);
+      put_row((R*)p.dx + r * p.ld_dx, d, at, r < p.rows);
     }
+    if (!kAhead<kN>) get(r + stride);
   }
   if (p.sums) leave_sums(sums, p.sums + (uint64_t)blockIdx.x * p.wide, p.wide, g, at, p.slots, columns);
 }
@@ -319,157 +373,149 @@ struct JoinArgs {
 // e^-a by the hardware's exponential and reciprocal (one unit in the last place each).
 __device__ __forceinline__ float logistic(float a) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(a * -1.4426950408889634f)); }
 
-// act(gate) of this lane's elements: of a row's one gate, of its own, or 1.
+// act(gate) of a row's elements, from their own gates or its only one.
 template <class T, int kN>
-__device__ __forceinline__ void fetch_gate(Raw<T> (&to)[kN], const JoinArgs& p, uint64_t r, const Columns<kN>& at, bool in) {
-  if (p.each) {
-    fetch_row(to, (const T*)p.gate + r * p.ld_gate, at, in && p.gate);
+__device__ __forceinline__ void open(Row<kN>& to, const Raw<T> (&gate)[kN], T only, const JoinArgs& p) {
+  if (!p.gate) {
+    each<kN>([&](int j, uint32_t e) { to[j][e] = 1.f; });
+  } else if (!p.each) {
+    const float a = p.sigmoid ? logistic((float)only) : (float)only;
+    each<kN>([&](int j, uint32_t e) { to[j][e] = a; });
+  } else if (p.sigmoid) {
+    each<kN>([&](int j, uint32_t e) { to[j][e] = logistic((float)gate[j].v[e]); });
   } else {
-    const T one = in && p.gate ? ((const T*)p.gate)[r * p.ld_gate] : (T)0.f;
-#pragma unroll
-    for (int j = 0; j < kN; ++j)
-#pragma unroll
-      for (uint32_t e = 0; e < kPack; ++e) to[j].v[e] = one;
+    widen(to, gate);
   }
 }
-template <class T>
-__device__ __forceinline__ float open(T z, const JoinArgs& p) {
-  return !p.gate ? 1.f : p.sigmoid ? logistic((float)z) : (float)z;
+
+// A row's operands as they are in memory.
+template <class R, class T, int kN>
+struct Operands {
+  Raw<R> x[kN], dout[kN];
+  Raw<T> y[kN], gate[kN], dnext[kN];
+  T only;   // a row's only gate
+};
+
+template <class T, int kN, bool kTiny>
+__device__ __forceinline__ void fetch_vectors(Row<kN>& weight, Row<kN>& next_weight, const JoinArgs& p, const Columns<kN, kTiny>& at) {
+  Row<kN> scale;
+  fetch_vector<T>(weight, p.weight, p.single, at, 1.f);
+  fetch_vector<T>(scale, p.scale, p.single, at, p.number);
+  if (p.then) fetch_vector<T>(next_weight, p.next_weight, p.single, at, 1.f);
+  each<kN>([&](int j, uint32_t e) { weight[j][e] *= scale[j][e]; });
 }
 
 // Bound by memory.
-template <class R, class T, int kN>
+template <class R, class T, Shape kShape>
 __global__ __launch_bounds__(kMostLanes) void k_join(JoinArgs p) {
-  __shared__ float shared[Group::kShared];
-  Group g(p.lanes, shared);
-  const Columns<kN> at(g, p.dim);
-  Row<kN> weight, scale, next_weight;
-  fetch_vector<T>(weight, p.weight, p.single, at, 1.f);
-  fetch_vector<T>(scale, p.scale, p.single, at, p.number);
-  fetch_vector<T>(next_weight, p.next_weight, p.single, at, 1.f);
-#pragma unroll
-  for (int j = 0; j < kN; ++j)
-#pragma unroll
-    for (uint32_t e = 0; e < kPack; ++e) weight[j][e] *= scale[j][e];
-  for (uint64_t r0 = (uint64_t)blockIdx.x * p.slots; r0 < p.rows; r0 += (uint64_t)gridDim.x * p.slots) {
-    const uint64_t r = r0 + g.slot;
-    const bool in = r < p.rows;
-    Raw<R> raw_x[kN];
-    Raw<T> raw_y[kN], raw_gate[kN];
-    fetch_row(raw_y, (const T*)p.y + r * p.ld_y, at, in);
-    fetch_gate(raw_gate, p, r, at, in);
-    fetch_row(raw_x, (const R*)p.x + r * p.ld_x, at, in);
-    Row<kN> v;
-    widen(v, raw_y);
+  constexpr int kN = packs_of(kShape);
+  constexpr bool kWide = kShape >= kWide1, kTiny = kShape == kTiny1;
+  __shared__ float shared[Group<kWide>::kShared];
+  Group<kWide> g(p.lanes, shared);
+  const Columns<kN, kTiny> at(g, p.dim);
+
+  Row<kN> weight, next_weight;
+  if (kAhead<kN>) fetch_vectors<T>(weight, next_weight, p, at);
+  const uint64_t stride = (uint64_t)gridDim.x * p.slots, last = p.rows - 1u;
+  uint64_t r = (uint64_t)blockIdx.x * p.slots + g.slot;
+  Operands<R, T, kN> now{};
+  auto get = [&](uint64_t r) {
+    const uint64_t there = r < last ? r : last;
+    fetch_row(now.y, (const T*)p.y + there * p.ld_y, at);
+    if (p.gate && p.each) fetch_row(now.gate, (const T*)p.gate + there * p.ld_gate, at);
+    if (p.gate && !p.each) now.only = ((const T*)p.gate)[there * p.ld_gate];
+    fetch_row(now.x, (const R*)p.x + there * p.ld_x, at);
+  };
+  get(r);
+  for (uint64_t r0 = (uint64_t)blockIdx.x * p.slots; r0 < p.rows; r0 += stride, r += stride) {
+    if (!kAhead<kN>) fetch_vectors<T>(weight, next_weight, p, at);
+    Row<kN> v, gate, x;
+    widen(v, now.y);
+    open(gate, now.gate, now.only, p);
+    widen(x, now.x);
+    if (kAhead<kN>) get(r + stride);
     if (p.post) normalise(v, g, at, p.layer, p.whole, p.eps);
-#pragma unroll
-    for (int j = 0; j < kN; ++j)
-#pragma unroll
-      for (uint32_t e = 0; e < kPack; ++e) v[j][e] = (float)raw_x[j].v[e] + open(raw_gate[j].v[e], p) * weight[j][e] * v[j][e];
-    put_row((R*)p.out + r * p.ld_out, v, at, in);
+    each<kN>([&](int j, uint32_t e) { v[j][e] = x[j][e] + gate[j][e] * weight[j][e] * v[j][e]; });
+    put_row((R*)p.out + r * p.ld_out, v, at, r < p.rows);
     if (p.then) {
-#pragma unroll
-      for (int j = 0; j < kN; ++j)
-#pragma unroll
-        for (uint32_t e = 0; e < kPack; ++e)
-          if (e >= at.n[j]) v[j][e] = 0.f;
       normalise(v, g, at, p.layer, p.whole, p.eps);
-#pragma unroll
-      for (int j = 0; j < kN; ++j)
-#pragma unroll
-        for (uint32_t e = 0; e < kPack; ++e) v[j][e] *= next_weight[j][e];
-      put_row((T*)p.next + r * p.ld_next, v, at, in);
+      each<kN>([&](int j, uint32_t e) { v[j][e] *= next_weight[j][e]; });
+      put_row((T*)p.next + r * p.ld_next, v, at, r < p.rows);
     }
+    if (!kAhead<kN>) get(r + stride);
   }
 }
 
-template <class R, class T, int kN>
+template <class R, class T, Shape kShape>
 __global__ __launch_bounds__(kMostLanes) void k_join_grad(JoinArgs p) {
-  __shared__ float shared[Group::kShared];
+  constexpr int kN = packs_of(kShape);
+  constexpr bool kWide = kShape >= kWide1, kTiny = kShape == kTiny1;
+  __shared__ float shared[Group<kWide>::kShared];
   extern __shared__ __attribute__((aligned(32))) float columns[];
-  Group g(p.lanes, shared);
-  const Columns<kN> at(g, p.dim);
+  Group<kWide> g(p.lanes, shared);
+  const Columns<kN, kTiny> at(g, p.dim);
+
   Row<kN> weight, next_weight, sums[2] = {};
-  {
-    Row<kN> scale;
-    fetch_vector<T>(weight, p.weight, p.single, at, 1.f);
-    fetch_vector<T>(scale, p.scale, p.single, at, p.number);
-    fetch_vector<T>(next_weight, p.next_weight, p.single, at, 1.f);
-#pragma unroll
-    for (int j = 0; j < kN; ++j)
-#pragma unroll
-      for (uint32_t e = 0; e < kPack; ++e) weight[j][e] *= scale[j][e];
-  }
-  for (uint64_t r0 = (uint64_t)blockIdx.x * p.slots; r0 < p.rows; r0 += (uint64_t)gridDim.x * p.slots) {
-    const uint64_t r = r0 + g.slot;
-    const bool in = r < p.rows;
-    Raw<R> raw_x[kN], raw_dout[kN];
-    Raw<T> raw_y[kN], raw_gate[kN], raw_dnext[kN];
-    fetch_row(raw_y, (const T*)p.y + r * p.ld_y, at, in);
-    fetch_gate(raw_gate, p, r, at, in);
+  if (kAhead<kN>) fetch_vectors<T>(weight, next_weight, p, at);
+  const uint64_t stride = (uint64_t)gridDim.x * p.slots, last = p.rows - 1u;
+  uint64_t r = (uint64_t)blockIdx.x * p.slots + g.slot;
+  Operands<R, T, kN> now{};
+  auto get = [&](uint64_t r) {
+    const uint64_t there = r < last ? r : last;
+    fetch_row(now.y, (const T*)p.y + there * p.ld_y, at);
+    if (p.gate && p.each) fetch_row(now.gate, (const T*)p.gate + there * p.ld_gate, at);
+    if (p.gate && !p.each) now.only = ((const T*)p.gate)[there * p.ld_gate];
     if (p.then) {
-      fetch_row(raw_x, (const R*)p.x + r * p.ld_x, at, in);
-      fetch_row(raw_dnext, (const T*)p.dnext + r * p.ld_dnext, at, in);
+      fetch_row(now.x, (const R*)p.x + there * p.ld_x, at);
+      fetch_row(now.dnext, (const T*)p.dnext + there * p.ld_dnext, at);
     }
-    fetch_row(raw_dout, (const R*)p.dout + r * p.ld_dout, at, in && p.dout);
-    Row<kN> unit, d;
-    widen(unit, raw_y);
+    if (p.dout) fetch_row(now.dout, (const R*)p.dout + there * p.ld_dout, at);
+  };
+  get(r);
+  for (uint64_t r0 = (uint64_t)blockIdx.x * p.slots; r0 < p.rows; r0 += stride, r += stride) {
+    const bool in = r < p.rows;
+    if (!kAhead<kN>) fetch_vectors<T>(weight, next_weight, p, at);
+    const Operands<R, T, kN> it = now;
+    if (kAhead<kN>) get(r + stride);
+    Row<kN> unit, gate, d;
+    widen(unit, it.y);
     float inverse = 1.f;
     if (p.post) inverse = normalise(unit, g, at, p.layer, p.whole, p.eps);
-    widen(d, raw_dout);
+    open(gate, it.gate, it.only, p);
+    if (p.dout) widen(d, it.dout);
+    else each<kN>([&](int j, uint32_t e) { d[j][e] = 0.f; });
     if (p.then) {
       Row<kN> after, q;
-      widen(q, raw_dnext);
-#pragma unroll
-      for (int j = 0; j < kN; ++j)
-#pragma unroll
-        for (uint32_t e = 0; e < kPack; ++e)
-          after[j][e] = e < at.n[j] ? (float)raw_x[j].v[e] + open(raw_gate[j].v[e], p) * weight[j][e] * unit[j][e] : 0.f;
+      each<kN>([&](int j, uint32_t e) { after[j][e] = (float)it.x[j].v[e] + gate[j][e] * weight[j][e] * unit[j][e]; });
       const float after_inverse = normalise(after, g, at, p.layer, p.whole, p.eps);
-#pragma unroll
-      for (int j = 0; j < kN; ++j)
-#pragma unroll
-        for (uint32_t e = 0; e < kPack; ++e) {
-          sums[1][j][e] += q[j][e] * after[j][e];
-          q[j][e] *= next_weight[j][e];
-        }
+      widen(q, it.dnext);
+      if (in) each<kN>([&](int j, uint32_t e) { sums[1][j][e] += q[j][e] * after[j][e]; });
+      each<kN>([&](int j, uint32_t e) { q[j][e] *= next_weight[j][e]; });
       float none = 0.f;
-      denormalise(q, after, after_inverse, g, p.layer, p.whole, none);
-#pragma unroll
-      for (int j = 0; j < kN; ++j)
-#pragma unroll
-        for (uint32_t e = 0; e < kPack; ++e) d[j][e] += q[j][e];
+      denormalise(q, after, after_inverse, g, at, p.layer, p.whole, false, none);
+      each<kN>([&](int j, uint32_t e) { d[j][e] += q[j][e]; });
     }
     if (p.dx) put_row((R*)p.dx + r * p.ld_dx, d, at, in);
-    // from here on: the gradient of what was added to x
-    Row<kN> dgate;
-    float all = 0.f;
-#pragma unroll
-    for (int j = 0; j < kN; ++j)
-#pragma unroll
-      for (uint32_t e = 0; e < kPack; ++e) {
-        if (e >= at.n[j]) d[j][e] = 0.f;
-        const float a = open(raw_gate[j].v[e], p), through = d[j][e] * unit[j][e], slope = through * weight[j][e];
-        sums[0][j][e] += through * a;
-        all += slope;
-        dgate[j][e] = p.sigmoid ? slope * a * (1.f - a) : slope;
-        d[j][e] *= weight[j][e] * a;
-      }
+    // from here on: the gradient of what was added to x, through the gate, the scale and the weight
+    if (in) each<kN>([&](int j, uint32_t e) { sums[0][j][e] += d[j][e] * gate[j][e] * unit[j][e]; });
+    const bool one = p.dgate && !p.each;
+    float all = one ? at.sum([&](int j, uint32_t e) { return d[j][e] * weight[j][e] * unit[j][e]; }) : 0.f;
+    if (p.dgate && p.each) {
+      Row<kN> slope;
+      each<kN>([&](int j, uint32_t e) { slope[j][e] = d[j][e] * weight[j][e] * unit[j][e] * (p.sigmoid ? gate[j][e] * (1.f - gate[j][e]) : 1.f); });
+      put_row((T*)p.dgate + r * p.ld_dgate, slope, at, in);
+    }
+    each<kN>([&](int j, uint32_t e) { d[j][e] *= weight[j][e] * gate[j][e]; });
     if (p.post) {
-      denormalise(d, unit, inverse, g, p.layer, p.whole, all);
-    } else if (p.gate && !p.each) {
+      denormalise(d, unit, inverse, g, at, p.layer, p.whole, one, all);
+    } else if (one) {
       float s[1] = {all};
       g.sum(s);
       all = s[0];
     }
     if (p.dy) put_row((T*)p.dy + r * p.ld_dy, d, at, in);
-    if (!p.dgate) continue;
-    if (p.each) {
-      put_row((T*)p.dgate + r * p.ld_dgate, dgate, at, in);
-    } else if (in && g.mine == 0u) {
-      const float a = open(raw_gate[0].v[0], p);
-      ((T*)p.dgate)[r * p.ld_dgate] = (T)(p.sigmoid ? all * a * (1.f - a) : all);
-    }
+    if (one && in && g.mine == 0u) ((T*)p.dgate)[r * p.ld_dgate] = (T)(p.sigmoid ? all * gate[0][kPack - 1] * (1.f - gate[0][kPack - 1]) : all);
+    if (!kAhead<kN>) get(r + stride);
   }
   if (p.sums) leave_sums(sums, p.sums + (uint64_t)blockIdx.x * 2u * p.wide, p.wide, g, at, p.slots, columns);
 }
@@ -484,16 +530,16 @@ struct SumArgs {
   uint32_t single, half;            // half: vectors that are not in 32 bits are in f16, not bf16
   float number;
 };
-constexpr uint32_t kStrips = 16;
-__global__ __launch_bounds__(64 * kStrips) void k_sum_columns(SumArgs p) {
-  __shared__ float shared[kStrips][64];
-  const uint32_t lane = threadIdx.x % 64u, strip = threadIdx.x / 64u, c = blockIdx.x * 64u + lane, which = blockIdx.y;
+constexpr uint32_t kStrips = 32, kAtOnce = 32;   // workgroups' sums that are read side by side, columns
+__global__ __launch_bounds__(kAtOnce * kStrips) void k_sum_columns(SumArgs p) {
+  __shared__ float shared[kStrips][kAtOnce];
+  const uint32_t lane = threadIdx.x % kAtOnce, strip = threadIdx.x / kAtOnce, c = blockIdx.x * kAtOnce + lane, which = blockIdx.y;
   const uint32_t each = (p.rows + kStrips - 1u) / kStrips, from = strip * each, to = from + each < p.rows ? from + each : p.rows;
   float s = 0.f;
   if (c < p.dim) {
     const float* in = p.sums + which * p.wide + c;
     const uint64_t step = (uint64_t)p.n_sums * p.wide;
-#pragma unroll 8
+#pragma unroll 16
     for (uint32_t r = from; r < to; ++r) s += in[r * step];
   }
   shared[strip][lane] = s;
@@ -525,14 +571,14 @@ struct Layout {
 Layout lay_out(uint64_t rows, uint32_t dim, bool backward) {
   Layout l;
   const uint32_t packs = (uint32_t)ceil_div(dim, kPack);
-  l.packs = packs > kMostLanes ? 2 : 1;
+  l.packs = 1;
+  while (packs > l.packs * kMostLanes) l.packs *= 2u;
   const uint32_t need = (uint32_t)ceil_div(packs, l.packs);
   l.lanes = 1;
   while (l.lanes < need && l.lanes < 64u) l.lanes *= 2u;
   if (need > 64u) l.lanes = (uint32_t)round_up(need, 64);
   const uint32_t target = backward ? 512 : 256;
   l.slots = l.lanes < target ? target / l.lanes : 1u;
-  while (l.lanes * l.slots % 64u) ++l.slots;
   const uint64_t blocks = ceil_div(rows, l.slots), most = backward ? 512 : 2048;
   l.blocks = (uint32_t)(blocks < most ? blocks : most);
   return l;
@@ -586,24 +632,27 @@ fbx_status check(const fbx_join* h) {
   return FBX_OK;
 }
 
-template <template <class, class, int> class K, class A>
+template <template <class, class, Shape> class K, class A>
 void launch(const A& p, const Layout& l, fbx_dtype stream, fbx_dtype block, uint32_t lds, hipStream_t on) {
   const dim3 grid(l.blocks), threads(l.threads());
-  auto go = [&](auto packs) {
-    constexpr int n = decltype(packs)::value;
-    if (stream == FBX_F32 && block == FBX_F32) launch_on(on, K<float, float, n>::kernel, grid, threads, lds, p);
-    else if (stream == FBX_F32 && block == FBX_F16) launch_on(on, K<float, _Float16, n>::kernel, grid, threads, lds, p);
-    else if (stream == FBX_F32) launch_on(on, K<float, __bf16, n>::kernel, grid, threads, lds, p);
-    else if (stream == FBX_F16) launch_on(on, K<_Float16, _Float16, n>::kernel, grid, threads, lds, p);
-    else launch_on(on, K<__bf16, __bf16, n>::kernel, grid, threads, lds, p);
+  auto go = [&](auto shape) {
+    constexpr Shape s = decltype(shape)::value;
+    if (stream == FBX_F32 && block == FBX_F32) launch_on(on, K<float, float, s>::kernel, grid, threads, lds, p);
+    else if (stream == FBX_F32 && block == FBX_F16) launch_on(on, K<float, _Float16, s>::kernel, grid, threads, lds, p);
+    else if (stream == FBX_F32) launch_on(on, K<float, __bf16, s>::kernel, grid, threads, lds, p);
+    else if (stream == FBX_F16) launch_on(on, K<_Float16, _Float16, s>::kernel, grid, threads, lds, p);
+    else launch_on(on, K<__bf16, __bf16, s>::kernel, grid, threads, lds, p);
   };
-  if (l.packs == 1) go(std::integral_constant<int, 1>());
-  else go(std::integral_constant<int, 2>());
+  if (p.dim < kPack) go(std::integral_constant<Shape, kTiny1>());
+  else if (l.lanes < 64u) go(std::integral_constant<Shape, kNarrow1>());
+  else if (l.packs == 1u) go(std::integral_constant<Shape, kWide1>());
+  else if (l.packs == 2u) go(std::integral_constant<Shape, kWide2>());
+  else go(std::integral_constant<Shape, kWide4>());
 }
-template <class R, class T, int kN> struct Norm { static constexpr auto kernel = k_norm<R, T, kN>; };
-template <class R, class T, int kN> struct NormGrad { static constexpr auto kernel = k_norm_grad<R, T, kN>; };
-template <class R, class T, int kN> struct Join { static constexpr auto kernel = k_join<R, T, kN>; };
-template <class R, class T, int kN> struct JoinGrad { static constexpr auto kernel = k_join_grad<R, T, kN>; };
+template <class R, class T, Shape kShape> struct Norm { static constexpr auto kernel = k_norm<R, T, kShape>; };
+template <class R, class T, Shape kShape> struct NormGrad { static constexpr auto kernel = k_norm_grad<R, T, kShape>; };
+template <class R, class T, Shape kShape> struct Join { static constexpr auto kernel = k_join<R, T, kShape>; };
+template <class R, class T, Shape kShape> struct JoinGrad { static constexpr auto kernel = k_join_grad<R, T, kShape>; };
 
 void sum_columns(SumArgs& s, uint32_t dim, uint32_t blocks, uint32_t n_sums, fbx_dtype vectors, hipStream_t stream) {
   s.dim = dim;
@@ -612,7 +661,7 @@ void sum_columns(SumArgs& s, uint32_t dim, uint32_t blocks, uint32_t n_sums, fbx
   s.n_sums = n_sums;
   s.single = vectors == FBX_F32;
   s.half = vectors == FBX_F16;
-  launch_on(stream, k_sum_columns, dim3((uint32_t)ceil_div(dim, 64), n_sums), dim3(64 * kStrips), 0, s);
+  launch_on(stream, k_sum_columns, dim3((uint32_t)ceil_div(dim, kAtOnce), n_sums), dim3(kAtOnce * kStrips), 0, s);
 }
 
 NormArgs args_of(const fbx_norm* h, const Layout& l) {
@@ -657,7 +706,10 @@ JoinArgs args_of(const fbx_join* h, const Layout& l) {
   p.number = (float)h->scale;
   return p;
 }
-uint32_t lds_of(const Layout& l, uint32_t dim, uint32_t sums) { return l.slots > 1 ? wide_of(dim) * sums * 4u : 0u; }
+uint32_t lds_of(const Layout& l, uint32_t dim, uint32_t sums) {
+  const uint32_t lines = l.lanes < 64u ? l.threads() / 64u : l.slots;
+  return lines > 1u ? lines * wide_of(dim) * sums * 4u : 0u;
+}
 uint64_t sums_bytes(uint64_t records, uint32_t dim, uint32_t sums) { return round_up((uint64_t)lay_out(records, dim, true).blocks * wide_of(dim) * sums * 4u, 256); }
 
 }  // namespace
