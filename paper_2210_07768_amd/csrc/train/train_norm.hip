@@ -63,11 +63,11 @@ struct Group {
 #pragma unroll
       for (int i = 0; i < kN; ++i) at[i * kWaves + wave] = v[i];
     __syncthreads();
-    // the row's wavefronts' sums, one a lane of sixteen
+    // the row's wavefronts' sums, one a lane of eight
 #pragma unroll
-    for (int i = 0; i < kN; ++i) v[i] = lane % 16u < waves ? at[i * kWaves + slot * waves + lane % 16u] : 0.f;
+    for (int i = 0; i < kN; ++i) v[i] = lane % kWaves < waves ? at[i * kWaves + slot * waves + lane % kWaves] : 0.f;
 #pragma unroll
-    for (int i = 0; i < kN; ++i) v[i] = sixteen(v[i], 64u);
+    for (int i = 0; i < kN; ++i) v[i] = sixteen(v[i], kWaves);
   }
   // Sums over 2, 4, 8 or 16 neighbouring lanes, as many as `n` reaches.
   __device__ __forceinline__ static float sixteen(float v, uint32_t n) {
@@ -188,26 +188,29 @@ __device__ __forceinline__ void fetch_vector(Row<kN>& to, const void* from, bool
 // v becomes (v - mean) / sqrt(variance + eps), or v / sqrt(mean square + eps); returns 1 / sqrt.  Squares are taken behind the mean:
 // sums of squares less a squared mean would lose what a large mean hides.  What rounding left of the mean is found beside them
 // and taken off too, so that a row of one large number is one of zeros.
+struct Scale {
+  float dim, one_dim, eps;   // one_dim: 1 / dim
+};
 template <int kN, bool kTiny, class G>
-__device__ __forceinline__ float normalise(Row<kN>& v, G& g, const Columns<kN, kTiny>& at, bool layer, float dim, float eps) {
+__device__ __forceinline__ float normalise(Row<kN>& v, G& g, const Columns<kN, kTiny>& at, bool layer, Scale by) {
   float square;
   if (layer) {
     float all[1] = {at.sum([&](int j, uint32_t e) { return v[j][e]; })};
     g.sum(all);
-    const float mean = all[0] / dim;
+    const float mean = all[0] / by.dim;   // (the quotient, so that the mean of equal numbers is theirs if their sum is exact)
     each<kN>([&](int j, uint32_t e) { v[j][e] -= mean; });
     float s[2] = {at.sum([&](int j, uint32_t e) { return v[j][e] * v[j][e]; }), at.sum([&](int j, uint32_t e) { return v[j][e]; })};
     g.sum(s);
-    const float rest = s[1] / dim;
+    const float rest = s[1] * by.one_dim;
     each<kN>([&](int j, uint32_t e) { v[j][e] -= rest; });
-    square = s[0] / dim - rest * rest;
+    square = s[0] * by.one_dim - rest * rest;
     if (square < 0.f) square = 0.f;
   } else {
     float s[1] = {at.sum([&](int j, uint32_t e) { return v[j][e] * v[j][e]; })};
     g.sum(s);
-    square = s[0] / dim;
+    square = s[0] * by.one_dim;
   }
-  const float inverse = 1.f / __builtin_sqrtf(square + eps);
+  const float inverse = __builtin_amdgcn_rsqf(square + by.eps);   // (a unit in the last place; eps is a normal number)
   each<kN>([&](int j, uint32_t e) { v[j][e] *= inverse; });
   return inverse;
 }
@@ -215,21 +218,20 @@ __device__ __forceinline__ float normalise(Row<kN>& v, G& g, const Columns<kN, k
 // p, the gradient of normalised rows, becomes that of what they were made from: inverse (p - mean p - unit mean(p unit)), the
 // first mean for a layer's norm only.  more: another sum over the row, where it is wanted too.
 template <int kN, bool kTiny, class G>
-__device__ __forceinline__ void denormalise(Row<kN>& p, const Row<kN>& unit, float inverse, G& g, const Columns<kN, kTiny>& at, bool layer, float dim, bool wanted, float& more) {
+__device__ __forceinline__ void denormalise(Row<kN>& p, const Row<kN>& unit, float inverse, G& g, const Columns<kN, kTiny>& at, bool layer, Scale by, bool wanted, float& more) {
   float along = at.sum([&](int j, uint32_t e) { return p[j][e] * unit[j][e]; }), mean = 0.f;
   if (layer || wanted) {
     float s[3] = {along, at.sum([&](int j, uint32_t e) { return p[j][e]; }), more};
     g.sum(s);
     along = s[0];
-    mean = layer ? s[1] / dim : 0.f;
+    mean = layer ? s[1] * by.one_dim * inverse : 0.f;
     more = s[2];
   } else {
     float s[1] = {along};
     g.sum(s);
     along = s[0];
   }
-  along *= inverse / dim;
-  mean *= inverse;
+  along *= inverse * by.one_dim;
   each<kN>([&](int j, uint32_t e) { p[j][e] = p[j][e] * inverse - mean - unit[j][e] * along; });
 }
 
@@ -286,7 +288,7 @@ struct NormArgs {
   uint64_t ld_x, ld_out, ld_dy, ld_dx, rows;
   uint32_t dim, wide, lanes, slots;
   uint32_t layer, single;           // single: vectors are in 32 bits
-  float eps, whole;                 // whole: dim
+  Scale by;
 };
 
 // R: of the residual stream; T: of the result.  A row's loads are on their way while the one before it is worked on, but for rows that
@@ -314,7 +316,7 @@ __global__ __launch_bounds__(kMostLanes) void k_norm(NormArgs p) {
     Row<kN> v;
     widen(v, raw);
     if (kAhead<kN>) get(r + stride);
-    normalise(v, g, at, p.layer, p.whole, p.eps);
+    normalise(v, g, at, p.layer, p.by);
     each<kN>([&](int j, uint32_t e) { v[j][e] *= weight[j][e]; });
     put_row((T*)p.out + r * p.ld_out, v, at, r < p.rows);
     if (!kAhead<kN>) get(r + stride);
@@ -347,12 +349,12 @@ __global__ __launch_bounds__(kMostLanes) void k_norm_grad(NormArgs p) {
     widen(unit, raw_x);
     widen(d, raw_dy);
     if (kAhead<kN>) get(r + stride);
-    const float inverse = normalise(unit, g, at, p.layer, p.whole, p.eps);
+    const float inverse = normalise(unit, g, at, p.layer, p.by);
     if (r < p.rows) each<kN>([&](int j, uint32_t e) { sums[0][j][e] += d[j][e] * unit[j][e]; });
     if (p.dx) {
       float none = 0.f;
       each<kN>([&](int j, uint32_t e) { d[j][e] *= weight[j][e]; });
-      denormalise(d, unit, inverse, g, at, p.layer, p.whole, false, none);
+      denormalise(d, unit, inverse, g, at, p.layer, p.by, false, none);
       put_row((R*)p.dx + r * p.ld_dx, d, at, r < p.rows);
     }
     if (!kAhead<kN>) get(r + stride);
@@ -367,7 +369,8 @@ struct JoinArgs {
   uint64_t ld_x, ld_y, ld_gate, ld_out, ld_next, ld_dout, ld_dnext, ld_dx, ld_dy, ld_dgate, rows;
   uint32_t dim, wide, lanes, slots;
   uint32_t layer, single, post, then, each, sigmoid;  // each: a gate for each element, not one a row
-  float eps, whole, number;         // whole: dim; number: the scale, where it is no vector
+  Scale by;
+  float number;                     // the scale, where it is no vector
 };
 
 // e^-a by the hardware's exponential and reciprocal (one unit in the last place each).
@@ -434,11 +437,11 @@ __global__ __launch_bounds__(kMostLanes) void k_join(JoinArgs p) {
     open(gate, now.gate, now.only, p);
     widen(x, now.x);
     if (kAhead<kN>) get(r + stride);
-    if (p.post) normalise(v, g, at, p.layer, p.whole, p.eps);
+    if (p.post) normalise(v, g, at, p.layer, p.by);
     each<kN>([&](int j, uint32_t e) { v[j][e] = x[j][e] + gate[j][e] * weight[j][e] * v[j][e]; });
     put_row((R*)p.out + r * p.ld_out, v, at, r < p.rows);
     if (p.then) {
-      normalise(v, g, at, p.layer, p.whole, p.eps);
+      normalise(v, g, at, p.layer, p.by);
       each<kN>([&](int j, uint32_t e) { v[j][e] *= next_weight[j][e]; });
       put_row((T*)p.next + r * p.ld_next, v, at, r < p.rows);
     }
@@ -477,37 +480,44 @@ __global__ __launch_bounds__(kMostLanes) void k_join_grad(JoinArgs p) {
     if (!kAhead<kN>) fetch_vectors<T>(weight, next_weight, p, at);
     const Operands<R, T, kN> it = now;
     if (kAhead<kN>) get(r + stride);
-    Row<kN> unit, gate, d;
+    Row<kN> unit, gate, by, d;   // by: gate times weight and scale
     widen(unit, it.y);
     float inverse = 1.f;
-    if (p.post) inverse = normalise(unit, g, at, p.layer, p.whole, p.eps);
+    if (p.post) inverse = normalise(unit, g, at, p.layer, p.by);
     open(gate, it.gate, it.only, p);
+    each<kN>([&](int j, uint32_t e) { by[j][e] = gate[j][e] * weight[j][e]; });
     if (p.dout) widen(d, it.dout);
     else each<kN>([&](int j, uint32_t e) { d[j][e] = 0.f; });
     if (p.then) {
       Row<kN> after, q;
-      each<kN>([&](int j, uint32_t e) { after[j][e] = (float)it.x[j].v[e] + gate[j][e] * weight[j][e] * unit[j][e]; });
-      const float after_inverse = normalise(after, g, at, p.layer, p.whole, p.eps);
+      each<kN>([&](int j, uint32_t e) { after[j][e] = (float)it.x[j].v[e] + by[j][e] * unit[j][e]; });
+      const float after_inverse = normalise(after, g, at, p.layer, p.by);
       widen(q, it.dnext);
       if (in) each<kN>([&](int j, uint32_t e) { sums[1][j][e] += q[j][e] * after[j][e]; });
       each<kN>([&](int j, uint32_t e) { q[j][e] *= next_weight[j][e]; });
       float none = 0.f;
-      denormalise(q, after, after_inverse, g, at, p.layer, p.whole, false, none);
+      denormalise(q, after, after_inverse, g, at, p.layer, p.by, false, none);
       each<kN>([&](int j, uint32_t e) { d[j][e] += q[j][e]; });
     }
     if (p.dx) put_row((R*)p.dx + r * p.ld_dx, d, at, in);
     // from here on: the gradient of what was added to x, through the gate, the scale and the weight
-    if (in) each<kN>([&](int j, uint32_t e) { sums[0][j][e] += d[j][e] * gate[j][e] * unit[j][e]; });
     const bool one = p.dgate && !p.each;
-    float all = one ? at.sum([&](int j, uint32_t e) { return d[j][e] * weight[j][e] * unit[j][e]; }) : 0.f;
-    if (p.dgate && p.each) {
-      Row<kN> slope;
-      each<kN>([&](int j, uint32_t e) { slope[j][e] = d[j][e] * weight[j][e] * unit[j][e] * (p.sigmoid ? gate[j][e] * (1.f - gate[j][e]) : 1.f); });
-      put_row((T*)p.dgate + r * p.ld_dgate, slope, at, in);
+    float all = 0.f;
+    {
+      Row<kN> through;
+      each<kN>([&](int j, uint32_t e) { through[j][e] = d[j][e] * unit[j][e]; });
+      if (in) each<kN>([&](int j, uint32_t e) { sums[0][j][e] += through[j][e] * gate[j][e]; });
+      if (one) {
+        all = at.sum([&](int j, uint32_t e) { return through[j][e] * weight[j][e]; });
+      } else if (p.dgate) {
+        if (p.sigmoid) each<kN>([&](int j, uint32_t e) { through[j][e] *= by[j][e] * (1.f - gate[j][e]); });
+        else each<kN>([&](int j, uint32_t e) { through[j][e] *= weight[j][e]; });
+        put_row((T*)p.dgate + r * p.ld_dgate, through, at, in);
+      }
     }
-    each<kN>([&](int j, uint32_t e) { d[j][e] *= weight[j][e] * gate[j][e]; });
+    each<kN>([&](int j, uint32_t e) { d[j][e] *= by[j][e]; });
     if (p.post) {
-      denormalise(d, unit, inverse, g, at, p.layer, p.whole, one, all);
+      denormalise(d, unit, inverse, g, at, p.layer, p.by, one, all);
     } else if (one) {
       float s[1] = {all};
       g.sum(s);
@@ -564,6 +574,7 @@ __global__ __launch_bounds__(kAtOnce * kStrips) void k_sum_columns(SumArgs p) {
 }
 
 // How rows go to lanes: `packs` of a lane, lanes of a row, rows a workgroup holds at a time, workgroups.
+constexpr uint64_t kMostBlocks = 1u << 20;   // (a launch's lanes are counted in 32 bits)
 struct Layout {
   uint32_t packs, lanes, slots, blocks;
   uint32_t threads() const { return lanes * slots; }
@@ -579,8 +590,11 @@ Layout lay_out(uint64_t rows, uint32_t dim, bool backward) {
   if (need > 64u) l.lanes = (uint32_t)round_up(need, 64);
   const uint32_t target = backward ? 512 : 256;
   l.slots = l.lanes < target ? target / l.lanes : 1u;
-  const uint64_t blocks = ceil_div(rows, l.slots), most = backward ? 512 : 2048;
-  l.blocks = (uint32_t)(blocks < most ? blocks : most);
+  // A gradient's workgroups leave sums of columns behind, so there are few; the others take a row four times, in which the weights that
+  // a lane holds serve again (65,536 x 2,624 in bf16, norm and join: 2,048 workgroups 135 and 483 us, 8,192 122 and 448, 16,384 118 and
+  // 437, 65,536 140 and 541), or less often where that leaves fewer than 2,048.
+  const uint64_t groups = ceil_div(rows, l.slots), fours = ceil_div(groups, 4), least = backward ? 512 : fours > 2048 ? fours : 2048;
+  l.blocks = (uint32_t)(groups < least ? groups : least < kMostBlocks ? least : kMostBlocks);
   return l;
 }
 
@@ -676,8 +690,7 @@ NormArgs args_of(const fbx_norm* h, const Layout& l) {
   p.slots = l.slots;
   p.layer = h->kind == FBX_NORM_LAYER;
   p.single = h->vectors == FBX_F32;
-  p.eps = (float)h->eps;
-  p.whole = (float)h->dim;
+  p.by = Scale{(float)h->dim, (float)(1.0 / h->dim), (float)h->eps};
   return p;
 }
 JoinArgs args_of(const fbx_join* h, const Layout& l) {
@@ -701,8 +714,7 @@ JoinArgs args_of(const fbx_join* h, const Layout& l) {
   p.post = h->post != 0;
   p.each = h->gate_columns != 1;
   p.sigmoid = h->gate_act == FBX_GATE_SIGMOID;
-  p.eps = (float)h->eps;
-  p.whole = (float)h->dim;
+  p.by = Scale{(float)h->dim, (float)(1.0 / h->dim), (float)h->eps};
   p.number = (float)h->scale;
   return p;
 }
