@@ -443,6 +443,16 @@ fbx_dtype code_of(PyObject* dtype, fbx_dtype none) {
 }
 at::ScalarType type_of(fbx_dtype t) { return t == FBX_F32 ? at::kFloat : t == FBX_F16 ? at::kHalf : at::kBFloat16; }
 const at::Tensor* maybe(PyObject* o, const char* name) { return o == Py_None ? nullptr : &input(o, name); }
+// Whether autograd is to be asked instead: an input wants its gradient.
+bool asks(std::initializer_list<const at::Tensor*> inputs, bool out) {
+  if (!c10::GradMode::is_enabled()) return false;
+  for (const at::Tensor* t : inputs)
+    if (t && t->requires_grad()) {
+      if (out) bad("a tensor given for a result cannot take part in autograd");
+      return true;
+    }
+  return false;
+}
 
 // Rows of a batch: n x columns, on the device of the others.
 uint64_t rows_of(const at::Tensor& t, const char* name, fbx_dtype type, const at::Tensor& like, int64_t n, int64_t columns) {
@@ -497,14 +507,15 @@ struct NormCall {
   }
 };
 
-// norm(x, weight, dtype, kind, eps, out)
+// norm(x, weight, dtype, kind, eps, out); NotImplemented where autograd is to be asked
 PyObject* norm(PyObject*, PyObject* args) {
   PyObject *x, *weight, *dtype, *out_o;
   int kind;
   double eps;
   if (!PyArg_ParseTuple(args, "OOOidO", &x, &weight, &dtype, &kind, &eps, &out_o)) return nullptr;
-  return guarded([&] {
+  return guarded([&]() -> PyObject* {
     const NormCall c(x, weight, dtype, kind, eps);
+    if (asks({&c.x, c.weight}, out_o != Py_None)) Py_RETURN_NOTIMPLEMENTED;
     if (out_o != Py_None) rows_of(result(out_o), "out", c.a.block, c.x, c.a.records, c.a.dim);
     const c10::DeviceGuard guard(c.x.device());
     at::Tensor out = out_o == Py_None ? at::empty({c.x.size(0), c.x.size(1)}, c.x.options().dtype(type_of(c.a.block)).memory_format(c10::nullopt)) : tensor(out_o, "out");
@@ -581,7 +592,7 @@ struct JoinCall {
   }
 };
 
-// join(x, y, weight, gate, scale, next_weight, post, then, gate_act, kind, eps, out, out_next)
+// join(x, y, weight, gate, scale, next_weight, post, then, gate_act, kind, eps, out, out_next); NotImplemented where autograd is to be asked
 PyObject* join(PyObject*, PyObject* args) {
   PyObject *what[6], *out_o[2];
   int post, then, gate_act, kind;
@@ -589,6 +600,7 @@ PyObject* join(PyObject*, PyObject* args) {
   if (!PyArg_ParseTuple(args, "OOOOOOppiidOO", &what[0], &what[1], &what[2], &what[3], &what[4], &what[5], &post, &then, &gate_act, &kind, &eps, &out_o[0], &out_o[1])) return nullptr;
   return guarded([&]() -> PyObject* {
     const JoinCall c(what, post, gate_act, kind, eps);
+    if (asks({&c.x, &c.y, c.weight, c.gate, c.scale, c.next_weight}, out_o[0] != Py_None || out_o[1] != Py_None)) Py_RETURN_NOTIMPLEMENTED;
     if (!then && (c.next_weight || out_o[1] != Py_None)) bad("next_weight and out_next are of the next norm: none without then");
     const fbx_dtype types[2] = {c.a.stream, c.a.block};
     at::Tensor out[2];

@@ -27,6 +27,7 @@ EXPORTS = [
 ACTS = {"silu": 0, "gelu": 1, "relu": 2, "sigmoid": 3}
 KINDS = {"rms": 0, "layer": 1}           # of a norm
 GATES = {"none": 0, "sigmoid": 1}
+_KINDS, _GATES = tuple(KINDS), tuple(GATES)   # (`in` a tuple takes what has no hash, too)
 NEWTON_SCHULZ = (3.4445, -4.7750, 2.0315)   # takes singular values from (0, 1] to near 1 in five steps
 BLOCK = 32   # elements that share a scale in 8-bit states
 NORM_MOST = 16384   # elements of a row that is normed
@@ -188,20 +189,12 @@ def _code(given, of: dict, name: str) -> int:
     return code
 
 
-def _asks(*tensors) -> bool:
-    return torch.is_grad_enabled() and any(isinstance(t, torch.Tensor) and t.requires_grad for t in tensors)
-
-
 def norm(x, weight=None, kind: str = "rms", eps: float = 1e-6, dtype=None, out=None):
     """Rows of x brought to unit size, times weight: x / sqrt(mean(x^2) + eps) (kind "rms"), or the same of x less its mean
     ("layer").  x: records x dim; weight: dim elements, of the result's type or float32; dtype: of the result: x's, or, where x is
     float32, float16 or bfloat16."""
-    _tensors(x=x)
-    if _asks(x, weight):
-        if out is not None:
-            _bad("out cannot take part in autograd")
-        return _Norm.apply(x, weight, kind, eps, dtype)
-    return _load().norm(x, weight, dtype, _code(kind, KINDS, "kind"), eps, out)
+    got = (_native or _load()).norm(x, weight, dtype, KINDS[kind] if kind in _KINDS else _code(kind, KINDS, "kind"), eps, out)
+    return _Norm.apply(x, weight, kind, eps, dtype) if got is NotImplemented else got   # (where an input asks for its gradient)
 
 
 def norm_backward(dy, x, weight=None, kind: str = "rms", eps: float = 1e-6, need_dx: bool = True, need_dw: bool = True):
@@ -221,13 +214,11 @@ def join(x, y, weight=None, gate=None, scale=1.0, next_weight=None, *, post: boo
     weight, next_weight, scale: dim elements, all of y's type or all float32; scale may be a number.
     gate: records x dim, or records x 1, of y's type; gate_act: "sigmoid", or "none" where it is to be taken as it is.
     post: false leaves out y's norm (and has no weight): x + scale * act(gate) * y."""
-    _tensors(x=x, y=y)
-    then = next_weight is not None if then is None else bool(then)
-    if _asks(x, y, weight, gate, scale, next_weight):
-        if out is not None or out_next is not None:
-            _bad("out and out_next cannot take part in autograd")
-        return _Join.apply(x, y, weight, gate, scale, next_weight, post, then, gate_act, kind, eps)
-    return _load().join(x, y, weight, gate, scale, next_weight, post, then, _code(gate_act, GATES, "gate_act"), _code(kind, KINDS, "kind"), eps, out, out_next)
+    if then is None:
+        then = next_weight is not None
+    got = (_native or _load()).join(x, y, weight, gate, scale, next_weight, post, then, GATES[gate_act] if gate_act in _GATES else _code(gate_act, GATES, "gate_act"),
+                                    KINDS[kind] if kind in _KINDS else _code(kind, KINDS, "kind"), eps, out, out_next)
+    return _Join.apply(x, y, weight, gate, scale, next_weight, post, then, gate_act, kind, eps) if got is NotImplemented else got
 
 
 class JoinGradients(NamedTuple):
