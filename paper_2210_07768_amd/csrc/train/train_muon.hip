@@ -24,7 +24,7 @@ namespace {
 typedef _Float16 f16;
 constexpr uint32_t kMatrices = 32;        // of a launch
 constexpr uint32_t kDepth = kStepBytes / sizeof(f16);
-constexpr uint32_t kMostPartials = 512;   // of a matrix's sum of squares
+constexpr uint32_t kMostPartials = 256;   // of a matrix's sum of squares
 constexpr int kX = 14;                    // X is held times 2^14, but for the first
 
 // One matrix of a launch: what it is made of, where its result goes, and its scratch.
@@ -66,85 +66,112 @@ struct List {
 
 struct PrepareArgs {
   List list;
-  uint32_t in, given;                     // types: of the matrix or gradient; given: there is momentum
   uint32_t nesterov;
   float momentum, grad_scale;
   double eps;
 };
 
-__device__ __forceinline__ float element(const void* p, uint64_t i, uint32_t type) {
-  return type == FBX_F32 ? ((const float*)p)[i] : type == FBX_F16 ? (float)((const f16*)p)[i] : (float)((const __bf16*)p)[i];
+// Eight adjacent elements from i on, of which the first n exist (more exist behind them where n is 8), wherever they begin.
+template <class X>
+__device__ __forceinline__ void fetch(float (&to)[8], const X* from, uint32_t n) {
+  Pack<X, 8> p = {};
+  if (n >= 8u) {
+    __builtin_memcpy(&p, from, sizeof p);
+  } else {
+#pragma unroll
+    for (uint32_t e = 0; e < 8u; ++e)
+      if (e < n) p.v[e] = from[e];
+  }
+#pragma unroll
+  for (uint32_t e = 0; e < 8u; ++e) to[e] = (float)p.v[e];
+}
+
+// Sum over a workgroup of 256 lanes, in all of them.
+__device__ __forceinline__ double sum_of(double v, double* shared) {
+#pragma unroll
+  for (int d = 32; d; d /= 2) v += __shfl_xor(v, d, 64);
+  if (threadIdx.x % 64u == 0u) shared[threadIdx.x / 64u] = v;
+  __syncthreads();
+  return (shared[0] + shared[1]) + (shared[2] + shared[3]);
 }
 
 // Sums of squares, in 64 bits so that they stay within range whatever the gradient's size; momentum is brought up to date.
 // A workgroup adds up `chunk` elements.
+template <class G, bool kGiven>
 __global__ __launch_bounds__(256) void k_measure(PrepareArgs) {
+#pragma clang fp contract(off)
   const PrepareArgs& p = launch_args<PrepareArgs>();
   const uint32_t which = same(p.list.find(blockIdx.x));
   const Matrix& t = p.list.of[which];
   const uint32_t part = blockIdx.x - p.list.first[which];
   const uint64_t all = (uint64_t)t.rows * t.columns, from = (uint64_t)part * t.chunk, to = from + t.chunk < all ? from + t.chunk : all;
   double sum = 0;
-  for (uint64_t i = from + threadIdx.x; i < to; i += 256u) {
-    float u;
-    if (p.given) {
-#pragma clang fp contract(off)
-      const float g = element(t.u, i, p.in) * p.grad_scale, m = t.m[i] * p.momentum + g;
-      t.m[i] = m;
-      u = p.nesterov ? g + m * p.momentum : m;
-    } else {
-      const uint64_t r = t.ld_u == t.columns ? 0u : i / t.columns;
-      u = element(t.u, i + r * (t.ld_u - t.columns), p.in);
+  if (kGiven || t.ld_u == t.columns) {
+    for (uint64_t i = from + threadIdx.x * 8u; i < to; i += 2048u) {
+      const uint32_t n = to - i < 8u ? (uint32_t)(to - i) : 8u;
+      float u[8];
+      fetch(u, (const G*)t.u + i, n);
+      if (kGiven) {
+        float m[8];
+        fetch(m, t.m + i, n);
+#pragma unroll
+        for (uint32_t e = 0; e < 8u; ++e) {
+          const float g = u[e] * p.grad_scale;
+          m[e] = m[e] * p.momentum + g;
+          u[e] = p.nesterov ? g + m[e] * p.momentum : m[e];
+        }
+        if (n == 8u) {
+          __builtin_memcpy(t.m + i, m, sizeof m);
+        } else {
+#pragma unroll
+          for (uint32_t e = 0; e < 8u; ++e)
+            if (e < n) t.m[i + e] = m[e];
+        }
+      }
+#pragma unroll
+      for (uint32_t e = 0; e < 8u; ++e) sum += (double)u[e] * u[e];   // (zeros behind the last)
     }
-    sum += (double)u * u;
+  } else {
+    for (uint64_t i = from + threadIdx.x; i < to; i += 256u) {
+      const float u = (float)((const G*)t.u)[i / t.columns * t.ld_u + i % t.columns];
+      sum += (double)u * u;
+    }
   }
-  __shared__ double sums[256];
-  sums[threadIdx.x] = sum;
-  __syncthreads();
-  for (uint32_t d = 128; d; d /= 2u) {
-    if (threadIdx.x < d) sums[threadIdx.x] += sums[threadIdx.x + d];
-    __syncthreads();
-  }
-  if (threadIdx.x == 0u) t.squares()[part] = sums[0];
+  __shared__ double sums[4];
+  sum = sum_of(sum, sums);
+  if (threadIdx.x == 0u) t.squares()[part] = sum;
 }
 
 // The matrix's parts of 16 bits, times the power of two that brings its norm into [2^13, 2^14): one times 2^14 for the
 // steps that follow, and the factor that makes X of it.  A workgroup takes 64 x 64 elements of X (zeros beyond them).
 constexpr uint32_t kSquare = 64;
+template <class G, bool kGiven>
 __global__ __launch_bounds__(256) void k_split(PrepareArgs) {
+#pragma clang fp contract(off)
   const PrepareArgs& p = launch_args<PrepareArgs>();
   const uint32_t which = same(p.list.find(blockIdx.x));
   const Matrix& t = p.list.of[which];
   const uint32_t tile = blockIdx.x - p.list.first[which], across = t.wide_n / kSquare, r0 = tile / across * kSquare, c0 = tile % across * kSquare;
-  __shared__ double sums[256];
+  __shared__ double sums[4];
   __shared__ float turned[kSquare][kSquare + 1];
-  double sum = 0;
-  for (uint32_t i = threadIdx.x; i < t.partials; i += 256u) sum += t.squares()[i];
-  sums[threadIdx.x] = sum;
-  const uint32_t lane = threadIdx.x % 64u, wave = threadIdx.x / 64u;
-  // rows of what is given: those of X, or its columns
-  const uint32_t row0 = t.tall ? c0 : r0, column = (t.tall ? r0 : c0) + lane;
-  float u[kSquare / 4];
+  const double square = threadIdx.x < t.partials ? t.squares()[threadIdx.x] : 0.0;
+  const uint32_t line = threadIdx.x / 8u, place = threadIdx.x % 8u * 8u;   // lines `line` and `line` + 32 of the tile, eight elements of each
+  // a tile of what is given has the rows of X, or its columns, for rows
+  const uint32_t row0 = (t.tall ? c0 : r0) + line, column = (t.tall ? r0 : c0) + place;
+  float u[2][8];
 #pragma unroll
-  for (uint32_t k = 0; k < kSquare / 4; ++k) {
-    const uint32_t row = row0 + wave + 4u * k;
-    u[k] = 0.f;
-    if (row >= t.rows || column >= t.columns) continue;
-    if (p.given) {
-#pragma clang fp contract(off)
-      const uint64_t i = (uint64_t)row * t.columns + column;
-      const float m = t.m[i];
-      u[k] = p.nesterov ? element(t.u, i, p.in) * p.grad_scale + m * p.momentum : m;
-    } else {
-      u[k] = element(t.u, row * t.ld_u + column, p.in);
+  for (uint32_t k = 0; k < 2u; ++k) {
+    const uint32_t row = row0 + 32u * k, n = row >= t.rows || column >= t.columns ? 0u : t.columns - column < 8u ? t.columns - column : 8u;
+    const uint64_t i = (uint64_t)(row < t.rows ? row : 0u) * t.ld_u + column;
+    fetch(u[k], (const G*)t.u + i, n);
+    if (kGiven) {
+      float m[8];
+      fetch(m, t.m + i, n);
+#pragma unroll
+      for (uint32_t e = 0; e < 8u; ++e) u[k][e] = p.nesterov ? u[k][e] * p.grad_scale + m[e] * p.momentum : m[e];
     }
   }
-  __syncthreads();
-  for (uint32_t d = 128; d; d /= 2u) {
-    if (threadIdx.x < d) sums[threadIdx.x] += sums[threadIdx.x + d];
-    __syncthreads();
-  }
-  const double norm = sqrt(sums[0]);
+  const double norm = sqrt(sum_of(square, sums));
   int k2 = 0;
   if (norm > 0 && norm <= DBL_MAX) {
     int e;
@@ -154,20 +181,29 @@ __global__ __launch_bounds__(256) void k_split(PrepareArgs) {
   if (tile == 0u && threadIdx.x == 0u) *t.factor() = norm == 0 ? 0.f : norm <= DBL_MAX ? (float)(1.0 / ldexp(norm + p.eps, k2)) : __builtin_nanf("");
   if (t.tall) {
 #pragma unroll
-    for (uint32_t k = 0; k < kSquare / 4; ++k) turned[wave + 4u * k][lane] = u[k];
+    for (uint32_t k = 0; k < 2u; ++k)
+#pragma unroll
+      for (uint32_t e = 0; e < 8u; ++e) turned[line + 32u * k][place + e] = u[k][e];
     __syncthreads();
 #pragma unroll
-    for (uint32_t k = 0; k < kSquare / 4; ++k) u[k] = turned[lane][wave + 4u * k];
+    for (uint32_t k = 0; k < 2u; ++k)
+#pragma unroll
+      for (uint32_t e = 0; e < 8u; ++e) u[k][e] = turned[place + e][line + 32u * k];
   }
 #pragma unroll
-  for (uint32_t k = 0; k < kSquare / 4; ++k) {
-    const uint32_t r = r0 + wave + 4u * k;
+  for (uint32_t k = 0; k < 2u; ++k) {
+    const uint32_t r = r0 + line + 32u * k;
     if (r >= t.m_side) continue;
-    const uint64_t at = (uint64_t)r * t.wide_n + c0 + lane;
-    const float v = ldexpf(u[k], k2);
-    const f16 high = (f16)v;
-    t.x(0, 0)[at] = high;
-    t.x(0, 1)[at] = (f16)(v - (float)high);
+    const uint64_t at = (uint64_t)r * t.wide_n + c0 + place;
+    Pack<f16, 8> high, low;
+#pragma unroll
+    for (uint32_t e = 0; e < 8u; ++e) {
+      const float v = ldexpf(u[k][e], k2);
+      high.v[e] = (f16)v;
+      low.v[e] = (f16)(v - (float)high.v[e]);
+    }
+    *(Pack<f16, 8>*)(t.x(0, 0) + at) = high;
+    *(Pack<f16, 8>*)(t.x(0, 1) + at) = low;
   }
 }
 
@@ -196,22 +232,57 @@ struct Halves {
     }
   }
 };
-__device__ __forceinline__ f32x4 whole(const f16* high, const f16* low) {
-  const Pack<f16, 4> h = *(const Pack<f16, 4>*)high;
-  f32x4 v = {(float)h.v[0], (float)h.v[1], (float)h.v[2], (float)h.v[3]};
-  if (low) {
-    const Pack<f16, 4> l = *(const Pack<f16, 4>*)low;
+// The result's elements of row r of X at four columns from c0 on, and from every 16th further on: as they are, or into the weights.
+template <class P, int kNF>
+__device__ __forceinline__ void leave(const ProductArgs& p, const Matrix& t, uint32_t r, uint32_t c0, const f32x4 (&v)[kNF]) {
+  if (r >= t.m_side) return;
+  float old[kNF][4] = {};
+  const bool tall = t.tall != 0u;
+  const uint64_t step = tall ? t.ld_out : 1u, base = tall ? r : r * t.ld_out;   // from column to column of X
+  P* to = (P*)t.out + base;
+  if (p.weights)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] += (float)l.v[e];
+    for (int j = 0; j < kNF; ++j)
+#pragma unroll
+      for (uint32_t e = 0; e < 4u; ++e) {
+        const uint32_t c = c0 + j * 16 + e;
+        old[j][e] = (float)to[(c < t.n_side ? c : 0u) * step];
+      }
+#pragma unroll
+  for (int j = 0; j < kNF; ++j) {
+    const uint32_t c = c0 + j * 16;
+    float o[4];
+#pragma unroll
+    for (uint32_t e = 0; e < 4u; ++e) {
+      o[e] = v[j][e] * t.step;
+      if (p.weights) o[e] = old[j][e] * p.decay - o[e];
+    }
+    if (!tall && c + 4u <= t.n_side) {
+      const Pack<P, 4> w = {{(P)o[0], (P)o[1], (P)o[2], (P)o[3]}};
+      __builtin_memcpy(to + c, &w, sizeof w);
+    } else {
+#pragma unroll
+      for (uint32_t e = 0; e < 4u; ++e)
+        if (c + e < t.n_side) to[(c + e) * step] = (P)o[e];
+    }
+    if (!t.copy) continue;
+    auto copy = [&](auto like) __attribute__((always_inline)) {
+      typedef decltype(like) C;
+      C* there = (C*)t.copy + base;
+#pragma unroll
+      for (uint32_t e = 0; e < 4u; ++e)
+        if (c + e < t.n_side) there[(c + e) * step] = (C)o[e];
+    };
+    if (p.copy == FBX_F16) copy((f16)0.f);
+    else copy((__bf16)0.f);
   }
-  return v;
 }
 
 // BM x BN of C a workgroup, its WM x WN wavefronts side by side.  C's rows come from A; its columns from B, which is the first side
 // of the matrix instructions, so that a lane holds four adjacent columns of a row.  Of a symmetric C tiles on and below the
 // diagonal are worked out, and stored on either side of it.
 template <Form kForm, int BM, int BN, int WM, int WN, int kStages>
-__global__ __launch_bounds__(WM * WN * 64) void k_product(ProductArgs) {
+__global__ __launch_bounds__(WM * WN * 64, 2) void k_product(ProductArgs) {
 #ifdef __HIP_DEVICE_COMPILE__
   constexpr bool kTwin = kForm == kGram || kForm == kPolynom;
   constexpr int kWaves = WM * WN, kRows = BM / WM, kCols = BN / WN, kMF = kRows / 16, kNF = kCols / 16;
@@ -331,60 +402,93 @@ __global__ __launch_bounds__(WM * WN * 64) void k_product(ProductArgs) {
   // The first X is held times 1 / f, every other one times 2^14.
   const float f = p.begins ? *t.factor() : 1.f;
   const float keep = p.keep * (kForm == kPolynom ? 1.f : f), product = p.sum * (kForm == kGram ? f * f : kForm == kPolynom ? 1.f : f);
+  constexpr int kAtOnce = kNF > 4 ? 1 : 16 / kNF < kMF ? 16 / kNF : kMF;   // 16 rows each whose other operand is asked for together
+  const uint32_t r_first = row0 + wm * kRows + lane % 16u, c_first = col0 + wn * kCols + lane / 16u * 4u;
+  if constexpr (kTwin) {
+    f16 *high = kForm == kGram ? t.a(0) : t.b(0), *low = kForm == kGram ? t.a(1) : t.b(1);
+    const bool both = t.exact != 0u;
+    const uint32_t wide = t.wide_m;
 #pragma unroll
-  for (int i = 0; i < kMF; ++i) {
-    const uint32_t r = row0 + wm * kRows + i * 16 + lane % 16u;
+    for (int i0 = 0; i0 < kMF; i0 += kAtOnce) {
+      Pack<f16, 4> there[kAtOnce][kNF][2] = {};
+      if (kForm == kPolynom)
 #pragma unroll
-    for (int j = 0; j < kNF; ++j) {
-      const uint32_t c = col0 + wn * kCols + j * 16 + lane / 16u * 4u;
-      if constexpr (kTwin) {
-        f32x4 v = sum[i][j] * product;
-        f16 *high = kForm == kGram ? t.a(0) : t.b(0), *low = kForm == kGram ? t.a(1) : t.b(1);
-        const uint64_t to = (uint64_t)r * t.wide_m + c;
-        if (r < m_side && c < t.wide_m) {
-          if (kForm == kPolynom) v += whole(t.a(0) + to, t.exact ? t.a(1) + to : nullptr) * keep;
+        for (int i = 0; i < kAtOnce; ++i)
+#pragma unroll
+          for (int j = 0; j < kNF; ++j) {
+            const uint32_t r = r_first + (i0 + i) * 16, c = c_first + j * 16;
+            const uint64_t from = (uint64_t)(r < m_side ? r : m_side - 1u) * wide + (c < wide ? c : 0u);
+            there[i][j][0] = *(const Pack<f16, 4>*)(t.a(0) + from);
+            if (both) there[i][j][1] = *(const Pack<f16, 4>*)(t.a(1) + from);
+          }
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i)
+#pragma unroll
+        for (int j = 0; j < kNF; ++j) {
+          const uint32_t r = r_first + (i0 + i) * 16, c = c_first + j * 16;
+          f32x4 v = sum[i0 + i][j] * product;
+          if (kForm == kPolynom)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += ((float)there[i][j][0].v[e] + (float)there[i][j][1].v[e]) * keep;
           const Halves w(v);
-          *(Pack<f16, 4>*)(high + to) = Pack<f16, 4>{{w.high[0], w.high[1], w.high[2], w.high[3]}};
-          if (t.exact) *(Pack<f16, 4>*)(low + to) = Pack<f16, 4>{{w.low[0], w.low[1], w.low[2], w.low[3]}};
-          if (row0 != col0) {
+          const uint64_t to = (uint64_t)r * wide + c;
+          if (r < m_side && c < wide) {
+            *(Pack<f16, 4>*)(high + to) = Pack<f16, 4>{{w.high[0], w.high[1], w.high[2], w.high[3]}};
+            if (both) *(Pack<f16, 4>*)(low + to) = Pack<f16, 4>{{w.low[0], w.low[1], w.low[2], w.low[3]}};
+          }
+          if (row0 != col0 && r < wide) {   // (columns are before the diagonal's tile, so within the rows; rows beyond the last are zeros)
 #pragma unroll
-            for (uint32_t e = 0; e < 4u; ++e) {   // (c is below the diagonal's tile: within the rows)
-              high[(uint64_t)(c + e) * t.wide_m + r] = w.high[e];
-              if (t.exact) low[(uint64_t)(c + e) * t.wide_m + r] = w.low[e];
+            for (uint32_t e = 0; e < 4u; ++e) {
+              high[(uint64_t)(c + e) * wide + r] = r < m_side ? w.high[e] : (f16)0.f;
+              if (both) low[(uint64_t)(c + e) * wide + r] = r < m_side ? w.low[e] : (f16)0.f;
             }
           }
-        } else if (row0 != col0 && r < t.wide_m) {  // (columns beyond the last row's: zeros)
-#pragma unroll
-          for (uint32_t e = 0; e < 4u; ++e) {
-            high[(uint64_t)(c + e) * t.wide_m + r] = (f16)0.f;
-            if (t.exact) low[(uint64_t)(c + e) * t.wide_m + r] = (f16)0.f;
-          }
         }
-      } else {
-        if (r >= m_side || c >= t.wide_n) continue;
-        const uint64_t from = (uint64_t)r * t.wide_n + c;
-        f32x4 v = whole(t.x(p.turn, 0) + from, t.x(p.turn, 1) + from);
+    }
+  } else {
+    const f16 *from_high = t.x(p.turn, 0), *from_low = t.x(p.turn, 1);
+    const uint32_t wide = t.wide_n;
+    auto finish = [&](auto use) __attribute__((always_inline)) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = v[e] * keep + sum[i][j][e] * product;
-        if constexpr (kForm == kNext) {
-          const Halves w(v);
-          *(Pack<f16, 4>*)(t.x(p.turn ^ 1u, 0) + from) = Pack<f16, 4>{{w.high[0], w.high[1], w.high[2], w.high[3]}};
-          *(Pack<f16, 4>*)(t.x(p.turn ^ 1u, 1) + from) = Pack<f16, 4>{{w.low[0], w.low[1], w.low[2], w.low[3]}};
-        } else {
+      for (int i0 = 0; i0 < kMF; i0 += kAtOnce) {
+        Pack<f16, 4> there[kAtOnce][kNF][2];
 #pragma unroll
-          for (uint32_t e = 0; e < 4u; ++e) {
-            if (c + e >= t.n_side) continue;
-            const uint64_t to = t.tall ? (uint64_t)(c + e) * t.ld_out + r : (uint64_t)r * t.ld_out + c + e;
-            float o = v[e] * t.step;
-            if (p.weights) o = element(t.out, to, p.out) * p.decay - o;
-            if (p.out == FBX_F32) ((float*)t.out)[to] = o;
-            else if (p.out == FBX_F16) ((f16*)t.out)[to] = (f16)o;
-            else ((__bf16*)t.out)[to] = (__bf16)o;
-            if (t.copy && p.copy == FBX_F16) ((f16*)t.copy)[to] = (f16)o;
-            else if (t.copy) ((__bf16*)t.copy)[to] = (__bf16)o;
+        for (int i = 0; i < kAtOnce; ++i)
+#pragma unroll
+          for (int j = 0; j < kNF; ++j) {
+            const uint32_t r = r_first + (i0 + i) * 16, c = c_first + j * 16;
+            const uint64_t from = (uint64_t)(r < m_side ? r : m_side - 1u) * wide + (c < wide ? c : 0u);
+            there[i][j][0] = *(const Pack<f16, 4>*)(from_high + from);
+            there[i][j][1] = *(const Pack<f16, 4>*)(from_low + from);
           }
-        }
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i)
+#pragma unroll
+          for (int j = 0; j < kNF; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[i0 + i][j][e] = sum[i0 + i][j][e] * product + ((float)there[i][j][0].v[e] + (float)there[i][j][1].v[e]) * keep;
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) use(i0 + i, sum[i0 + i]);
       }
+    };
+    if constexpr (kForm == kNext) {
+      f16 *high = t.x(p.turn ^ 1u, 0), *low = t.x(p.turn ^ 1u, 1);
+      finish([&](int i, const f32x4 (&v)[kNF]) __attribute__((always_inline)) {
+        const uint32_t r = r_first + i * 16;
+#pragma unroll
+        for (int j = 0; j < kNF; ++j) {
+          const uint32_t c = c_first + j * 16;
+          if (r >= m_side || c >= wide) continue;
+          const Halves w(v[j]);
+          const uint64_t to = (uint64_t)r * wide + c;
+          *(Pack<f16, 4>*)(high + to) = Pack<f16, 4>{{w.high[0], w.high[1], w.high[2], w.high[3]}};
+          *(Pack<f16, 4>*)(low + to) = Pack<f16, 4>{{w.low[0], w.low[1], w.low[2], w.low[3]}};
+        }
+      });
+    } else {
+      if (p.out == FBX_F32) finish([&](int i, const f32x4 (&v)[kNF]) __attribute__((always_inline)) { leave<float, kNF>(p, t, r_first + i * 16, c_first, v); });
+      else if (p.out == FBX_F16) finish([&](int i, const f32x4 (&v)[kNF]) __attribute__((always_inline)) { leave<f16, kNF>(p, t, r_first + i * 16, c_first, v); });
+      else finish([&](int i, const f32x4 (&v)[kNF]) __attribute__((always_inline)) { leave<__bf16, kNF>(p, t, r_first + i * 16, c_first, v); });
     }
   }
 #endif
@@ -533,6 +637,17 @@ uint64_t scratch_of(std::vector<Matrix>& all) {
   return most;
 }
 
+template <class G, bool kGiven>
+void prepare_as(const PrepareArgs& q, bool measure, hipStream_t stream) {
+  launch_on(stream, measure ? k_measure<G, kGiven> : k_split<G, kGiven>, dim3(q.list.first[q.list.n]), dim3(256), 0, q);
+}
+void prepare(const PrepareArgs& q, bool measure, const Whole& w, hipStream_t stream) {
+  const bool given = q.list.of[0].m != nullptr;
+  if (w.in == FBX_F32) given ? prepare_as<float, true>(q, measure, stream) : prepare_as<float, false>(q, measure, stream);
+  else if (w.in == FBX_F16) given ? prepare_as<f16, true>(q, measure, stream) : prepare_as<f16, false>(q, measure, stream);
+  else given ? prepare_as<__bf16, true>(q, measure, stream) : prepare_as<__bf16, false>(q, measure, stream);
+}
+
 void run(Whole& w, const std::vector<Step>& steps, char* scratch, hipStream_t stream) {
   for (const Batch& b : batches(w.all)) {
     PrepareArgs q{};
@@ -545,16 +660,14 @@ void run(Whole& w, const std::vector<Step>& steps, char* scratch, hipStream_t st
       at += lay_out(t, t.rows, t.columns);
       p.list.of[i] = t;
     }
-    q.in = w.in;
-    q.given = q.list.of[0].m != nullptr;
     q.nesterov = w.nesterov != 0;
     q.momentum = w.momentum;
     q.grad_scale = w.grad_scale;
     q.eps = w.h->eps;
     for (uint32_t i = 0; i < q.list.n; ++i) q.list.first[i + 1] = q.list.first[i] + q.list.of[i].partials;
-    launch_on(stream, k_measure, dim3(q.list.first[q.list.n]), dim3(256), 0, q);
+    prepare(q, true, w, stream);
     for (uint32_t i = 0; i < q.list.n; ++i) q.list.first[i + 1] = q.list.first[i] + (uint32_t)(ceil_div(q.list.of[i].m_side, kSquare) * (q.list.of[i].wide_n / kSquare));
-    launch_on(stream, k_split, dim3(q.list.first[q.list.n]), dim3(256), 0, q);
+    prepare(q, false, w, stream);
     p.out = w.out;
     p.copy = w.copy;
     p.weights = w.weights;
