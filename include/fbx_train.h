@@ -257,14 +257,14 @@ fbx_status fbx_join_backward(const fbx_join* h, const fbx_join_gradients* g, voi
  * first part overflows; sums are in 32 bits.
  *   exact = 1: products are of both parts of both sides (all but second by second): errors like those of
  *     products in 32 bits.
- *   exact = 0: products are of first parts, a third of the work; a X is of both.  The result's error is that of
+ *   exact = 0: products are of first parts, a third of the work; a times X's second part is added.  The result's error is that of
  *     rounding it to bf16: about 1.7e-3 of its size, twice that for small matrices.
  *   exact = FBX_EXACT_BY_SIZE: 0 for results in bf16 of matrices of more than 256 rows and columns, else 1.
  *
  *   coefficients : HOST, steps triples
  *   matrices     : HOST, n entries; elements of a row are adjacent; results may not overlap
  * Limits: 1 <= rows, columns <= FBX_ORTHO_MOST; 1 <= steps <= 64; coefficients whose iteration takes a singular value from
- * [0, 1] above 3, or b s^2 + c s^4 of one beyond 256, are refused.
+ * [0, 1] above 3, or a + b s^2 + c s^4 of one beyond 256, are refused.
  * Errors: FBX_E_ARG, FBX_E_NOMEM, FBX_E_HIP.
  */
 #define FBX_ORTHO_MOST 65536u

@@ -209,15 +209,17 @@ __global__ __launch_bounds__(256) void k_split(PrepareArgs) {
 
 // One launch's products, of every matrix of the list:
 //   kGram     A = X X^T
-//   kPolynom  B = b A + c A A (A is its own transpose)
-//   kNext     X = a X + B X, into the other of two places
+//   kPolynom  B = a I + b A + c A A (A is its own transpose)
+//   kNext     X = B X, into the other of two places
 //   kLast     the same, and it leaves as the result, or goes into the weights
+// The a X of a step is part of the product so that X need not be read again behind it (8 bytes an element in place of 4 are more than a
+// tenth of a large product's time); where products are of first parts only a times X's second part is added.
 enum Form { kGram, kPolynom, kNext, kLast };
 struct ProductArgs {
   List list;
   uint32_t turn;                          // which X is read
   uint32_t begins;                        // X is what k_split left
-  float keep, sum;                        // C = keep (what is there) + sum (the product), but for the scale of the first X
+  float keep, sum, diagonal;              // C = keep (what is there) + sum (the product) + diagonal I, but for the scale of the first X
   uint32_t out, copy, weights;            // kLast: types; the result goes into weights
   float decay;                            // of them: 1 - lr weight_decay
 };
@@ -402,7 +404,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_product(ProductArgs) {
   // The first X is held times 1 / f, every other one times 2^14.
   const float f = p.begins ? *t.factor() : 1.f;
   const float keep = p.keep * (kForm == kPolynom ? 1.f : f), product = p.sum * (kForm == kGram ? f * f : kForm == kPolynom ? 1.f : f);
-  constexpr int kAtOnce = kNF > 4 ? 1 : 16 / kNF < kMF ? 16 / kNF : kMF;   // 16 rows each whose other operand is asked for together
+  constexpr int kAtOnce = 16 / kNF < kMF ? 16 / kNF : kMF;   // 16 rows each, whose other operand is asked for together
   const uint32_t r_first = row0 + wm * kRows + lane % 16u, c_first = col0 + wn * kCols + lane / 16u * 4u;
   if constexpr (kTwin) {
     f16 *high = kForm == kGram ? t.a(0) : t.b(0), *low = kForm == kGram ? t.a(1) : t.b(1);
@@ -429,7 +431,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_product(ProductArgs) {
           f32x4 v = sum[i0 + i][j] * product;
           if (kForm == kPolynom)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] += ((float)there[i][j][0].v[e] + (float)there[i][j][1].v[e]) * keep;
+            for (uint32_t e = 0; e < 4u; ++e) v[e] += ((float)there[i][j][0].v[e] + (float)there[i][j][1].v[e]) * keep + (r == c + e && r < m_side ? p.diagonal : 0.f);
           const Halves w(v);
           const uint64_t to = (uint64_t)r * wide + c;
           if (r < m_side && c < wide) {
@@ -446,27 +448,26 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_product(ProductArgs) {
         }
     }
   } else {
-    const f16 *from_high = t.x(p.turn, 0), *from_low = t.x(p.turn, 1);
+    const f16* second = t.x(p.turn, 1);
     const uint32_t wide = t.wide_n;
     auto finish = [&](auto use) __attribute__((always_inline)) {
 #pragma unroll
       for (int i0 = 0; i0 < kMF; i0 += kAtOnce) {
-        Pack<f16, 4> there[kAtOnce][kNF][2];
+        Pack<f16, 4> there[kAtOnce][kNF] = {};
+        if (!t.exact)
 #pragma unroll
-        for (int i = 0; i < kAtOnce; ++i)
+          for (int i = 0; i < kAtOnce; ++i)
 #pragma unroll
-          for (int j = 0; j < kNF; ++j) {
-            const uint32_t r = r_first + (i0 + i) * 16, c = c_first + j * 16;
-            const uint64_t from = (uint64_t)(r < m_side ? r : m_side - 1u) * wide + (c < wide ? c : 0u);
-            there[i][j][0] = *(const Pack<f16, 4>*)(from_high + from);
-            there[i][j][1] = *(const Pack<f16, 4>*)(from_low + from);
-          }
+            for (int j = 0; j < kNF; ++j) {
+              const uint32_t r = r_first + (i0 + i) * 16, c = c_first + j * 16;
+              there[i][j] = *(const Pack<f16, 4>*)(second + (uint64_t)(r < m_side ? r : m_side - 1u) * wide + (c < wide ? c : 0u));
+            }
 #pragma unroll
         for (int i = 0; i < kAtOnce; ++i)
 #pragma unroll
           for (int j = 0; j < kNF; ++j)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sum[i0 + i][j][e] = sum[i0 + i][j][e] * product + ((float)there[i][j][0].v[e] + (float)there[i][j][1].v[e]) * keep;
+            for (int e = 0; e < 4; ++e) sum[i0 + i][j][e] = sum[i0 + i][j][e] * product + (float)there[i][j].v[e] * keep;
 #pragma unroll
         for (int i = 0; i < kAtOnce; ++i) use(i0 + i, sum[i0 + i]);
       }
@@ -512,8 +513,8 @@ const char* plan(const fbx_ortho* h, std::vector<Step>* steps) {
     double next = 0, polynom = 0;
     constexpr int kPlaces = 2048;
     for (int k = 0; k <= kPlaces; ++k) {
-      const double v = most * k / kPlaces, q = v * v * (s.b + s.c * v * v);
-      next = fmax(next, fabs(v * (s.a + q)));
+      const double v = most * k / kPlaces, q = s.a + v * v * (s.b + s.c * v * v);
+      next = fmax(next, fabs(v * q));
       polynom = fmax(polynom, fabs(q));
     }
     // (between two places a polynomial of the fifth degree moves by less than this)
@@ -681,6 +682,7 @@ void run(Whole& w, const std::vector<Step>& steps, char* scratch, hipStream_t st
       p.sum = (float)(a / (x * x));
       multiply<kGram>(p, stream);
       p.keep = (float)(s.b * bb / a);
+      p.diagonal = (float)(s.a * bb);
       p.sum = (float)(s.c * bb / (a * a));
       multiply<kPolynom>(p, stream);
       p.keep = (float)(s.a * next / x);

@@ -383,9 +383,9 @@ def _step_bound(x, ex, part, coefficients=C):
     gram, eg = m @ mt, product(m, mt, ex, et)
     eg = eg * (1 + part) + part * gram + small
     g2, eg2 = gram @ gram, product(gram, gram, eg, eg)
-    poly = b * gram + c * g2
+    poly = b * gram + c * g2 + a * torch.eye(len(gram), dtype=torch.float64, device="cuda")   # (a X is part of the product with X)
     ep = (b * eg + c * eg2) * (1 + 4 * U32) + (part + 8 * U32) * poly + small
-    return a * ex + product(poly, m, ep, ex) + 2.0 ** -21 * (a * m + poly @ m) + small
+    return product(poly, m, ep, ex) + 2.0 ** -21 * (poly @ m) + small
 
 
 def _decaying(g, rows, columns, dtype=F32):
