@@ -259,6 +259,7 @@ fbx_status fbx_join_backward(const fbx_join* h, const fbx_join_gradients* g, voi
  *     products in 32 bits.
  *   exact = 0: products are of first parts, a third of the work; a times X's second part is added.  The result's error is that of
  *     rounding it to bf16: about 1.7e-3 of its size, twice that for small matrices.
+ *     Matrices that a workgroup's memory holds (up to 128 x 128, 32 x 1,024 or so) are always worked out exactly.
  *   exact = FBX_EXACT_BY_SIZE: 0 for results in bf16 of matrices of more than 256 rows and columns, else 1.
  *
  *   coefficients : HOST, steps triples

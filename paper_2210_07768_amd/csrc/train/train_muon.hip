@@ -64,11 +64,21 @@ struct List {
   }
 };
 
-struct PrepareArgs {
-  List list;
+// What is made of a gradient, and of a norm.
+struct Given {
   uint32_t nesterov;
   float momentum, grad_scale;
   double eps;
+};
+struct PrepareArgs {
+  List list;
+  Given given;
+};
+
+// How results leave.
+struct Leaving {
+  uint32_t out, copy, weights;            // types; results go into weights
+  float decay;                            // of them: 1 - lr weight_decay
 };
 
 // Eight adjacent elements from i on, of which the first n exist (more exist behind them where n is 8), wherever they begin.
@@ -95,6 +105,18 @@ __device__ __forceinline__ double sum_of(double v, double* shared) {
   return (shared[0] + shared[1]) + (shared[2] + shared[3]);
 }
 
+// The power of two that brings a norm into [2^13, 2^14), and the factor that then makes X of a matrix: 1 / (norm + eps).  A matrix of zeros
+// stays one, one that is not finite becomes NaN.
+__device__ __forceinline__ int power_of(double norm) {
+  if (!(norm > 0 && norm <= DBL_MAX)) return 0;
+  int e;
+  (void)frexp(norm, &e);   // norm in [2^(e - 1), 2^e)
+  return kX - e;
+}
+__device__ __forceinline__ float factor_of(double norm, int k2, double eps) {
+  return norm == 0 ? 0.f : norm <= DBL_MAX ? (float)(1.0 / ldexp(norm + eps, k2)) : __builtin_nanf("");
+}
+
 // Sums of squares, in 64 bits so that they stay within range whatever the gradient's size; momentum is brought up to date.
 // A workgroup adds up `chunk` elements.
 template <class G, bool kGiven>
@@ -116,9 +138,9 @@ __global__ __launch_bounds__(256) void k_measure(PrepareArgs) {
         fetch(m, t.m + i, n);
 #pragma unroll
         for (uint32_t e = 0; e < 8u; ++e) {
-          const float g = u[e] * p.grad_scale;
-          m[e] = m[e] * p.momentum + g;
-          u[e] = p.nesterov ? g + m[e] * p.momentum : m[e];
+          const float g = u[e] * p.given.grad_scale;
+          m[e] = m[e] * p.given.momentum + g;
+          u[e] = p.given.nesterov ? g + m[e] * p.given.momentum : m[e];
         }
         if (n == 8u) {
           __builtin_memcpy(t.m + i, m, sizeof m);
@@ -168,17 +190,12 @@ __global__ __launch_bounds__(256) void k_split(PrepareArgs) {
       float m[8];
       fetch(m, t.m + i, n);
 #pragma unroll
-      for (uint32_t e = 0; e < 8u; ++e) u[k][e] = p.nesterov ? u[k][e] * p.grad_scale + m[e] * p.momentum : m[e];
+      for (uint32_t e = 0; e < 8u; ++e) u[k][e] = p.given.nesterov ? u[k][e] * p.given.grad_scale + m[e] * p.given.momentum : m[e];
     }
   }
   const double norm = sqrt(sum_of(square, sums));
-  int k2 = 0;
-  if (norm > 0 && norm <= DBL_MAX) {
-    int e;
-    (void)frexp(norm, &e);   // norm in [2^(e - 1), 2^e)
-    k2 = kX - e;
-  }
-  if (tile == 0u && threadIdx.x == 0u) *t.factor() = norm == 0 ? 0.f : norm <= DBL_MAX ? (float)(1.0 / ldexp(norm + p.eps, k2)) : __builtin_nanf("");
+  const int k2 = power_of(norm);
+  if (tile == 0u && threadIdx.x == 0u) *t.factor() = factor_of(norm, k2, p.given.eps);
   if (t.tall) {
 #pragma unroll
     for (uint32_t k = 0; k < 2u; ++k)
@@ -220,8 +237,7 @@ struct ProductArgs {
   uint32_t turn;                          // which X is read
   uint32_t begins;                        // X is what k_split left
   float keep, sum, diagonal;              // C = keep (what is there) + sum (the product) + diagonal I, but for the scale of the first X
-  uint32_t out, copy, weights;            // kLast: types; the result goes into weights
-  float decay;                            // of them: 1 - lr weight_decay
+  Leaving last;
 };
 
 struct Halves {
@@ -236,7 +252,7 @@ struct Halves {
 };
 // The result's elements of row r of X at four columns from c0 on, and from every 16th further on: as they are, or into the weights.
 template <class P, int kNF>
-__device__ __forceinline__ void leave(const ProductArgs& p, const Matrix& t, uint32_t r, uint32_t c0, const f32x4 (&v)[kNF]) {
+__device__ __forceinline__ void leave(const Leaving& p, const Matrix& t, uint32_t r, uint32_t c0, const f32x4 (&v)[kNF]) {
   if (r >= t.m_side) return;
   float old[kNF][4] = {};
   const bool tall = t.tall != 0u;
@@ -487,12 +503,185 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_product(ProductArgs) {
         }
       });
     } else {
-      if (p.out == FBX_F32) finish([&](int i, const f32x4 (&v)[kNF]) __attribute__((always_inline)) { leave<float, kNF>(p, t, r_first + i * 16, c_first, v); });
-      else if (p.out == FBX_F16) finish([&](int i, const f32x4 (&v)[kNF]) __attribute__((always_inline)) { leave<f16, kNF>(p, t, r_first + i * 16, c_first, v); });
-      else finish([&](int i, const f32x4 (&v)[kNF]) __attribute__((always_inline)) { leave<__bf16, kNF>(p, t, r_first + i * 16, c_first, v); });
+      if (p.last.out == FBX_F32) finish([&](int i, const f32x4 (&v)[kNF]) __attribute__((always_inline)) { leave<float, kNF>(p.last, t, r_first + i * 16, c_first, v); });
+      else if (p.last.out == FBX_F16) finish([&](int i, const f32x4 (&v)[kNF]) __attribute__((always_inline)) { leave<f16, kNF>(p.last, t, r_first + i * 16, c_first, v); });
+      else finish([&](int i, const f32x4 (&v)[kNF]) __attribute__((always_inline)) { leave<__bf16, kNF>(p.last, t, r_first + i * 16, c_first, v); });
     }
   }
 #endif
+}
+
+// A matrix that one workgroup's LDS holds: everything in one launch, a matrix a workgroup, where every product of its own would take
+// the others' launches and ways through memory.  Products are of both parts.  X and A (and B in its place) lie in LDS as two
+// parts each, rows 16 bytes longer than they need be so that those a read takes lie in different banks; a wavefront takes 32 x 32 of
+// a product at a time, up to kBlocks of them, and what it worked out replaces an operand when all are done with it.
+constexpr uint32_t kSmallLanes = 1024, kRoom = 158 * 1024;
+constexpr int kBlocks = 3;
+struct StepNumbers {
+  float gram, keep, square, diagonal, next;
+};
+struct SmallArgs {
+  List list;
+  Given given;
+  Leaving last;
+  uint32_t steps;
+  StepNumbers of[64];
+};
+__host__ __device__ inline uint32_t small_side(uint32_t n) { return (n + 31u) / 32u * 32u; }
+__host__ __device__ inline uint32_t small_line(uint32_t n) { return 2u * n + 16u; }   // bytes of a row
+
+template <class G>
+__device__ __forceinline__ float given_element(const SmallArgs& p, const Matrix& t, uint32_t r, uint32_t c, bool first) {
+#pragma clang fp contract(off)
+  const float u = (float)((const G*)t.u)[r * t.ld_u + c];
+  if (!t.m) return u;
+  const uint64_t i = (uint64_t)r * t.columns + c;
+  const float g = u * p.given.grad_scale, m = first ? t.m[i] * p.given.momentum + g : t.m[i];
+  if (first) t.m[i] = m;
+  return p.given.nesterov ? g + m * p.given.momentum : m;
+}
+
+template <class G>
+__global__ __launch_bounds__(kSmallLanes) void k_small(SmallArgs) {
+#ifdef __HIP_DEVICE_COMPILE__
+  typedef Frag<f16>::type F;
+  __shared__ alignas(1024) char lds[kRoom];
+  __shared__ double sums[kSmallLanes / 64];
+  const SmallArgs& p = launch_args<SmallArgs>();
+  const Matrix& t = p.list.of[blockIdx.x];
+  const uint32_t lane = threadIdx.x % 64u, wave = same(threadIdx.x / 64u), i = lane % 16u, g = lane / 16u;
+  const uint32_t m_side = same(t.m_side), n_side = same(t.n_side), rows = small_side(m_side), columns = small_side(n_side);
+  const uint32_t line_x = small_line(columns), line_a = small_line(rows), part_x = rows * line_x, part_a = rows * line_a;
+  lds_char *x = (lds_char*)lds, *a = x + 2u * part_x;
+
+  for (uint32_t at = threadIdx.x * 16u; at < 2u * (part_x + part_a); at += kSmallLanes * 16u) *(__attribute__((address_space(3))) f32x4*)(x + at) = f32x4{0.f, 0.f, 0.f, 0.f};
+  // The same lane reads an element twice: for the norm (and its momentum), then to split it.
+  double square = 0;
+  const uint32_t all = t.rows * t.columns, most = t.columns;
+  for (uint32_t at = threadIdx.x; at < all; at += kSmallLanes) {
+    const float u = given_element<G>(p, t, at / most, at % most, true);
+    square += (double)u * u;
+  }
+#pragma unroll
+  for (int d = 32; d; d /= 2) square += __shfl_xor(square, d, 64);
+  if (lane == 0u) sums[wave] = square;
+  __syncthreads();
+  square = 0;
+#pragma unroll
+  for (uint32_t w = 0; w < kSmallLanes / 64u; ++w) square += sums[w];
+  const double norm = sqrt(square);
+  const int k2 = power_of(norm);
+  const float f = factor_of(norm, k2, p.given.eps);
+  for (uint32_t at = threadIdx.x; at < all; at += kSmallLanes) {
+    const uint32_t r = at / most, c = at % most;
+    const float v = ldexpf(given_element<G>(p, t, r, c, false), k2);
+    const f16 high = (f16)v;
+    lds_char* to = x + (t.tall ? c : r) * line_x + (t.tall ? r : c) * 2u;
+    *(__attribute__((address_space(3))) f16*)to = high;
+    *(__attribute__((address_space(3))) f16*)(to + part_x) = (f16)(v - (float)high);
+  }
+  __syncthreads();
+
+  // 16 rows from `first` on over 32 of depth from k on: along rows, or across them (a transposing read).
+  auto along = [&](const lds_char* from, uint32_t line, uint32_t first, uint32_t k) { return *(const __attribute__((address_space(3))) F*)(from + (first + i) * line + k * 2u + g * 16u); };
+  auto across = [&](const lds_char* from, uint32_t line, uint32_t first, uint32_t k) {
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    typedef short s16x8 __attribute__((ext_vector_type(8)));
+    s16x4 h[2];
+#pragma unroll
+    for (uint32_t q = 0; q < 2u; ++q)
+      h[q] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(from + (k + 8u * g + 4u * q + i / 4u) * line + first * 2u + (i % 4u) * 8u));
+    return __builtin_bit_cast(F, (s16x8)__builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+  f32x4 sum[kBlocks][2][2];
+  // This wavefront's blocks of a product: rows of `left` over `depth`, by rows of `right` (or across them).
+  auto multiply = [&](const lds_char* left, uint32_t line_l, uint32_t part_l, const lds_char* right, uint32_t line_r, uint32_t part_r, uint32_t wide, uint32_t depth, auto is_across) __attribute__((always_inline)) {
+    const uint32_t over = wide / 32u, blocks = rows / 32u * over;
+#pragma unroll
+    for (int n = 0; n < kBlocks; ++n) {
+      const uint32_t block = wave + n * (kSmallLanes / 64u);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[n][e / 2][e % 2] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (block >= blocks) continue;
+      const uint32_t r0 = same(block / over * 32u), c0 = same(block % over * 32u);
+      for (uint32_t k = 0; k < depth; k += 32u) {
+        F l[2][2], r[2][2];   // of 16 rows each, first and second parts
+#pragma unroll
+        for (uint32_t h = 0; h < 2u; ++h)
+#pragma unroll
+          for (uint32_t q = 0; q < 2u; ++q) {
+            l[h][q] = along(left + q * part_l, line_l, r0 + 16u * h, k);
+            if constexpr (decltype(is_across)::value) r[h][q] = across(right + q * part_r, line_r, c0 + 16u * h, k);
+            else r[h][q] = along(right + q * part_r, line_r, c0 + 16u * h, k);
+          }
+#pragma unroll
+        for (int pair = 0; pair < 3; ++pair)
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) sum[n][h][j] = mma(r[j][pair == 1], l[h][pair == 2], sum[n][h][j]);
+      }
+    }
+  };
+  // f(row, first of four columns, sums) of every place that this wavefront has worked out.
+  auto every = [&](uint32_t wide, auto f) __attribute__((always_inline)) {
+    const uint32_t over = wide / 32u, blocks = rows / 32u * over;
+#pragma unroll
+    for (int n = 0; n < kBlocks; ++n) {
+      const uint32_t block = wave + n * (kSmallLanes / 64u);
+      if (block >= blocks) continue;
+#pragma unroll
+      for (uint32_t h = 0; h < 2u; ++h)
+#pragma unroll
+        for (uint32_t j = 0; j < 2u; ++j) f(block / over * 32u + 16u * h + i, block % over * 32u + 16u * j + 4u * g, sum[n][h][j]);
+    }
+  };
+  auto put = [&](lds_char* to, uint32_t part, f32x4 v) {
+    const Halves w(v);
+#pragma unroll
+    for (uint32_t e = 0; e < 4u; ++e) {
+      ((__attribute__((address_space(3))) f16*)to)[e] = w.high[e];
+      ((__attribute__((address_space(3))) f16*)(to + part))[e] = w.low[e];
+    }
+  };
+  for (uint32_t s = 0; s < p.steps; ++s) {
+    const StepNumbers by = p.of[s];
+    const float first = s ? 1.f : f;
+    multiply(x, line_x, part_x, x, line_x, part_x, rows, columns, Kind<0>());
+    every(rows, [&](uint32_t r, uint32_t c, f32x4& v) { put(a + r * line_a + c * 2u, part_a, v * (by.gram * first * first)); });
+    __syncthreads();
+    multiply(a, line_a, part_a, a, line_a, part_a, rows, rows, Kind<0>());
+    every(rows, [&](uint32_t r, uint32_t c, f32x4& v) {
+      const lds_char* at = a + r * line_a + c * 2u;
+#pragma unroll
+      for (uint32_t e = 0; e < 4u; ++e) {
+        const float there = (float)((const __attribute__((address_space(3))) f16*)at)[e] + (float)((const __attribute__((address_space(3))) f16*)(at + part_a))[e];
+        v[e] = v[e] * by.square + there * by.keep + (r == c + e && r < m_side ? by.diagonal : 0.f);
+      }
+    });
+    __syncthreads();
+    every(rows, [&](uint32_t r, uint32_t c, f32x4& v) { put(a + r * line_a + c * 2u, part_a, v); });
+    __syncthreads();
+    multiply(a, line_a, part_a, x, line_x, part_x, columns, rows, Kind<1>());
+    if (s + 1u == p.steps) break;
+    __syncthreads();
+    every(columns, [&](uint32_t r, uint32_t c, f32x4& v) { put(x + r * line_x + c * 2u, part_x, v * (by.next * first)); });
+    __syncthreads();
+  }
+  const float scale = p.of[p.steps - 1u].next * (p.steps == 1u ? f : 1.f);
+  every(columns, [&](uint32_t r, uint32_t c, f32x4& v) {
+    const f32x4 one[1] = {v * scale};
+    if (p.last.out == FBX_F32) leave<float, 1>(p.last, t, r, c, one);
+    else if (p.last.out == FBX_F16) leave<f16, 1>(p.last, t, r, c, one);
+    else leave<__bf16, 1>(p.last, t, r, c, one);
+  });
+#endif
+}
+bool is_small(uint32_t rows, uint32_t columns) {
+  const uint32_t m = small_side(rows < columns ? rows : columns);
+  const uint64_t n = small_side(rows < columns ? columns : rows), blocks = m / 32u * (n / 32u);
+  return blocks <= (uint64_t)kBlocks * (kSmallLanes / 64) && m / 32u * (m / 32u) <= (uint64_t)kBlocks * (kSmallLanes / 64) &&
+         2ull * m * (small_line((uint32_t)n) + small_line(m)) <= kRoom;
 }
 
 // The steps' scales: A is held times 2^a, B times 2^b, so that no first part reaches f16's end (65,504).
@@ -539,8 +728,8 @@ const char* plan(const fbx_ortho* h, std::vector<Step>* steps) {
 struct Whole {
   const fbx_ortho* h;
   fbx_dtype in, out, copy;
-  bool weights;
-  float nesterov, momentum, grad_scale, decay;
+  bool weights, nesterov;
+  float momentum, grad_scale, decay;
   std::vector<Matrix> all;
 };
 
@@ -619,16 +808,33 @@ uint64_t lay_out(Matrix& t, uint32_t rows, uint32_t columns) {
   return at;
 }
 
+// The numbers of a step, for a first X held as k_split leaves it and others held times 2^14.
+StepNumbers numbers_of(const std::vector<Step>& steps, size_t i) {
+  const Step& s = steps[i];
+  const double x = i ? ldexp(1, kX) : 1, a = ldexp(1, s.at_a), b = ldexp(1, s.at_b), next = i + 1 < steps.size() ? ldexp(1, kX) : 1;
+  return StepNumbers{(float)(a / (x * x)), (float)(s.b * b / a), (float)(s.c * b / (a * a)), (float)(s.a * b), (float)(next / (b * x))};
+}
+
 // Matrices go together until there are kMatrices of them or their scratch is more than this: by then they fill the card.
 constexpr uint64_t kTogether = 1ull << 30;
-struct Batch { uint32_t from, to; uint64_t bytes; };
+struct Batch {
+  std::vector<uint32_t> of;
+  uint64_t bytes;
+  bool small;
+};
 std::vector<Batch> batches(std::vector<Matrix>& all) {
   std::vector<Batch> b;
+  int open[2] = {-1, -1};   // the last batch of matrices of either kind
   for (uint32_t i = 0; i < all.size(); ++i) {
-    const uint64_t bytes = lay_out(all[i], all[i].rows, all[i].columns);
-    if (b.empty() || b.back().to - b.back().from == kMatrices || b.back().bytes + bytes > kTogether) b.push_back({i, i, 0});
-    b.back().to = i + 1;
-    b.back().bytes += bytes;
+    const bool small = is_small(all[i].rows, all[i].columns);
+    const uint64_t bytes = lay_out(all[i], all[i].rows, all[i].columns) * !small;
+    int& at = open[small];
+    if (at < 0 || b[at].of.size() == kMatrices || b[at].bytes + bytes > kTogether) {
+      at = (int)b.size();
+      b.push_back(Batch{{}, 0, small});
+    }
+    b[at].of.push_back(i);
+    b[at].bytes += bytes;
   }
   return b;
 }
@@ -650,43 +856,52 @@ void prepare(const PrepareArgs& q, bool measure, const Whole& w, hipStream_t str
 }
 
 void run(Whole& w, const std::vector<Step>& steps, char* scratch, hipStream_t stream) {
+  const Given given{w.nesterov, w.momentum, w.grad_scale, w.h->eps};
+  const Leaving last{(uint32_t)w.out, (uint32_t)w.copy, w.weights, w.decay};
   for (const Batch& b : batches(w.all)) {
+    const uint32_t n = (uint32_t)b.of.size();
+    if (b.small) {
+      SmallArgs p{};
+      p.list.n = n;
+      for (uint32_t i = 0; i < n; ++i) p.list.of[i] = w.all[b.of[i]];
+      p.given = given;
+      p.last = last;
+      p.steps = (uint32_t)steps.size();
+      for (size_t i = 0; i < steps.size(); ++i) p.of[i] = numbers_of(steps, i);
+      if (w.in == FBX_F32) launch_on(stream, k_small<float>, dim3(n), dim3(kSmallLanes), 0, p);
+      else if (w.in == FBX_F16) launch_on(stream, k_small<f16>, dim3(n), dim3(kSmallLanes), 0, p);
+      else launch_on(stream, k_small<__bf16>, dim3(n), dim3(kSmallLanes), 0, p);
+      continue;
+    }
     PrepareArgs q{};
     ProductArgs p{};
-    q.list.n = p.list.n = b.to - b.from;
+    q.given = given;
+    p.last = last;
+    q.list.n = p.list.n = n;
     char* at = scratch;
-    for (uint32_t i = 0; i < q.list.n; ++i) {
-      Matrix& t = q.list.of[i] = w.all[b.from + i];
+    for (uint32_t i = 0; i < n; ++i) {
+      Matrix& t = q.list.of[i] = w.all[b.of[i]];
       t.scratch = at;
       at += lay_out(t, t.rows, t.columns);
       p.list.of[i] = t;
     }
-    q.nesterov = w.nesterov != 0;
-    q.momentum = w.momentum;
-    q.grad_scale = w.grad_scale;
-    q.eps = w.h->eps;
-    for (uint32_t i = 0; i < q.list.n; ++i) q.list.first[i + 1] = q.list.first[i] + q.list.of[i].partials;
+    for (uint32_t i = 0; i < n; ++i) q.list.first[i + 1] = q.list.first[i] + q.list.of[i].partials;
     prepare(q, true, w, stream);
-    for (uint32_t i = 0; i < q.list.n; ++i) q.list.first[i + 1] = q.list.first[i] + (uint32_t)(ceil_div(q.list.of[i].m_side, kSquare) * (q.list.of[i].wide_n / kSquare));
+    for (uint32_t i = 0; i < n; ++i) q.list.first[i + 1] = q.list.first[i] + (uint32_t)(ceil_div(q.list.of[i].m_side, kSquare) * (q.list.of[i].wide_n / kSquare));
     prepare(q, false, w, stream);
-    p.out = w.out;
-    p.copy = w.copy;
-    p.weights = w.weights;
-    p.decay = w.decay;
     for (size_t i = 0; i < steps.size(); ++i) {
-      const Step& s = steps[i];
-      const double x = i ? ldexp(1, kX) : 1, a = ldexp(1, s.at_a), bb = ldexp(1, s.at_b), next = i + 1 < steps.size() ? ldexp(1, kX) : 1;
+      const StepNumbers s = numbers_of(steps, i);
       p.turn = i & 1u;
       p.begins = i == 0;
       p.keep = 0;
-      p.sum = (float)(a / (x * x));
+      p.sum = s.gram;
       multiply<kGram>(p, stream);
-      p.keep = (float)(s.b * bb / a);
-      p.diagonal = (float)(s.a * bb);
-      p.sum = (float)(s.c * bb / (a * a));
+      p.keep = s.keep;
+      p.sum = s.square;
+      p.diagonal = s.diagonal;
       multiply<kPolynom>(p, stream);
-      p.keep = (float)(s.a * next / x);
-      p.sum = (float)(next / (bb * x));
+      p.keep = (float)(steps[i].a * (i + 1 < steps.size() ? ldexp(1, kX) : 1) / (i ? ldexp(1, kX) : 1));
+      p.sum = s.next;
       if (i + 1 < steps.size()) multiply<kNext>(p, stream);
       else multiply<kLast>(p, stream);
     }

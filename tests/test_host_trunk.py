@@ -163,7 +163,7 @@ def test_orthogonalise_refuses(change, matrix, why):
 
 
 def test_orthogonalise_refuses_lists_and_scratch():
-    L, need, m = _library(), u64(), (OrthoMatrix * 1)(_made(OrthoMatrix, MATRIX, {}))
+    L, need, m = _library(), u64(), (OrthoMatrix * 1)(_made(OrthoMatrix, MATRIX, dict(rows=300, columns=400, ld_u=400, ld_out=400)))   # (more than needs no scratch)
     assert L.fbx_orthogonalise(None, m, 1, P, 1 << 40, None) == B.E_ARG
     assert L.fbx_orthogonalise(_ortho(), None, 1, P, 1 << 40, None) == B.E_ARG
     assert L.fbx_orthogonalise(_ortho(), None, 0, None, 0, None) == B.OK   # nothing to do
