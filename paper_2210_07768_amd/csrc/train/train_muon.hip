@@ -53,14 +53,11 @@ struct List {
   uint32_t first[kMatrices + 1];          // the first workgroup (or tile) of each
   uint32_t n;
 
+  // The matrix that a workgroup is of: all of `first` is looked at at once, a lane each.  (A search among them waits for the arguments'
+  // memory once a step, microseconds in all.)
   __device__ uint32_t find(uint32_t block) const {
-    uint32_t lo = 0u, hi = n;
-    while (hi - lo > 1u) {
-      const uint32_t mid = (lo + hi) / 2u;
-      if (first[mid] <= block) lo = mid;
-      else hi = mid;
-    }
-    return lo;
+    const uint32_t lane = threadIdx.x % 64u, begins = lane < n ? first[lane] : 0xffffffffu;
+    return (uint32_t)__popcll(__ballot(begins <= block)) - 1u;
   }
 };
 
