@@ -730,11 +730,11 @@ struct Whole {
   std::vector<Matrix> all;
 };
 
-// Tiles of 256 x 256 read least from LDS, smaller ones begin sooner and leave fewer compute units idle; the times are those that
-// the gated block's products were measured to take (microseconds: a workgroup's begin and each step, alone on a compute unit or among
-// as many as fit one).
-struct Size { uint32_t side, at_once; double begin, lone, full; };
-constexpr Size kSizes[3] = {{256, 1, 8, 1.4, 1.6}, {128, 2, 5.5, 0.5, 0.95}, {64, 2, 3.5, 0.22, 0.3}};
+// Tiles of 256 x 256 read least from LDS, smaller ones begin sooner, end sooner and leave fewer compute units idle.  What they were
+// measured to take (2,624 x 4,096, 384 x 1,024; microseconds): `begin` before the first step and behind the last, a step alone on a compute unit,
+// and among as many as fit one; kNext's results are twice what the others store.
+struct Size { uint32_t side, at_once; double begin[2], lone, full; };
+constexpr Size kSizes[3] = {{256, 1, {14, 24}, 1.45, 1.8}, {128, 2, {9, 10.5}, 0.78, 0.9}, {64, 2, {7, 7}, 0.35, 0.43}};
 uint64_t tiles_of(const Matrix& t, Form form, uint32_t side) {
   const uint64_t rows = ceil_div(t.m_side, side);
   return form == kGram || form == kPolynom ? rows * (rows + 1) / 2 : rows * ceil_div(t.n_side, side);
@@ -744,6 +744,7 @@ uint32_t choose(const Matrix* t, uint32_t n, Form form) {
   double least = 0;
   for (uint32_t i = 0; i < 3; ++i) {
     const Size& s = kSizes[i];
+    const double begin = s.begin[form == kNext || form == kLast], slots = 256.0 * s.at_once;
     double tiles = 0, steps = 0, longest = 0;
     for (uint32_t k = 0; k < n; ++k) {
       const double count = (double)tiles_of(t[k], form, s.side), depth = (double)(form == kGram ? t[k].wide_n : t[k].wide_m) / kDepth * (t[k].exact ? 3 : 1);
@@ -752,9 +753,8 @@ uint32_t choose(const Matrix* t, uint32_t n, Form form) {
       longest = fmax(longest, depth);
     }
     if (tiles >= most_blocks(512)) continue;
-    const double slots = 256.0 * s.at_once, rounds = floor(tiles / slots), rest = tiles - rounds * slots, mean = steps / tiles;
-    const double busy = ceil(fmin(rest, slots) / 256.0), step = fmax(s.lone, s.full * busy / s.at_once);
-    const double takes = rounds * (s.begin + mean * s.full) + (rest > 0 ? s.begin + (rounds > 0 ? mean : longest) * step : 0);
+    const double rounds = floor(tiles / slots), rest = tiles - rounds * slots, mean = steps / tiles;
+    const double takes = rounds * (begin + mean * s.full) + (rest > 0 ? begin + (rounds > 0 ? mean : longest) * (rest > 256.0 ? s.full : s.lone) : 0);
     if (!least || takes < least) {
       least = takes;
       best = i;

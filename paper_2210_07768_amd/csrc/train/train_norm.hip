@@ -193,7 +193,7 @@ struct Scale {
 };
 template <int kN, bool kTiny, class G>
 __device__ __forceinline__ float normalise(Row<kN>& v, G& g, const Columns<kN, kTiny>& at, bool layer, Scale by) {
-  float square;
+  float square, rest = 0.f;
   if (layer) {
     float all[1] = {at.sum([&](int j, uint32_t e) { return v[j][e]; })};
     g.sum(all);
@@ -201,8 +201,7 @@ __device__ __forceinline__ float normalise(Row<kN>& v, G& g, const Columns<kN, k
     each<kN>([&](int j, uint32_t e) { v[j][e] -= mean; });
     float s[2] = {at.sum([&](int j, uint32_t e) { return v[j][e] * v[j][e]; }), at.sum([&](int j, uint32_t e) { return v[j][e]; })};
     g.sum(s);
-    const float rest = s[1] * by.one_dim;
-    each<kN>([&](int j, uint32_t e) { v[j][e] -= rest; });
+    rest = s[1] * by.one_dim;
     square = s[0] * by.one_dim - rest * rest;
     if (square < 0.f) square = 0.f;
   } else {
@@ -211,7 +210,12 @@ __device__ __forceinline__ float normalise(Row<kN>& v, G& g, const Columns<kN, k
     square = s[0] * by.one_dim;
   }
   const float inverse = __builtin_amdgcn_rsqf(square + by.eps);   // (a unit in the last place; eps is a normal number)
-  each<kN>([&](int j, uint32_t e) { v[j][e] *= inverse; });
+  if (layer) {
+    rest *= inverse;
+    each<kN>([&](int j, uint32_t e) { v[j][e] = v[j][e] * inverse - rest; });
+  } else {
+    each<kN>([&](int j, uint32_t e) { v[j][e] *= inverse; });
+  }
   return inverse;
 }
 
@@ -220,12 +224,18 @@ __device__ __forceinline__ float normalise(Row<kN>& v, G& g, const Columns<kN, k
 template <int kN, bool kTiny, class G>
 __device__ __forceinline__ void denormalise(Row<kN>& p, const Row<kN>& unit, float inverse, G& g, const Columns<kN, kTiny>& at, bool layer, Scale by, bool wanted, float& more) {
   float along = at.sum([&](int j, uint32_t e) { return p[j][e] * unit[j][e]; }), mean = 0.f;
-  if (layer || wanted) {
+  if (layer && wanted) {
     float s[3] = {along, at.sum([&](int j, uint32_t e) { return p[j][e]; }), more};
     g.sum(s);
     along = s[0];
-    mean = layer ? s[1] * by.one_dim * inverse : 0.f;
+    mean = s[1] * by.one_dim * inverse;
     more = s[2];
+  } else if (layer || wanted) {
+    float s[2] = {along, layer ? at.sum([&](int j, uint32_t e) { return p[j][e]; }) : more};
+    g.sum(s);
+    along = s[0];
+    if (layer) mean = s[1] * by.one_dim * inverse;
+    else more = s[1];
   } else {
     float s[1] = {along};
     g.sum(s);
