@@ -513,7 +513,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_product(ProductArgs) {
 // parts each, rows 16 bytes longer than they need be so that those a read takes lie in different banks; a wavefront takes 32 x 32 of
 // a product at a time, up to kBlocks of them, and what it worked out replaces an operand when all are done with it.
 constexpr uint32_t kSmallLanes = 1024, kRoom = 158 * 1024;
-constexpr int kBlocks = 3;
+constexpr int kBlocks = 2;
 struct StepNumbers {
   float gram, keep, square, diagonal, next;
 };
@@ -526,17 +526,6 @@ struct SmallArgs {
 };
 __host__ __device__ inline uint32_t small_side(uint32_t n) { return (n + 31u) / 32u * 32u; }
 __host__ __device__ inline uint32_t small_line(uint32_t n) { return 2u * n + 16u; }   // bytes of a row
-
-template <class G>
-__device__ __forceinline__ float given_element(const SmallArgs& p, const Matrix& t, uint32_t r, uint32_t c, bool first) {
-#pragma clang fp contract(off)
-  const float u = (float)((const G*)t.u)[r * t.ld_u + c];
-  if (!t.m) return u;
-  const uint64_t i = (uint64_t)r * t.columns + c;
-  const float g = u * p.given.grad_scale, m = first ? t.m[i] * p.given.momentum + g : t.m[i];
-  if (first) t.m[i] = m;
-  return p.given.nesterov ? g + m * p.given.momentum : m;
-}
 
 template <class G>
 __global__ __launch_bounds__(kSmallLanes) void k_small(SmallArgs) {
@@ -552,12 +541,56 @@ __global__ __launch_bounds__(kSmallLanes) void k_small(SmallArgs) {
   lds_char *x = (lds_char*)lds, *a = x + 2u * part_x;
 
   for (uint32_t at = threadIdx.x * 16u; at < 2u * (part_x + part_a); at += kSmallLanes * 16u) *(__attribute__((address_space(3))) f32x4*)(x + at) = f32x4{0.f, 0.f, 0.f, 0.f};
-  // The same lane reads an element twice: for the norm (and its momentum), then to split it.
-  double square = 0;
+  __syncthreads();
+  // An element's 32 bits wait for the norm in the two places of its parts.
+  typedef __attribute__((address_space(3))) uint16_t Half;
   const uint32_t all = t.rows * t.columns, most = t.columns;
-  for (uint32_t at = threadIdx.x; at < all; at += kSmallLanes) {
-    const float u = given_element<G>(p, t, at / most, at % most, true);
-    square += (double)u * u;
+  const uint32_t further_r = kSmallLanes / most, further_c = kSmallLanes % most;
+  auto place = [&](uint32_t r, uint32_t c) { return x + (t.tall ? c : r) * line_x + (t.tall ? r : c) * 2u; };
+  double square = 0;
+  {
+#pragma clang fp contract(off)
+    constexpr uint32_t kAtOnce = 4;
+    uint32_t r[kAtOnce], c[kAtOnce];
+    r[0] = threadIdx.x / most;
+    c[0] = threadIdx.x % most;
+    for (uint32_t at = threadIdx.x; at < all; at += kAtOnce * kSmallLanes) {
+      float u[kAtOnce], m[kAtOnce];
+#pragma unroll
+      for (uint32_t e = 0; e < kAtOnce; ++e) {
+        if (e) {
+          r[e] = r[e - 1] + further_r;
+          c[e] = c[e - 1] + further_c;
+          if (c[e] >= most) {
+            c[e] -= most;
+            ++r[e];
+          }
+        }
+        const uint32_t there = r[e] < t.rows ? r[e] : 0u;   // (beyond the last element: one that is there)
+        u[e] = (float)((const G*)t.u)[there * t.ld_u + c[e]];
+        if (t.m) m[e] = t.m[there * most + c[e]];
+      }
+#pragma unroll
+      for (uint32_t e = 0; e < kAtOnce; ++e) {
+        if (at + e * kSmallLanes >= all) continue;
+        float v = u[e];
+        if (t.m) {
+          const float grad = v * p.given.grad_scale, now = m[e] * p.given.momentum + grad;
+          t.m[r[e] * most + c[e]] = now;
+          v = p.given.nesterov ? grad + now * p.given.momentum : now;
+        }
+        square += (double)v * v;
+        lds_char* to = place(r[e], c[e]);
+        *(Half*)to = (uint16_t)(__float_as_uint(v) >> 16);
+        *(Half*)(to + part_x) = (uint16_t)__float_as_uint(v);
+      }
+      r[0] = r[kAtOnce - 1] + further_r;
+      c[0] = c[kAtOnce - 1] + further_c;
+      if (c[0] >= most) {
+        c[0] -= most;
+        ++r[0];
+      }
+    }
   }
 #pragma unroll
   for (int d = 32; d; d /= 2) square += __shfl_xor(square, d, 64);
@@ -569,11 +602,10 @@ __global__ __launch_bounds__(kSmallLanes) void k_small(SmallArgs) {
   const double norm = sqrt(square);
   const int k2 = power_of(norm);
   const float f = factor_of(norm, k2, p.given.eps);
-  for (uint32_t at = threadIdx.x; at < all; at += kSmallLanes) {
-    const uint32_t r = at / most, c = at % most;
-    const float v = ldexpf(given_element<G>(p, t, r, c, false), k2);
+  for (uint32_t at = threadIdx.x * 2u; at < part_x; at += kSmallLanes * 2u) {   // (zeros stay zeros)
+    lds_char* to = x + at;
+    const float v = ldexpf(__uint_as_float((uint32_t)*(Half*)to << 16 | *(Half*)(to + part_x)), k2);
     const f16 high = (f16)v;
-    lds_char* to = x + (t.tall ? c : r) * line_x + (t.tall ? r : c) * 2u;
     *(__attribute__((address_space(3))) f16*)to = high;
     *(__attribute__((address_space(3))) f16*)(to + part_x) = (f16)(v - (float)high);
   }
@@ -591,16 +623,25 @@ __global__ __launch_bounds__(kSmallLanes) void k_small(SmallArgs) {
     return __builtin_bit_cast(F, (s16x8)__builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7));
   };
   f32x4 sum[kBlocks][2][2];
-  // This wavefront's blocks of a product: rows of `left` over `depth`, by rows of `right` (or across them).
-  auto multiply = [&](const lds_char* left, uint32_t line_l, uint32_t part_l, const lds_char* right, uint32_t line_r, uint32_t part_r, uint32_t wide, uint32_t depth, auto is_across) __attribute__((always_inline)) {
-    const uint32_t over = wide / 32u, blocks = rows / 32u * over;
+  // where this wavefront's blocks begin in a product of `rows` x `rows`, and of `rows` x `columns`; none: beyond the rows
+  uint32_t block_r[2][kBlocks], block_c[2][kBlocks];
+#pragma unroll
+  for (int w = 0; w < 2; ++w)
 #pragma unroll
     for (int n = 0; n < kBlocks; ++n) {
-      const uint32_t block = wave + n * (kSmallLanes / 64u);
+      const uint32_t over = (w ? columns : rows) / 32u, block = wave + n * (kSmallLanes / 64u);
+      block_r[w][n] = same(block / over * 32u);
+      block_c[w][n] = same(block % over * 32u);
+    }
+  // This wavefront's blocks of a product: rows of `left` over `depth`, by rows of `right` (or across them).
+  auto multiply = [&](const lds_char* left, uint32_t line_l, uint32_t part_l, const lds_char* right, uint32_t line_r, uint32_t part_r, uint32_t depth, auto is_across) __attribute__((always_inline)) {
+    constexpr int w = decltype(is_across)::value;
+#pragma unroll
+    for (int n = 0; n < kBlocks; ++n) {
+      const uint32_t r0 = block_r[w][n], c0 = block_c[w][n];
+      if (r0 >= rows) continue;
 #pragma unroll
       for (int e = 0; e < 4; ++e) sum[n][e / 2][e % 2] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if (block >= blocks) continue;
-      const uint32_t r0 = same(block / over * 32u), c0 = same(block % over * 32u);
       for (uint32_t k = 0; k < depth; k += 32u) {
         F l[2][2], r[2][2];   // of 16 rows each, first and second parts
 #pragma unroll
@@ -611,6 +652,7 @@ __global__ __launch_bounds__(kSmallLanes) void k_small(SmallArgs) {
             if constexpr (decltype(is_across)::value) r[h][q] = across(right + q * part_r, line_r, c0 + 16u * h, k);
             else r[h][q] = along(right + q * part_r, line_r, c0 + 16u * h, k);
           }
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int pair = 0; pair < 3; ++pair)
 #pragma unroll
@@ -621,52 +663,48 @@ __global__ __launch_bounds__(kSmallLanes) void k_small(SmallArgs) {
     }
   };
   // f(row, first of four columns, sums) of every place that this wavefront has worked out.
-  auto every = [&](uint32_t wide, auto f) __attribute__((always_inline)) {
-    const uint32_t over = wide / 32u, blocks = rows / 32u * over;
+  auto every = [&](auto which, auto f) __attribute__((always_inline)) {
+    constexpr int w = decltype(which)::value;
 #pragma unroll
     for (int n = 0; n < kBlocks; ++n) {
-      const uint32_t block = wave + n * (kSmallLanes / 64u);
-      if (block >= blocks) continue;
+      if (block_r[w][n] >= rows) continue;
 #pragma unroll
       for (uint32_t h = 0; h < 2u; ++h)
 #pragma unroll
-        for (uint32_t j = 0; j < 2u; ++j) f(block / over * 32u + 16u * h + i, block % over * 32u + 16u * j + 4u * g, sum[n][h][j]);
+        for (uint32_t j = 0; j < 2u; ++j) f(block_r[w][n] + 16u * h + i, block_c[w][n] + 16u * j + 4u * g, sum[n][h][j]);
     }
   };
+  typedef f16 f16x4 __attribute__((ext_vector_type(4)));
+  typedef __attribute__((address_space(3))) f16x4 Four;
   auto put = [&](lds_char* to, uint32_t part, f32x4 v) {
     const Halves w(v);
-#pragma unroll
-    for (uint32_t e = 0; e < 4u; ++e) {
-      ((__attribute__((address_space(3))) f16*)to)[e] = w.high[e];
-      ((__attribute__((address_space(3))) f16*)(to + part))[e] = w.low[e];
-    }
+    *(Four*)to = f16x4{w.high[0], w.high[1], w.high[2], w.high[3]};
+    *(Four*)(to + part) = f16x4{w.low[0], w.low[1], w.low[2], w.low[3]};
   };
   for (uint32_t s = 0; s < p.steps; ++s) {
     const StepNumbers by = p.of[s];
     const float first = s ? 1.f : f;
-    multiply(x, line_x, part_x, x, line_x, part_x, rows, columns, Kind<0>());
-    every(rows, [&](uint32_t r, uint32_t c, f32x4& v) { put(a + r * line_a + c * 2u, part_a, v * (by.gram * first * first)); });
+    multiply(x, line_x, part_x, x, line_x, part_x, columns, Kind<0>());
+    every(Kind<0>(), [&](uint32_t r, uint32_t c, f32x4& v) { put(a + r * line_a + c * 2u, part_a, v * (by.gram * first * first)); });
     __syncthreads();
-    multiply(a, line_a, part_a, a, line_a, part_a, rows, rows, Kind<0>());
-    every(rows, [&](uint32_t r, uint32_t c, f32x4& v) {
+    multiply(a, line_a, part_a, a, line_a, part_a, rows, Kind<0>());
+    every(Kind<0>(), [&](uint32_t r, uint32_t c, f32x4& v) {
       const lds_char* at = a + r * line_a + c * 2u;
+      const f16x4 high = *(const Four*)at, low = *(const Four*)(at + part_a);
 #pragma unroll
-      for (uint32_t e = 0; e < 4u; ++e) {
-        const float there = (float)((const __attribute__((address_space(3))) f16*)at)[e] + (float)((const __attribute__((address_space(3))) f16*)(at + part_a))[e];
-        v[e] = v[e] * by.square + there * by.keep + (r == c + e && r < m_side ? by.diagonal : 0.f);
-      }
+      for (uint32_t e = 0; e < 4u; ++e) v[e] = v[e] * by.square + ((float)high[e] + (float)low[e]) * by.keep + (r == c + e && r < m_side ? by.diagonal : 0.f);
     });
     __syncthreads();
-    every(rows, [&](uint32_t r, uint32_t c, f32x4& v) { put(a + r * line_a + c * 2u, part_a, v); });
+    every(Kind<0>(), [&](uint32_t r, uint32_t c, f32x4& v) { put(a + r * line_a + c * 2u, part_a, v); });
     __syncthreads();
-    multiply(a, line_a, part_a, x, line_x, part_x, columns, rows, Kind<1>());
+    multiply(a, line_a, part_a, x, line_x, part_x, rows, Kind<1>());
     if (s + 1u == p.steps) break;
     __syncthreads();
-    every(columns, [&](uint32_t r, uint32_t c, f32x4& v) { put(x + r * line_x + c * 2u, part_x, v * (by.next * first)); });
+    every(Kind<1>(), [&](uint32_t r, uint32_t c, f32x4& v) { put(x + r * line_x + c * 2u, part_x, v * (by.next * first)); });
     __syncthreads();
   }
   const float scale = p.of[p.steps - 1u].next * (p.steps == 1u ? f : 1.f);
-  every(columns, [&](uint32_t r, uint32_t c, f32x4& v) {
+  every(Kind<1>(), [&](uint32_t r, uint32_t c, f32x4& v) {
     const f32x4 one[1] = {v * scale};
     if (p.last.out == FBX_F32) leave<float, 1>(p.last, t, r, c, one);
     else if (p.last.out == FBX_F16) leave<f16, 1>(p.last, t, r, c, one);
