@@ -460,6 +460,12 @@ uint64_t rows_of(const at::Tensor& t, const char* name, fbx_dtype type, const at
   if (code(t) != type) bad(std::string(name) + " must be of type " + c10::toString(type_of(type)));
   return matrix(t, name, nullptr, n, columns);
 }
+// A result may not be one of the inputs: another wavefront may still have to read it.
+void apart(const at::Tensor& out, std::initializer_list<const at::Tensor*> inputs) {
+  if (!out.numel()) return;
+  for (const at::Tensor* t : inputs)
+    if (t && t->data_ptr() == out.data_ptr()) bad("a tensor given for a result is one of the inputs");
+}
 // A gradient as autograd gives it may be one element seen many times.
 at::Tensor gradient_rows(const at::Tensor& t) {
   const bool fine = t.dim() != 2 || ((t.size(1) <= 1 || t.stride(1) == 1) && (t.size(0) <= 1 || t.stride(0) >= t.size(1)));
@@ -605,7 +611,11 @@ PyObject* join(PyObject*, PyObject* args) {
     const fbx_dtype types[2] = {c.a.stream, c.a.block};
     at::Tensor out[2];
     for (int i = 0; i < 2; ++i)
-      if (out_o[i] != Py_None) rows_of(result(out_o[i]), i ? "out_next" : "out", types[i], c.x, c.a.records, c.a.dim);
+      if (out_o[i] != Py_None) {
+        const at::Tensor& o = result(out_o[i]);
+        rows_of(o, i ? "out_next" : "out", types[i], c.x, c.a.records, c.a.dim);
+        apart(o, {&c.x, &c.y, c.gate, i && out_o[0] != Py_None ? &tensor(out_o[0], "out") : nullptr});
+      }
     const c10::DeviceGuard guard(c.x.device());
     for (int i = 0; i < 1 + then; ++i)
       out[i] = out_o[i] == Py_None ? at::empty({c.x.size(0), c.x.size(1)}, c.x.options().dtype(type_of(types[i])).memory_format(c10::nullopt)) : tensor(out_o[i], "out");
@@ -718,6 +728,9 @@ PyObject* orthogonalise(PyObject*, PyObject* args) {
         if (out[i].numel()) seen.push_back(out[i].data_ptr());
       }
     }
+    for (Py_ssize_t i = 0; given.seq && i < n; ++i)   // (its own matrix is read before it is written)
+      for (Py_ssize_t k = 0; k < n; ++k)
+        if (i != k) apart(out[i], {&in[k]});
     std::sort(seen.begin(), seen.end());
     if (std::adjacent_find(seen.begin(), seen.end()) != seen.end()) bad("a result is given twice");
     const c10::DeviceGuard guard(like.device());

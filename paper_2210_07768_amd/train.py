@@ -192,7 +192,7 @@ def _code(given, of: dict, name: str) -> int:
 def norm(x, weight=None, kind: str = "rms", eps: float = 1e-6, dtype=None, out=None):
     """Rows of x brought to unit size, times weight: x / sqrt(mean(x^2) + eps) (kind "rms"), or the same of x less its mean
     ("layer").  x: records x dim; weight: dim elements, of the result's type or float32; dtype: of the result: x's, or, where x is
-    float32, float16 or bfloat16."""
+    float32, float16 or bfloat16.  out may be x."""
     got = (_native or _load()).norm(x, weight, dtype, KINDS[kind] if kind in _KINDS else _code(kind, KINDS, "kind"), eps, out)
     return _Norm.apply(x, weight, kind, eps, dtype) if got is NotImplemented else got   # (where an input asks for its gradient)
 
@@ -213,7 +213,7 @@ def join(x, y, weight=None, gate=None, scale=1.0, next_weight=None, *, post: boo
     x, y: records x dim; x: of y's type or float32, and so is the stream returned; what is normed is of y's.
     weight, next_weight, scale: dim elements, all of y's type or all float32; scale may be a number.
     gate: records x dim, or records x 1, of y's type; gate_act: "sigmoid", or "none" where it is to be taken as it is.
-    post: false leaves out y's norm (and has no weight): x + scale * act(gate) * y."""
+    post: false leaves out y's norm (and has no weight): x + scale * act(gate) * y.  out and out_next may not be inputs."""
     if then is None:
         then = next_weight is not None
     got = (_native or _load()).join(x, y, weight, gate, scale, next_weight, post, then, GATES[gate_act] if gate_act in _GATES else _code(gate_act, GATES, "gate_act"),
@@ -301,7 +301,8 @@ def orthogonalise(x, steps: int = 5, coefficients=NEWTON_SCHULZ, eps: float = 1e
 
     coefficients: three numbers, or three for each step.  dtype: of the results (the matrices').  exact: products of 32-bit accuracy, of three
     times the work; by default for all but results in bfloat16 of matrices of more than 256 rows and columns, whose products are then in
-    half precision, with an error of about that of the results' rounding.  out: a tensor, or a list of them.  Without derivative."""
+    half precision, with an error of about that of the results' rounding.  out: a tensor, or a list of them (a matrix's own result
+    may be written over it).  Without derivative."""
     one = isinstance(x, torch.Tensor)
     if out is not None and one != isinstance(out, torch.Tensor):
         _bad("out must be a tensor for a tensor, and a list for a list")

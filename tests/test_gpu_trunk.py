@@ -356,6 +356,24 @@ def test_a_table_of_rows_beyond_32_bits():
     assert torch.equal(x, T.norm(near))
 
 
+def test_results_over_inputs():
+    """Where a result may lie over its input it is the same, and elsewhere it is refused."""
+    g = _gen(15)
+    for d in (5, 60, 411, 2624, 9001):
+        x, w = _r(g, 37, d, dtype=BF16), _r(g, d, shift=1.0)
+        want = T.norm(x, w, kind="layer")
+        assert T.norm(x, w, kind="layer", out=x) is x and torch.equal(x, want)
+    u = [_decaying(g, 30, 50), _decaying(g, 300, 200)]
+    want = T.orthogonalise(u)
+    T.orthogonalise(u, out=u)
+    assert all(torch.equal(a, b) for a, b in zip(u, want))
+    x, y, z = (_r(g, 4, 24) for _ in range(3))
+    for call in (lambda: T.join(x, y, None, z, out=x), lambda: T.join(x, y, None, z, out=y), lambda: T.join(x, y, None, z, then=True, out_next=z),
+                 lambda: T.join(x, y, then=True, out=z, out_next=z), lambda: T.orthogonalise([x, y], out=[y, x])):
+        with pytest.raises(B.FbxError):
+            call()
+
+
 # ------------------------------------------------------------------ orthogonalised matrices
 C = T.NEWTON_SCHULZ
 
