@@ -295,8 +295,8 @@ __device__ __forceinline__ void leave(const Leaving& p, const Matrix& t, uint32_
 
 // BM x BN of C a workgroup, its WM x WN wavefronts side by side.  C's rows come from A; its columns from B, which is the first side
 // of the matrix instructions, so that a lane holds four adjacent columns of a row.  Of a symmetric C tiles on and below the
-// diagonal are worked out, and stored on either side of it.
-template <Form kForm, int BM, int BN, int WM, int WN, int kStages>
+// diagonal are worked out, and stored on either side of it.  kStages: steps whose tiles are in LDS or on their way there.
+template <Form kForm, int BM, int BN, int WM, int WN, int kStages, bool kBoth>
 __global__ __launch_bounds__(WM * WN * 64, 2) void k_product(ProductArgs) {
 #ifdef __HIP_DEVICE_COMPILE__
   constexpr bool kTwin = kForm == kGram || kForm == kPolynom;
@@ -306,6 +306,9 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_product(ProductArgs) {
   __shared__ alignas(1024) char a0[BM * kStepBytes], b0[BN * kStepBytes], a1[BM * kStepBytes], b1[BN * kStepBytes];
   __shared__ alignas(1024) char a2[kStages > 2 ? BM * kStepBytes : 16], b2[kStages > 2 ? BN * kStepBytes : 16];
   __shared__ alignas(1024) char a3[kStages > 2 ? BM * kStepBytes : 16], b3[kStages > 2 ? BN * kStepBytes : 16];
+  // kBoth: second parts
+  __shared__ alignas(1024) char c0[kBoth ? BM * kStepBytes : 16], d0[kBoth ? BN * kStepBytes : 16], c1[kBoth ? BM * kStepBytes : 16], d1[kBoth ? BN * kStepBytes : 16];
+  static_assert(!kBoth || kStages == 2, "");
   const ProductArgs& p = launch_args<ProductArgs>();
   const uint32_t lane = threadIdx.x % 64u, wave = same(threadIdx.x / 64u), wm = wave % WM, wn = wave / WM;
   uint32_t at;
@@ -331,7 +334,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_product(ProductArgs) {
   }
   const uint32_t m_side = same(t.m_side), wide_a = same(kForm == kGram ? t.wide_n : t.wide_m), wide_b = same(kForm == kPolynom ? t.wide_m : t.wide_n);
   const uint64_t ld_a = wide_a * 2u, ld_b = wide_b * 2u;
-  const uint32_t each = wide_a / kDepth, end = t.exact ? 3u * each : each;   // steps: of one product of parts, of all
+  const uint32_t each = wide_a / kDepth, end = t.exact && !kBoth ? 3u * each : each;   // steps: of one product of parts, of all
   const char* of_a = (const char*)(kForm == kGram ? t.x(p.turn, 0) : kForm == kPolynom ? t.a(0) : t.b(0));
   const char* of_b = (const char*)(kForm == kPolynom ? t.a(0) : t.x(p.turn, 0));
   const uint64_t part_a = (uint64_t)m_side * ld_a, part_b = (uint64_t)m_side * ld_b;
@@ -342,35 +345,47 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_product(ProductArgs) {
   ta.begin(wave, lane, ld_a, 0);
   tb.begin(wave, lane, ld_b, wide_b - col0);
   // (behind the last step: of nothing, so that every step's loads are as many)
-  auto load = [&](char* to_a, char* to_b, uint32_t s) {
+  auto load_part = [&](char* to_a, char* to_b, uint32_t s, uint32_t k, bool second_a, bool second_b) {
     const bool none = s >= end;
-    const uint32_t pair = s >= 2u * each ? 2u : s >= each ? 1u : 0u, k = s - pair * each;  // first by first, first by second, second by first
-    const char *a = of_a + (pair == 2u ? part_a : 0u), *b = of_b + (pair == 1u ? part_b : 0u);
+    const char *a = of_a + (second_a ? part_a : 0u), *b = of_b + (second_b ? part_b : 0u);
     const uint32_t left = wide_a - k * kDepth;
     ta.load((lds_char*)to_a, a + (uint64_t)k * kStepBytes, ld_a, none ? 0u : m_side - row0, left, left * 2u, wave);
     if (kTwin) tb.load((lds_char*)to_b, b + (uint64_t)k * kStepBytes, ld_b, none ? 0u : m_side - col0, left, left * 2u, wave);
     else tb.load((lds_char*)to_b, b + (uint64_t)k * kDepth * ld_b, ld_b, none || m_side <= k * kDepth ? 0u : m_side - k * kDepth, 0, (wide_b - col0) * 2u, wave);
   };
 
+  auto load = [&](char* to_a, char* to_b, uint32_t s) {
+    const uint32_t pair = kBoth || s < each ? 0u : s < 2u * each ? 1u : 2u;  // first by first, first by second, second by first
+    load_part(to_a, to_b, s, s - pair * each, pair == 2u, pair == 1u);
+    if constexpr (kBoth) load_part(to_a == a0 ? c0 : c1, to_b == b0 ? d0 : d1, s, s, true, true);
+  };
+
   // Two halves of a step's depth in turn: while one is multiplied out of registers the other's rows are read from LDS.
   // A step's barrier lies between the halves: behind it the next step's tile is there and nobody reads this step's any more, so
   // the loads of the step kStages later go there.
   f32x4 sum[kMF][kNF] = {};
-  typename Frag<f16>::type fa[2][kMF], fb[2][kNF];
+  constexpr int kParts = kBoth ? 2 : 1;
+  typename Frag<f16>::type fa[2][kParts][kMF], fb[2][kParts][kNF];
   auto read = [&](int part, const char* in_a, const char* in_b) {
 #pragma unroll
-    for (int i = 0; i < kMF; ++i) fa[part][i] = TileA::read((const lds_char*)in_a, wm * kRows + i * 16, part, lane);
+    for (int q = 0; q < kParts; ++q) {
+      const char *from_a = q ? (in_a == a0 ? c0 : c1) : in_a, *from_b = q ? (in_b == b0 ? d0 : d1) : in_b;
 #pragma unroll
-    for (int j = 0; j < kNF; ++j) fb[part][j] = TileB::read((const lds_char*)in_b, wn * kCols + j * 16, part, lane);
+      for (int i = 0; i < kMF; ++i) fa[part][q][i] = TileA::read((const lds_char*)from_a, wm * kRows + i * 16, part, lane);
+#pragma unroll
+      for (int j = 0; j < kNF; ++j) fb[part][q][j] = TileB::read((const lds_char*)from_b, wn * kCols + j * 16, part, lane);
+    }
   };
   auto multiply = [&](int part) {
 #pragma unroll
-    for (int j = 0; j < kNF; ++j)
+    for (int pair = 0; pair < (kBoth ? 3 : 1); ++pair)
 #pragma unroll
-      for (int i = 0; i < kMF; ++i) sum[i][j] = mma(fb[part][j], fa[part][i], sum[i][j]);
+      for (int j = 0; j < kNF; ++j)
+#pragma unroll
+        for (int i = 0; i < kMF; ++i) sum[i][j] = mma(fb[part][pair == 1][j], fa[part][pair == 2][i], sum[i][j]);
   };
   auto arrived = [](auto steps) {
-    constexpr int n = decltype(steps)::value * (TileA::kLoads + TileB::kLoads);
+    constexpr int n = decltype(steps)::value * (TileA::kLoads + TileB::kLoads) * kParts;
     static_assert(n < 64, "");
     __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_waitcnt((n & 15) | (n >> 4) << 14 | 0x0070);  // (vmcnt n, lgkmcnt 0)
@@ -771,8 +786,10 @@ struct Whole {
 // Tiles of 256 x 256 read least from LDS, smaller ones begin sooner, end sooner and leave fewer compute units idle.  What they were
 // measured to take (2,624 x 4,096, 384 x 1,024; microseconds): `begin` before the first step and behind the last, a step alone on a compute unit,
 // and among as many as fit one; kNext's results are twice what the others store.
+// Where both parts are multiplied small tiles bring them into LDS together, once for three products (kBoth: 18 of 384 x 1,024, A 26 -> 18.6 us, B
+// 15.7 -> 13.1); for tiles of 128 two workgroups would not fit a compute unit.
 struct Size { uint32_t side, at_once; double begin[2], lone, full; };
-constexpr Size kSizes[3] = {{256, 1, {14, 24}, 1.45, 1.8}, {128, 2, {9, 10.5}, 0.78, 0.9}, {64, 2, {7, 7}, 0.35, 0.43}};
+constexpr Size kSizes[4] = {{256, 1, {14, 24}, 1.45, 1.8}, {128, 2, {9, 10.5}, 0.78, 0.9}, {64, 2, {7, 7}, 0.35, 0.43}, {64, 2, {6.5, 6.5}, 0.17, 0.25}};
 uint64_t tiles_of(const Matrix& t, Form form, uint32_t side) {
   const uint64_t rows = ceil_div(t.m_side, side);
   return form == kGram || form == kPolynom ? rows * (rows + 1) / 2 : rows * ceil_div(t.n_side, side);
@@ -781,7 +798,7 @@ uint32_t choose(const Matrix* t, uint32_t n, Form form) {
   uint32_t best = 2;
   double least = 0;
   for (uint32_t i = 0; i < 3; ++i) {
-    const Size& s = kSizes[i];
+    const Size& s = kSizes[i == 2 && t[0].exact ? 3 : i];   // (a launch's matrices are of one kind)
     const double begin = s.begin[form == kNext || form == kLast], slots = 256.0 * s.at_once;
     double tiles = 0, steps = 0, longest = 0;
     for (uint32_t k = 0; k < n; ++k) {
@@ -806,9 +823,10 @@ void multiply(ProductArgs& p, hipStream_t stream) {
   const uint32_t size = choose(p.list.of, p.list.n, kForm), side = kSizes[size].side;
   for (uint32_t i = 0; i < p.list.n; ++i) p.list.first[i + 1] = p.list.first[i] + (uint32_t)tiles_of(p.list.of[i], kForm, side);
   const dim3 grid(p.list.first[p.list.n]);
-  if (size == 0) launch_on(stream, k_product<kForm, 256, 256, 2, 4, 2>, grid, dim3(512), 0, p);
-  else if (size == 1) launch_on(stream, k_product<kForm, 128, 128, 2, 2, 2>, grid, dim3(256), 0, p);
-  else launch_on(stream, k_product<kForm, 64, 64, 2, 2, 4>, grid, dim3(256), 0, p);
+  if (size == 0) launch_on(stream, k_product<kForm, 256, 256, 2, 4, 2, false>, grid, dim3(512), 0, p);
+  else if (size == 1) launch_on(stream, k_product<kForm, 128, 128, 2, 2, 2, false>, grid, dim3(256), 0, p);
+  else if (p.list.of[0].exact) launch_on(stream, k_product<kForm, 64, 64, 2, 2, 2, true>, grid, dim3(256), 0, p);
+  else launch_on(stream, k_product<kForm, 64, 64, 2, 2, 4, false>, grid, dim3(256), 0, p);
 }
 
 // Left to this, products are of both parts where results keep more than bf16 does, and for small matrices: their products take little
@@ -850,7 +868,7 @@ StepNumbers numbers_of(const std::vector<Step>& steps, size_t i) {
   return StepNumbers{(float)(a / (x * x)), (float)(s.b * b / a), (float)(s.c * b / (a * a)), (float)(s.a * b), (float)(next / (b * x))};
 }
 
-// Matrices go together until there are kMatrices of them or their scratch is more than this: by then they fill the card.
+// Matrices of a kind go together until there are kMatrices of them or their scratch is more than this: by then they fill the card.
 constexpr uint64_t kTogether = 1ull << 30;
 struct Batch {
   std::vector<uint32_t> of;
@@ -859,11 +877,11 @@ struct Batch {
 };
 std::vector<Batch> batches(std::vector<Matrix>& all) {
   std::vector<Batch> b;
-  int open[2] = {-1, -1};   // the last batch of matrices of either kind
+  int open[3] = {-1, -1, -1};   // the last batch of matrices of each kind: small, of both parts, of first parts
   for (uint32_t i = 0; i < all.size(); ++i) {
     const bool small = is_small(all[i].rows, all[i].columns);
     const uint64_t bytes = lay_out(all[i], all[i].rows, all[i].columns) * !small;
-    int& at = open[small];
+    int& at = open[small ? 0 : all[i].exact ? 1 : 2];
     if (at < 0 || b[at].of.size() == kMatrices || b[at].bytes + bytes > kTogether) {
       at = (int)b.size();
       b.push_back(Batch{{}, 0, small});
