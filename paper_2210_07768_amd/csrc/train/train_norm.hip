@@ -303,7 +303,7 @@ struct NormArgs {
 
 // R: of the residual stream; T: of the result.  A row's loads are on their way while the one before it is worked on, but for rows that
 // leave no registers for it (kAhead).
-// Bound by memory.
+// Bound by memory: 65,536 x 2,624 in bf16, 0.69 GB, takes 118 us, 5.8 TB/s (a copy of 1 GiB: 5.0).  One row: 2.0 us, the call 4.3 to 5.
 template <int kN>
 constexpr bool kAhead = kN == 1;
 
@@ -333,6 +333,8 @@ __global__ __launch_bounds__(kMostLanes) void k_norm(NormArgs p) {
   }
 }
 
+// dx, and a workgroup's sums of dy times the unit rows.  16,384 x 411 in f16, a layer's norm, rows 414 apart: 13.4 us of the call's 14.8, 40 MB at
+// 3.0 TB/s; 300 vector instructions a row of 64 lanes are 8 us of it.  4,096 x 384 in f32: 6.5 of 9.5 us.
 template <class R, class T, Shape kShape>
 __global__ __launch_bounds__(kMostLanes) void k_norm_grad(NormArgs p) {
   constexpr int kN = packs_of(kShape);
@@ -418,7 +420,8 @@ __device__ __forceinline__ void fetch_vectors(Row<kN>& weight, Row<kN>& next_wei
   each<kN>([&](int j, uint32_t e) { weight[j][e] *= scale[j][e]; });
 }
 
-// Bound by memory.
+// Bound by memory: 65,536 x 2,624, a stream in f32, the block's side in bf16, a gate for each element, the next norm: 2.4 GB in 440 us,
+// 5.5 TB/s.  One row of 1,536: 3.0 us, the call 5.4 to 6.
 template <class R, class T, Shape kShape>
 __global__ __launch_bounds__(kMostLanes) void k_join(JoinArgs p) {
   constexpr int kN = packs_of(kShape);
@@ -459,6 +462,11 @@ __global__ __launch_bounds__(kMostLanes) void k_join(JoinArgs p) {
   }
 }
 
+// The stream is worked out again from x, y and the gate: to keep it would cost the forward pass a write of what is read here anyway.
+// 16,384 x 2,624 in bf16 with a gate for each element and the next norm: 0.69 GB in 165 to 176 us, 3.9 to 4.2 TB/s.  141 registers let twelve
+// wavefronts be on a compute unit; 463 vector instructions and 16 exponentials and reciprocals a row and wavefront are 0.1 ms of it, hidden in
+// part.  With loads that depended on conditions, waited for at once, it took 346.  1,000 x 411: 8.5 of the call's 14 us, of which
+// one row takes 6.8: instructions come from memory once a launch.
 template <class R, class T, Shape kShape>
 __global__ __launch_bounds__(kMostLanes) void k_join_grad(JoinArgs p) {
   constexpr int kN = packs_of(kShape);
@@ -541,7 +549,7 @@ __global__ __launch_bounds__(kMostLanes) void k_join_grad(JoinArgs p) {
 }
 
 // Adds up the workgroups' sums of columns, in their order, and makes gradients of them: of the first, times the scale, the
-// weight's; times the weight, the scale's; of the second the next weight's.
+// weight's; times the weight, the scale's; of the second the next weight's.  3 to 5 us.
 struct SumArgs {
   const float* sums;
   const void *weight, *scale;
