@@ -257,8 +257,8 @@ fbx_status fbx_join_backward(const fbx_join* h, const fbx_join_gradients* g, voi
  * first part overflows; sums are in 32 bits.
  *   exact = 1: products are of both parts of both sides (all but second by second): errors like those of
  *     products in 32 bits.
- *   exact = 0: products are of first parts, a third of the work; a times X's second part is added.  The result's error is that of
- *     rounding it to bf16: about 1.7e-3 of its size, twice that for small matrices.
+ *   exact = 0: products are of first parts, a third of the work; a times X's second part is added.  The result is off by 0.6e-3 to
+ *     1.6e-3 of its size, about what rounding it to bf16 leaves (1.7e-3).
  *     Matrices that a workgroup's memory holds (up to 128 x 128, 32 x 1,024 or so) are always worked out exactly.
  *   exact = FBX_EXACT_BY_SIZE: 0 for results in bf16 of matrices of more than 256 rows and columns, else 1.
  *
