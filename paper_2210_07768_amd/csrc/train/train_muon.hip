@@ -244,8 +244,12 @@ struct Halves {
   __device__ explicit Halves(f32x4 v, float second = kSecond) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      high[e] = (f16)v[e];
-      low[e] = (f16)((v[e] - (float)high[e]) * second);
+      // (what v was made of may not be rounded to f16 at once where the first part is stored, and by way of 32 bits where it is taken off:
+      // now and then the two are a unit apart, and the second part is then that much wrong)
+      float x = v[e];
+      asm("" : "+v"(x));
+      high[e] = (f16)x;
+      low[e] = (f16)((x - (float)high[e]) * second);
     }
   }
 };

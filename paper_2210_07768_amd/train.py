@@ -1,7 +1,9 @@
 """The trainer's operators of ``libfbx.so`` (see ``include/fbx_train.h``) on torch tensors: rows of a table pooled per
 record and slot of signs (``embed``), a gated feed-forward block (``gated``), and an AdamW step over many tensors at
-once (``adamw``, and ``AdamW``, which keeps the states).  Beside each forward function stands its gradient; ``embed`` and
-``gated`` also take part in autograd where an input asks for it (backward mode; a tangent is refused).
+once (``adamw``, and ``AdamW``, which keeps the states); for a trunk of several blocks norms (``norm``), what joins a block's
+result to the residual stream (``join``), and updates made orthogonal (``orthogonalise``, ``muon``, and ``Muon``, which
+keeps the momenta).  Beside each forward function stands its gradient; ``embed``, ``gated``, ``norm`` and ``join`` also take
+part in autograd where an input asks for it (backward mode; a tangent is refused).
 
 Argument checks and marshalling only, natively in ``csrc/train/train_native.cpp``: all arithmetic runs in the library's
 kernels, enqueued on torch's current stream of the tensors' device.  Nothing waits for the GPU.  Scratch and results

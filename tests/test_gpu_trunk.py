@@ -439,6 +439,18 @@ def _ortho64_step(x, coefficients=C):
     return a * x + torch.mm(b * gram + c * torch.mm(gram, gram), x)
 
 
+@pytest.mark.parametrize("shape", [(16, 16), (20, 33), (96, 128), (128, 128), (64, 500), (31, 1000), (300, 200)])
+def test_both_parts_are_those_of_one_number(shape):
+    """An element's second part is what its first leaves; where the two were rounded from values a bit apart (one in some thousands, a unit of
+    the first part) two steps are 4e-6 to 2e-5 off.  In the norm every one of eight roundings a step (X, A and B held, and a
+    sum of each; each product's two factors) leaves 2^-22 at most, and two steps twice that: 3.8e-6."""
+    for seed in range(12):
+        u = _decaying(_gen(100 + seed), *shape)
+        want = _ortho64(u, 2)
+        off = float((T.orthogonalise(u, steps=2, exact=True).double() - want).norm() / want.norm())
+        assert off <= 2 * 8 * 2.0 ** -22, (seed, off)
+
+
 @pytest.mark.parametrize("dtype", [F32, F16, BF16])
 def test_orthogonalise(dtype):
     """Five steps.  A step's own error, in the norm, is that of its bound; every later step multiplies it by the polynomial's largest
