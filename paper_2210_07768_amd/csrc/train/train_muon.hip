@@ -239,20 +239,18 @@ struct ProductArgs {
   Leaving last;
 };
 
+typedef f16 f16x4 __attribute__((ext_vector_type(4)));
 struct Halves {
-  f16 high[4], low[4];
+  f16x4 high, low;
   __device__ explicit Halves(f32x4 v, float second = kSecond) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      // (what v was made of may not be rounded to f16 at once where the first part is stored, and by way of 32 bits where it is taken off:
-      // now and then the two are a unit apart, and the second part is then that much wrong)
-      float x = v[e];
-      asm("" : "+v"(x));
-      high[e] = (f16)x;
-      low[e] = (f16)((x - (float)high[e]) * second);
-    }
+    // (what v was made of may not be rounded to f16 at once where the first part is stored, and by way of 32 bits where it is taken off: now
+    // and then the two are a unit apart, and the second part is then that much wrong)
+    asm("" : "+v"(v));
+    high = __builtin_convertvector(v, f16x4);
+    low = __builtin_convertvector((v - __builtin_convertvector(high, f32x4)) * second, f16x4);
   }
 };
+
 // The result's elements of row r of X at four columns from c0 on, and from every 16th further on: as they are, or into the weights.
 template <class P, int kNF>
 __device__ __forceinline__ void leave(const Leaving& p, const Matrix& t, uint32_t r, uint32_t c0, const f32x4 (&v)[kNF]) {
@@ -497,8 +495,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_product(ProductArgs) {
           const Halves w(v);
           const uint64_t to = (uint64_t)r * wide + c;
           if (r < m_side && c < wide) {
-            *(Pack<f16, 4>*)(high + to) = Pack<f16, 4>{{w.high[0], w.high[1], w.high[2], w.high[3]}};
-            if (kExact) *(Pack<f16, 4>*)(low + to) = Pack<f16, 4>{{w.low[0], w.low[1], w.low[2], w.low[3]}};
+            *(f16x4*)(high + to) = w.high;
+            if (kExact) *(f16x4*)(low + to) = w.low;
           }
           if (row0 != col0 && r < wide) {   // (columns are before the diagonal's tile, so within the rows; rows beyond the last are zeros)
 #pragma unroll
@@ -544,8 +542,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_product(ProductArgs) {
           if (r >= m_side || c >= wide) continue;
           const Halves w(v[j]);
           const uint64_t to = (uint64_t)r * wide + c;
-          *(Pack<f16, 4>*)(high + to) = Pack<f16, 4>{{w.high[0], w.high[1], w.high[2], w.high[3]}};
-          *(Pack<f16, 4>*)(low + to) = Pack<f16, 4>{{w.low[0], w.low[1], w.low[2], w.low[3]}};
+          *(f16x4*)(high + to) = w.high;
+          *(f16x4*)(low + to) = w.low;
         }
       });
     } else {
@@ -561,7 +559,10 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_product(ProductArgs) {
 // the others' launches and ways through memory.  Products are of both parts.  X and A (and B in its place) lie in LDS as two
 // parts each, rows 16 bytes longer than they need be so that those a read takes lie in different banks; a wavefront takes 32 x 32 of
 // a product at a time, up to kBlocks of them, and what it worked out replaces an operand when all are done with it.
-// One of 128 x 96, five steps: 38 us, where 17 launches took 98; 128 x 128: 53.  A step is 7 us: three products of which
+// All four products of the parts are added up, the smallest first: second by second too, which costs 3 us, as the second parts are not held
+// larger here and a small matrix's errors average out least (five steps from
+// 64 bits: 16 x 16 7.7e-7 -> 5.5e-7, 128 x 96 1.3e-6 -> 1.1e-6; products in 32 bits: 6.6e-7, 1.2e-6).
+// One of 128 x 96, five steps: 41 us, where 17 launches took 98.  A step is 8 us: three products of which
 // LDS's reads are 3, and as much for splitting and storing what they give, sixteen wavefronts sharing four SIMDs.
 constexpr uint32_t kSmallLanes = 1024, kRoom = 158 * 1024;
 constexpr int kBlocks = 2;
@@ -586,7 +587,8 @@ __global__ __launch_bounds__(kSmallLanes) void k_small(SmallArgs) {
   __shared__ double sums[kSmallLanes / 64];
   const SmallArgs& p = launch_args<SmallArgs>();
   const Matrix& t = p.list.of[blockIdx.x];
-  const uint32_t lane = threadIdx.x % 64u, wave = same(threadIdx.x / 64u), i = lane % 16u, g = lane / 16u;
+  const uint32_t lane = threadIdx.x % 64u, wave = same(threadIdx.x / 64u);
+  uint32_t i = lane % 16u, g = lane / 16u;
   const uint32_t m_side = same(t.m_side), n_side = same(t.n_side), rows = small_side(m_side), columns = small_side(n_side);
   const uint32_t line_x = small_line(columns), line_a = small_line(rows), part_x = rows * line_x, part_a = rows * line_a;
   lds_char *x = (lds_char*)lds, *a = x + 2u * part_x;
@@ -684,11 +686,14 @@ __global__ __launch_bounds__(kSmallLanes) void k_small(SmallArgs) {
       block_r[w][n] = same(block / over * 32u);
       block_c[w][n] = same(block % over * 32u);
     }
+  // Places are worked out anew for every product and every store: kept from step to step they would not all fit the registers.
+  auto anew = [&] { asm volatile("" : "+v"(i), "+v"(g)); };
   // This wavefront's blocks of a product: rows of `left` over `depth`, by rows of `right` (or across them).
   auto multiply = [&](const lds_char* left, uint32_t line_l, uint32_t part_l, const lds_char* right, uint32_t line_r, uint32_t part_r, uint32_t depth, auto is_across) __attribute__((always_inline)) {
     constexpr int w = decltype(is_across)::value;
 #pragma unroll
     for (int n = 0; n < kBlocks; ++n) {
+      anew();
       const uint32_t r0 = block_r[w][n], c0 = block_c[w][n];
       if (r0 >= rows) continue;
 #pragma unroll
@@ -705,11 +710,11 @@ __global__ __launch_bounds__(kSmallLanes) void k_small(SmallArgs) {
           }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int pair = 0; pair < 3; ++pair)
+        for (int pair = 3; pair >= 0; --pair)   // (the smallest first)
 #pragma unroll
           for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int j = 0; j < 2; ++j) sum[n][h][j] = mma(r[j][pair == 1], l[h][pair == 2], sum[n][h][j]);
+            for (int j = 0; j < 2; ++j) sum[n][h][j] = mma(r[j][pair & 1], l[h][pair >> 1], sum[n][h][j]);
       }
     }
   };
@@ -718,6 +723,7 @@ __global__ __launch_bounds__(kSmallLanes) void k_small(SmallArgs) {
     constexpr int w = decltype(which)::value;
 #pragma unroll
     for (int n = 0; n < kBlocks; ++n) {
+      anew();
       if (block_r[w][n] >= rows) continue;
 #pragma unroll
       for (uint32_t h = 0; h < 2u; ++h)
@@ -725,12 +731,11 @@ __global__ __launch_bounds__(kSmallLanes) void k_small(SmallArgs) {
         for (uint32_t j = 0; j < 2u; ++j) f(block_r[w][n] + 16u * h + i, block_c[w][n] + 16u * j + 4u * g, sum[n][h][j]);
     }
   };
-  typedef f16 f16x4 __attribute__((ext_vector_type(4)));
   typedef __attribute__((address_space(3))) f16x4 Four;
   auto put = [&](lds_char* to, uint32_t part, f32x4 v) {
     const Halves w(v, 1.f);
-    *(Four*)to = f16x4{w.high[0], w.high[1], w.high[2], w.high[3]};
-    *(Four*)(to + part) = f16x4{w.low[0], w.low[1], w.low[2], w.low[3]};
+    *(Four*)to = w.high;
+    *(Four*)(to + part) = w.low;
   };
   for (uint32_t s = 0; s < p.steps; ++s) {
     const StepNumbers by = p.of[s];
