@@ -171,7 +171,8 @@ fbx_status fbx_adamw_step(const fbx_adamw* h, const fbx_adamw_tensor* tensors, u
  *   eps     : above 0
  * Limits: 1 <= dim <= FBX_NORM_MOST, records and strides < 2^40.
  *
- * fbx_norm_forward: out = N(x) * weight, rounded to the block's type (weight NULL: 1)
+ * fbx_norm_forward: out = N(x) * weight, rounded to the block's type (weight NULL: 1).  d_out may be d_x, of its type and stride;
+ *   results overlap inputs in no other way.
  * fbx_norm_backward, given dy of the block's type: dx, of the stream's type, and dweight, of the vectors';
  *   either may be NULL.  Scratch is for dweight.
  * Errors: FBX_E_ARG, FBX_E_NOMEM, FBX_E_HIP.
@@ -263,7 +264,7 @@ fbx_status fbx_join_backward(const fbx_join* h, const fbx_join_gradients* g, voi
  *   exact = FBX_EXACT_BY_SIZE: 0 for results in bf16 of matrices of more than 256 rows and columns, else 1.
  *
  *   coefficients : HOST, steps triples
- *   matrices     : HOST, n entries; elements of a row are adjacent; results may not overlap
+ *   matrices     : HOST, n entries; elements of a row are adjacent; results may not overlap, but d_out may be d_u
  * Limits: 1 <= rows, columns <= FBX_ORTHO_MOST; 1 <= steps <= 64; coefficients whose iteration takes a singular value from
  * [0, 1] above 3, or a + b s^2 + c s^4 of one beyond 256, are refused.
  * Errors: FBX_E_ARG, FBX_E_NOMEM, FBX_E_HIP.

@@ -522,7 +522,12 @@ PyObject* norm(PyObject*, PyObject* args) {
   return guarded([&]() -> PyObject* {
     const NormCall c(x, weight, dtype, kind, eps);
     if (asks({&c.x, c.weight}, out_o != Py_None)) Py_RETURN_NOTIMPLEMENTED;
-    if (out_o != Py_None) rows_of(result(out_o), "out", c.a.block, c.x, c.a.records, c.a.dim);
+    if (out_o != Py_None) {
+      const at::Tensor& o = result(out_o);
+      const uint64_t ld = rows_of(o, "out", c.a.block, c.x, c.a.records, c.a.dim);
+      if (c.a.block != c.a.stream || (ld != c.a.ld_x && c.a.records > 1)) apart(o, {&c.x});   // (rows in the place of others that may still have to be read)
+      apart(o, {c.weight});
+    }
     const c10::DeviceGuard guard(c.x.device());
     at::Tensor out = out_o == Py_None ? at::empty({c.x.size(0), c.x.size(1)}, c.x.options().dtype(type_of(c.a.block)).memory_format(c10::nullopt)) : tensor(out_o, "out");
     check(g.norm_forward(&c.a, out.data_ptr(), matrix(out, "out"), stream_of(c.x)));
@@ -614,7 +619,7 @@ PyObject* join(PyObject*, PyObject* args) {
       if (out_o[i] != Py_None) {
         const at::Tensor& o = result(out_o[i]);
         rows_of(o, i ? "out_next" : "out", types[i], c.x, c.a.records, c.a.dim);
-        apart(o, {&c.x, &c.y, c.gate, i && out_o[0] != Py_None ? &tensor(out_o[0], "out") : nullptr});
+        apart(o, {&c.x, &c.y, c.gate, c.weight, c.scale, c.next_weight, i && out_o[0] != Py_None ? &tensor(out_o[0], "out") : nullptr});
       }
     const c10::DeviceGuard guard(c.x.device());
     for (int i = 0; i < 1 + then; ++i)
@@ -804,6 +809,8 @@ PyObject* muon(PyObject*, PyObject* args) {
     }
     std::sort(seen.begin(), seen.end());
     if (std::adjacent_find(seen.begin(), seen.end()) != seen.end()) bad("a matrix, momentum or copy is given twice");
+    for (Py_ssize_t i = 0; i < n; ++i)
+      if (grad[i].numel() && std::binary_search(seen.begin(), seen.end(), grad[i].data_ptr())) bad("a gradient is a matrix, momentum or copy that is written");
     on_gpu(p[0]);
     uint64_t need = 0;
     check(g.muon_scratch(&h, all.data(), static_cast<uint32_t>(all.size()), &need));

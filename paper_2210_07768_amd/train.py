@@ -8,6 +8,10 @@ part in autograd where an input asks for it (backward mode; a tangent is refused
 Argument checks and marshalling only, natively in ``csrc/train/train_native.cpp``: all arithmetic runs in the library's
 kernels, enqueued on torch's current stream of the tensors' device.  Nothing waits for the GPU.  Scratch and results
 come from torch's allocator.  What is refused raises ``FbxError``.
+
+All of it can be captured into a graph.  A backward pass is captured through the gradient functions, or through autograd where no
+eager graph of the same leaves is alive: torch accumulates a leaf's gradient on the stream of the first graph that holds the leaf, which
+a capture does not allow.
 """
 from __future__ import annotations
 
@@ -194,7 +198,7 @@ def _code(given, of: dict, name: str) -> int:
 def norm(x, weight=None, kind: str = "rms", eps: float = 1e-6, dtype=None, out=None):
     """Rows of x brought to unit size, times weight: x / sqrt(mean(x^2) + eps) (kind "rms"), or the same of x less its mean
     ("layer").  x: records x dim; weight: dim elements, of the result's type or float32; dtype: of the result: x's, or, where x is
-    float32, float16 or bfloat16.  out may be x."""
+    float32, float16 or bfloat16.  out may be x itself; it may not overlap an input in another way."""
     got = (_native or _load()).norm(x, weight, dtype, KINDS[kind] if kind in _KINDS else _code(kind, KINDS, "kind"), eps, out)
     return _Norm.apply(x, weight, kind, eps, dtype) if got is NotImplemented else got   # (where an input asks for its gradient)
 
@@ -215,7 +219,7 @@ def join(x, y, weight=None, gate=None, scale=1.0, next_weight=None, *, post: boo
     x, y: records x dim; x: of y's type or float32, and so is the stream returned; what is normed is of y's.
     weight, next_weight, scale: dim elements, all of y's type or all float32; scale may be a number.
     gate: records x dim, or records x 1, of y's type; gate_act: "sigmoid", or "none" where it is to be taken as it is.
-    post: false leaves out y's norm (and has no weight): x + scale * act(gate) * y.  out and out_next may not be inputs."""
+    post: false leaves out y's norm (and has no weight): x + scale * act(gate) * y.  out and out_next may not overlap inputs."""
     if then is None:
         then = next_weight is not None
     got = (_native or _load()).join(x, y, weight, gate, scale, next_weight, post, then, GATES[gate_act] if gate_act in _GATES else _code(gate_act, GATES, "gate_act"),

@@ -744,6 +744,68 @@ def test_training_steps_on_another_stream_and_in_a_graph():
         assert all(torch.equal(a, b) for a, b in zip(captured, eager))
 
 
+def test_autograd_in_a_graph():
+    """Forward and backward through autograd, captured where no eager graph of the leaves is alive, and replayed among eager work on new inputs."""
+    g = _gen(45)
+    shapes, vectors = [(70, 411), (70, 411), (70, 1)], [(411,)] * 3
+    leaves = [_r(g, *shape, dtype=BF16).requires_grad_() for shape in shapes] + [_r(g, *shape, shift=1.0).requires_grad_() for shape in vectors]
+    ends = [_r(g, 70, 411, dtype=BF16) for _ in range(2)]
+
+    def work():
+        x, y, gate, *w = leaves
+        out, nxt = T.join(x, T.norm(y, w[0], kind="layer"), w[1], gate, 0.5, w[2])
+        return [out.detach(), nxt.detach(), *torch.autograd.grad([out, nxt], leaves, ends)]
+
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        work()
+    torch.cuda.current_stream().wait_stream(s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = work()
+    for i in range(4):
+        with torch.no_grad():
+            for t in leaves + ends:
+                t.mul_(1.0 + 0.25 * i)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in captured]
+        assert all(torch.equal(a, b) for a, b in zip(got, work()))
+
+
+def test_results_over_other_inputs_are_refused():
+    """What lies over an input in a way that a row may be written before it is read, or a matrix that is both read and written, is refused."""
+    g = _gen(46)
+    both = _r(g, 8, 60)
+    x, w = both[:4, :24], _r(g, 1, 24)
+    shorter = torch.as_strided(both, (4, 24), (30, 1))
+    p = [_r(g, 8, 9) for _ in range(3)]
+    for call in (lambda: T.norm(x, out=shorter), lambda: T.norm(x.contiguous(), w[0], out=x.contiguous()[:3]), lambda: T.norm(x[:1], w[0], out=w), lambda: T.join(x[:1], x[:1], w[0], out=w),
+                 lambda: T.join(x[:1], x[:1], None, None, w[0], out=w), lambda: T.join(x[:1], x[:1], None, None, 0.5, w[0], out_next=w), lambda: T.norm(x, out=x.view(BF16)[:, :24], dtype=BF16),
+                 lambda: T.muon([p[0]], [p[0]], [p[1]]), lambda: T.muon([p[0]], [p[1]], [p[1]]), lambda: T.muon([p[0], p[1]], [p[2], p[0]], [torch.zeros(8, 9, device="cuda") for _ in range(2)])):
+        before = [t.clone() for t in (both, w, *p)]
+        with pytest.raises(B.FbxError) as e:
+            call()
+        assert e.value.status == B.E_ARG and all(torch.equal(a, b) for a, b in zip(before, (both, w, *p)))
+    assert T.norm(x[:1], w[0], out=torch.as_strided(both, (1, 24), (30, 1))) is not None   # (one row: its stride says nothing)
+
+
+def test_orthogonalise_many_steps():
+    """As many steps as there may be, of coefficients that take every singular value to 1: what is left is off by the last steps'
+    roundings and by what the first ones left in the directions of the smallest singular value (a 2^-21 of each product, 2 sqrt(rows) of
+    them in a norm, over that value, which the steps make 1.875 times larger each: less than 3 times the first)."""
+    g = _gen(47)
+    for rows, columns in ((48, 80), (200, 320)):
+        u = _r(g, rows, columns)
+        d = u.double().cpu()
+        left, s, right = torch.linalg.svd(d, full_matrices=False)
+        want = (left @ right).cuda()
+        small = float(s[-1] / d.norm())
+        got = T.orthogonalise(u, steps=64, coefficients=(1.875, -1.25, 0.375))
+        assert float((got.double() - want).norm()) <= 3 * 8 * 2.0 ** -21 * 2 * rows ** 0.5 / small
+
+
 def test_two_threads_at_once():
     """Two calls at a time, on streams of their own: neither's results depend on the other."""
     g = _gen(44)
