@@ -35,6 +35,7 @@ def command() -> list:
         # atomics whose one lane asks for a work item stay plain: rewritten as a wavefront-wide
         # reduction they would wait for the answer at once instead of where it is used
         "-mllvm", "-amdgpu-atomic-optimizer-strategy=None",
+        "-parallel-jobs=8",   # sources at once: 2.6 minutes in place of 4.5
         "-x", "hip",
     ] + (["-DFBX_TILE_PROF"] if os.environ.get("FBX_TILE_PROF") else []) + [
         "-I", os.path.join(_ROOT, "include"), "-I", CSRC,
