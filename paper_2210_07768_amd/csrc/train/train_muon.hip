@@ -1021,8 +1021,9 @@ fbx_status check_scratch(const void* d_scratch, uint64_t bytes, uint64_t need) {
   if (need && (!d_scratch || (uintptr_t)d_scratch % 256u)) return refuse(FBX_E_ARG, "d_scratch is NULL or not 256-byte aligned");
   return bytes < need ? refuse(FBX_E_NOMEM, "scratch too small: the scratch function gives its size") : FBX_OK;
 }
+// What batches go by, for a call and for the size of its scratch alike: the matrices' sides, and the kind of their products.
 template <class M>
-fbx_status sides(const M* matrices, uint32_t n, std::vector<Matrix>* all) {
+fbx_status sides(const M* matrices, uint32_t n, uint32_t exact, fbx_dtype out, std::vector<Matrix>* all) {
   if (!matrices && n) return refuse(FBX_E_ARG, "matrices is NULL");
   for (uint32_t i = 0; i < n; ++i) {
     const fbx_status st = check_sides(matrices[i].rows, matrices[i].columns);
@@ -1030,6 +1031,7 @@ fbx_status sides(const M* matrices, uint32_t n, std::vector<Matrix>* all) {
     Matrix t{};
     t.rows = matrices[i].rows;
     t.columns = matrices[i].columns;
+    t.exact = is_exact(t, exact, out);
     all->push_back(t);
   }
   return FBX_OK;
@@ -1054,7 +1056,7 @@ extern "C" fbx_status fbx_ortho_scratch(const fbx_ortho* h, const fbx_ortho_matr
   return guarded([&] {
     if (!h || !bytes) return refuse(FBX_E_ARG, "h or bytes is NULL");
     std::vector<Matrix> all;
-    const fbx_status st = sides(matrices, n, &all);
+    const fbx_status st = sides(matrices, n, h->exact, h->out, &all);
     if (st == FBX_OK) *bytes = scratch_of(all);
     return st;
   });
@@ -1067,7 +1069,7 @@ extern "C" fbx_status fbx_orthogonalise(const fbx_ortho* h, const fbx_ortho_matr
     std::vector<Step> steps;
     if (!known(h->in) || !known(h->out)) return refuse(FBX_E_ARG, "unknown dtype");
     fbx_status st = check(h, &steps);
-    if (st == FBX_OK) st = sides(matrices, n, &w.all);
+    if (st == FBX_OK) st = sides(matrices, n, h->exact, h->out, &w.all);
     if (st != FBX_OK) return st;
     for (uint32_t i = 0; i < n; ++i) {
       const fbx_ortho_matrix& m = matrices[i];
@@ -1080,7 +1082,6 @@ extern "C" fbx_status fbx_orthogonalise(const fbx_ortho* h, const fbx_ortho_matr
       t.out = m.d_out;
       t.ld_out = m.ld_out;
       t.step = 1.f;
-      t.exact = is_exact(t, h->exact, h->out);
     }
     st = check_scratch(d_scratch, scratch_bytes, scratch_of(w.all));
     if (st != FBX_OK || !n) return st;
@@ -1096,7 +1097,7 @@ extern "C" fbx_status fbx_muon_scratch(const fbx_muon* h, const fbx_muon_matrix*
   return guarded([&] {
     if (!h || !bytes) return refuse(FBX_E_ARG, "h or bytes is NULL");
     std::vector<Matrix> all;
-    const fbx_status st = sides(matrices, n, &all);
+    const fbx_status st = sides(matrices, n, h->ortho.exact, h->param_dtype, &all);
     if (st == FBX_OK) *bytes = scratch_of(all);
     return st;
   });
@@ -1111,7 +1112,7 @@ extern "C" fbx_status fbx_muon_step(const fbx_muon* h, const fbx_muon_matrix* ma
     if (!(h->momentum >= 0 && h->momentum < 1)) return refuse(FBX_E_ARG, "momentum must be in [0, 1)");
     if (!isfinite((float)h->lr) || !isfinite((float)h->weight_decay) || !isfinite((float)h->grad_scale)) return refuse(FBX_E_ARG, "lr, weight_decay and grad_scale must be finite");
     fbx_status st = check(&h->ortho, &steps);
-    if (st == FBX_OK) st = sides(matrices, n, &w.all);
+    if (st == FBX_OK) st = sides(matrices, n, h->ortho.exact, h->param_dtype, &w.all);
     if (st != FBX_OK) return st;
     bool copy = false;
     for (uint32_t i = 0; i < n; ++i) copy |= matrices[i].d_copy != nullptr;
@@ -1130,7 +1131,6 @@ extern "C" fbx_status fbx_muon_step(const fbx_muon* h, const fbx_muon_matrix* ma
       t.copy = m.d_copy;
       t.ld_u = t.ld_out = m.columns;
       t.step = (float)(h->lr * m.factor);
-      t.exact = is_exact(t, h->ortho.exact, h->param_dtype);
     }
     st = check_scratch(d_scratch, scratch_bytes, scratch_of(w.all));
     if (st != FBX_OK || !n) return st;

@@ -1,0 +1,70 @@
+"""Orthogonalised matrices, Muon, norms and joins where a call's edges lie: lists of several kinds, every tile of the products, what overlaps.
+
+Tolerances are what the header promises: products of both parts are off like products in 32 bits (held to twice what the same formula in torch's
+32 bits is off), products of first parts by 1.6e-3 of the result's size; what is stored adds half a unit of its type."""
+import math
+
+import pytest
+import torch
+
+from paper_2210_07768_amd import binding as B
+from paper_2210_07768_amd import train as T
+
+pytestmark = pytest.mark.gpu
+F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
+HALF_UNIT = {F32: 2.0 ** -24, F16: 2.0 ** -11, BF16: 2.0 ** -8}
+
+
+def _gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def _r(g, *shape, dtype=F32, size=1.0, shift=0.0):
+    return (torch.randn(*shape, device="cuda", generator=g) * size + shift).to(dtype)
+
+
+def _decaying(g, rows, columns, dtype=F32):
+    n = min(rows, columns)
+    s = torch.arange(1, n + 1, device="cuda").float().pow(-0.7)
+    return ((_r(g, rows, n) * s) @ _r(g, n, columns) + 0.1 * _r(g, rows, columns)).to(dtype)
+
+
+def _iterated(u, dtype, steps=5, eps=1e-7):
+    """The formula in `dtype`, the norm in 64 bits."""
+    tall = u.shape[0] > u.shape[1]
+    x = u.double().t().contiguous() if tall else u.double()
+    x = (x / (x.norm() + eps)).to(dtype)
+    a, b, c = T.NEWTON_SCHULZ
+    for _ in range(steps):
+        gram = torch.mm(x, x.t().contiguous())
+        x = a * x + torch.mm(b * gram + c * torch.mm(gram, gram), x)
+    return x.t() if tall else x
+
+
+def _goal(u, exact, dtype, steps=5):
+    """(the result in 64 bits, how far in the norm a result stored in `dtype` may be from it)"""
+    want = _iterated(u, torch.float64, steps)
+    off = 2 * float((_iterated(u, F32, steps).double() - want).norm()) if exact else 1.6e-3 * float(want.norm())
+    return want, off + HALF_UNIT[dtype] * (float(want.norm()) + off)
+
+
+def _near(got, want, off, what):
+    far = float((got.double() - want).norm())
+    assert torch.isfinite(got).all() and far <= off, f"{what}: {far:.3g} off, {off:.3g} allowed"
+
+
+# ------------------------------------------------------------------ lists
+def test_lists_of_several_kinds():
+    """More matrices of either kind of products than a launch holds, and of those that a workgroup holds, in turn."""
+    g = _gen(60)
+    shapes = [(64, 700), (257, 260), (20, 30), (270, 257)] * 33
+    given = [_decaying(g, r, c, BF16) for r, c in shapes]
+    got = T.orthogonalise(given)
+    start = [torch.zeros(s, device="cuda", dtype=BF16) for s in shapes]
+    p, m = [t.clone() for t in start], [torch.zeros(s, device="cuda") for s in shapes]
+    T.muon(p, given, m, lr=1.0, momentum=0.5, nesterov=False, weight_decay=0.0, adjust="none")   # (0 - O(gradient))
+    for u, o, w, x in zip(given, got, p, m):
+        want, off = _goal(u, min(u.shape) <= 256, BF16)
+        _near(o, want, off, tuple(u.shape))
+        _near(-w, want, off, f"weights {tuple(u.shape)}")
+        assert torch.equal(x, u.float())

@@ -240,3 +240,24 @@ def test_muon_loads_only_states_of_its_weights():
         with pytest.raises(B.FbxError):
             b.load_state_dict({"step": 9, "m": wrong})
         assert b.step_count == 7 and all(torch.equal(x, y) for x, y in zip(a.m, b.m))
+
+
+BF16 = 2
+LISTS = [[(256, 1024), (257, 257)] * 32, [(256, 1024), (1024, 1024)] * 32, [(256, 4096), (512, 512)] * 24, [(128, 2048), (512, 2048), (512, 512)] * 16, [(300, 200), (1024, 1024), (20, 30)] * 40,
+         [(1200, 65536), (256, 65536), (256, 65536), (1100, 65536), (256, 65536)]]
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="what is not refused would be launched, on addresses that are none")
+@pytest.mark.parametrize("exact", [0, 1, 2])
+@pytest.mark.parametrize("shapes", LISTS, ids=lambda s: f"{len(s)}x{s[0]}")
+def test_scratch_of_lists_of_several_kinds(shapes, exact):
+    """What the scratch functions give is enough for lists whose matrices go through products of both kinds, and no byte less is."""
+    L, need, n = _library(), u64(), len(shapes)
+    lists = ((OrthoMatrix * n)(*[_made(OrthoMatrix, MATRIX, dict(rows=r, columns=c, ld_u=c, ld_out=c)) for r, c in shapes]),
+             (MuonMatrix * n)(*[_made(MuonMatrix, MUON_MATRIX, dict(rows=r, columns=c)) for r, c in shapes]))
+    h = _ortho(exact=exact, out=BF16)
+    muon = Muon(ortho=h, param_dtype=BF16, grad_dtype=BF16, copy_dtype=BF16, nesterov=1, lr=1e-3, momentum=0.95, grad_scale=1.0)
+    for a, m, size, call in ((h, lists[0], L.fbx_ortho_scratch, L.fbx_orthogonalise), (muon, lists[1], L.fbx_muon_scratch, L.fbx_muon_step)):
+        assert size(a, m, n, ctypes.byref(need)) == B.OK and need.value > 0
+        assert call(a, m, n, P, need.value - 1, None) == B.E_NOMEM
+        assert call(a, m, n, P, need.value, None) == B.E_HIP   # (there is no GPU to launch it on)
