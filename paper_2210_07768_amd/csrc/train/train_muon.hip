@@ -873,10 +873,10 @@ void multiply(ProductArgs& p, hipStream_t stream) {
   else launch(std::false_type());
 }
 
-// Left to this, products are of both parts where results keep more than bf16 does, and for small matrices: their products take little
-// beside their launches, and their roundings average out less.  Error against 64 bits of results in bf16 (whose own rounding is
-// 1.66e-3), products of first parts: normally distributed 300 x 400 2.27e-3, 2,624 x 4,096 1.98e-3; a decaying spectrum 257 x 300 2.01e-3, 2,624 x
-// 4,096 1.76e-3, and with A and B rounded once more 48 x 16 2.8e-3.
+// Left to this (for weights; a result that is handed out is of both parts unless the caller says otherwise), products are of both parts where
+// weights keep more than bf16 does, and for small matrices: their products take little beside their launches.  Weights in bf16 end up
+// as near 64 bits either way (2,624 x 4,096: 1.66e-3, their own rounding), in 2.05 and 5.25 ms for three.  A result in bf16 would not: products of first
+// parts leave it off by 1.76e-3 in place of 1.66e-3 (a decaying spectrum, 2,624 x 4,096), 2.27e-3 (normally distributed, 300 x 400), 9e-3 (a unit matrix of 319).
 constexpr uint32_t kSmall = 256;
 uint32_t is_exact(const Matrix& t, uint32_t asked, fbx_dtype out) {
   return asked != FBX_EXACT_BY_SIZE ? asked : out != FBX_BF16 || (t.rows < t.columns ? t.rows : t.columns) <= kSmall;

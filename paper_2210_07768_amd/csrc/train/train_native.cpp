@@ -716,7 +716,7 @@ PyObject* orthogonalise(PyObject*, PyObject* args) {
     const at::Tensor& like = in[0];
     h.in = code(like);
     h.out = code_of(dtype, h.in);
-    h.exact = exact < 0 ? FBX_EXACT_BY_SIZE : exact;   // (below 0: nothing was asked for)
+    h.exact = exact;
     std::vector<fbx_ortho_matrix> list;
     std::vector<at::Tensor> out(n);
     std::vector<const void*> seen;
@@ -781,7 +781,7 @@ PyObject* muon(PyObject*, PyObject* args) {
     h.grad_dtype = code(grad[0]);
     h.copy_dtype = copy.seq ? code(copy[0]) : FBX_F32;
     h.nesterov = nesterov;
-    h.ortho.exact = exact < 0 ? FBX_EXACT_BY_SIZE : exact;
+    h.ortho.exact = exact < 0 ? FBX_EXACT_BY_SIZE : exact;   // (below 0: nothing was asked for)
     const at::Device where = p[0].device();
     std::vector<const void*> seen;
     auto same = [&](const at::Tensor& t, bool written) {

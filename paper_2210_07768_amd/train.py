@@ -305,14 +305,13 @@ def orthogonalise(x, steps: int = 5, coefficients=NEWTON_SCHULZ, eps: float = 1e
     """A matrix, or each of a list of them, with its singular values brought near 1 by Newton-Schulz products (the formulas:
     fbx_orthogonalise in ``include/fbx_train.h``).  All matrices of a list go through the same launches.
 
-    coefficients: three numbers, or three for each step.  dtype: of the results (the matrices').  exact: products of 32-bit accuracy, of three
-    times the work; by default for all but results in bfloat16 of matrices of more than 256 rows and columns, whose products are then in
-    half precision, with an error of about that of the results' rounding.  out: a tensor, or a list of them (a matrix's own result
-    may be written over it).  Without derivative."""
+    coefficients: three numbers, or three for each step.  dtype: of the results (the matrices').  exact: products of 32-bit accuracy, which is
+    the default; False: products in half precision, a third of the work, off by about what rounding to bfloat16 leaves, or several times that
+    (``exact`` there).  out: a tensor, or a list of them (a matrix's own result may be written over it).  Without derivative."""
     one = isinstance(x, torch.Tensor)
     if out is not None and one != isinstance(out, torch.Tensor):
         _bad("out must be a tensor for a tensor, and a list for a list")
-    got = _load().orthogonalise([x] if one else x, None if out is None else [out] if one else out, dtype, -1 if exact is None else int(bool(exact)), _steps(steps, coefficients), eps)
+    got = _load().orthogonalise([x] if one else x, None if out is None else [out] if one else out, dtype, 1 if exact is None else int(bool(exact)), _steps(steps, coefficients), eps)
     return got[0] if one else got
 
 
@@ -337,7 +336,8 @@ def muon(params: Sequence, grads: Sequence, momenta: Sequence, copies: Optional[
 
     momenta: float32, of the weights' sizes; copies: float16 or bfloat16 tensors that receive float32 weights too.  All weights are of one type, and
     so are all gradients.  adjust: what the update is multiplied by, "rms" 0.2 sqrt(max(rows, columns)), "spectral" sqrt(max(1, rows / columns)),
-    "none" 1.  exact: see ``orthogonalise`` (the weights' type decides)."""
+    "none" 1.  exact: see ``orthogonalise``; by default for all but bfloat16 weights of more than 256 rows and columns, whose rounding hides what half
+    precision leaves."""
     params = list(params)
     _load().muon(params, grads, momenta, copies, _factors(adjust, params), lr, momentum, nesterov, weight_decay, grad_scale, -1 if exact is None else int(bool(exact)),
                  _steps(steps, coefficients), eps, False)

@@ -68,3 +68,45 @@ def test_lists_of_several_kinds():
         _near(o, want, off, tuple(u.shape))
         _near(-w, want, off, f"weights {tuple(u.shape)}")
         assert torch.equal(x, u.float())
+
+
+# ------------------------------------------------------------------ products of both parts, and of first parts
+def _made(kind, rows, columns):
+    g = _gen(rows + columns)
+    if kind == "decaying":
+        return _decaying(g, rows, columns)
+    if kind == "normal":
+        return _r(g, rows, columns)
+    if kind == "one direction":
+        return _r(g, rows, 1) @ _r(g, 1, columns) + 1e-3 * _r(g, rows, columns)
+    if kind == "most rows zero":
+        return _r(g, rows, columns) * (torch.arange(rows, device="cuda") % 5 == 0)[:, None]
+    u = torch.zeros(rows, columns, device="cuda")   # "unit 319": 319 equal singular values
+    u.diagonal()[:int(kind.split()[1])] = 1.0
+    return u
+
+
+@pytest.mark.parametrize("kind, rows, columns", [("decaying", 1000, 400), ("normal", 300, 400), ("one direction", 400, 1000), ("most rows zero", 257, 257), ("unit 319", 319, 319), ("unit 3", 300, 600),
+                                                 ("unit 2", 700, 260)])
+def test_results_are_rounded_once_unless_asked(kind, rows, columns):
+    """Left to itself `orthogonalise` gives 32-bit accuracy, rounded to the result's type; half precision is the caller's to ask for.  (Products of first
+    parts of unit matrices are off by more than bfloat16's half unit, 2^-8: their roundings are all the same.)"""
+    u = _made(kind, rows, columns)
+    want, off = _goal(u, True, F32)
+    floor = 2.0 ** -21 * float(want.norm())   # (where 32 bits make no mistake at all: two parts have 22 bits)
+    single = T.orthogonalise(u)
+    _near(single, want, off + 15 * floor, kind)   # (three products a step)
+    assert not torch.equal(single, T.orthogonalise(u, exact=False))
+    for dtype in (F16, BF16):
+        got = T.orthogonalise(u, dtype=dtype)
+        assert torch.equal(got, single.to(dtype))
+        assert torch.equal(got, T.orthogonalise(u, dtype=dtype, exact=True))
+
+
+@pytest.mark.parametrize("kind, rows, columns, most", [("decaying", 1000, 400, 1.6e-3), ("normal", 300, 400, 1.6e-3), ("one direction", 400, 1000, 2.8e-3), ("most rows zero", 257, 257, 2.8e-3),
+                                                       ("unit 319", 319, 319, 27e-3), ("unit 2", 700, 260, 27e-3)])
+def test_products_of_first_parts(kind, rows, columns, most):
+    """As far off as the header says, before the result is rounded."""
+    u = _made(kind, rows, columns)
+    want = _iterated(u, torch.float64)
+    _near(T.orthogonalise(u, exact=False), want, most * float(want.norm()), kind)
