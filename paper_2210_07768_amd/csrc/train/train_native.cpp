@@ -460,11 +460,39 @@ uint64_t rows_of(const at::Tensor& t, const char* name, fbx_dtype type, const at
   if (code(t) != type) bad(std::string(name) + " must be of type " + c10::toString(type_of(type)));
   return matrix(t, name, nullptr, n, columns);
 }
-// A result may not be one of the inputs: another wavefront may still have to read it.
+// The bytes of a matrix's rows (or of a vector): n times `wide`, `apart` from one to the next.
+struct Bytes {
+  uintptr_t at;
+  int64_t n, wide, apart;
+  explicit Bytes(const at::Tensor& t) : at(reinterpret_cast<uintptr_t>(t.data_ptr())), n(t.dim() == 2 ? t.size(0) : 1), wide(t.size(-1) * t.itemsize()), apart(n > 1 ? t.stride(0) * t.itemsize() : wide) {
+    if (!t.numel()) n = 0;
+  }
+  uintptr_t end() const { return at + (n - 1) * apart + wide; }
+};
+// Whether two matrices have a byte in common: columns cut out of one buffer have none, though they lie in each other's range.
+bool meet(const Bytes& a, const Bytes& b) {
+  if (!a.n || !b.n || a.at >= b.end() || b.at >= a.end()) return false;
+  if (a.n > b.n) return meet(b, a);
+  // the first row of b that ends behind where a's row begins
+  auto row_meets = [&](uintptr_t from) {
+    const int64_t before = static_cast<int64_t>(from - b.at) - b.wide, k = before < 0 ? 0 : before / b.apart + 1;
+    return k < b.n && b.at + k * b.apart < from + a.wide;
+  };
+  // (rows of one distance lie to each other as their first ones do: one row of a that is in b's range, and the one before and behind it, stand for all)
+  int64_t first = 0, last = a.n - 1;
+  if (a.apart == b.apart && a.n > 3) {
+    if (b.at > a.at) first = static_cast<int64_t>(b.at - a.at) / a.apart;
+    if (first + 2 < last) last = first + 2;
+  }
+  for (int64_t i = first; i <= last; ++i)
+    if (row_meets(a.at + i * a.apart)) return true;
+  return false;
+}
+// A result may not overlap an input: another wavefront may still have to read it.
 void apart(const at::Tensor& out, std::initializer_list<const at::Tensor*> inputs) {
-  if (!out.numel()) return;
+  const Bytes o(out);
   for (const at::Tensor* t : inputs)
-    if (t && t->data_ptr() == out.data_ptr()) bad("a tensor given for a result is one of the inputs");
+    if (t && meet(o, Bytes(*t))) bad("a tensor given for a result overlaps an input, or another result");
 }
 // A gradient as autograd gives it may be one element seen many times.
 at::Tensor gradient_rows(const at::Tensor& t) {
@@ -509,7 +537,7 @@ struct NormCall {
     Vectors v{x, x.size(1)};
     a.d_weight = v(weight, "weight");
     a.vectors = v.type;
-    a.d_x = on_gpu(x);
+    a.d_x = x.data_ptr();
   }
 };
 
@@ -525,9 +553,10 @@ PyObject* norm(PyObject*, PyObject* args) {
     if (out_o != Py_None) {
       const at::Tensor& o = result(out_o);
       const uint64_t ld = rows_of(o, "out", c.a.block, c.x, c.a.records, c.a.dim);
-      if (c.a.block != c.a.stream || (ld != c.a.ld_x && c.a.records > 1)) apart(o, {&c.x});   // (rows in the place of others that may still have to be read)
-      apart(o, {c.weight});
+      const bool own = o.data_ptr() == c.x.data_ptr() && c.a.block == c.a.stream && (ld == c.a.ld_x || c.a.records <= 1);   // (each row in its own place)
+      apart(o, {own ? nullptr : &c.x, c.weight});
     }
+    on_gpu(c.x);
     const c10::DeviceGuard guard(c.x.device());
     at::Tensor out = out_o == Py_None ? at::empty({c.x.size(0), c.x.size(1)}, c.x.options().dtype(type_of(c.a.block)).memory_format(c10::nullopt)) : tensor(out_o, "out");
     check(g.norm_forward(&c.a, out.data_ptr(), matrix(out, "out"), stream_of(c.x)));
@@ -544,6 +573,7 @@ PyObject* norm_backward(PyObject*, PyObject* args) {
   if (!PyArg_ParseTuple(args, "OOOidpp", &dy_o, &x, &weight, &kind, &eps, &need_dx, &need_dw)) return nullptr;
   return guarded([&]() -> PyObject* {
     NormCall c(x, weight, Py_None, kind, eps);
+    on_gpu(c.x);
     const at::Tensor dy = gradient_rows(input(dy_o, "dy"));
     c.a.block = code(dy);
     const uint64_t ld_dy = rows_of(dy, "dy", c.a.block, c.x, c.a.records, c.a.dim);
@@ -599,7 +629,7 @@ struct JoinCall {
     a.d_next_weight = v(next_weight, "next_weight");
     a.vectors = v.type;
     a.d_y = y.data_ptr();
-    a.d_x = on_gpu(x);
+    a.d_x = x.data_ptr();
   }
 };
 
@@ -621,6 +651,7 @@ PyObject* join(PyObject*, PyObject* args) {
         rows_of(o, i ? "out_next" : "out", types[i], c.x, c.a.records, c.a.dim);
         apart(o, {&c.x, &c.y, c.gate, c.weight, c.scale, c.next_weight, i && out_o[0] != Py_None ? &tensor(out_o[0], "out") : nullptr});
       }
+    on_gpu(c.x);
     const c10::DeviceGuard guard(c.x.device());
     for (int i = 0; i < 1 + then; ++i)
       out[i] = out_o[i] == Py_None ? at::empty({c.x.size(0), c.x.size(1)}, c.x.options().dtype(type_of(types[i])).memory_format(c10::nullopt)) : tensor(out_o[i], "out");
@@ -645,6 +676,7 @@ PyObject* join_backward(PyObject*, PyObject* args) {
   if (!PyArg_ParseTuple(args, "OOOOOOOOpiidI", &given[0], &given[1], &what[0], &what[1], &what[2], &what[3], &what[4], &what[5], &post, &gate_act, &kind, &eps, &need)) return nullptr;
   return guarded([&]() -> PyObject* {
     const JoinCall c(what, post, gate_act, kind, eps);
+    on_gpu(c.x);
     if (given[0] == Py_None && given[1] == Py_None) bad("dout or dnext is needed");
     fbx_join_gradients d{};
     at::Tensor in[2];
@@ -719,25 +751,21 @@ PyObject* orthogonalise(PyObject*, PyObject* args) {
     h.exact = exact;
     std::vector<fbx_ortho_matrix> list;
     std::vector<at::Tensor> out(n);
-    std::vector<const void*> seen;
     for (Py_ssize_t i = 0; i < n; ++i) {
       const at::Tensor& t = in[i];
       if (t._fw_grad(0).defined() || (t.requires_grad() && c10::GradMode::is_enabled())) bad("orthogonalise has no derivative");
       sides_fit(t, "a matrix");
       if (t.scalar_type() != like.scalar_type() || t.device() != like.device()) bad("matrices must be of one type and on one device");
       matrix(t, "a matrix");
-      on_gpu(t);
       if (given.seq) {
         out[i] = result(PySequence_Fast_GET_ITEM(given.seq, i));
         rows_of(out[i], "out", h.out, like, t.size(0), t.size(1));
-        if (out[i].numel()) seen.push_back(out[i].data_ptr());
       }
     }
     for (Py_ssize_t i = 0; given.seq && i < n; ++i)   // (its own matrix is read before it is written)
       for (Py_ssize_t k = 0; k < n; ++k)
-        if (i != k) apart(out[i], {&in[k]});
-    std::sort(seen.begin(), seen.end());
-    if (std::adjacent_find(seen.begin(), seen.end()) != seen.end()) bad("a result is given twice");
+        if (i != k) apart(out[i], {&in[k], k < i ? &out[k] : nullptr});
+    on_gpu(like);
     const c10::DeviceGuard guard(like.device());
     for (Py_ssize_t i = 0; i < n; ++i) {
       const at::Tensor& t = in[i];
@@ -783,10 +811,14 @@ PyObject* muon(PyObject*, PyObject* args) {
     h.nesterov = nesterov;
     h.ortho.exact = exact < 0 ? FBX_EXACT_BY_SIZE : exact;   // (below 0: nothing was asked for)
     const at::Device where = p[0].device();
-    std::vector<const void*> seen;
-    auto same = [&](const at::Tensor& t, bool written) {
+    std::vector<std::pair<uintptr_t, uintptr_t>> written;   // (first byte, the one behind the last)
+    auto range = [](const at::Tensor& t) {
+      const uintptr_t at = reinterpret_cast<uintptr_t>(t.data_ptr());
+      return std::make_pair(at, at + t.nbytes());
+    };
+    auto same = [&](const at::Tensor& t, bool out) {
       if (t.device() != where || !t.is_contiguous()) bad("all matrices must be contiguous and on one device");
-      if (written && t.numel()) seen.push_back(t.data_ptr());
+      if (out && t.numel()) written.push_back(range(t));
       return t.data_ptr();
     };
     std::vector<fbx_muon_matrix> all;
@@ -807,10 +839,15 @@ PyObject* muon(PyObject*, PyObject* args) {
       t.factor = factor[i];
       if (p[i].numel()) all.push_back(t);
     }
-    std::sort(seen.begin(), seen.end());
-    if (std::adjacent_find(seen.begin(), seen.end()) != seen.end()) bad("a matrix, momentum or copy is given twice");
-    for (Py_ssize_t i = 0; i < n; ++i)
-      if (grad[i].numel() && std::binary_search(seen.begin(), seen.end(), grad[i].data_ptr())) bad("a gradient is a matrix, momentum or copy that is written");
+    std::sort(written.begin(), written.end());
+    for (size_t i = 1; i < written.size(); ++i)
+      if (written[i].first < written[i - 1].second) bad("a matrix, momentum or copy is given twice, or overlaps another");
+    for (Py_ssize_t i = 0; i < n; ++i) {
+      if (!grad[i].numel()) continue;
+      const auto r = range(grad[i]);   // (of what is written, the last that begins before its end ends last)
+      const auto behind = std::lower_bound(written.begin(), written.end(), std::make_pair(r.second, uintptr_t{0}));
+      if (behind != written.begin() && (behind - 1)->second > r.first) bad("a gradient overlaps a matrix, momentum or copy that is written");
+    }
     on_gpu(p[0]);
     uint64_t need = 0;
     check(g.muon_scratch(&h, all.data(), static_cast<uint32_t>(all.size()), &need));

@@ -110,3 +110,40 @@ def test_products_of_first_parts(kind, rows, columns, most):
     u = _made(kind, rows, columns)
     want = _iterated(u, torch.float64)
     _near(T.orthogonalise(u, exact=False), want, most * float(want.norm()), kind)
+
+
+# ------------------------------------------------------------------ results beside and over what they are made of
+def test_results_in_the_same_buffer():
+    """Columns beside an input's are no part of it; a matrix's own result may lie over it anyhow, as all of it is read before."""
+    g = _gen(61)
+    for n, d in ((37, 24), (300, 270)):
+        both = _r(g, n, 3 * d)
+        a, b, c = (both[:, i * d:(i + 1) * d] for i in range(3))
+        w = _r(g, d, shift=1.0)
+        want = T.norm(a.contiguous(), w)
+        assert torch.equal(T.norm(a, w, out=c), want) and torch.equal(c, want)
+        want = T.join(a.contiguous(), b.contiguous(), w)
+        assert torch.equal(T.join(a, b, w, out=c), want) and torch.equal(c, want)
+        want = T.orthogonalise([t.contiguous() for t in (a, b, c)])
+        T.orthogonalise([a, b, c], out=[a, b, c])
+        assert all(torch.equal(t, o) for t, o in zip((a, b, c), want))
+        rows = _r(g, n + 3, d)
+        want = T.orthogonalise(rows[:n].clone())
+        T.orthogonalise(rows[:n], out=rows[3:])
+        assert torch.equal(rows[3:], want)
+
+
+def test_shifted_results_are_refused():
+    g = _gen(62)
+    rows, w = _r(g, 5000, 64), _r(g, 64, shift=1.0)
+    flat = torch.zeros(4 * 48 * 40, device="cuda")
+    p = [flat[i * 1920 - (i == 1):][:1920].view(48, 40) for i in range(2)]
+    grads, m = [_r(g, 48, 40) for _ in range(2)], [torch.zeros(48, 40, device="cuda") for _ in range(2)]
+    before = rows.clone()
+    for call in (lambda: T.norm(rows[:-1], w, out=rows[1:]), lambda: T.norm(rows[1:], w, out=rows[:-1]), lambda: T.join(rows[:100], rows[100:200], w, out=rows[150:250]),
+                 lambda: T.join(rows[:100], rows[100:200], w, next_weight=w, out=rows[300:400], out_next=rows[399:499]), lambda: T.muon(p, grads, m),
+                 lambda: T.orthogonalise([rows[:50], rows[50:100]], out=[rows[40:90], rows[200:250]])):
+        with pytest.raises(B.FbxError) as e:
+            call()
+        assert e.value.status == B.E_ARG and "overlaps" in str(e.value)
+    assert torch.equal(rows, before) and not flat.any() and not any(t.any() for t in m)

@@ -261,3 +261,57 @@ def test_scratch_of_lists_of_several_kinds(shapes, exact):
         assert size(a, m, n, ctypes.byref(need)) == B.OK and need.value > 0
         assert call(a, m, n, P, need.value - 1, None) == B.E_NOMEM
         assert call(a, m, n, P, need.value, None) == B.E_HIP   # (there is no GPU to launch it on)
+
+
+def _refusal(call):
+    with pytest.raises(B.FbxError) as e:
+        call()
+    assert e.value.status == B.E_ARG
+    return str(e.value)
+
+
+def _view(buffer, n, d, stride, at):
+    return torch.as_strided(buffer, (n, d), (stride, 1), at)
+
+
+def test_results_that_overlap_are_refused():
+    """Views of one buffer, at random: a result that has an element in common with an input is refused as that, and one that has none (columns
+    beside it, say) is not.  (Then for lying on the CPU.)"""
+    rng = torch.Generator().manual_seed(3)
+    pick = lambda a, b: int(torch.randint(a, b + 1, (1,), generator=rng))  # noqa: E731
+    buffer, met, missed = torch.zeros(400), 0, 0
+    elements = lambda t: set((torch.arange(t.shape[0])[:, None] * (t.stride(0) if t.shape[0] > 1 else 0) + torch.arange(t.shape[1]) + t.storage_offset()).flatten().tolist())  # noqa: E731
+    apart = torch.zeros(400)
+    for k in range(3000):
+        n, d = pick(1, 9), pick(1, 6)
+        strides = [pick(d, 3 * d + 4)] * 2 if k % 3 else [pick(d, 3 * d + 4), pick(d, 3 * d + 4)]
+        x, out = (_view(buffer, n, d, s, pick(0, 400 - (n - 1) * s - d) if k % 4 else pick(0, min(12, 400 - (n - 1) * s - d))) for s in strides)
+        own = x.storage_offset() == out.storage_offset() and (strides[0] == strides[1] or n == 1)
+        meet = bool(elements(x) & elements(out))
+        y, z = (_view(apart, n, d, d, at) for at in (0, 200))
+        met, missed = met + meet, missed + (not meet)
+        said = "GPU" if not meet else "overlaps"
+        assert ("GPU" if own else said) in _refusal(lambda: T.norm(x, out=out))
+        for call in (lambda: T.join(x, y, out=out), lambda: T.join(y, x, out=out), lambda: T.join(y, z, None, x, then=True, out_next=out), lambda: T.join(y, z, then=True, out=x, out_next=out),
+                     lambda: T.orthogonalise([x, y], out=[z, out]), lambda: T.orthogonalise([y, z], out=[x, out])):
+            assert said in _refusal(call)
+        w = buffer[out.storage_offset():out.storage_offset() + d]
+        if x.shape[0] > 1 and elements(x) & set(range(out.storage_offset(), out.storage_offset() + d)):
+            assert "overlaps" in _refusal(lambda: T.norm(y, w, out=x)) and "overlaps" in _refusal(lambda: T.join(y, z, None, None, w, out=x))
+    assert met > 300 and missed > 300
+    assert "GPU" in _refusal(lambda: T.orthogonalise([x, y], out=[x, y]))   # (each over itself)
+
+
+def test_matrices_that_overlap_are_refused_by_muon():
+    """Weights, momenta and copies that share an element with each other or with a gradient; gradients may share theirs."""
+    b, half, free = torch.zeros(600), torch.zeros(600, dtype=torch.bfloat16), torch.zeros(600)
+    at = lambda t, k, n=4: t[k:k + 5 * n].view(n, 5)  # noqa: E731
+    p, g, m, c = [at(b, 0), at(b, 20)], [at(free, 0), at(free, 7)], [at(b, 40), at(b, 60)], [at(half, 0), at(half, 20)]
+    muon = lambda **k: _refusal(lambda: T.muon(**{**dict(params=p, grads=g, momenta=m, copies=c), **k}))  # noqa: E731
+    assert "GPU" in muon()
+    for change, why in ((dict(params=[p[0], at(b, 19)]), "another"), (dict(params=[p[0], at(b, 21)]), "another"), (dict(momenta=[at(b, 39), m[1]]), "another"), (dict(momenta=[m[0], at(b, 59)]), "another"),
+                        (dict(params=[at(b, 15, 12), p[1]], grads=[at(free, 0, 12), g[1]], momenta=[at(b, 100, 12), m[1]], copies=None), "another"),
+                        (dict(copies=[c[0], at(half, 1)]), "another"), (dict(grads=[at(b, 79), g[1]]), "gradient"), (dict(grads=[g[0], at(b, 10)]), "gradient"),
+                        (dict(grads=[g[0], at(half, 39).view(4, 5)]), "one type")):
+        assert why in muon(**change), change
+    assert "GPU" in muon(grads=[at(b, 80), at(b, 99)])
