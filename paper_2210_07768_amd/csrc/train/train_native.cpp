@@ -827,7 +827,7 @@ PyObject* muon(PyObject*, PyObject* args) {
       sides_fit(p[i], "a matrix of weights");
       if (p[i].scalar_type() != p[0].scalar_type() || grad[i].scalar_type() != grad[0].scalar_type() || (copy.seq && copy[i].scalar_type() != copy[0].scalar_type()))
         bad("all weights are of one type, and so are all gradients and all copies");
-      if (grad[i].sizes() != p[i].sizes() || m[i].numel() != p[i].numel() || (copy.seq && copy[i].numel() != p[i].numel())) bad("a gradient, momentum or copy is not of its weights' size");
+      if (grad[i].sizes() != p[i].sizes() || m[i].sizes() != p[i].sizes() || (copy.seq && copy[i].sizes() != p[i].sizes())) bad("a gradient, momentum or copy is not of its weights' size");
       if (m[i].scalar_type() != at::kFloat) bad("momenta are float32");
       if (copy.seq && (h.copy_dtype == FBX_F32 || h.param_dtype != FBX_F32)) bad("a copy is in float16 or bfloat16, of weights in float32");
       t.d_param = same(p[i], true);

@@ -334,7 +334,7 @@ def muon(params: Sequence, grads: Sequence, momenta: Sequence, copies: Optional[
     """One step of Muon over all matrices, in place (the formulas: fbx_muon_step in ``include/fbx_train.h``): the momentum takes the
     gradient in, and the weights move by the orthogonalised momentum (nesterov: the gradient and momentum times it).
 
-    momenta: float32, of the weights' sizes; copies: float16 or bfloat16 tensors that receive float32 weights too.  All weights are of one type, and
+    momenta: float32, of the weights' shapes; copies: float16 or bfloat16 tensors of theirs that receive float32 weights too.  All weights are of one type, and
     so are all gradients.  adjust: what the update is multiplied by, "rms" 0.2 sqrt(max(rows, columns)), "spectral" sqrt(max(1, rows / columns)),
     "none" 1.  exact: see ``orthogonalise``; by default for all but bfloat16 weights of more than 256 rows and columns, whose rounding hides what half
     precision leaves."""

@@ -315,3 +315,14 @@ def test_matrices_that_overlap_are_refused_by_muon():
                         (dict(grads=[g[0], at(half, 39).view(4, 5)]), "one type")):
         assert why in muon(**change), change
     assert "GPU" in muon(grads=[at(b, 80), at(b, 99)])
+
+
+def test_muon_refuses_states_of_another_shape():
+    """A momentum or copy of as many elements, but other rows and columns, would be filled in the weights' order."""
+    d = dict(params=[torch.zeros(4, 6)], grads=[torch.zeros(4, 6)], momenta=[torch.zeros(4, 6)], copies=[torch.zeros(4, 6, dtype=torch.float16)])
+    for name in ("grads", "momenta", "copies"):
+        for shape in ((6, 4), (24,), (1, 4, 6)):
+            assert "size" in _refusal(lambda: T.muon(**{**d, name: [d[name][0].reshape(shape)]})), (name, shape)
+    assert "GPU" in _refusal(lambda: T.muon(**d))
+    w = [torch.zeros(4, 6)]
+    assert "size" in _refusal(lambda: T.Muon(w, copies=[d["copies"][0].reshape(6, 4)]).step([torch.zeros(4, 6)]))
