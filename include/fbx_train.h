@@ -300,6 +300,8 @@ fbx_status fbx_orthogonalise(const fbx_ortho* h, const fbx_ortho_matrix* matrice
  *   d_copy : DEVICE or NULL: receives the new weights in copy_dtype as well (for weights kept in f32)
  *   factor : of the matrix: an orthogonal matrix's elements have a mean square of 1 / max(rows, columns)
  * Elements of a matrix are adjacent.
+ * fbx_muon_check refuses what fbx_muon_step refuses, but for its scratch, and does nothing else: where several calls make one step, all
+ * can be checked before the first is made.
  * Errors: FBX_E_ARG, FBX_E_NOMEM, FBX_E_HIP.
  */
 typedef struct {
@@ -316,6 +318,7 @@ typedef struct {
   int nesterov;
   double lr, momentum, weight_decay, grad_scale;
 } fbx_muon;
+fbx_status fbx_muon_check(const fbx_muon* h, const fbx_muon_matrix* matrices, uint32_t n);
 fbx_status fbx_muon_scratch(const fbx_muon* h, const fbx_muon_matrix* matrices, uint32_t n, uint64_t* bytes);
 fbx_status fbx_muon_step(const fbx_muon* h, const fbx_muon_matrix* matrices, uint32_t n, void* d_scratch,
                          uint64_t scratch_bytes, void* hip_stream);

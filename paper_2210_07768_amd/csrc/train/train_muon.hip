@@ -1036,6 +1036,44 @@ fbx_status sides(const M* matrices, uint32_t n, uint32_t exact, fbx_dtype out, s
   }
   return FBX_OK;
 }
+// All that a step refuses but for its scratch, and what it is made of.
+fbx_status check(const fbx_muon* h, const fbx_muon_matrix* matrices, uint32_t n, Whole* w, std::vector<Step>* steps) {
+  if (!h) return refuse(FBX_E_ARG, "h is NULL");
+  if (!known(h->param_dtype) || !known(h->grad_dtype)) return refuse(FBX_E_ARG, "unknown dtype");
+  if (!(h->momentum >= 0 && h->momentum < 1)) return refuse(FBX_E_ARG, "momentum must be in [0, 1)");
+  if (!isfinite((float)h->lr) || !isfinite((float)h->weight_decay) || !isfinite((float)h->grad_scale)) return refuse(FBX_E_ARG, "lr, weight_decay and grad_scale must be finite");
+  fbx_status st = check(&h->ortho, steps);
+  if (st == FBX_OK) st = sides(matrices, n, h->ortho.exact, h->param_dtype, &w->all);
+  if (st != FBX_OK) return st;
+  bool copy = false;
+  for (uint32_t i = 0; i < n; ++i) copy |= matrices[i].d_copy != nullptr;
+  for (uint32_t i = 0; i < n; ++i) {
+    const fbx_muon_matrix& m = matrices[i];
+    Matrix& t = w->all[i];
+    if (!m.d_param || !m.d_grad || !m.d_m) return refuse(FBX_E_ARG, "a matrix lacks its weights, gradient or momentum");
+    if ((uintptr_t)m.d_param % size_of(h->param_dtype) || (uintptr_t)m.d_grad % size_of(h->grad_dtype) || (uintptr_t)m.d_m % 4u) return refuse(FBX_E_ARG, "a matrix is not aligned to its elements");
+    if (m.d_copy && (h->copy_dtype == FBX_F32 || !known(h->copy_dtype) || h->param_dtype != FBX_F32 || (uintptr_t)m.d_copy % 2u))
+      return refuse(FBX_E_ARG, "a copy is in f16 or bf16, of weights in f32");
+    if (copy && !m.d_copy) return refuse(FBX_E_ARG, "either all matrices have a copy or none");
+    if (!isfinite((float)(h->lr * m.factor))) return refuse(FBX_E_ARG, "factor must be finite");
+    t.u = m.d_grad;
+    t.m = (float*)m.d_m;
+    t.out = m.d_param;
+    t.copy = m.d_copy;
+    t.ld_u = t.ld_out = m.columns;
+    t.step = (float)(h->lr * m.factor);
+  }
+  w->h = &h->ortho;
+  w->in = h->grad_dtype;
+  w->out = h->param_dtype;
+  w->copy = h->copy_dtype;
+  w->weights = true;
+  w->nesterov = h->nesterov != 0;
+  w->momentum = (float)h->momentum;
+  w->grad_scale = (float)h->grad_scale;
+  w->decay = (float)(1.0 - h->lr * h->weight_decay);
+  return FBX_OK;
+}
 // (no exception may leave a call)
 template <class F>
 fbx_status guarded(F f) {
@@ -1103,46 +1141,21 @@ extern "C" fbx_status fbx_muon_scratch(const fbx_muon* h, const fbx_muon_matrix*
   });
 }
 
-extern "C" fbx_status fbx_muon_step(const fbx_muon* h, const fbx_muon_matrix* matrices, uint32_t n, void* d_scratch, uint64_t scratch_bytes, void* hip_stream) {
+extern "C" fbx_status fbx_muon_check(const fbx_muon* h, const fbx_muon_matrix* matrices, uint32_t n) {
   return guarded([&] {
-    if (!h) return refuse(FBX_E_ARG, "h is NULL");
     Whole w{};
     std::vector<Step> steps;
-    if (!known(h->param_dtype) || !known(h->grad_dtype)) return refuse(FBX_E_ARG, "unknown dtype");
-    if (!(h->momentum >= 0 && h->momentum < 1)) return refuse(FBX_E_ARG, "momentum must be in [0, 1)");
-    if (!isfinite((float)h->lr) || !isfinite((float)h->weight_decay) || !isfinite((float)h->grad_scale)) return refuse(FBX_E_ARG, "lr, weight_decay and grad_scale must be finite");
-    fbx_status st = check(&h->ortho, &steps);
-    if (st == FBX_OK) st = sides(matrices, n, h->ortho.exact, h->param_dtype, &w.all);
-    if (st != FBX_OK) return st;
-    bool copy = false;
-    for (uint32_t i = 0; i < n; ++i) copy |= matrices[i].d_copy != nullptr;
-    for (uint32_t i = 0; i < n; ++i) {
-      const fbx_muon_matrix& m = matrices[i];
-      Matrix& t = w.all[i];
-      if (!m.d_param || !m.d_grad || !m.d_m) return refuse(FBX_E_ARG, "a matrix lacks its weights, gradient or momentum");
-      if ((uintptr_t)m.d_param % size_of(h->param_dtype) || (uintptr_t)m.d_grad % size_of(h->grad_dtype) || (uintptr_t)m.d_m % 4u) return refuse(FBX_E_ARG, "a matrix is not aligned to its elements");
-      if (m.d_copy && (h->copy_dtype == FBX_F32 || !known(h->copy_dtype) || h->param_dtype != FBX_F32 || (uintptr_t)m.d_copy % 2u))
-        return refuse(FBX_E_ARG, "a copy is in f16 or bf16, of weights in f32");
-      if (copy && !m.d_copy) return refuse(FBX_E_ARG, "either all matrices have a copy or none");
-      if (!isfinite((float)(h->lr * m.factor))) return refuse(FBX_E_ARG, "factor must be finite");
-      t.u = m.d_grad;
-      t.m = (float*)m.d_m;
-      t.out = m.d_param;
-      t.copy = m.d_copy;
-      t.ld_u = t.ld_out = m.columns;
-      t.step = (float)(h->lr * m.factor);
-    }
-    st = check_scratch(d_scratch, scratch_bytes, scratch_of(w.all));
+    return check(h, matrices, n, &w, &steps);
+  });
+}
+
+extern "C" fbx_status fbx_muon_step(const fbx_muon* h, const fbx_muon_matrix* matrices, uint32_t n, void* d_scratch, uint64_t scratch_bytes, void* hip_stream) {
+  return guarded([&] {
+    Whole w{};
+    std::vector<Step> steps;
+    fbx_status st = check(h, matrices, n, &w, &steps);
+    if (st == FBX_OK) st = check_scratch(d_scratch, scratch_bytes, scratch_of(w.all));
     if (st != FBX_OK || !n) return st;
-    w.h = &h->ortho;
-    w.in = h->grad_dtype;
-    w.out = h->param_dtype;
-    w.copy = h->copy_dtype;
-    w.weights = true;
-    w.nesterov = h->nesterov != 0;
-    w.momentum = (float)h->momentum;
-    w.grad_scale = (float)h->grad_scale;
-    w.decay = (float)(1.0 - h->lr * h->weight_decay);
     run(w, steps, (char*)d_scratch, (hipStream_t)hip_stream);
     return launched();
   });

@@ -34,6 +34,7 @@ struct {
   decltype(&fbx_join_backward) join_backward;
   decltype(&fbx_ortho_scratch) ortho_scratch;
   decltype(&fbx_orthogonalise) orthogonalise;
+  decltype(&fbx_muon_check) muon_check;
   decltype(&fbx_muon_scratch) muon_scratch;
   decltype(&fbx_muon_step) muon_step;
 } g;
@@ -848,10 +849,11 @@ PyObject* muon(PyObject*, PyObject* args) {
       const auto behind = std::lower_bound(written.begin(), written.end(), std::make_pair(r.second, uintptr_t{0}));
       if (behind != written.begin() && (behind - 1)->second > r.first) bad("a gradient overlaps a matrix, momentum or copy that is written");
     }
+    if (check_only) check(g.muon_check(&h, all.data(), static_cast<uint32_t>(all.size())));
     on_gpu(p[0]);
+    if (check_only) Py_RETURN_NONE;
     uint64_t need = 0;
     check(g.muon_scratch(&h, all.data(), static_cast<uint32_t>(all.size()), &need));
-    if (check_only) Py_RETURN_NONE;
     const c10::DeviceGuard guard(where);
     const at::Tensor s = scratch(need, p[0]);
     check(g.muon_step(&h, all.data(), static_cast<uint32_t>(all.size()), pointer(s), need, stream_of(p[0])));

@@ -28,7 +28,7 @@ EXPORTS = [
     "fbx_train_last_error", "fbx_embed_forward", "fbx_embed_backward_scratch", "fbx_embed_backward",
     "fbx_gated_scratch", "fbx_gated_forward", "fbx_gated_backward", "fbx_adamw_step",
     "fbx_norm_forward", "fbx_norm_scratch", "fbx_norm_backward", "fbx_join_forward", "fbx_join_scratch", "fbx_join_backward",
-    "fbx_ortho_scratch", "fbx_orthogonalise", "fbx_muon_scratch", "fbx_muon_step",
+    "fbx_ortho_scratch", "fbx_orthogonalise", "fbx_muon_check", "fbx_muon_scratch", "fbx_muon_step",
 ]
 ACTS = {"silu": 0, "gelu": 1, "relu": 2, "sigmoid": 3}
 KINDS = {"rms": 0, "layer": 1}           # of a norm

@@ -147,3 +147,17 @@ def test_shifted_results_are_refused():
             call()
         assert e.value.status == B.E_ARG and "overlaps" in str(e.value)
     assert torch.equal(rows, before) and not flat.any() and not any(t.any() for t in m)
+
+
+# ------------------------------------------------------------------ Muon's lists
+def test_muon_steps_all_lists_or_none():
+    """Weights of two types are two calls; what only the library refuses of the second (3e38 times 0.2 sqrt(64)) leaves the first one's alone."""
+    w = [torch.ones(1, 1, device="cuda"), torch.ones(64, 64, device="cuda", dtype=BF16)]
+    opt = T.Muon(w, lr=3e38)
+    grads = [torch.ones_like(t) for t in w]
+    with pytest.raises(B.FbxError) as e:
+        opt.step(grads)
+    assert "factor" in str(e.value)
+    assert all((t == 1).all() for t in w) and not any(m.any() for m in opt.m) and opt.step_count == 0
+    opt.step(grads, lr=1.0)
+    assert all((t != 1).any() for t in w) and all(m.all() for m in opt.m) and opt.step_count == 1

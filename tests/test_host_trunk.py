@@ -326,3 +326,29 @@ def test_muon_refuses_states_of_another_shape():
     assert "GPU" in _refusal(lambda: T.muon(**d))
     w = [torch.zeros(4, 6)]
     assert "size" in _refusal(lambda: T.Muon(w, copies=[d["copies"][0].reshape(6, 4)]).step([torch.zeros(4, 6)]))
+
+
+MUON_REFUSED = test_muon_refuses.pytestmark[0].args[1]
+
+
+@pytest.mark.parametrize("change, matrix, why", MUON_REFUSED + [({}, {}, "")])
+def test_muon_check_refuses_what_a_step_refuses(change, matrix, why):
+    L = _library()
+    L.fbx_muon_check.argtypes = [ctypes.POINTER(Muon), ctypes.POINTER(MuonMatrix), u32]
+    a = dict(param_dtype=0, grad_dtype=0, copy_dtype=2, nesterov=1, lr=1e-3, momentum=0.95, weight_decay=0.0, grad_scale=1.0, ortho={})
+    a.update(change)
+    h = Muon(**{**a, "ortho": _ortho(**a["ortho"])})
+    m = (MuonMatrix * 2)(_made(MuonMatrix, MUON_MATRIX, {}), _made(MuonMatrix, MUON_MATRIX, matrix))
+    if why:
+        assert L.fbx_muon_check(h, m, 2) == B.E_ARG and why in _why(), _why()
+    else:
+        assert L.fbx_muon_check(h, m, 2) == B.OK and L.fbx_muon_check(h, None, 0) == B.OK
+    assert L.fbx_muon_check(None, m, 2) == B.E_ARG
+
+
+def test_muon_checks_a_list_before_another_is_stepped():
+    """What is checked of every list before one is stepped holds all that the library refuses: 3e38 times a factor of 1.6 is no number of 32 bits."""
+    p = [torch.zeros(64, 64)]
+    how = [0.95, True, 0.0, 1.0, -1, [3.4445, -4.7750, 2.0315], 1e-7, True]
+    check = lambda lr, factor: _refusal(lambda: T._load().muon(p, [torch.zeros(64, 64)], [torch.zeros(64, 64)], None, [factor], lr, *how))  # noqa: E731
+    assert "factor" in check(3e38, 1.6) and "lr" in check(float("inf"), 1.0) and "GPU" in check(3e38, 1.0)
