@@ -161,3 +161,80 @@ def test_muon_steps_all_lists_or_none():
     assert all((t == 1).all() for t in w) and not any(m.any() for m in opt.m) and opt.step_count == 0
     opt.step(grads, lr=1.0)
     assert all((t != 1).any() for t in w) and all(m.all() for m in opt.m) and opt.step_count == 1
+
+
+# ------------------------------------------------------------------ every tile of the products
+LISTS = {"tiles of 64": [(400, 300), (300, 400)], "tiles of 128": [(513, 520)] * 16 + [(520, 513)] * 16, "A and B in tiles of 256": [(700, 701)] * 16 + [(715, 699)] * 16,
+         "X in tiles of 256": [(1050, 701)] * 8 + [(700, 1050)] * 8}   # (as the library's rule has it; with both parts the last list's A is in tiles of 64)
+
+
+@pytest.mark.parametrize("exact", [True, False])
+@pytest.mark.parametrize("name", list(LISTS))
+def test_every_tile(name, exact):
+    """Results against 64 bits; into weights of each type, with copies: what the results themselves give, rounded a few times in 32 bits and once to
+    the weights' type."""
+    g = _gen(70)
+    shapes = LISTS[name]
+    given = [_decaying(g, r, c) for r, c in shapes]
+    got = T.orthogonalise(given, exact=exact)
+    for i, (u, o) in enumerate(zip(given, got)):
+        want, off = _goal(u, exact, F32)
+        _near(o, want, off, (name, i))
+    assert all(torch.equal(a, b) for a, b in zip(got, T.orthogonalise(given, exact=exact)))   # the same inputs, the same bits
+    lr, decay = 0.05, 0.1
+    for kind in (F32, F16, BF16):
+        p = [_r(g, *s, size=0.05, dtype=kind) for s in shapes]
+        before, m = [t.double() for t in p], [torch.zeros(s, device="cuda") for s in shapes]
+        copies = [torch.zeros(s, dtype=BF16, device="cuda") for s in shapes] if kind == F32 else None
+        T.muon(p, given, m, copies, lr=lr, momentum=0.9, nesterov=False, weight_decay=decay, exact=exact)
+        for i, (s, w, b, o) in enumerate(zip(shapes, p, before, got)):
+            step = lr * 0.2 * math.sqrt(max(s))
+            want = b * (1 - lr * decay) - step * o.double()
+            terms = 4 * HALF_UNIT[F32] * (b.abs() + step * o.double().abs())   # (the two factors, the product and the difference)
+            limit = terms + HALF_UNIT[kind] * (want.abs() + terms) + 2.0 ** -25
+            assert ((w.double() - want).abs() <= limit).all(), (name, kind, i)
+            assert torch.equal(m[i], given[i])
+            if copies is not None:
+                assert ((copies[i].double() - want).abs() <= terms + HALF_UNIT[BF16] * (want.abs() + terms) + 2.0 ** -133).all(), (name, i)
+
+
+@pytest.mark.parametrize("shape", [(300, 400), (520, 270)])
+@pytest.mark.parametrize("exact", [True, False])
+def test_extremes_of_larger_matrices(exact, shape):
+    """Zeros, one number, what is not finite, and sizes near the ends of 32 bits, in the launches that larger matrices go through."""
+    g = _gen(71)
+    zero, one, nan, inf, usual = torch.zeros(shape, device="cuda"), torch.zeros(shape, device="cuda"), *(_r(g, *shape) for _ in range(3))
+    one[shape[0] - 1, 5] = -2.5
+    nan[2, 2], inf[-1, -1] = float("nan"), float("-inf")
+    tiny, huge = usual * 2.0 ** -110, usual * 2.0 ** 120
+    got = T.orthogonalise([zero, one, nan, inf, tiny, huge, usual], eps=1e-30, exact=exact)
+    assert not got[0].any() and torch.isnan(got[2]).all() and torch.isnan(got[3]).all()
+    most = 1.6e-3 if not exact else 2.0 ** -17   # (one number: 15 products, 2^-21 each)
+    alone = _iterated(one, torch.float64)
+    assert (got[1] != 0).sum() == 1 and abs(float(got[1][-1, 5] - alone[-1, 5])) <= most * abs(float(alone[-1, 5]))
+    want, off = _goal(usual, exact, F32)
+    for i in (5, 6):
+        _near(got[i], want, off, i)
+    assert torch.equal(got[5], got[6])   # (a power of two apart)
+    near = _iterated(tiny, torch.float64, eps=1e-30)
+    _near(got[4], near, 2 * off, "tiny")
+
+
+@pytest.mark.parametrize("param", [F32, F16, BF16])
+def test_what_muon_is_left_to(param):
+    """Without the caller's word products are of both parts, but for bfloat16 weights of more than 256 rows and columns."""
+    g = _gen(72)
+    shapes = [(256, 600), (600, 256), (257, 257), (20, 30)]
+    grads = [_decaying(g, *s) for s in shapes]
+
+    def step(**how):
+        p = [torch.zeros(s, dtype=param, device="cuda") for s in shapes]
+        T.muon(p, grads, [torch.zeros(s, device="cuda") for s in shapes], lr=1.0, adjust="none", **how)
+        return p
+
+    left, both, first = step(), step(exact=True), step(exact=False)
+    for i in range(4):
+        assert not torch.equal(both[i], first[i]) or i == 3
+        alone = [torch.zeros(shapes[i], dtype=param, device="cuda")]
+        T.muon(alone, [grads[i]], [torch.zeros(shapes[i], device="cuda")], lr=1.0, adjust="none", exact=param != BF16 or i != 2)
+        assert torch.equal(left[i], alone[0]), i
