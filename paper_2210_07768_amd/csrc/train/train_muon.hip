@@ -301,7 +301,7 @@ __device__ __forceinline__ void leave(const Leaving& p, const Matrix& t, uint32_
 // of the matrix instructions, so that a lane holds four adjacent columns of a row.  Of a symmetric C tiles on and below the
 // diagonal are worked out, and stored on either side of it.  kStages: steps whose tiles are in LDS or on their way there.
 // Two of 2,624 x 4,096, products of first parts: A 70 to 76 us, B 53 to 57, X 150 to 163: 0.77, 0.66 and 0.72 PFLOP/s of what is needed; a library's
-// product takes 59 us for each X, without a X and without storing two parts (0.95 PFLOP/s).  In tiles of 128 two workgroups on a
+// product takes 59 us for each X, without a X and without storing two parts (0.95 PFLOP/s).  Of both parts: A 163 to 192, B 129 to 134, X 336 to 370.  In tiles of 128 two workgroups on a
 // compute unit take 0.9 us for a step, of which reading and filling LDS is 0.73; 2 to 3 us before the first step and 6 to 8 behind the last (when all
 // of them store at once) come on top, and the last of 2.6 rounds leaves units idle.  Measured and not faster: tiles of 256 x 128 by eight wavefronts
 // with three steps in LDS (157 to 166), wavefronts that have a SIMD to themselves and read a quarter to a half less from LDS

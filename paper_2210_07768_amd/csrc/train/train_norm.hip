@@ -421,7 +421,8 @@ __device__ __forceinline__ void fetch_vectors(Row<kN>& weight, Row<kN>& next_wei
 }
 
 // Bound by memory: 65,536 x 2,624, a stream in f32, the block's side in bf16, a gate for each element, the next norm: 2.4 GB in 440 us,
-// 5.5 TB/s.  One row of 1,536: 3.0 us, the call 5.4 to 6.
+// 5.5 TB/s.  One row of 1,536: 3.0 us, the call 5.4 to 6.  Above 8,192 columns (kWide4) a lane's 32 elements of each do not fit the registers,
+// 45 to 111 of which go by way of scratch memory: 2,048 x 16,384 of the same types 184 us, 2.6 TB/s.
 template <class R, class T, Shape kShape>
 __global__ __launch_bounds__(kMostLanes) void k_join(JoinArgs p) {
   constexpr int kN = packs_of(kShape);
@@ -466,7 +467,8 @@ __global__ __launch_bounds__(kMostLanes) void k_join(JoinArgs p) {
 // 16,384 x 2,624 in bf16 with a gate for each element and the next norm: 0.69 GB in 165 to 176 us, 3.9 to 4.2 TB/s.  141 registers let twelve
 // wavefronts be on a compute unit; 463 vector instructions and 16 exponentials and reciprocals a row and wavefront are 0.1 ms of it, hidden in
 // part.  With loads that depended on conditions, waited for at once, it took 346.  1,000 x 411: 8.5 of the call's 14 us, of which
-// one row takes 6.8: instructions come from memory once a launch.
+// one row takes 6.8: instructions come from memory once a launch.  Scratch memory holds what the registers do not: above 4,096 columns 9 to 21
+// registers (4,096 x 8,192, a stream in f32: 177 us, 4.2 TB/s), above 8,192 about 700 (2,048 x 16,384: 690 us, 1.1 TB/s).
 template <class R, class T, Shape kShape>
 __global__ __launch_bounds__(kMostLanes) void k_join_grad(JoinArgs p) {
   constexpr int kN = packs_of(kShape);
