@@ -489,11 +489,12 @@ bool meet(const Bytes& a, const Bytes& b) {
     if (row_meets(a.at + i * a.apart)) return true;
   return false;
 }
+constexpr const char* kOverlaps = "a tensor given for a result overlaps an input, or another result";
 // A result may not overlap an input: another wavefront may still have to read it.
 void apart(const at::Tensor& out, std::initializer_list<const at::Tensor*> inputs) {
   const Bytes o(out);
   for (const at::Tensor* t : inputs)
-    if (t && meet(o, Bytes(*t))) bad("a tensor given for a result overlaps an input, or another result");
+    if (t && meet(o, Bytes(*t))) bad(kOverlaps);
 }
 // A gradient as autograd gives it may be one element seen many times.
 at::Tensor gradient_rows(const at::Tensor& t) {
@@ -763,9 +764,16 @@ PyObject* orthogonalise(PyObject*, PyObject* args) {
         rows_of(out[i], "out", h.out, like, t.size(0), t.size(1));
       }
     }
-    for (Py_ssize_t i = 0; given.seq && i < n; ++i)   // (its own matrix is read before it is written)
-      for (Py_ssize_t k = 0; k < n; ++k)
-        if (i != k) apart(out[i], {&in[k], k < i ? &out[k] : nullptr});
+    if (given.seq) {
+      std::vector<Bytes> read, written;
+      for (Py_ssize_t i = 0; i < n; ++i) {
+        read.emplace_back(in[i]);
+        written.emplace_back(out[i]);
+      }
+      for (Py_ssize_t i = 0; i < n; ++i)   // (its own matrix is read before it is written)
+        for (Py_ssize_t k = 0; k < n; ++k)
+          if (i != k && (meet(written[i], read[k]) || (k < i && meet(written[i], written[k])))) bad(kOverlaps);
+    }
     on_gpu(like);
     const c10::DeviceGuard guard(like.device());
     for (Py_ssize_t i = 0; i < n; ++i) {
