@@ -258,8 +258,8 @@ fbx_status fbx_join_backward(const fbx_join* h, const fbx_join_gradients* g, voi
  * first part overflows; sums are in 32 bits.
  *   exact = 1: products are of both parts of both sides (all but second by second): errors like those of
  *     products in 32 bits.
- *   exact = 0: products are of first parts, a third of the work; a times X's second part is added.  After five steps the result is off by 0.3e-3
- *     to 2.8e-3 of its size (rounding it to bf16 leaves 1.7e-3): 0.5e-3 to 1.6e-3 where singular values are many and unlike.  Where few numbers make up the
+ *   exact = 0: products are of first parts, a third of the work; a times X's second part is added.  After five steps the result is off by 0.2e-3
+ *     to 3.5e-3 of its size, by the spectrum (rounding it to bf16 leaves 1.7e-3): 0.5e-3 to 1.6e-3 of decaying and of normally distributed matrices.  Where few numbers make up the
  *     matrix, their roundings are the same everywhere and do not average out: 9e-3 for a unit matrix of 319, and up to 27e-3 for one singular value of all.
  *     Matrices that a workgroup's memory holds (up to 128 x 128, 32 x 1,024 or so) are always worked out exactly.
  *   exact = FBX_EXACT_BY_SIZE: 0 for results in bf16 of matrices of more than 256 rows and columns, else 1: for weights in bf16, whose
